@@ -351,6 +351,161 @@ hg_status hg_cache_image_bits_per_elem(const hg_cache *cache, double *bits);
 hg_status hg_select_heads(const float *g_scores, const float *o_scores, int32_t num_layers,
                           int32_t num_q_heads, int32_t num_kv_heads, int32_t k, uint8_t *mask_out);
 
+/* ------------------------------------------------------------------------
+ * Requests whose cache stays 16-bit: a paged cache, and the prompt's attention
+ * (no counterpart in the paper; what a serving program runs beside the packed
+ * cache above).  The conventions at the top of this file hold, with these
+ * differences: entries are BF16 or FP16, head_dim is 128, rows may be strided
+ * (hg_rows), and the tensors are device memory.
+ * ------------------------------------------------------------------------ */
+
+typedef enum hg_dtype { HG_DTYPE_BF16 = 0, HG_DTYPE_F16 = 1 } hg_dtype;
+
+/* Rows of 128 dense channels, one per (token, head): row (t, h) starts at
+ * data + t * token_stride + h * head_stride.  Strides in elements, multiples of
+ * 8, 0 <= stride < 2^38; data 16-byte aligned.  data NULL: absent.  So
+ * [tokens][heads][128], [heads][tokens][128] (what hg_quantize_kv takes, at one
+ * batch row) and a slice of a fused projection's output are all taken as they
+ * are.  Rows that are written must not overlap. */
+typedef struct hg_rows {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} hg_rows;
+
+/* Position rotation (rotary embedding) of queries and keys.  Channels [0,
+ * rot_dim) are turned in rot_dim / 2 pairs, the others pass: pair i of a token
+ * at position p becomes (a c - b s, b c + a s) with c = table[p][i], s =
+ * table[p][rot_dim / 2 + i], in binary32, each result rounded once.
+ *   table        device float [table_len][rot_dim], 16-byte aligned
+ *   rot_dim      multiple of 16, 16..128
+ *   interleaved  0: pair i is channels i and i + rot_dim / 2; 1: channels 2i
+ *                and 2i + 1
+ *   sections     all 0: one position per token.  Else three multiples of 8 that
+ *                add up to rot_dim / 2: a token has three positions (time,
+ *                height and width of a vision-language model); the first
+ *                sections[0] pairs turn by the first one, the next sections[1]
+ *                by the second, the rest by the third.
+ * Positions are device int32 [tokens], or [3][tokens] with sections; one
+ * outside [0, table_len) is taken as the nearest inside. */
+typedef struct hg_rotation {
+    const float *table;
+    int32_t table_len;
+    int32_t rot_dim;
+    int32_t interleaved;
+    int32_t sections[3];
+} hg_rotation;
+
+/* Geometry of a page pool, for keys and values alike: token t (0 <= t <
+ * page_size) of head h in page p starts at p * page_stride + h * head_stride +
+ * t * token_stride elements.  page_size: 16, 32, 64, 128 or 256.  All strides 0:
+ * dense [num_pages][num_kv_heads][page_size][128].  Strides are multiples of 8
+ * elements below 2^38, at least 128 (page_stride at least 1 where num_pages is
+ * 1), and rows must not overlap; num_pages * page_size < 2^31. */
+typedef struct hg_page_shape {
+    int32_t dtype;          /* hg_dtype */
+    int32_t num_pages;
+    int32_t page_size;
+    int32_t num_kv_heads;   /* 1..64 */
+    int32_t head_dim;       /* must be 128 */
+    int64_t page_stride;
+    int64_t head_stride;
+    int64_t token_stride;
+} hg_page_shape;
+
+/* Opaque host-side descriptor of a page pool; the pool's memory stays the
+ * caller's.  It never changes after its creation: any number of host threads and
+ * streams may use one. */
+typedef struct hg_pages hg_pages;
+
+/* Descriptor of the pool whose keys start at k_pages and values at v_pages
+ * (device, 16-byte aligned, the same geometry).  The entries need no
+ * initialisation: what lies in a page beyond a request's length is never used,
+ * whatever its bits.  Encodes two tensor maps (no device work). */
+hg_status hg_pages_create(const hg_page_shape *shape, void *k_pages, void *v_pages, hg_pages **out);
+void hg_pages_destroy(hg_pages *pages);
+
+/* The rows of hg_pages_append. */
+typedef struct hg_append_io {
+    hg_rows q, k, v;              /* [num_tokens][heads]; q absent where num_q_heads is 0 */
+    hg_rows q_out, k_out, v_out;  /* q_out with q; k_out and v_out may be absent */
+} hg_append_io;
+
+/* New tokens into a paged cache: rotates q and k, writes the rotated q to
+ * q_out, and the rotated k and the v of token i to slot slots[i] = page *
+ * page_size + token in page, and to k_out / v_out where these are given (for
+ * hg_prompt_attention, hg_quantize_kv).  An output may be its own input (same
+ * data and strides).  slots: device int32 [num_tokens]; a token whose slot is
+ * outside the pool (-1, say) is rotated but not stored; no two tokens may have
+ * the same slot.  rotation NULL: no rotation (positions then unused).  A count
+ * of 0 tokens does nothing. */
+hg_status hg_pages_append(const hg_pages *pages, int32_t num_tokens, int32_t num_q_heads,
+                          const hg_append_io *io, const hg_rotation *rotation, const int32_t *positions,
+                          const int32_t *slots, hg_stream_t stream);
+
+/* The rows of an attention: q, out [tokens][num_q_heads], k, v
+ * [tokens][num_kv_heads]. */
+typedef struct hg_attention_io {
+    hg_rows q, k, v, out;
+} hg_attention_io;
+
+/* Workspace bytes of hg_pages_decode_attention and hg_pages_decode_step for up to
+ * `batch` requests on the current device.  Used as a decode workspace is: zeroed
+ * once by hg_workspace_clear, one launch at a time, status by
+ * hg_workspace_status; it serves any pool and any smaller batch. */
+hg_status hg_pages_decode_workspace_size(const hg_pages *pages, int32_t batch, int32_t num_q_heads,
+                                         size_t *bytes);
+
+/* Attention of one new token per request over the paged cache.  Request b's
+ * token t lies in page page_table[b * table_stride + t / page_size] at t %
+ * page_size; it attends over its first lengths[b] tokens (clamped to [0,
+ * table_stride * page_size]).  num_q_heads is a multiple of num_kv_heads, at
+ * most 16 times it; query head qh attends with KV head qh / G, score =
+ * softmax_scale * <q, k> (softmax_scale <= 0: 1/sqrt(128)).  io: q, out; k and v
+ * unused.  lse (or NULL): device float [batch][num_q_heads], the natural
+ * logarithm of the sum of exp(score).  A request of length 0 gets out = 0, lse =
+ * -inf.  page_table, lengths: device int32, read by the launch; a page outside
+ * the pool reads as zeros.  Everything is read in stream order, so the call can
+ * be captured in a graph and replayed with other lengths. */
+hg_status hg_pages_decode_attention(const hg_pages *pages, int32_t batch, int32_t num_q_heads,
+                                    const hg_attention_io *io, const int32_t *page_table, int32_t table_stride,
+                                    const int32_t *lengths, float *lse, float softmax_scale, void *workspace,
+                                    size_t workspace_bytes, hg_stream_t stream);
+
+/* One decode step: rotates q and the new token's k (positions as in
+ * hg_pages_append, one token per request), stores k and v at token lengths[b] -
+ * 1 of request b, and attends over the lengths[b] tokens, the new one included
+ * (rounded to the cache's type as it is stored).  io: q, k, v, out; none of q, k,
+ * v is changed.  A request of length 0 stores nothing; one whose last page is
+ * outside the pool neither, and attends to its new token all the same.  The other
+ * arguments as for hg_pages_decode_attention. */
+hg_status hg_pages_decode_step(const hg_pages *pages, int32_t batch, int32_t num_q_heads,
+                               const hg_attention_io *io, const hg_rotation *rotation, const int32_t *positions,
+                               const int32_t *page_table, int32_t table_stride, const int32_t *lengths, float *lse,
+                               float softmax_scale, void *workspace, size_t workspace_bytes, hg_stream_t stream);
+
+/* Workspace bytes of hg_prompt_attention on the current device, for any sizes.
+ * Zeroed once by hg_workspace_clear, one launch at a time, status by
+ * hg_workspace_status. */
+hg_status hg_prompt_workspace_size(size_t *bytes);
+
+/* Attention of whole prompts, packed one after the other.  Prompt i has the
+ * query rows [q_begin[i], q_begin[i + 1]) and the keys and values [k_begin[i],
+ * k_begin[i + 1]) (HOST int32 [num_prompts + 1], not decreasing, from 0 or
+ * above; read before the call returns).  causal != 0: the last query sees every
+ * key, and each earlier one a key less (query r of nq sees the first r + 1 + nk -
+ * nq of nk keys: a prompt whose first tokens are cached has more keys than
+ * queries); causal 0: every query sees every key of its prompt.  A row that sees
+ * nothing gets out = 0, lse = -inf.  Grouped heads, softmax_scale and lse
+ * ([tokens][num_q_heads], rows as in q) as for hg_pages_decode_attention.  Keys
+ * and values of other prompts are never used, whatever their bits; a prompt's
+ * own V rows that are later than a query (masked) must be finite.  num_q_heads at
+ * most 16 times num_kv_heads (1..64). */
+hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_heads, int32_t num_kv_heads,
+                              const hg_attention_io *io, const int32_t *q_begin, const int32_t *k_begin, float *lse,
+                              int32_t causal, float softmax_scale, void *workspace, size_t workspace_bytes,
+                              hg_stream_t stream);
+
 /* Static description of a status code (no counterpart in the paper). */
 const char *hg_status_string(hg_status status);
 

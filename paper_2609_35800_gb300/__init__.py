@@ -26,6 +26,9 @@ __all__ = [
     "hg_decode_attention",
     "hg_decode_step", "hg_decode_attention_noalloc", "hg_cache_image_bits_per_elem",
     "hg_status_string",
+    "HG_DTYPE_BF16", "HG_DTYPE_F16", "PageShape", "Pages", "Rotation",
+    "hg_pages_create", "hg_pages_destroy", "hg_pages_append", "hg_pages_decode_workspace_size",
+    "hg_pages_decode_attention", "hg_pages_decode_step", "hg_prompt_workspace_size", "hg_prompt_attention",
     "library", "library_path",
 ]
 
@@ -35,6 +38,8 @@ HG_BASE_AKVQ_HADAMARD = 2
 HG_HEAD_QUANTIZED = 0
 HG_HEAD_KEYS_ONLY = 1
 HG_HEAD_PROTECTED = 2
+HG_DTYPE_BF16 = 0
+HG_DTYPE_F16 = 1
 NONE_OFFSET = (1 << 64) - 1
 
 STATUS = {
@@ -71,6 +76,16 @@ class HeadRegions(ctypes.Structure):
                                                  "vq_bstride", "vqm_bstride", "kimg_bstride",
                                                  "sal", "sal_bstride")] +
                 [(n, ctypes.c_int32) for n in ("n_coded", "n_salient")])
+
+
+class PageShape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "num_pages", "page_size", "num_kv_heads", "head_dim")] +
+                [(n, ctypes.c_int64) for n in ("page_stride", "head_stride", "token_stride")])
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_len", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("sections", ctypes.c_int32 * 3)]
 
 
 _lib = None
@@ -111,6 +126,14 @@ def library():
         "hg_decode_step": ([P, i32, i32, P, P, P, P, ctypes.c_float, P, sz, P], st),
         "hg_decode_attention_noalloc": ([P, i32, i32, P, P, ctypes.c_float, P], st),
         "hg_cache_image_bits_per_elem": ([P, ctypes.POINTER(ctypes.c_double)], st),
+        "hg_pages_create": ([P, P, P, ctypes.POINTER(P)], st),
+        "hg_pages_destroy": ([P], None),
+        "hg_pages_append": ([P, i32, i32, P, P, P, P, P], st),
+        "hg_pages_decode_workspace_size": ([P, i32, i32, ctypes.POINTER(sz)], st),
+        "hg_pages_decode_attention": ([P, i32, i32, P, P, i32, P, P, ctypes.c_float, P, sz, P], st),
+        "hg_pages_decode_step": ([P, i32, i32, P, P, P, P, i32, P, P, ctypes.c_float, P, sz, P], st),
+        "hg_prompt_workspace_size": ([ctypes.POINTER(sz)], st),
+        "hg_prompt_attention": ([i32, i32, i32, i32, P, P, P, P, i32, ctypes.c_float, P, sz, P], st),
         "hg_status_string": ([st], ctypes.c_char_p),
     }
     for name, (args, res) in sigs.items():
@@ -383,3 +406,199 @@ def hg_cache_image_bits_per_elem(cache):
     _check(library().hg_cache_image_bits_per_elem(cache.handle, ctypes.byref(out)),
            "hg_cache_image_bits_per_elem")
     return out.value
+
+
+# ---------------------------------------------------------------------------
+# Caches that stay 16-bit: page pools, append, paged decode, prompts
+# ---------------------------------------------------------------------------
+
+_DTYPES = {"torch.bfloat16": HG_DTYPE_BF16, "torch.float16": HG_DTYPE_F16}
+
+
+class Pages:
+    """Owning handle of an hg_pages descriptor (the pool's tensors stay the caller's)."""
+
+    def __init__(self, handle, k_pages, v_pages, shape):
+        self.handle = handle
+        self.k_pages = k_pages
+        self.v_pages = v_pages
+        self.shape = shape
+        self.dtype = k_pages.dtype
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.hg_pages_destroy(self.handle)
+            self.handle = None
+
+
+class Rotation:
+    """Position rotation of queries and keys: `table` float32 [positions][rot_dim] on the GPU, cosines of the
+    rot_dim / 2 pairs, then sines; `sections`: the pairs that turn by each of a token's three positions (None: one
+    position a token).  See hg_rotation."""
+
+    def __init__(self, table, interleaved=False, sections=None):
+        import torch
+        if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous():
+            raise ValueError("Rotation: table must be a contiguous float32 [positions][rot_dim]")
+        if not table.is_cuda:
+            raise ValueError("Rotation: table must be a CUDA tensor")
+        self.table = table
+        self.positions = 3 if sections is not None else 1
+        self.raw = _Rotation(table.data_ptr(), table.shape[0], table.shape[1], int(interleaved),
+                             (ctypes.c_int32 * 3)(*(sections or (0, 0, 0))))
+        self.pointer = ctypes.addressof(self.raw)
+
+
+def _rows(where, name, x, tokens, heads, dtype):
+    """(address, token stride, head stride) of a tensor seen as [tokens][heads][128] with dense channels."""
+    if x.shape != (tokens, heads, 128) or x.dtype != dtype:
+        raise ValueError("%s: %s is %s %s, the call takes %s [%d][%d][128]"
+                         % (where, name, x.dtype, list(x.shape), dtype, tokens, heads))
+    ts, hs, cs = x.stride()
+    if cs != 1:
+        raise ValueError("%s: %s must have dense channels" % (where, name))
+    if not x.is_cuda:
+        raise ValueError("%s: %s must be a CUDA tensor" % (where, name))
+    # a stride that is never taken may be anything in torch
+    return x.data_ptr(), ts if tokens > 1 else 0, hs if heads > 1 else 0
+
+
+_NO_ROWS = (0, 0, 0)
+
+
+def _ints(where, name, x, need, device="CUDA"):
+    """Address of a dense int32 tensor of at least `need` entries."""
+    import torch
+    if x.dtype != torch.int32 or not x.is_contiguous():
+        raise ValueError("%s: %s must be contiguous int32" % (where, name))
+    if x.numel() < need:
+        raise ValueError("%s: %s holds %d entries, the call reads %d" % (where, name, x.numel(), need))
+    if x.is_cuda != (device == "CUDA"):
+        raise ValueError("%s: %s must be a %s tensor" % (where, name, device))
+    return x.data_ptr()
+
+
+def _lse(where, x, tokens, heads):
+    import torch
+    if x is None:
+        return None
+    if x.dtype != torch.float32 or x.shape != (tokens, heads) or not x.is_contiguous():
+        raise ValueError("%s: lse must be contiguous float32 [%d][%d]" % (where, tokens, heads))
+    if not x.is_cuda:
+        raise ValueError("%s: lse must be a CUDA tensor" % where)
+    return x.data_ptr()
+
+
+def _rotated_by(where, rotation, positions, tokens):
+    if rotation is None:
+        return None, None
+    return rotation.pointer, _ints(where, "positions", positions, rotation.positions * tokens)
+
+
+def hg_pages_create(k_pages, v_pages):
+    """Descriptor of the page pool whose keys and values are these tensors, each seen as
+    [pages][kv heads][page size][128] (any strides: pages that lie [tokens][heads] are passed transposed)."""
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
+        raise ValueError("hg_pages_create: k_pages and v_pages must be [pages][heads][tokens][128] of one type")
+    if str(k_pages.dtype) not in _DTYPES:
+        raise ValueError("hg_pages_create: pages must be bfloat16 or float16")
+    n, heads, size, dim = k_pages.shape
+    # the stride of an axis of length 1 is never taken: a dense one stands for it
+    strides = [tuple(s if d > 1 else dim for s, d in zip(x.stride(), x.shape)) for x in (k_pages, v_pages)]
+    if strides[0] != strides[1] or k_pages.stride(3) != 1:
+        raise ValueError("hg_pages_create: k_pages and v_pages must have the same strides and dense channels")
+    if not (k_pages.is_cuda and v_pages.is_cuda):
+        raise ValueError("hg_pages_create: k_pages and v_pages must be CUDA tensors")
+    shape = PageShape(_DTYPES[str(k_pages.dtype)], n, size, heads, dim, *strides[0][:3])
+    h = ctypes.c_void_p()
+    _check(library().hg_pages_create(ctypes.byref(shape), k_pages.data_ptr(), v_pages.data_ptr(), ctypes.byref(h)),
+           "hg_pages_create")
+    return Pages(h, k_pages, v_pages, shape)
+
+
+def hg_pages_destroy(pages):
+    if pages.handle:
+        library().hg_pages_destroy(pages.handle)
+        pages.handle = None
+
+
+def hg_pages_append(pages, q, k, v, rotation, positions, slots, q_out=None, k_out=None, v_out=None, stream=None):
+    """Rotate q and k ([tokens][heads][128], any token and head strides; q None: no queries) and store k and v at
+    `slots` (int32, page * page size + place; negative: nowhere).  The rotated rows also go to q_out and, where
+    given, k_out; v to v_out."""
+    w, d = "hg_pages_append", pages.dtype
+    n, heads, hq = k.shape[0], pages.shape.num_kv_heads, 0 if q is None else q.shape[1]
+    if q is not None and q_out is None:
+        raise ValueError("hg_pages_append: q needs q_out")
+    io = struct.pack("=18q", *(_rows(w, "q", q, n, hq, d) if hq else _NO_ROWS), *_rows(w, "k", k, n, heads, d),
+                     *_rows(w, "v", v, n, heads, d), *(_rows(w, "q_out", q_out, n, hq, d) if hq else _NO_ROWS),
+                     *(_NO_ROWS if k_out is None else _rows(w, "k_out", k_out, n, heads, d)),
+                     *(_NO_ROWS if v_out is None else _rows(w, "v_out", v_out, n, heads, d)))
+    rp, pp = _rotated_by(w, rotation, positions, n)
+    _check(library().hg_pages_append(pages.handle, n, hq, io, rp, pp, _ints(w, "slots", slots, n), _stream(stream)), w)
+
+
+def hg_pages_decode_workspace_size(pages, batch, num_q_heads):
+    out = ctypes.c_size_t(0)
+    _check(library().hg_pages_decode_workspace_size(pages.handle, batch, num_q_heads, ctypes.byref(out)),
+           "hg_pages_decode_workspace_size")
+    return out.value
+
+
+def _decode_table(where, page_table, lengths, batch):
+    if page_table.dim() != 2 or page_table.shape[0] < batch:
+        raise ValueError("%s: page_table must be [%d][pages]" % (where, batch))
+    return (_ints(where, "page_table", page_table, batch * page_table.shape[1]), page_table.shape[1],
+            _ints(where, "lengths", lengths, batch))
+
+
+def hg_pages_decode_attention(pages, q, page_table, lengths, out, lse, softmax_scale, workspace, stream=None):
+    """Attention of one token per request (q, out [batch][heads][128]) over the first lengths[b] tokens of its pages
+    page_table[b]; lse float32 [batch][heads] or None."""
+    w, d = "hg_pages_decode_attention", pages.dtype
+    n, hq = q.shape[0], q.shape[1]
+    io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), 0, 0, 0, 0, 0, 0, *_rows(w, "out", out, n, hq, d))
+    tp, ts, lp = _decode_table(w, page_table, lengths, n)
+    wp, = _devs(w, (workspace, 0, "workspace"))
+    _check(library().hg_pages_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse(w, lse, n, hq),
+                                               softmax_scale, wp, workspace.nbytes, _stream(stream)), w)
+
+
+def hg_pages_decode_step(pages, q, k, v, rotation, positions, page_table, lengths, out, lse, softmax_scale, workspace,
+                         stream=None):
+    """One decode step: q and the new token's k rotated, k and v stored as token lengths[b] - 1 of request b, attention
+    over its lengths[b] tokens."""
+    w, d = "hg_pages_decode_step", pages.dtype
+    n, hq, heads = q.shape[0], q.shape[1], pages.shape.num_kv_heads
+    io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, n, heads, d),
+                     *_rows(w, "v", v, n, heads, d), *_rows(w, "out", out, n, hq, d))
+    rp, pp = _rotated_by(w, rotation, positions, n)
+    tp, ts, lp = _decode_table(w, page_table, lengths, n)
+    wp, = _devs(w, (workspace, 0, "workspace"))
+    _check(library().hg_pages_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse(w, lse, n, hq),
+                                          softmax_scale, wp, workspace.nbytes, _stream(stream)), w)
+
+
+def hg_prompt_workspace_size():
+    out = ctypes.c_size_t(0)
+    _check(library().hg_prompt_workspace_size(ctypes.byref(out)), "hg_prompt_workspace_size")
+    return out.value
+
+
+def hg_prompt_attention(q, k, v, q_begin, k_begin, out, lse, causal, softmax_scale, workspace, stream=None):
+    """Attention of packed prompts: q, out [tokens][heads][128], k, v [keys][kv heads][128] (any token and head
+    strides); prompt i has the rows q_begin[i]..q_begin[i + 1] and the keys k_begin[i]..k_begin[i + 1] (CPU int32
+    tensors [prompts + 1]); lse float32 [tokens][heads] or None."""
+    w, d = "hg_prompt_attention", q.dtype
+    if str(d) not in _DTYPES:
+        raise ValueError("%s: q must be bfloat16 or float16" % w)
+    n, hq, nk, heads, count = q.shape[0], q.shape[1], k.shape[0], k.shape[1], q_begin.numel() - 1
+    io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, nk, heads, d),
+                     *_rows(w, "v", v, nk, heads, d), *_rows(w, "out", out, n, hq, d))
+    qb, kb = _ints(w, "q_begin", q_begin, 1, "CPU"), _ints(w, "k_begin", k_begin, count + 1, "CPU")
+    if q_begin[-1] > n or k_begin[count] > nk:
+        raise ValueError("%s: the prompts end at %d and %d, q and k hold %d and %d rows"
+                         % (w, q_begin[-1], k_begin[count], n, nk))
+    wp, = _devs(w, (workspace, 0, "workspace"))
+    _check(library().hg_prompt_attention(_DTYPES[str(d)], count, hq, heads, io, qb, kb, _lse(w, lse, n, hq),
+                                         1 if causal else 0, softmax_scale, wp, workspace.nbytes, _stream(stream)), w)

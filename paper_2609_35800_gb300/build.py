@@ -14,14 +14,18 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
+CSRC_ATTENTION = os.path.join(HERE, "csrc_attention")  # caches that stay 16-bit, prompt attention
 INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB_NAME = "libheadguard.so"
 LIB = os.path.join(OUT_DIR, LIB_NAME)
-SOURCES = ["hg_api.cu", "hg_quantize.cu", "hg_decode.cu", "hg_decode_m16.cu", "hg_noalloc.cu"]
+SOURCES = [os.path.join(CSRC, f) for f in ("hg_api.cu", "hg_quantize.cu", "hg_decode.cu", "hg_decode_m16.cu",
+                                            "hg_noalloc.cu")]
+SOURCES += [os.path.join(CSRC_ATTENTION, f) for f in ("hg_pages_api.cu", "hg_pages_append.cu", "hg_pages_decode.cu",
+                                                      "hg_prompt.cu")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
-              "-I" + INCLUDE, "-I" + CSRC]
+              "-I" + INCLUDE, "-I" + CSRC, "-I" + CSRC_ATTENTION]
 
 
 def nvcc():
@@ -35,7 +39,7 @@ def nvcc():
 
 
 def _inputs():
-    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
+    files = [os.path.join(d, f) for d in (CSRC, CSRC_ATTENTION) for f in os.listdir(d)]
     files.append(os.path.join(INCLUDE, "headguard.h"))
     files.append(os.path.abspath(__file__))
     return files
@@ -49,8 +53,8 @@ def _stale():
 
 
 def _compile(src, extra):
-    obj = os.path.join(OUT_DIR, os.path.splitext(src)[0] + ".o")
-    cmd = [nvcc()] + ARCH + NVCC_FLAGS + extra + ["-c", os.path.join(CSRC, src), "-o", obj]
+    obj = os.path.join(OUT_DIR, os.path.splitext(os.path.basename(src))[0] + ".o")
+    cmd = [nvcc()] + ARCH + NVCC_FLAGS + extra + ["-c", src, "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("nvcc failed for %s:\n%s\n%s" % (src, " ".join(cmd), res.stderr))

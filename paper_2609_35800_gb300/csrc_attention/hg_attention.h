@@ -1,0 +1,116 @@
+// Launch parameters and launchers shared by the host code and the kernels of the 16-bit caches: paged append, paged
+// decode attention and prompt attention.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "../../include/headguard.h"
+
+namespace hg {
+
+constexpr int kHeadDim = 128;
+constexpr int kMaxGroup = 16;
+constexpr int kMaxKvHeads = 64;
+constexpr size_t kAttnHeaderBytes = 512;  // workspace header: status word at byte 0, as the packed cache's has
+constexpr float kLog2e = 1.4426950408889634f;
+
+// hg_rows as the kernels take them.
+struct Rows {
+  uint16_t* data;
+  int64_t token_stride, head_stride;
+};
+inline Rows rows_of(const hg_rows& r) { return {static_cast<uint16_t*>(r.data), r.token_stride, r.head_stride}; }
+
+struct Rotation {
+  const float* table;  // null: no rotation
+  int table_len, half;  // half = rot_dim / 2
+  int interleaved;
+  int end0, end1;  // first pair of the second and of the third position; both `half` with one position a token
+  const int* positions;
+  int position_stride;  // tokens: distance between a token's first, second and third position
+};
+
+struct PagePool {
+  uint16_t *k, *v;
+  int num_pages, page_size, page_shift, heads;
+  int64_t page_stride, head_stride, token_stride;
+};
+
+struct PagesAppendParams {
+  PagePool pool;
+  Rotation rot;
+  int tokens, q_heads;
+  Rows q, k, v, q_out, k_out, v_out;
+  const int* slots;
+};
+
+struct PagesDecodeParams {
+  CUtensorMap k_map, v_map;  // see page_tensor_map
+  PagePool pool;
+  Rotation rot;
+  int batch, group;
+  int store;  // a decode step: k, v hold the new token, which is stored
+  Rows q, k, v, out;
+  const int* table;
+  int table_stride;
+  const int* lengths;
+  float* lse;
+  float scale;
+  uint32_t* status;
+  uint32_t* counters;  // [batch][heads]
+  float* partials;
+};
+
+// Prompts of one launch (they travel in its parameters).
+constexpr int kPromptsPerLaunch = 256;
+struct PromptRange {
+  int q0, q_len, k0, k_len;
+};
+struct PromptParams {
+  Rows q, k, v, out;
+  float* lse;
+  int prompts, q_heads, kv_heads, group, causal;
+  float scale;
+  uint32_t* status;
+  PromptRange range[kPromptsPerLaunch];
+};
+
+cudaError_t launch_pages_append(const PagesAppendParams& p, bool f16, cudaStream_t s);
+cudaError_t launch_pages_decode(const PagesDecodeParams& p, bool f16, cudaStream_t s);
+cudaError_t launch_prompt(const PromptParams& p, bool f16, cudaStream_t s);
+
+// A launch that may be scheduled while the kernel before it on the stream still runs (the kernel waits itself).
+template <class... P, class... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+                              const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// Streaming multiprocessors of the current device, looked up once per device.
+inline int device_sms() {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 152;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 152;
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+}  // namespace hg

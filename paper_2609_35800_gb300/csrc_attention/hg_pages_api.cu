@@ -1,0 +1,267 @@
+// C ABI of the 16-bit caches: page pools, append, paged decode attention, prompt attention.  Every argument is checked
+// here, on the host, before anything is enqueued.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "hg_attention.h"
+
+struct hg_pages {
+  hg::PagePool pool;
+  int dtype;
+};
+
+namespace {
+
+using namespace hg;
+
+constexpr int64_t kMaxStride = int64_t(1) << 38;  // elements; a tensor map's strides are below 2^40 bytes
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+hg_status of_cuda(cudaError_t e) { return e == cudaSuccess ? HG_OK : HG_ERR_CUDA; }
+
+// One set of rows: present, aligned, strides in range.
+hg_status check_rows(const hg_rows& r) {
+  if (!r.data || r.token_stride < 0 || r.head_stride < 0 || r.token_stride >= kMaxStride || r.head_stride >= kMaxStride)
+    return HG_ERR_INVALID_ARG;
+  return aligned16(r.data) && r.token_stride % 8 == 0 && r.head_stride % 8 == 0 ? HG_OK : HG_ERR_ALIGNMENT;
+}
+
+hg_status check_all(std::initializer_list<const hg_rows*> rows) {
+  hg_status first = HG_OK;
+  for (const hg_rows* r : rows) {
+    const hg_status st = check_rows(*r);
+    if (st == HG_ERR_INVALID_ARG) return st;
+    if (first == HG_OK) first = st;
+  }
+  return first;
+}
+
+hg_status check_rotation(const hg_rotation* r, const int32_t* positions) {
+  if (!r) return HG_OK;
+  if (!r->table || !positions || r->table_len < 1 || r->interleaved < 0 || r->interleaved > 1) return HG_ERR_INVALID_ARG;
+  if (!aligned16(r->table) || !aligned4(positions)) return HG_ERR_ALIGNMENT;
+  if (r->rot_dim < 16 || r->rot_dim > kHeadDim || r->rot_dim % 16 != 0) return HG_ERR_UNSUPPORTED;
+  const int32_t* s = r->sections;
+  if (s[0] < 0 || s[1] < 0 || s[2] < 0) return HG_ERR_INVALID_ARG;
+  if (s[0] || s[1] || s[2]) {
+    if (s[0] > 64 || s[1] > 64 || s[2] > 64 || s[0] + s[1] + s[2] != r->rot_dim / 2) return HG_ERR_INVALID_ARG;
+    if (s[0] % 8 || s[1] % 8 || s[2] % 8) return HG_ERR_UNSUPPORTED;
+  }
+  return HG_OK;
+}
+
+Rotation rotation_of(const hg_rotation* r, const int32_t* positions, int tokens) {
+  Rotation o = {};
+  if (!r) return o;
+  o.table = r->table;
+  o.table_len = r->table_len;
+  o.half = r->rot_dim / 2;
+  o.interleaved = r->interleaved;
+  const bool three = r->sections[0] || r->sections[1] || r->sections[2];
+  o.end0 = three ? r->sections[0] : o.half;
+  o.end1 = three ? r->sections[0] + r->sections[1] : o.half;
+  o.positions = positions;
+  o.position_stride = three ? tokens : 0;
+  return o;
+}
+
+float scale_of(float softmax_scale) { return softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)kHeadDim); }
+
+size_t decode_workspace_bytes(const hg_pages* p, int batch) {
+  return kAttnHeaderBytes + (((size_t)batch * p->pool.heads * sizeof(uint32_t) + 255) & ~size_t(255));
+}
+
+hg_status decode_batch_ok(const hg_pages* p, int32_t batch, int32_t num_q_heads) {
+  if (!p || batch < 0 || num_q_heads < 1 || num_q_heads % p->pool.heads != 0) return HG_ERR_INVALID_ARG;
+  if (num_q_heads / p->pool.heads > kMaxGroup || batch > (1 << 20)) return HG_ERR_UNSUPPORTED;
+  return HG_OK;
+}
+
+hg_status pages_decode(const hg_pages* pages, int32_t batch, int32_t num_q_heads, const hg_attention_io* io,
+                       const hg_rotation* rotation, const int32_t* positions, const int32_t* page_table,
+                       int32_t table_stride, const int32_t* lengths, float* lse, float softmax_scale, void* ws,
+                       size_t ws_bytes, bool store, cudaStream_t stream) {
+  hg_status st = decode_batch_ok(pages, batch, num_q_heads);
+  if (st != HG_OK) return st;
+  if (!io || table_stride < 0 || !(softmax_scale == softmax_scale)) return HG_ERR_INVALID_ARG;
+  if (batch == 0) return HG_OK;
+  if ((table_stride > 0 && !page_table) || !lengths || !ws) return HG_ERR_INVALID_ARG;
+  if ((int64_t)table_stride * pages->pool.page_size > INT32_MAX) return HG_ERR_UNSUPPORTED;
+  st = store ? check_all({&io->q, &io->k, &io->v, &io->out}) : check_all({&io->q, &io->out});
+  if (st != HG_OK) return st;
+  st = check_rotation(rotation, positions);
+  if (st != HG_OK) return st;
+  if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(lse) || !aligned16(ws)) return HG_ERR_ALIGNMENT;
+  if (ws_bytes < decode_workspace_bytes(pages, batch)) return HG_ERR_WORKSPACE_TOO_SMALL;
+  PagesDecodeParams p;
+  std::memset(&p, 0, sizeof p);
+  p.pool = pages->pool;
+  p.rot = rotation_of(rotation, positions, batch);
+  p.batch = batch;
+  p.group = num_q_heads / pages->pool.heads;
+  p.store = store ? 1 : 0;
+  p.q = rows_of(io->q);
+  p.out = rows_of(io->out);
+  if (store) {
+    p.k = rows_of(io->k);
+    p.v = rows_of(io->v);
+  }
+  p.table = page_table;
+  p.table_stride = table_stride;
+  p.lengths = lengths;
+  p.lse = lse;
+  p.scale = scale_of(softmax_scale);
+  char* w = static_cast<char*>(ws);
+  p.status = reinterpret_cast<uint32_t*>(w);
+  p.counters = reinterpret_cast<uint32_t*>(w + kAttnHeaderBytes);
+  return of_cuda(launch_pages_decode(p, pages->dtype == HG_DTYPE_F16, stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+hg_status hg_pages_create(const hg_page_shape* s, void* k_pages, void* v_pages, hg_pages** out) {
+  if (!s || !k_pages || !v_pages || !out) return HG_ERR_INVALID_ARG;
+  if (s->dtype != HG_DTYPE_BF16 && s->dtype != HG_DTYPE_F16) return HG_ERR_INVALID_ARG;
+  if (s->num_pages < 1 || s->num_kv_heads < 1 || s->page_size < 1) return HG_ERR_INVALID_ARG;
+  if (s->page_stride < 0 || s->head_stride < 0 || s->token_stride < 0) return HG_ERR_INVALID_ARG;
+  if (s->head_dim != kHeadDim || s->num_kv_heads > kMaxKvHeads) return HG_ERR_UNSUPPORTED;
+  if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1))) return HG_ERR_UNSUPPORTED;
+  if ((int64_t)s->num_pages * s->page_size > INT32_MAX) return HG_ERR_UNSUPPORTED;
+  int64_t token = s->token_stride, head = s->head_stride, page = s->page_stride;
+  if (token == 0 && head == 0 && page == 0) {
+    token = kHeadDim;
+    head = token * s->page_size;
+    page = head * s->num_kv_heads;
+  }
+  if (token < kHeadDim || (s->num_kv_heads > 1 && head < kHeadDim) || (s->num_pages > 1 && page < kHeadDim))
+    return HG_ERR_INVALID_ARG;
+  if (token >= kMaxStride || head >= kMaxStride || page >= kMaxStride) return HG_ERR_UNSUPPORTED;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || token % 8 || head % 8 || page % 8) return HG_ERR_ALIGNMENT;
+  hg_pages* p = new (std::nothrow) hg_pages();
+  if (!p) return HG_ERR_CUDA;
+  int shift = 0;
+  while ((1 << shift) < s->page_size) ++shift;
+  p->pool = {static_cast<uint16_t*>(k_pages), static_cast<uint16_t*>(v_pages), s->num_pages, s->page_size, shift,
+             s->num_kv_heads, page, head, token};
+  p->dtype = s->dtype;
+  *out = p;
+  return HG_OK;
+}
+
+void hg_pages_destroy(hg_pages* pages) { delete pages; }
+
+hg_status hg_pages_append(const hg_pages* pages, int32_t num_tokens, int32_t num_q_heads, const hg_append_io* io,
+                          const hg_rotation* rotation, const int32_t* positions, const int32_t* slots,
+                          hg_stream_t stream) {
+  if (!pages || num_tokens < 0 || num_q_heads < 0 || !io) return HG_ERR_INVALID_ARG;
+  if (num_q_heads > kMaxGroup * kMaxKvHeads) return HG_ERR_UNSUPPORTED;
+  if (num_tokens == 0) return HG_OK;
+  if (!slots) return HG_ERR_INVALID_ARG;
+  const hg_rows none = io->k;  // stands in for an absent set, which is not checked
+  hg_status st = check_all({&io->k, &io->v, num_q_heads ? &io->q : &none, num_q_heads ? &io->q_out : &none,
+                            io->k_out.data ? &io->k_out : &none, io->v_out.data ? &io->v_out : &none});
+  if (st != HG_OK) return st;
+  st = check_rotation(rotation, positions);
+  if (st != HG_OK) return st;
+  if (!aligned4(slots)) return HG_ERR_ALIGNMENT;
+  PagesAppendParams p;
+  std::memset(&p, 0, sizeof p);
+  p.pool = pages->pool;
+  p.rot = rotation_of(rotation, positions, num_tokens);
+  p.tokens = num_tokens;
+  p.q_heads = num_q_heads;
+  p.q = rows_of(io->q);
+  p.k = rows_of(io->k);
+  p.v = rows_of(io->v);
+  p.q_out = rows_of(io->q_out);
+  p.k_out = rows_of(io->k_out);
+  p.v_out = rows_of(io->v_out);
+  p.slots = slots;
+  return of_cuda(launch_pages_append(p, pages->dtype == HG_DTYPE_F16, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+hg_status hg_pages_decode_workspace_size(const hg_pages* pages, int32_t batch, int32_t num_q_heads, size_t* bytes) {
+  if (!bytes) return HG_ERR_INVALID_ARG;
+  const hg_status st = decode_batch_ok(pages, batch, num_q_heads);
+  if (st != HG_OK) return st;
+  *bytes = decode_workspace_bytes(pages, batch);
+  return HG_OK;
+}
+
+hg_status hg_pages_decode_attention(const hg_pages* pages, int32_t batch, int32_t num_q_heads,
+                                    const hg_attention_io* io, const int32_t* page_table, int32_t table_stride,
+                                    const int32_t* lengths, float* lse, float softmax_scale, void* workspace,
+                                    size_t workspace_bytes, hg_stream_t stream) {
+  return pages_decode(pages, batch, num_q_heads, io, nullptr, nullptr, page_table, table_stride, lengths, lse,
+                      softmax_scale, workspace, workspace_bytes, false, reinterpret_cast<cudaStream_t>(stream));
+}
+
+hg_status hg_pages_decode_step(const hg_pages* pages, int32_t batch, int32_t num_q_heads, const hg_attention_io* io,
+                               const hg_rotation* rotation, const int32_t* positions, const int32_t* page_table,
+                               int32_t table_stride, const int32_t* lengths, float* lse, float softmax_scale,
+                               void* workspace, size_t workspace_bytes, hg_stream_t stream) {
+  return pages_decode(pages, batch, num_q_heads, io, rotation, positions, page_table, table_stride, lengths, lse,
+                      softmax_scale, workspace, workspace_bytes, true, reinterpret_cast<cudaStream_t>(stream));
+}
+
+hg_status hg_prompt_workspace_size(size_t* bytes) {
+  if (!bytes) return HG_ERR_INVALID_ARG;
+  *bytes = kAttnHeaderBytes;
+  return HG_OK;
+}
+
+hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_heads, int32_t num_kv_heads,
+                              const hg_attention_io* io, const int32_t* q_begin, const int32_t* k_begin, float* lse,
+                              int32_t causal, float softmax_scale, void* workspace, size_t workspace_bytes,
+                              hg_stream_t stream) {
+  if ((dtype != HG_DTYPE_BF16 && dtype != HG_DTYPE_F16) || num_prompts < 0 || num_kv_heads < 1 || num_q_heads < 1 ||
+      num_q_heads % num_kv_heads != 0 || !io || causal < 0 || causal > 1 || !(softmax_scale == softmax_scale))
+    return HG_ERR_INVALID_ARG;
+  if (num_kv_heads > kMaxKvHeads || num_q_heads / num_kv_heads > kMaxGroup) return HG_ERR_UNSUPPORTED;
+  if (num_prompts == 0) return HG_OK;
+  if (!q_begin || !k_begin || q_begin[0] < 0 || k_begin[0] < 0) return HG_ERR_INVALID_ARG;
+  for (int i = 0; i < num_prompts; ++i)
+    if (q_begin[i + 1] < q_begin[i] || k_begin[i + 1] < k_begin[i]) return HG_ERR_INVALID_ARG;
+  if (q_begin[num_prompts] == q_begin[0]) return HG_OK;
+  // prompts without a key have no rows of k and v to point at
+  const bool keys = k_begin[num_prompts] > k_begin[0];
+  hg_status st = keys ? check_all({&io->q, &io->out, &io->k, &io->v}) : check_all({&io->q, &io->out});
+  if (st != HG_OK) return st;
+  if (!workspace) return HG_ERR_INVALID_ARG;
+  if (!aligned16(workspace) || !aligned4(lse)) return HG_ERR_ALIGNMENT;
+  size_t need = 0;
+  st = hg_prompt_workspace_size(&need);
+  if (st != HG_OK) return st;
+  if (workspace_bytes < need) return HG_ERR_WORKSPACE_TOO_SMALL;
+  for (int done = 0; done < num_prompts; done += kPromptsPerLaunch) {
+    const int n = std::min(kPromptsPerLaunch, num_prompts - done);
+    PromptParams p;
+    std::memset(&p, 0, sizeof p);
+    p.q = rows_of(io->q);
+    p.k = rows_of(io->k);
+    p.v = rows_of(io->v);
+    p.out = rows_of(io->out);
+    p.lse = lse;
+    p.prompts = n;
+    p.q_heads = num_q_heads;
+    p.kv_heads = num_kv_heads;
+    p.group = num_q_heads / num_kv_heads;
+    p.causal = causal;
+    p.scale = scale_of(softmax_scale);
+    p.status = static_cast<uint32_t*>(workspace);
+    for (int i = 0; i < n; ++i) {
+      const int j = done + i;
+      p.range[i] = {q_begin[j], q_begin[j + 1] - q_begin[j], k_begin[j], k_begin[j + 1] - k_begin[j]};
+    }
+    st = of_cuda(launch_prompt(p, dtype == HG_DTYPE_F16, reinterpret_cast<cudaStream_t>(stream)));
+    if (st != HG_OK) return st;
+  }
+  return HG_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,82 @@
+"""A serving program's 16-bit requests, put together: prompts packed into one call, their keys rotated and stored in
+pages, then tokens one step at a time.  Allocation and marshalling only -- every step runs in the library."""
+import torch
+
+from . import (Pages, hg_pages_append, hg_pages_create, hg_pages_decode_step, hg_pages_decode_workspace_size,
+               hg_prompt_attention, hg_prompt_workspace_size, hg_workspace_clear)
+
+__all__ = ["PagedRunner", "Pages"]
+
+
+class PagedRunner:
+    """Requests of one attention layer that share a page pool: `admit` prompts, `step` them, `release` them."""
+
+    def __init__(self, num_pages, page_size, q_heads, kv_heads, rotation=None, dtype=torch.bfloat16, device="cuda",
+                 max_batch=64, max_tokens=32768):
+        self.page_size, self.q_heads, self.kv_heads = page_size, q_heads, kv_heads
+        self.rotation, self.dtype, self.device = rotation, dtype, device
+        self.k_pages = torch.empty(num_pages, kv_heads, page_size, 128, dtype=dtype, device=device)
+        self.v_pages = torch.empty_like(self.k_pages)
+        self.pages = hg_pages_create(self.k_pages, self.v_pages)
+        self.free = list(range(num_pages - 1, -1, -1))
+        self.owned, self.lengths = [], []  # pages and tokens of each request, on the host
+        self.per_request = -(-max_tokens // page_size)
+        self.table = torch.zeros(max_batch, self.per_request, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(max_batch, dtype=torch.int32, device=device)
+        self.ws = torch.empty(max(hg_pages_decode_workspace_size(self.pages, max_batch, q_heads),
+                                  hg_prompt_workspace_size()), dtype=torch.uint8, device=device)
+        hg_workspace_clear(self.ws)
+
+    def _grow(self, request, tokens):
+        need = -(-tokens // self.page_size)
+        if need > self.per_request or need - len(self.owned[request]) > len(self.free):
+            raise RuntimeError("no page left for request %d" % request)
+        while len(self.owned[request]) < need:
+            page = self.free.pop()
+            self.table[request, len(self.owned[request])] = page
+            self.owned[request].append(page)
+        self.lengths[request] = tokens
+
+    def admit(self, q, k, v, prompt_lengths, positions, k_out=None, v_out=None):
+        """Prompts one after the other, q / k / v [tokens][heads][128] not yet rotated: their attention
+        [tokens][q_heads][128].  k_out / v_out: where the rotated keys and the values go as dense tensors as well (a
+        request that goes on in the packed cache takes hg_quantize_kv's layout from there)."""
+        first = len(self.owned)
+        if first + len(prompt_lengths) > self.table.shape[0]:
+            raise RuntimeError("more requests than the batch holds")
+        slots = []
+        for i, n in enumerate(prompt_lengths):
+            self.owned.append([])
+            self.lengths.append(0)
+            self._grow(first + i, n)
+            at = torch.arange(n)
+            pages = torch.tensor(self.owned[first + i], dtype=torch.int64)
+            slots.append(pages[at // self.page_size] * self.page_size + at % self.page_size)
+        slots = torch.cat(slots).to(torch.int32).to(self.device)
+        self.lens[first:first + len(prompt_lengths)] = torch.tensor(prompt_lengths, dtype=torch.int32)
+        q_rot = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=self.dtype, device=self.device)
+        hg_pages_append(self.pages, q, k, v, self.rotation, positions, slots, q_rot, k_out, v_out)
+        begin = torch.tensor([0] + list(prompt_lengths)).cumsum(0).to(torch.int32)
+        out = torch.empty_like(q_rot)
+        hg_prompt_attention(q_rot, k_out, v, begin, begin, out, None, True, 0.0, self.ws)
+        return out
+
+    def step(self, q, k, v, positions):
+        """One new token of every request: q [requests][q_heads][128], k, v [requests][kv_heads][128]."""
+        n = len(self.owned)
+        for i in range(n):
+            self._grow(i, self.lengths[i] + 1)
+        self.lens[:n] += 1
+        out = torch.empty(n, self.q_heads, 128, dtype=self.dtype, device=self.device)
+        hg_pages_decode_step(self.pages, q, k, v, self.rotation, positions, self.table[:n], self.lens, out, None, 0.0,
+                             self.ws)
+        return out
+
+    def release(self):
+        """Every request ends; its pages are free again."""
+        for pages in self.owned:
+            self.free.extend(reversed(pages))
+        self.owned, self.lengths = [], []
+        self.lens.zero_()
