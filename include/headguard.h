@@ -421,7 +421,7 @@ typedef struct hg_pages hg_pages;
 /* Descriptor of the pool whose keys start at k_pages and values at v_pages
  * (device, 16-byte aligned, the same geometry).  The entries need no
  * initialisation: what lies in a page beyond a request's length is never used,
- * whatever its bits.  Encodes two tensor maps (no device work). */
+ * whatever its bits.  Host only; no CUDA call. */
 hg_status hg_pages_create(const hg_page_shape *shape, void *k_pages, void *v_pages, hg_pages **out);
 void hg_pages_destroy(hg_pages *pages);
 

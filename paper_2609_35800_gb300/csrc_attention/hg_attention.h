@@ -47,8 +47,13 @@ struct PagesAppendParams {
   const int* slots;
 };
 
+// Tokens of a tile of the paged decode; a tensor map's box covers a tile of one page, or the page where that is smaller.
+constexpr int kDecodeTile = 64;
+// A query's part in the workspace: m, l, two unused, 128 channels.
+constexpr int kPartialFloats = kHeadDim + 4;
+
 struct PagesDecodeParams {
-  CUtensorMap k_map, v_map;  // see page_tensor_map
+  CUtensorMap k_map, v_map;  // the pool as [pages][heads][2][page_size][64 channels]
   PagePool pool;
   Rotation rot;
   int batch, group;
@@ -112,5 +117,8 @@ inline int device_sms() {
   }
   return n;
 }
+
+// CTAs of a paged decode launch: two to an SM.
+inline int decode_ctas() { return 2 * device_sms(); }
 
 }  // namespace hg

@@ -3,13 +3,20 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <mutex>
 #include <new>
+
+#include <cudaTypedefs.h>
 
 #include "hg_attention.h"
 
 struct hg_pages {
   hg::PagePool pool;
   int dtype;
+  // tensor maps, encoded by the first decode call
+  std::mutex mutex;
+  std::atomic<bool> mapped{false};
+  CUtensorMap k_map, v_map;
 };
 
 namespace {
@@ -70,8 +77,54 @@ Rotation rotation_of(const hg_rotation* r, const int32_t* positions, int tokens)
 
 float scale_of(float softmax_scale) { return softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)kHeadDim); }
 
+// cuTensorMapEncodeTiled through the runtime (no link against the driver library).
+PFN_cuTensorMapEncodeTiled_v12000 map_encoder() {
+  static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> cached{nullptr};
+  PFN_cuTensorMapEncodeTiled_v12000 fn = cached.load(std::memory_order_acquire);
+  if (!fn) {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+    cached.store(fn, std::memory_order_release);
+  }
+  return fn;
+}
+
+// A page pool as [pages][heads][2][page_size][64]: both halves of a row's channels as rows of 128 bytes, the span of
+// the swizzle.  A box is a tile's tokens of one page and head: first halves, then second halves.
+CUresult encode_pages(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map, void* data, const PagePool& p, bool f16) {
+  const cuuint64_t dims[5] = {64, (cuuint64_t)p.page_size, 2, (cuuint64_t)p.heads, (cuuint64_t)p.num_pages};
+  // the stride of an axis of length 1 is never taken
+  const cuuint64_t strides[4] = {(cuuint64_t)p.token_stride * 2, 128, p.heads > 1 ? (cuuint64_t)p.head_stride * 2 : 256,
+                                 p.num_pages > 1 ? (cuuint64_t)p.page_stride * 2 : 256};
+  const cuuint32_t box[5] = {64, (cuuint32_t)std::min(p.page_size, kDecodeTile), 2, 1, 1};
+  const cuuint32_t steps[5] = {1, 1, 1, 1, 1};
+  return encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, data, dims, strides, box,
+                steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+hg_status map_pages(hg_pages* p) {
+  if (p->mapped.load(std::memory_order_acquire)) return HG_OK;
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
+  if (!encode) return HG_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(p->mutex);
+  if (p->mapped.load(std::memory_order_relaxed)) return HG_OK;
+  const bool f16 = p->dtype == HG_DTYPE_F16;
+  if (encode_pages(encode, &p->k_map, p->pool.k, p->pool, f16) != CUDA_SUCCESS ||
+      encode_pages(encode, &p->v_map, p->pool.v, p->pool, f16) != CUDA_SUCCESS)
+    return HG_ERR_CUDA;
+  p->mapped.store(true, std::memory_order_release);
+  return HG_OK;
+}
+
+// Decode workspace: header, the parts that CTAs leave (two each, at the largest group whatever the call's, so that the
+// counters behind them lie at one place for every call), a counter per (request, KV head).
+size_t decode_parts_bytes() { return (size_t)decode_ctas() * 2 * kMaxGroup * kPartialFloats * sizeof(float); }
 size_t decode_workspace_bytes(const hg_pages* p, int batch) {
-  return kAttnHeaderBytes + (((size_t)batch * p->pool.heads * sizeof(uint32_t) + 255) & ~size_t(255));
+  return kAttnHeaderBytes + decode_parts_bytes() + (((size_t)batch * p->pool.heads * sizeof(uint32_t) + 255) & ~size_t(255));
 }
 
 hg_status decode_batch_ok(const hg_pages* p, int32_t batch, int32_t num_q_heads) {
@@ -96,8 +149,12 @@ hg_status pages_decode(const hg_pages* pages, int32_t batch, int32_t num_q_heads
   if (st != HG_OK) return st;
   if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(lse) || !aligned16(ws)) return HG_ERR_ALIGNMENT;
   if (ws_bytes < decode_workspace_bytes(pages, batch)) return HG_ERR_WORKSPACE_TOO_SMALL;
+  st = map_pages(const_cast<hg_pages*>(pages));
+  if (st != HG_OK) return st;
   PagesDecodeParams p;
   std::memset(&p, 0, sizeof p);
+  p.k_map = pages->k_map;
+  p.v_map = pages->v_map;
   p.pool = pages->pool;
   p.rot = rotation_of(rotation, positions, batch);
   p.batch = batch;
@@ -116,7 +173,8 @@ hg_status pages_decode(const hg_pages* pages, int32_t batch, int32_t num_q_heads
   p.scale = scale_of(softmax_scale);
   char* w = static_cast<char*>(ws);
   p.status = reinterpret_cast<uint32_t*>(w);
-  p.counters = reinterpret_cast<uint32_t*>(w + kAttnHeaderBytes);
+  p.partials = reinterpret_cast<float*>(w + kAttnHeaderBytes);
+  p.counters = reinterpret_cast<uint32_t*>(w + kAttnHeaderBytes + decode_parts_bytes());
   return of_cuda(launch_pages_decode(p, pages->dtype == HG_DTYPE_F16, stream));
 }
 

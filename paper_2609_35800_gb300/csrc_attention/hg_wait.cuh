@@ -1,0 +1,50 @@
+// Bounded waits and shared-memory addresses of the asynchronous kernels.
+#pragma once
+#include "hg_mma.cuh"
+
+namespace hg {
+
+constexpr uint32_t kWaitTimeoutBit = 1;    // status word: a wait ran out
+constexpr uint32_t kAsyncRounds = 20000;   // rounds of up to kAsyncSleepNs each: about a second
+constexpr uint32_t kAsyncSleepNs = 50000;
+
+// Wait for a phase of `bar`.  One that runs out flags the workspace's status word and *abort, by which every other
+// wait of the CTA ends too, and returns false: the caller leaves its work.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
+  for (uint32_t i = 0; i < kAsyncRounds; ++i) {
+    if (mbar_try_wait_sleep(bar, parity, kAsyncSleepNs)) return true;
+    if (*abort) return false;
+  }
+  *abort = 1;
+  atomicOr(status, kWaitTimeoutBit);
+  return false;
+}
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
+}
+
+template <int THREADS>
+__device__ __forceinline__ void named_barrier(int id) {
+  asm volatile("bar.sync %0, %1;\n" ::"r"(id), "n"(THREADS) : "memory");
+}
+
+// Byte offset of 16-byte chunk `chunk` of row r in rows of 128 bytes under the 128-byte swizzle (base 1024-aligned).
+__device__ __forceinline__ uint32_t swizzled(int r, int chunk) { return (uint32_t)(r * 128 + ((chunk ^ (r & 7)) << 4)); }
+
+__device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+
+}  // namespace hg
