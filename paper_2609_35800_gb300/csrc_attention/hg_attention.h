@@ -74,13 +74,25 @@ constexpr int kPromptsPerLaunch = 256;
 struct PromptRange {
   int q0, q_len, k0, k_len;
 };
+constexpr int kPromptBlock = 128;  // keys of a block
+// An item's part in the workspace: M, r, l of its 256 rows, then their 128 channels.
+constexpr int kPromptPartFloats = 3 * 256 + 256 * kHeadDim;
+constexpr int kPromptParts = 608;
 struct PromptParams {
-  Rows q, k, v, out;
+  CUtensorMap q_map, k_map, v_map;  // [tokens][heads][128] (q), [heads][tokens][128]: boxes of 64 channels
+  Rows out;
   float* lse;
   int prompts, q_heads, kv_heads, group, causal;
+  int tile_tokens;  // tokens of a tile: 128 / group
+  int items;        // work items: pieces, tile pairs and KV heads of every prompt
+  int chunk;        // key blocks of a piece
+  int split;        // some item has several pieces
   float scale;
   uint32_t* status;
-  PromptRange range[kPromptsPerLaunch];
+  uint32_t* counters;  // items taken, CTAs that have finished; zero between launches
+  float* parts;
+  PromptRange range[kPromptsPerLaunch];     // longest first
+  int first_unit[kPromptsPerLaunch];  // (piece, tile pair) number of each prompt's first
 };
 
 cudaError_t launch_pages_append(const PagesAppendParams& p, bool f16, cudaStream_t s);

@@ -23,6 +23,8 @@ namespace {
 
 using namespace hg;
 
+constexpr double kPromptSplitGain = 8;  // blocks by which the longest item has to pass the even share
+constexpr int kPromptLeastChunk = 4;
 constexpr int64_t kMaxStride = int64_t(1) << 38;  // elements; a tensor map's strides are below 2^40 bytes
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -104,6 +106,70 @@ CUresult encode_pages(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map
   return encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, data, dims, strides, box,
                 steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+// Rows of a prompt's tensor: [a][b][128] in boxes of box_a x box_b x 64 channels.
+CUresult encode_rows(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map, void* data, int a, int64_t stride_a, int box_a,
+                     int b, int64_t stride_b, int box_b, bool f16) {
+  const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)b, (cuuint64_t)a};
+  const cuuint64_t strides[2] = {b > 1 ? (cuuint64_t)stride_b * 2 : 256, a > 1 ? (cuuint64_t)stride_a * 2 : 256};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_b, (cuuint32_t)box_a};
+  const cuuint32_t steps[3] = {1, 1, 1};
+  return encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, data, dims, strides, box,
+                steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+// A stride that is taken has to reach past the row (a tensor map has no broadcast axis).
+bool rows_mappable(const hg_rows& r, int tokens, int heads) {
+  return (tokens <= 1 || r.token_stride >= kHeadDim) && (heads <= 1 || r.head_stride >= kHeadDim);
+}
+
+// Pieces, tile pairs and heads of the launch's prompts, in blocks of kPromptBlock keys a piece at most `chunk`.
+int64_t count_items(PromptParams* p) {
+  int64_t units = 0;
+  for (int i = 0; i < p->prompts; ++i) {
+    const PromptRange& r = p->range[i];
+    p->first_unit[i] = (int)std::min<int64_t>(units, INT32_MAX);
+    const int64_t tiles = (r.q_len + 2 * p->tile_tokens - 1) / (2 * p->tile_tokens);
+    const int64_t blocks = (r.k_len + kPromptBlock - 1) / kPromptBlock;
+    units += tiles * std::max<int64_t>(1, (blocks + p->chunk - 1) / p->chunk);
+  }
+  return units * p->kv_heads;
+}
+
+// How the launch's keys are cut.  Uncut, the launch lasts as long as its longest item at least; cut, as long as the
+// SMs' even share of all blocks, and the parts' way through memory besides (a few blocks' time).
+hg_status plan_prompts(PromptParams* p) {
+  p->tile_tokens = 128 / p->group;
+  std::stable_sort(p->range, p->range + p->prompts, [](const PromptRange& a, const PromptRange& b) { return a.k_len > b.k_len; });
+  p->chunk = INT32_MAX / 2;
+  int64_t items = count_items(p);
+  double blocks = 0.;
+  for (int i = 0; i < p->prompts; ++i) {
+    const PromptRange& r = p->range[i];
+    const double keys = p->causal ? std::max(r.k_len - 0.5 * r.q_len, 0.5 * r.k_len) : r.k_len;
+    blocks += ((r.q_len + 2 * p->tile_tokens - 1) / (2 * p->tile_tokens)) * (keys / kPromptBlock);
+  }
+  const double share = blocks * p->kv_heads / device_sms();
+  const int longest = (p->range[0].k_len + kPromptBlock - 1) / kPromptBlock;
+  if (longest > share + kPromptSplitGain) {
+    for (int chunk = std::max((int)share + 1, kPromptLeastChunk); chunk < longest; chunk *= 2) {
+      p->chunk = chunk;
+      items = count_items(p);
+      if (items <= kPromptParts) {
+        p->split = 1;
+        break;
+      }
+    }
+    if (!p->split) {
+      p->chunk = INT32_MAX / 2;
+      items = count_items(p);
+    }
+  }
+  if (items * 8 > INT32_MAX) return HG_ERR_UNSUPPORTED;
+  p->items = (int)items;
+  return HG_OK;
 }
 
 hg_status map_pages(hg_pages* p) {
@@ -269,7 +335,7 @@ hg_status hg_pages_decode_step(const hg_pages* pages, int32_t batch, int32_t num
 
 hg_status hg_prompt_workspace_size(size_t* bytes) {
   if (!bytes) return HG_ERR_INVALID_ARG;
-  *bytes = kAttnHeaderBytes;
+  *bytes = kAttnHeaderBytes + (size_t)kPromptParts * kPromptPartFloats * sizeof(float);
   return HG_OK;
 }
 
@@ -290,33 +356,51 @@ hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_
   const bool keys = k_begin[num_prompts] > k_begin[0];
   hg_status st = keys ? check_all({&io->q, &io->out, &io->k, &io->v}) : check_all({&io->q, &io->out});
   if (st != HG_OK) return st;
+  const int rows = q_begin[num_prompts], key_rows = k_begin[num_prompts];
+  if (!rows_mappable(io->q, rows, num_q_heads) ||
+      (keys && (!rows_mappable(io->k, key_rows, num_kv_heads) || !rows_mappable(io->v, key_rows, num_kv_heads))))
+    return HG_ERR_UNSUPPORTED;
   if (!workspace) return HG_ERR_INVALID_ARG;
   if (!aligned16(workspace) || !aligned4(lse)) return HG_ERR_ALIGNMENT;
   size_t need = 0;
   st = hg_prompt_workspace_size(&need);
   if (st != HG_OK) return st;
   if (workspace_bytes < need) return HG_ERR_WORKSPACE_TOO_SMALL;
+  PromptParams p;
+  std::memset(&p, 0, sizeof p);
+  p.out = rows_of(io->out);
+  p.lse = lse;
+  p.q_heads = num_q_heads;
+  p.kv_heads = num_kv_heads;
+  p.group = num_q_heads / num_kv_heads;
+  p.causal = causal;
+  p.scale = scale_of(softmax_scale);
+  char* w = static_cast<char*>(workspace);
+  p.status = reinterpret_cast<uint32_t*>(w);
+  p.counters = reinterpret_cast<uint32_t*>(w + 256);
+  p.parts = reinterpret_cast<float*>(w + kAttnHeaderBytes);
+  const bool f16 = dtype == HG_DTYPE_F16;
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
+  if (!encode ||
+      encode_rows(encode, &p.q_map, io->q.data, rows, io->q.token_stride, 128 / p.group, num_q_heads, io->q.head_stride,
+                  p.group, f16) != CUDA_SUCCESS)
+    return HG_ERR_CUDA;
+  if (keys && (encode_rows(encode, &p.k_map, io->k.data, num_kv_heads, io->k.head_stride, 1, key_rows, io->k.token_stride,
+                           kPromptBlock, f16) != CUDA_SUCCESS ||
+               encode_rows(encode, &p.v_map, io->v.data, num_kv_heads, io->v.head_stride, 1, key_rows, io->v.token_stride,
+                           kPromptBlock, f16) != CUDA_SUCCESS))
+    return HG_ERR_CUDA;
   for (int done = 0; done < num_prompts; done += kPromptsPerLaunch) {
     const int n = std::min(kPromptsPerLaunch, num_prompts - done);
-    PromptParams p;
-    std::memset(&p, 0, sizeof p);
-    p.q = rows_of(io->q);
-    p.k = rows_of(io->k);
-    p.v = rows_of(io->v);
-    p.out = rows_of(io->out);
-    p.lse = lse;
-    p.prompts = n;
-    p.q_heads = num_q_heads;
-    p.kv_heads = num_kv_heads;
-    p.group = num_q_heads / num_kv_heads;
-    p.causal = causal;
-    p.scale = scale_of(softmax_scale);
-    p.status = static_cast<uint32_t*>(workspace);
+    p.prompts = p.split = 0;
     for (int i = 0; i < n; ++i) {
       const int j = done + i;
-      p.range[i] = {q_begin[j], q_begin[j + 1] - q_begin[j], k_begin[j], k_begin[j + 1] - k_begin[j]};
+      if (q_begin[j + 1] > q_begin[j])  // a prompt without a query has nothing to write
+        p.range[p.prompts++] = {q_begin[j], q_begin[j + 1] - q_begin[j], k_begin[j], k_begin[j + 1] - k_begin[j]};
     }
-    st = of_cuda(launch_prompt(p, dtype == HG_DTYPE_F16, reinterpret_cast<cudaStream_t>(stream)));
+    if (p.prompts == 0) continue;
+    st = plan_prompts(&p);
+    if (st == HG_OK) st = of_cuda(launch_prompt(p, f16, reinterpret_cast<cudaStream_t>(stream)));
     if (st != HG_OK) return st;
   }
   return HG_OK;

@@ -1,40 +1,562 @@
-// Attention of packed prompts.
-#include "hg_simple.cuh"
+// Attention of packed prompts on the fifth-generation tensor cores.
+//
+// For a prompt's query row: s_t = scale q.k_t over the keys it sees, m = max s_t, out = sum e^(s_t - m) v_t / sum
+// e^(s_t - m).  4 * 128 flop a (query head, key) pair: from about a thousand keys on the kernel is bound by the tensor
+// cores, or by the exponentials, of which there is one for 512 flop.
+//
+// A work item is two tiles of 128 rows of one prompt and KV head.  A tile's rows are 128 / G consecutive tokens times
+// the G query heads of the KV head, so short prompts fill their tiles and a causal tile spans few tokens; both tiles use
+// every key block that is loaded.  One persistent CTA per SM takes items from a counter, longest first; its warps:
+//   warp 9      loads: the items' queries, then 128-key blocks of K and V into a ring, by TMA (128-byte swizzle)
+//   warp 8      issues the products: S = Q K^T into tensor memory, then O += P V with P read from tensor memory
+//   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a thread to a row: S out of tensor memory, P back over it (so a
+//               tile's next S follows its P V), O scaled there when a maximum moves, written out at the end
+// While one tile's softmax runs the tensor cores work on the other tile.  Tensor memory: S 2 x 128 columns, O 2 x 128.
+//
+// Scores, maxima, sums and O are held in 32 bits; P is rounded to the inputs' type for the second product.  The running
+// maximum moves when a score passes it by more than 2^8, which bounds P by 256 and makes changes of O rare.
+// Where the items are fewer than the SMs can share (few rows over long keys), an item's keys are cut into pieces whose
+// (m, l, O) go to the workspace, and a second kernel joins them.
+#include <algorithm>
+
+#include "hg_rows.cuh"
+#include "hg_tcgen05.cuh"
 
 namespace hg {
 namespace {
 
+constexpr int kBlock = kPromptBlock;        // keys of a block
+constexpr int kTileRows = 128;
+constexpr int kHalfBytes = 128 * 128;       // 64 channels of 128 rows
+constexpr int kTileBytes = 2 * kHalfBytes;  // a tile of queries, a block of keys or of values
+constexpr int kStages = 5;
+constexpr int kThreads = 320;
+constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr float kRescale = 8.0f;
+constexpr uint32_t kScoreColumn = 0, kOutColumn = 256;  // + 128 for tile 1
+constexpr unsigned kAll = 0xffffffffu;
+
+// Shared memory from a 1024-byte boundary.
+constexpr int kQueryOffset = 0;
+constexpr int kRingOffset = 2 * kTileBytes;
+constexpr int kBarOffset = kRingOffset + kStages * kTileBytes;
+constexpr int kSmemBytes = kBarOffset + 512 + 1024;
+enum Bar { kQueryFull = 0, kQueryFree, kScoreFull, kProbFull = kScoreFull + 2, kOutFull = kProbFull + 2,
+           kItemFull = kOutFull + 2, kItemFree = kItemFull + 2, kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages,
+           kBars = kRingFree + kStages };
+constexpr int kItemOffset = kBarOffset + 256;  // two Items
+constexpr int kMiscOffset = kItemOffset + 2 * 64;  // abort flag, tensor memory address
+static_assert(kBars * 8 <= 256, "barriers");
+
+struct Item {
+  int q0;         // first query row (token of the tensors) of the prompt
+  int tok0;       // first token of tile 0, in the prompt
+  int q_len, k_len, k0;
+  int head;       // KV head
+  int first;      // first key block
+  int n[2];       // key blocks of each tile from `first` on
+  int width[2];   // keys of the last of them that some row sees
+  int slot;       // where the item's part goes; -1: the item is whole
+  int slot_step;  // from a piece's slot to the next one's
+  int none;       // no further item
+};
+static_assert(sizeof(Item) <= 64, "items");
+
+__device__ __forceinline__ int seen_by(const PromptParams& p, int q_len, int k_len, int tok) {
+  return p.causal ? min(max(tok + 1 + k_len - q_len, 0), k_len) : k_len;
+}
+
+// Item number -> work: prompt by prompt (longest first), piece by piece, tile pair by tile pair (last tokens first), heads
+// innermost.  False: the piece holds no key of its tiles.
+__device__ bool item_at(const PromptParams& p, int index, Item& it) {
+  const int head = index % p.kv_heads, unit = index / p.kv_heads;
+  int lo = 0, hi = p.prompts;  // the prompt that holds the unit
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (p.first_unit[mid] <= unit) lo = mid;
+    else hi = mid;
+  }
+  const PromptRange r = p.range[lo];
+  const int tiles = (r.q_len + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens), local = unit - p.first_unit[lo];
+  const int piece = local / tiles, tile = local - piece * tiles;
+  it.q0 = r.q0;
+  it.q_len = r.q_len;
+  it.k0 = r.k0;
+  it.k_len = r.k_len;
+  it.tok0 = (tiles - 1 - tile) * 2 * p.tile_tokens;
+  it.head = head;
+  it.first = piece * p.chunk;
+  it.none = 0;
+  int blocks = 0;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int from = it.tok0 + t * p.tile_tokens, to = min(from + p.tile_tokens, r.q_len) - 1;  // the last row sees most
+    const int seen = from < r.q_len ? seen_by(p, r.q_len, r.k_len, to) : 0;
+    const int n = (seen + kBlock - 1) / kBlock;
+    blocks = max(blocks, n);
+    const int end = min(n, it.first + p.chunk);
+    it.n[t] = max(0, end - it.first);
+    it.width[t] = min(kBlock, seen - (end - 1) * kBlock);
+  }
+  it.slot = blocks > p.chunk ? index : -1;
+  it.slot_step = tiles * p.kv_heads;
+  return piece == 0 || blocks > it.first;
+}
+
+// Waits of a whole warp, which stays together: all of its threads go on, or none.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
+  return __all_sync(kAll, wait_phase(bar, parity, abort, status));
+}
+
+// One warp: items from the counter to the others, queries and key blocks into shared memory.  Returns the ring's fills.
+__device__ void load_items(const PromptParams& p, uint32_t base, char* smem, volatile int* misc, uint32_t& fills, uint32_t& queries) {
+  const int lane = threadIdx.x % 32;
+  const uint32_t bars = base + kBarOffset;
+  Item* items = reinterpret_cast<Item*>(smem + kItemOffset);
+  const uint32_t q_bytes = (uint32_t)p.group * p.tile_tokens * 128;
+  int index = blockIdx.x;
+  fills = queries = 0;
+  for (uint32_t n = 0;; ++n) {
+    Item it;
+    it.none = 1;
+    while (index < p.items) {
+      const bool some = item_at(p, index, it);
+      if (lane == 0) index = (int)gridDim.x + (int)atomicAdd(p.counters, 1u);
+      index = __shfl_sync(kAll, index, 0);
+      if (some) break;
+      it.none = 1;
+    }
+    const uint32_t s = n & 1;
+    if (n >= 2 && !wait_warp(bars + 8 * (kItemFree + s), ((n >> 1) - 1) & 1, misc, p.status)) return;
+    if (lane == 0) {
+      items[s] = it;
+      mbar_arrive(bars + 8 * (kItemFull + s));
+    }
+    if (it.none) return;
+    const int blocks = max(it.n[0], it.n[1]);
+    if (blocks == 0) continue;
+    if (queries > 0 && !wait_warp(bars + 8 * kQueryFree, (queries - 1) & 1, misc, p.status)) return;
+    if (lane == 0) {
+      const uint32_t bar = bars + 8 * kQueryFull;
+      mbar_arrive_expect_tx(bar, (uint32_t)((it.n[0] > 0) + (it.n[1] > 0)) * 2 * q_bytes);
+      for (int t = 0; t < 2; ++t)
+        if (it.n[t] > 0)
+          for (int half = 0; half < 2; ++half)
+            tma_load_3d(base + kQueryOffset + t * kTileBytes + half * kHalfBytes, &p.q_map, 64 * half, it.head * p.group,
+                        it.q0 + it.tok0 + t * p.tile_tokens, bar);
+    }
+    ++queries;
+    for (int j = 0; j < blocks; ++j) {
+      for (int kv = 0; kv < 2; ++kv, ++fills) {
+        const uint32_t stage = fills % kStages, round = fills / kStages;
+        if (round > 0 && !wait_warp(bars + 8 * (kRingFree + stage), (round - 1) & 1, misc, p.status)) return;
+        if (lane == 0) {
+          const uint32_t bar = bars + 8 * (kRingFull + stage), dst = base + kRingOffset + stage * kTileBytes;
+          mbar_arrive_expect_tx(bar, kTileBytes);
+          for (int half = 0; half < 2; ++half)
+            tma_load_3d(dst + half * kHalfBytes, kv ? &p.v_map : &p.k_map, 64 * half, it.k0 + (it.first + j) * kBlock, it.head, bar);
+        }
+        __syncwarp();
+      }
+    }
+  }
+}
+
+// One warp, of which one thread issues every product.
 template <bool F16>
-__global__ void __launch_bounds__(128) prompt_kernel(const __grid_constant__ PromptParams p) {
+__device__ void issue_products(const PromptParams& p, uint32_t base, const char* smem, uint32_t tmem, volatile int* misc) {
+  const int lane = threadIdx.x % 32;
+  const uint32_t bars = base + kBarOffset;
+  const volatile Item* items = reinterpret_cast<const volatile Item*>(smem + kItemOffset);
+  uint32_t fill = 0, queries = 0, probs[2] = {0, 0};
+  for (uint32_t n = 0;; ++n) {
+    const uint32_t slot = n & 1;
+    if (!wait_warp(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc, p.status)) return;
+    const int none = items[slot].none, first = items[slot].first, k_len = items[slot].k_len;
+    const int count[2] = {items[slot].n[0], items[slot].n[1]}, width[2] = {items[slot].width[0], items[slot].width[1]};
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bars + 8 * (kItemFree + slot));
+    if (none) return;
+    const int blocks = max(count[0], count[1]);
+    if (blocks == 0) continue;
+    if (!wait_warp(bars + 8 * kQueryFull, queries & 1, misc, p.status)) return;
+    ++queries;
+
+    // S of tile t and block j: 128 rows by the block's keys that any of them sees, 16 channels at a time
+    auto scores = [&](int t, int j, uint32_t stage) {
+      if (j >= count[t] || lane != 0) return;
+      const int keys = j == count[t] - 1 ? (width[t] + 15) & ~15 : kBlock;
+      const uint32_t shape = mma_shape(F16, keys, false), q = base + kQueryOffset + t * kTileBytes;
+      const uint32_t k = base + kRingOffset + stage * kTileBytes;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t at = (i / 4) * kHalfBytes + (i % 4) * 32;
+        tc_mma_ss(tmem + kScoreColumn + 128 * t, smem_operand(q + at, 16, 1024), smem_operand(k + at, 16, 1024), shape, i > 0);
+      }
+      tc_commit(bars + 8 * (kScoreFull + t));
+      if (j == count[t] - 1 && count[t] == blocks && (t == 1 || count[1] < blocks)) tc_commit(bars + 8 * kQueryFree);
+    };
+    auto wait_fill = [&](uint32_t f) { return wait_warp(bars + 8 * (kRingFull + f % kStages), (f / kStages) & 1, misc, p.status); };
+
+    // the ring holds K, V of block 0, K, V of block 1, ...: block j's K is fill + 2 j
+    if (!wait_fill(fill)) return;
+    scores(0, 0, fill % kStages);
+    scores(1, 0, fill % kStages);
+    if (lane == 0) tc_commit(bars + 8 * (kRingFree + fill % kStages));
+    for (int j = 0; j < blocks; ++j) {
+      const uint32_t fv = fill + 2 * j + 1, fk = fv + 1;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (j >= count[t]) continue;
+        if (!wait_warp(bars + 8 * (kProbFull + t), probs[t] & 1, misc, p.status)) return;
+        ++probs[t];
+        if (t == 0 || j >= count[0]) {  // the first that reads this block's values
+          if (!wait_fill(fv)) return;
+          const int valid = k_len - (first + j) * kBlock;
+          if (valid < kBlock && valid % 16 != 0) {
+            // rows past the prompt's last value may be anything, and 0 times NaN is no 0: zeros up to a step's end
+            const uint32_t v = base + kRingOffset + (fv % kStages) * kTileBytes;
+            for (int i = lane; i < (16 - valid % 16) * 16; i += 32)
+              st_shared16(v + (i / 8 % 2) * kHalfBytes + swizzled(valid + i / 16, i % 8), make_uint4(0u, 0u, 0u, 0u));
+            fence_proxy_async_shared();
+            __syncwarp();
+          }
+        }
+        tc_fence_after();
+        if (lane == 0) {
+          const int steps = j == count[t] - 1 ? (width[t] + 15) / 16 : kBlock / 16;
+          const uint32_t shape = mma_shape(F16, kHeadDim, true), v = base + kRingOffset + (fv % kStages) * kTileBytes;
+          for (int i = 0; i < steps; ++i)
+            tc_mma_ts(tmem + kOutColumn + 128 * t, tmem + kScoreColumn + 128 * t + 8 * i,
+                      smem_operand(v + i * 2048, kHalfBytes, 1024), shape, j > 0 || i > 0);
+          if (j == count[t] - 1) tc_commit(bars + 8 * (kOutFull + t));
+        }
+        __syncwarp();
+        if (j + 1 < count[t]) {
+          if (!wait_fill(fk)) return;
+          scores(t, j + 1, fk % kStages);
+        }
+      }
+      if (lane == 0) {
+        tc_commit(bars + 8 * (kRingFree + fv % kStages));
+        if (j + 1 < blocks) tc_commit(bars + 8 * (kRingFree + fk % kStages));
+      }
+      __syncwarp();
+    }
+    fill += 2 * blocks;
+  }
+}
+
+// A row's softmax so far.  Its probabilities are 2^(s c - (M + r)), c = scale log2(e): M is the maximum times c, rounded;
+// r, what the rounding took, where M is so large that it shows, else 0.
+struct RowSum {
+  float M, r, l;
+};
+
+__device__ __forceinline__ float residual(float top, float c, float M) {
+  return fabsf(M) >= 1048576.f && fabsf(M) < INFINITY ? fmaf(top, c, -M) : 0.f;
+}
+
+// 128 threads, a row each, of tile t.
+template <bool F16>
+__device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const char* smem, uint32_t tmem, volatile int* misc) {
+  const int lane = threadIdx.x % 32, row = threadIdx.x % kTileRows;
+  const uint32_t bars = base + kBarOffset;
+  const volatile Item* items = reinterpret_cast<const volatile Item*>(smem + kItemOffset);
+  const uint32_t mine = (uint32_t)(row / 32 * 32) << 16;  // this warp's lanes of tensor memory
+  const uint32_t s_at = tmem + mine + kScoreColumn + 128 * t, o_at = tmem + mine + kOutColumn + 128 * t;
+  const float c = p.scale * kLog2e;
+  const int tok_of_row = row / p.group, head_of_row = row - tok_of_row * p.group;
+  uint32_t scores = 0, outs = 0;
+  for (uint32_t n = 0;; ++n) {
+    const uint32_t slot = n & 1;
+    if (!wait_warp(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc, p.status)) return;
+    Item it;
+    it.none = items[slot].none;
+    it.q0 = items[slot].q0;
+    it.tok0 = items[slot].tok0;
+    it.q_len = items[slot].q_len;
+    it.k_len = items[slot].k_len;
+    it.head = items[slot].head;
+    it.first = items[slot].first;
+    it.slot = items[slot].slot;
+    const int blocks = items[slot].n[t];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bars + 8 * (kItemFree + slot));
+    if (it.none) return;
+    const int tok = it.tok0 + t * p.tile_tokens + tok_of_row;
+    const bool valid = tok_of_row < p.tile_tokens && tok < it.q_len;
+    const int seen = seen_by(p, it.q_len, it.k_len, tok);
+    const int limit = valid ? seen : 0x7fffffff;  // rows of nobody need no mask
+    const int least = __reduce_min_sync(kAll, limit);
+    RowSum st = {-INFINITY, 0.f, 0.f};
+    for (int j = 0; j < blocks; ++j, ++scores) {
+      if (!wait_warp(bars + 8 * (kScoreFull + t), scores & 1, misc, p.status)) return;
+      tc_fence_after();
+      uint32_t w[4][32];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmem_load32(w[i], s_at + 32 * i);
+      tmem_wait_loads();
+      const int key0 = (it.first + j) * kBlock;
+      if (least < key0 + kBlock) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (key0 + i >= limit) w[i / 32][i % 32] = 0xff800000u;  // -inf
+      }
+      float top[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        top[i] = __uint_as_float(w[i][0]);
+#pragma unroll
+        for (int k = 1; k < 31; k += 2) top[i] = fmaxf(fmaxf(top[i], __uint_as_float(w[i][k])), __uint_as_float(w[i][k + 1]));
+        top[i] = fmaxf(top[i], __uint_as_float(w[i][31]));
+      }
+      const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      const float M = best * c;
+      // each row by itself (rows of nobody hold what shared memory held, and must not change the others' rounding)
+      const bool moves = valid && M - st.M > kRescale;
+      if (__any_sync(kAll, moves)) {
+        float keep = 1.f;
+        if (moves) {
+          const float r = residual(best, c, M);
+          keep = exp2_approx((st.M - M) + (st.r - r));
+          st.M = M;
+          st.r = r;
+          st.l *= keep;
+        }
+        __syncwarp();
+        if (j > 0) {
+          // S of this block is complete, so P V of the one before is, and nothing writes O now
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t o[32];
+            tmem_load32(o, o_at + 32 * i);
+            tmem_wait_loads();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
+            tmem_store32(o_at + 32 * i, o);
+          }
+        }
+      }
+      const float shift = st.M == -INFINITY ? 0.f : -st.M;
+      const uint64_t c2 = f32x2(__float_as_uint(c), __float_as_uint(c)), shift2 = f32x2(__float_as_uint(shift), __float_as_uint(shift));
+      const bool exactly = __any_sync(kAll, st.r != 0.f);
+      const uint64_t r2 = f32x2(__float_as_uint(-st.r), __float_as_uint(-st.r));
+      uint64_t sum[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t pw[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          uint64_t x = f32x2_fma(f32x2(w[i][2 * k], w[i][2 * k + 1]), c2, shift2);
+          if (exactly) x = f32x2_add(x, r2);
+          const float a = exp2_approx(__uint_as_float((uint32_t)x)), b = exp2_approx(__uint_as_float((uint32_t)(x >> 32)));
+          sum[k % 2] = f32x2_add(sum[k % 2], f32x2(__float_as_uint(a), __float_as_uint(b)));
+          pw[k] = pack2<F16>(a, b);
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) w[i / 2][16 * (i % 2) + k] = pw[k];
+      }
+      tmem_store32(s_at, w[0]);
+      tmem_store32(s_at + 32, w[1]);
+      sum[0] = f32x2_add(sum[0], sum[1]);
+      st.l += __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
+      tmem_wait_stores();
+      tc_fence_before();
+      mbar_arrive(bars + 8 * (kProbFull + t));
+    }
+
+    // the tile's end
+    if (blocks > 0) {
+      if (!wait_warp(bars + 8 * (kOutFull + t), outs & 1, misc, p.status)) return;
+      ++outs;
+      tc_fence_after();
+    }
+    const bool whole = it.slot < 0;
+    const int head = it.head * p.group + head_of_row;
+    const int64_t token = (int64_t)it.q0 + tok;
+    if (whole && valid && p.lse)
+      p.lse[token * p.q_heads + head] = st.l == 0.f ? -INFINITY : ((st.M + st.r) + log2f(st.l)) * 0.69314718055994531f;
+    const float scale = seen > 0 ? 1.0f / st.l : 0.f;
+    uint16_t* out = p.out.data + token * p.out.token_stride + head * p.out.head_stride;
+    float* part = p.parts + (int64_t)it.slot * kPromptPartFloats;
+    const int part_row = t * kTileRows + row;
+    if (!whole && valid) {
+      part[part_row] = st.M;
+      part[256 + part_row] = st.r;
+      part[512 + part_row] = st.l;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t o[32];
+      if (blocks > 0) {
+        tmem_load32(o, o_at + 32 * i);
+        tmem_wait_loads();
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) o[k] = 0u;
+      }
+      if (valid && whole) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] = pack2<F16>(__uint_as_float(o[8 * k + 2 * e]) * scale, __uint_as_float(o[8 * k + 2 * e + 1]) * scale);
+          *reinterpret_cast<uint4*>(out + 32 * i + 8 * k) = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+      } else if (valid) {
+        // [channel / 4][row][4]: a warp's rows lie side by side
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          *reinterpret_cast<uint4*>(part + 768 + ((8 * i + k) * 256 + part_row) * 4) =
+              make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+      }
+      __syncwarp();
+    }
+    tc_fence_before();
+  }
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_constant__ PromptParams p) {
+  extern __shared__ char raw[];
+  char* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+  const uint32_t base = smem_u32(smem), bars = base + kBarOffset;
+  volatile int* misc = reinterpret_cast<int*>(smem + kMiscOffset);
+  const int warp = threadIdx.x / 32;
+  if (threadIdx.x == 0) {
+    mbar_init(bars + 8 * kQueryFull, 1);
+    mbar_init(bars + 8 * kQueryFree, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(bars + 8 * (kScoreFull + t), 1);
+      mbar_init(bars + 8 * (kProbFull + t), kTileRows);
+      mbar_init(bars + 8 * (kOutFull + t), 1);
+      mbar_init(bars + 8 * (kItemFull + t), 1);
+      mbar_init(bars + 8 * (kItemFree + t), 9);  // eight softmax warps and the one that issues
+    }
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(bars + 8 * (kRingFull + i), 1);
+      mbar_init(bars + 8 * (kRingFree + i), 1);
+    }
+    mbar_init_fence();
+    misc[0] = 0;
+  }
+  if (warp == kMmaWarp) tmem_alloc(base + kMiscOffset + 4, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)misc[1];
   grid_launch_dependents();
   grid_dependency_wait();
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, h = blockIdx.y;
-  const int64_t row = (int64_t)blockIdx.x * 4 + warp;
-  int at = 0, i = 0;
-  for (; i < p.prompts && at + p.range[i].q_len <= row; ++i) at += p.range[i].q_len;
-  if (i == p.prompts) return;
-  const PromptRange r = p.range[i];
-  const int in_prompt = (int)(row - at), token = r.q0 + in_prompt;
-  const float4 q = lane_channels4<F16>(p.q.data + token * p.q.token_stride + h * p.q.head_stride, lane);
-  const int seen = p.causal ? max(0, in_prompt + 1 + r.k_len - r.q_len) : r.k_len;
-  const int64_t kvh = h / p.group;
-  RowState st;
-  for (int t = 0; t < seen; ++t)
-    attend_key<F16>(st, q, p.scale, p.k.data + (r.k0 + t) * p.k.token_stride + kvh * p.k.head_stride,
-                    p.v.data + (r.k0 + t) * p.v.token_stride + kvh * p.v.head_stride, lane);
-  store_row<F16>(st, p.out.data + token * p.out.token_stride + h * p.out.head_stride,
-                 p.lse ? p.lse + (int64_t)token * p.q_heads + h : nullptr, lane, seen <= 0);
+  uint32_t fills = 0, queries = 0;
+  if (warp == kLoadWarp) {
+    fence_proxy_async_global();  // inputs written by ordinary stores of earlier launches
+    load_items(p, base, smem, misc, fills, queries);
+  } else if (warp == kMmaWarp) {
+    issue_products<F16>(p, base, smem, tmem, misc);
+  } else {
+    softmax_rows<F16>(p, warp / 4, base, smem, tmem, misc);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (misc[0] && warp == kLoadWarp) {  // a CTA that gave up leaves once the copies it asked for have landed
+    for (uint32_t n = fills > kStages ? fills - kStages : 0; n < fills; ++n)
+      for (uint32_t i = 0; i < kAsyncRounds && !mbar_try_wait_sleep(bars + 8 * (kRingFull + n % kStages), (n / kStages) & 1, kAsyncSleepNs); ++i) {
+      }
+    for (uint32_t i = 0; queries > 0 && i < kAsyncRounds && !mbar_try_wait_sleep(bars + 8 * kQueryFull, (queries - 1) & 1, kAsyncSleepNs); ++i) {
+    }
+  }
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_free(tmem, 512);
+  }
+  // the last CTA leaves the counters at zero for the next launch: no other takes an item any more
+  if (threadIdx.x == 0 && atomicAdd(p.counters + 1, 1u) == gridDim.x - 1) {
+    p.counters[0] = 0u;
+    p.counters[1] = 0u;
+  }
+}
+
+// Joins the pieces of an item: a CTA takes 32 of its 256 rows, a warp 16 channels of them, a lane a row.
+template <bool F16>
+__global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant__ PromptParams p) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int row = (blockIdx.x % 8) * 32 + lane, index = blockIdx.x / 8;
+  Item it;
+  item_at(p, index, it);
+  if (it.slot < 0 || it.first > 0) return;  // whole, or not the item's first piece
+  const int t = row / kTileRows, in_tile = row % kTileRows;
+  const int tok_of_row = in_tile / p.group, tok = it.tok0 + t * p.tile_tokens + tok_of_row;
+  if (tok_of_row >= p.tile_tokens || tok >= it.q_len) return;
+  const int seen = seen_by(p, it.q_len, it.k_len, tok), head = it.head * p.group + in_tile % p.group;
+  const int64_t token = (int64_t)it.q0 + tok;
+  // pieces that hold a key of either tile were written
+  const int last_tok = min(it.tok0 + 2 * p.tile_tokens, it.q_len) - 1;
+  const int blocks = (seen_by(p, it.q_len, it.k_len, last_tok) + kBlock - 1) / kBlock;
+  const int pieces = (blocks + p.chunk - 1) / p.chunk;
+  const float* part = p.parts + (int64_t)it.slot * kPromptPartFloats;
+  float M = -INFINITY, r = 0.f;
+  const int64_t step = (int64_t)it.slot_step * kPromptPartFloats;
+  for (int i = 0; i < pieces; ++i) {
+    const float m = part[i * step + row], mr = part[i * step + 256 + row];
+    if (m > M) {
+      M = m;
+      r = mr;
+    }
+  }
+  float l = 0.f, acc[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) acc[k] = 0.f;
+  for (int i = 0; i < pieces; ++i) {
+    const float* from = part + i * step;
+    const float m = from[row];
+    const float e = m == -INFINITY ? 0.f : exp2_approx((m - M) + (from[256 + row] - r));
+    l += from[512 + row] * e;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(from + 768 + ((4 * warp + k) * 256 + row) * 4);
+      if (m == -INFINITY) continue;
+      acc[4 * k] += x.x * e;
+      acc[4 * k + 1] += x.y * e;
+      acc[4 * k + 2] += x.z * e;
+      acc[4 * k + 3] += x.w * e;
+    }
+  }
+  const float scale = seen > 0 ? 1.0f / l : 0.f;
+  uint32_t x[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] = pack2<F16>(acc[2 * k] * scale, acc[2 * k + 1] * scale);
+  uint16_t* out = p.out.data + token * p.out.token_stride + head * p.out.head_stride + 16 * warp;
+  *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<uint4*>(out + 8) = make_uint4(x[4], x[5], x[6], x[7]);
+  if (p.lse && warp == 0) p.lse[token * p.q_heads + head] = l == 0.f ? -INFINITY : ((M + r) + log2f(l)) * 0.69314718055994531f;
+}
+
+template <bool F16>
+cudaError_t launch(const PromptParams& p, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};  // devices whose shared-memory limit is raised
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(prompt_kernel<F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  e = launch_overlapped(prompt_kernel<F16>, dim3((unsigned)std::min(p.items, device_sms())), kThreads, kSmemBytes, s, p);
+  if (e != cudaSuccess || !p.split) return e;
+  return launch_overlapped(prompt_join_kernel<F16>, dim3((unsigned)(p.items * 8)), 256, 0, s, p);
 }
 
 }  // namespace
 
 cudaError_t launch_prompt(const PromptParams& p, bool f16, cudaStream_t s) {
-  int64_t rows = 0;
-  for (int i = 0; i < p.prompts; ++i) rows += p.range[i].q_len;
-  if (rows == 0) return cudaSuccess;
-  const dim3 grid((unsigned)((rows + 3) / 4), (unsigned)p.q_heads);
-  return f16 ? launch_overlapped(prompt_kernel<true>, grid, 128, 0, s, p)
-             : launch_overlapped(prompt_kernel<false>, grid, 128, 0, s, p);
+  return f16 ? launch<true>(p, s) : launch<false>(p, s);
 }
 
 }  // namespace hg
