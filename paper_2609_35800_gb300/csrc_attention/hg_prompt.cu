@@ -30,7 +30,10 @@ constexpr int kTileRows = 128;
 constexpr int kHalfBytes = 128 * 128;       // 64 channels of 128 rows
 constexpr int kTileBytes = 2 * kHalfBytes;  // a tile of queries, a block of keys or of values
 constexpr int kStages = 5;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;  // the last two warps have nothing to do: registers are divided by warpgroups
+// Registers a thread: at launch 65,536 / 384 give 168; the softmax rows need more, the others less.
+constexpr int kRowRegisters = 208, kOtherRegisters = 88;
+static_assert(256 * kRowRegisters + 128 * kOtherRegisters <= kThreads * 168, "what the launch has");
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
 constexpr float kRescale = 8.0f;
 constexpr uint32_t kScoreColumn = 0, kOutColumn = 256;  // + 128 for tile 1
@@ -168,6 +171,8 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
   const int lane = threadIdx.x % 32;
   const uint32_t bars = base + kBarOffset;
   const volatile Item* items = reinterpret_cast<const volatile Item*>(smem + kItemOffset);
+  const uint32_t q_operand = smem_operand(base + kQueryOffset, 16), k_operand = smem_operand(base + kRingOffset, 16);
+  const uint32_t v_operand = smem_operand(base + kRingOffset, kHalfBytes), v_shape = mma_shape(F16, kHeadDim, true);
   uint32_t fill = 0, queries = 0, probs[2] = {0, 0};
   for (uint32_t n = 0;; ++n) {
     const uint32_t slot = n & 1;
@@ -184,14 +189,14 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
 
     // S of tile t and block j: 128 rows by the block's keys that any of them sees, 16 channels at a time
     auto scores = [&](int t, int j, uint32_t stage) {
-      if (j >= count[t] || lane != 0) return;
+      if (j >= count[t] || !elect_one()) return;
       const int keys = j == count[t] - 1 ? (width[t] + 15) & ~15 : kBlock;
-      const uint32_t shape = mma_shape(F16, keys, false), q = base + kQueryOffset + t * kTileBytes;
-      const uint32_t k = base + kRingOffset + stage * kTileBytes;
+      const uint32_t shape = mma_shape(F16, keys, false), q = q_operand + t * (kTileBytes >> 4);
+      const uint32_t k = k_operand + stage * (kTileBytes >> 4);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t at = (i / 4) * kHalfBytes + (i % 4) * 32;
-        tc_mma_ss(tmem + kScoreColumn + 128 * t, smem_operand(q + at, 16, 1024), smem_operand(k + at, 16, 1024), shape, i > 0);
+        const uint32_t at = ((i / 4) * kHalfBytes + (i % 4) * 32) >> 4;
+        tc_mma_ss(tmem + kScoreColumn + 128 * t, q + at, k + at, shape, i > 0);
       }
       tc_commit(bars + 8 * (kScoreFull + t));
       if (j == count[t] - 1 && count[t] == blocks && (t == 1 || count[1] < blocks)) tc_commit(bars + 8 * kQueryFree);
@@ -202,7 +207,7 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
     if (!wait_fill(fill)) return;
     scores(0, 0, fill % kStages);
     scores(1, 0, fill % kStages);
-    if (lane == 0) tc_commit(bars + 8 * (kRingFree + fill % kStages));
+    if (elect_one()) tc_commit(bars + 8 * (kRingFree + fill % kStages));
     for (int j = 0; j < blocks; ++j) {
       const uint32_t fv = fill + 2 * j + 1, fk = fv + 1;
 #pragma unroll
@@ -223,13 +228,17 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
           }
         }
         tc_fence_after();
-        if (lane == 0) {
-          const int steps = j == count[t] - 1 ? (width[t] + 15) / 16 : kBlock / 16;
-          const uint32_t shape = mma_shape(F16, kHeadDim, true), v = base + kRingOffset + (fv % kStages) * kTileBytes;
-          for (int i = 0; i < steps; ++i)
-            tc_mma_ts(tmem + kOutColumn + 128 * t, tmem + kScoreColumn + 128 * t + 8 * i,
-                      smem_operand(v + i * 2048, kHalfBytes, 1024), shape, j > 0 || i > 0);
-          if (j == count[t] - 1) tc_commit(bars + 8 * (kOutFull + t));
+        if (elect_one()) {
+          const uint32_t v = v_operand + (fv % kStages) * (kTileBytes >> 4), o = tmem + kOutColumn + 128 * t;
+          const uint32_t prob = tmem + kScoreColumn + 128 * t;
+          if (j < count[t] - 1) {
+#pragma unroll
+            for (int i = 0; i < kBlock / 16; ++i) tc_mma_ts(o, prob + 8 * i, v + i * (2048 >> 4), v_shape, i > 0 ? 1u : j > 0);
+          } else {
+            const int steps = (width[t] + 15) / 16;
+            for (int i = 0; i < steps; ++i) tc_mma_ts(o, prob + 8 * i, v + i * (2048 >> 4), v_shape, j > 0 || i > 0);
+            tc_commit(bars + 8 * (kOutFull + t));
+          }
         }
         __syncwarp();
         if (j + 1 < count[t]) {
@@ -237,7 +246,7 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
           scores(t, j + 1, fk % kStages);
         }
       }
-      if (lane == 0) {
+      if (elect_one()) {
         tc_commit(bars + 8 * (kRingFree + fv % kStages));
         if (j + 1 < blocks) tc_commit(bars + 8 * (kRingFree + fk % kStages));
       }
@@ -338,18 +347,23 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
           }
         }
       }
-      const float shift = st.M == -INFINITY ? 0.f : -st.M;
-      const uint64_t c2 = f32x2(__float_as_uint(c), __float_as_uint(c)), shift2 = f32x2(__float_as_uint(shift), __float_as_uint(shift));
-      const bool exactly = __any_sync(kAll, st.r != 0.f);
-      const uint64_t r2 = f32x2(__float_as_uint(-st.r), __float_as_uint(-st.r));
+      float shift = st.M == -INFINITY ? 0.f : -st.M, factor = c;
+      if (__any_sync(kAll, st.r != 0.f)) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          w[i / 32][i % 32] = __float_as_uint(fmaf(__uint_as_float(w[i / 32][i % 32]), c, shift) - st.r);
+        shift = 0.f;
+        factor = 1.f;
+      }
+      const uint64_t c2 = f32x2(__float_as_uint(factor), __float_as_uint(factor));
+      const uint64_t shift2 = f32x2(__float_as_uint(shift), __float_as_uint(shift));
       uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t pw[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-          uint64_t x = f32x2_fma(f32x2(w[i][2 * k], w[i][2 * k + 1]), c2, shift2);
-          if (exactly) x = f32x2_add(x, r2);
+          const uint64_t x = f32x2_fma(f32x2(w[i][2 * k], w[i][2 * k + 1]), c2, shift2);
           const float a = exp2_approx(__uint_as_float((uint32_t)x)), b = exp2_approx(__uint_as_float((uint32_t)(x >> 32)));
           sum[k % 2] = f32x2_add(sum[k % 2], f32x2(__float_as_uint(a), __float_as_uint(b)));
           pw[k] = pack2<F16>(a, b);
@@ -450,12 +464,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   grid_launch_dependents();
   grid_dependency_wait();
   uint32_t fills = 0, queries = 0;
-  if (warp == kLoadWarp) {
-    fence_proxy_async_global();  // inputs written by ordinary stores of earlier launches
-    load_items(p, base, smem, misc, fills, queries);
-  } else if (warp == kMmaWarp) {
-    issue_products<F16>(p, base, smem, tmem, misc);
+  if (warp >= kMmaWarp) {
+    set_registers_down<kOtherRegisters>();
+    if (warp == kLoadWarp) {
+      fence_proxy_async_global();  // inputs written by ordinary stores of earlier launches
+      load_items(p, base, smem, misc, fills, queries);
+    } else if (warp == kMmaWarp) {
+      issue_products<F16>(p, base, smem, tmem, misc);
+    }
   } else {
+    set_registers_up<kRowRegisters>();
     softmax_rows<F16>(p, warp / 4, base, smem, tmem, misc);
   }
   tc_fence_before();

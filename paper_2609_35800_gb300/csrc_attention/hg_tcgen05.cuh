@@ -22,31 +22,44 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
 }
 
-// D[tmem] (+)= A B, 16 deep: A from shared memory (descriptor) or from tensor memory.
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+// Shared-memory operands under the 128-byte swizzle.  The descriptor's low word holds the address and the byte stride of
+// the outer axis along M or N (of B with N contiguous: from 64 channels to the next 64), the high one that of 8 rows to
+// the next 8, 1024 bytes in every operand here, and the swizzle.  Addresses advance by adding to the low word.
+constexpr uint32_t kOperandHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t smem_operand(uint32_t addr, uint32_t leading) {
+  return (addr & 0x3ffff) >> 4 | (leading >> 4) << 16;
+}
+
+// D[tmem] (+)= A B, 16 deep: A from shared memory or from tensor memory.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.u32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(kOperandHigh)
       : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.u32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(kOperandHigh)
       : "memory");
 }
 
-// Shared-memory operand under the 128-byte swizzle: address, and the byte strides of its two outer axes.
-__device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t leading, uint32_t stride) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 |
-         (uint64_t)2 << 61;
-}
 // Instruction descriptor: fp32 accumulators, A and B of one 16-bit type, M = 128 rows, B with N contiguous if b_mn.
 __device__ __forceinline__ uint32_t mma_shape(bool f16, int n, bool b_mn) {
   const uint32_t type = f16 ? 0u : 1u;
   return 1u << 4 | type << 7 | type << 10 | (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
+}
+
+// Registers of a warpgroup's threads, which all call it.
+template <int N>
+__device__ __forceinline__ void set_registers_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void set_registers_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(N));
 }
 
 // 32 columns of this warp's 32 lanes: a thread has its lane's row.

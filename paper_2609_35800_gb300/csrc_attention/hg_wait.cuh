@@ -11,6 +11,8 @@ constexpr uint32_t kAsyncSleepNs = 50000;
 // Wait for a phase of `bar`.  One that runs out flags the workspace's status word and *abort, by which every other
 // wait of the CTA ends too, and returns false: the caller leaves its work.
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
+  for (int i = 0; i < 64; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
   for (uint32_t i = 0; i < kAsyncRounds; ++i) {
     if (mbar_try_wait_sleep(bar, parity, kAsyncSleepNs)) return true;
     if (*abort) return false;
