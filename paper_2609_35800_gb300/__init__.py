@@ -412,7 +412,19 @@ def hg_cache_image_bits_per_elem(cache):
 # Caches that stay 16-bit: page pools, append, paged decode, prompts
 # ---------------------------------------------------------------------------
 
-_DTYPES = {"torch.bfloat16": HG_DTYPE_BF16, "torch.float16": HG_DTYPE_F16}
+
+class _Types:
+    """The torch types that the calls below compare with, looked up at the first call (the package itself can be
+    imported without torch)."""
+
+    def __getattr__(self, name):
+        import torch
+        self.code = {torch.bfloat16: HG_DTYPE_BF16, torch.float16: HG_DTYPE_F16}
+        self.int32, self.float32 = torch.int32, torch.float32
+        return self.__dict__[name]
+
+
+_types = _Types()
 
 
 class Pages:
@@ -451,42 +463,42 @@ class Rotation:
 
 def _rows(where, name, x, tokens, heads, dtype):
     """(address, token stride, head stride) of a tensor seen as [tokens][heads][128] with dense channels."""
+    if x.dtype is dtype and x.shape == (tokens, heads, 128) and x.is_cuda:
+        ts, hs, cs = x.stride()
+        if cs == 1:
+            # a stride that is never taken may be anything in torch
+            return x.data_ptr(), ts if tokens > 1 else 0, hs if heads > 1 else 0
     if x.shape != (tokens, heads, 128) or x.dtype != dtype:
         raise ValueError("%s: %s is %s %s, the call takes %s [%d][%d][128]"
                          % (where, name, x.dtype, list(x.shape), dtype, tokens, heads))
-    ts, hs, cs = x.stride()
-    if cs != 1:
+    if x.stride(2) != 1:
         raise ValueError("%s: %s must have dense channels" % (where, name))
-    if not x.is_cuda:
-        raise ValueError("%s: %s must be a CUDA tensor" % (where, name))
-    # a stride that is never taken may be anything in torch
-    return x.data_ptr(), ts if tokens > 1 else 0, hs if heads > 1 else 0
+    raise ValueError("%s: %s must be a CUDA tensor" % (where, name))
 
 
 _NO_ROWS = (0, 0, 0)
+_Int = ctypes.c_int32
 
 
-def _ints(where, name, x, need, device="CUDA"):
+def _ints(where, name, x, need, cuda=True):
     """Address of a dense int32 tensor of at least `need` entries."""
-    import torch
-    if x.dtype != torch.int32 or not x.is_contiguous():
+    if x.dtype is _types.int32 and x.is_contiguous() and x.numel() >= need and x.is_cuda is cuda:
+        return x.data_ptr()
+    if x.dtype != _types.int32 or not x.is_contiguous():
         raise ValueError("%s: %s must be contiguous int32" % (where, name))
     if x.numel() < need:
         raise ValueError("%s: %s holds %d entries, the call reads %d" % (where, name, x.numel(), need))
-    if x.is_cuda != (device == "CUDA"):
-        raise ValueError("%s: %s must be a %s tensor" % (where, name, device))
-    return x.data_ptr()
+    raise ValueError("%s: %s must be a %s tensor" % (where, name, "CUDA" if cuda else "CPU"))
 
 
 def _lse(where, x, tokens, heads):
-    import torch
     if x is None:
         return None
-    if x.dtype != torch.float32 or x.shape != (tokens, heads) or not x.is_contiguous():
+    if x.dtype is _types.float32 and x.shape == (tokens, heads) and x.is_contiguous() and x.is_cuda:
+        return x.data_ptr()
+    if x.dtype != _types.float32 or x.shape != (tokens, heads) or not x.is_contiguous():
         raise ValueError("%s: lse must be contiguous float32 [%d][%d]" % (where, tokens, heads))
-    if not x.is_cuda:
-        raise ValueError("%s: lse must be a CUDA tensor" % where)
-    return x.data_ptr()
+    raise ValueError("%s: lse must be a CUDA tensor" % where)
 
 
 def _rotated_by(where, rotation, positions, tokens):
@@ -500,7 +512,7 @@ def hg_pages_create(k_pages, v_pages):
     [pages][kv heads][page size][128] (any strides: pages that lie [tokens][heads] are passed transposed)."""
     if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
         raise ValueError("hg_pages_create: k_pages and v_pages must be [pages][heads][tokens][128] of one type")
-    if str(k_pages.dtype) not in _DTYPES:
+    if k_pages.dtype not in _types.code:
         raise ValueError("hg_pages_create: pages must be bfloat16 or float16")
     n, heads, size, dim = k_pages.shape
     # the stride of an axis of length 1 is never taken: a dense one stands for it
@@ -509,7 +521,7 @@ def hg_pages_create(k_pages, v_pages):
         raise ValueError("hg_pages_create: k_pages and v_pages must have the same strides and dense channels")
     if not (k_pages.is_cuda and v_pages.is_cuda):
         raise ValueError("hg_pages_create: k_pages and v_pages must be CUDA tensors")
-    shape = PageShape(_DTYPES[str(k_pages.dtype)], n, size, heads, dim, *strides[0][:3])
+    shape = PageShape(_types.code[k_pages.dtype], n, size, heads, dim, *strides[0][:3])
     h = ctypes.c_void_p()
     _check(library().hg_pages_create(ctypes.byref(shape), k_pages.data_ptr(), v_pages.data_ptr(), ctypes.byref(h)),
            "hg_pages_create")
@@ -548,8 +560,16 @@ def hg_pages_decode_workspace_size(pages, batch, num_q_heads):
 def _decode_table(where, page_table, lengths, batch):
     if page_table.dim() != 2 or page_table.shape[0] < batch:
         raise ValueError("%s: page_table must be [%d][pages]" % (where, batch))
-    return (_ints(where, "page_table", page_table, batch * page_table.shape[1]), page_table.shape[1],
-            _ints(where, "lengths", lengths, batch))
+    per = page_table.shape[1]
+    return _ints(where, "page_table", page_table, batch * per), per, _ints(where, "lengths", lengths, batch)
+
+
+def _workspace(where, x):
+    if x is None or isinstance(x, int):
+        raise ValueError("%s: workspace must be a tensor" % where)
+    if x.is_cuda and x.is_contiguous():
+        return x.data_ptr(), x.nbytes
+    _refuse(where, [(x, 0, "workspace")])
 
 
 def hg_pages_decode_attention(pages, q, page_table, lengths, out, lse, softmax_scale, workspace, stream=None):
@@ -559,9 +579,8 @@ def hg_pages_decode_attention(pages, q, page_table, lengths, out, lse, softmax_s
     n, hq = q.shape[0], q.shape[1]
     io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), 0, 0, 0, 0, 0, 0, *_rows(w, "out", out, n, hq, d))
     tp, ts, lp = _decode_table(w, page_table, lengths, n)
-    wp, = _devs(w, (workspace, 0, "workspace"))
     _check(library().hg_pages_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse(w, lse, n, hq),
-                                               softmax_scale, wp, workspace.nbytes, _stream(stream)), w)
+                                               softmax_scale, *_workspace(w, workspace), _stream(stream)), w)
 
 
 def hg_pages_decode_step(pages, q, k, v, rotation, positions, page_table, lengths, out, lse, softmax_scale, workspace,
@@ -574,9 +593,8 @@ def hg_pages_decode_step(pages, q, k, v, rotation, positions, page_table, length
                      *_rows(w, "v", v, n, heads, d), *_rows(w, "out", out, n, hq, d))
     rp, pp = _rotated_by(w, rotation, positions, n)
     tp, ts, lp = _decode_table(w, page_table, lengths, n)
-    wp, = _devs(w, (workspace, 0, "workspace"))
     _check(library().hg_pages_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse(w, lse, n, hq),
-                                          softmax_scale, wp, workspace.nbytes, _stream(stream)), w)
+                                          softmax_scale, *_workspace(w, workspace), _stream(stream)), w)
 
 
 def hg_prompt_workspace_size():
@@ -590,15 +608,17 @@ def hg_prompt_attention(q, k, v, q_begin, k_begin, out, lse, causal, softmax_sca
     strides); prompt i has the rows q_begin[i]..q_begin[i + 1] and the keys k_begin[i]..k_begin[i + 1] (CPU int32
     tensors [prompts + 1]); lse float32 [tokens][heads] or None."""
     w, d = "hg_prompt_attention", q.dtype
-    if str(d) not in _DTYPES:
+    code = _types.code.get(d)
+    if code is None:
         raise ValueError("%s: q must be bfloat16 or float16" % w)
-    n, hq, nk, heads, count = q.shape[0], q.shape[1], k.shape[0], k.shape[1], q_begin.numel() - 1
+    n, hq, _ = q.shape
+    nk, heads, _ = k.shape
+    count = q_begin.numel() - 1
     io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, nk, heads, d),
                      *_rows(w, "v", v, nk, heads, d), *_rows(w, "out", out, n, hq, d))
-    qb, kb = _ints(w, "q_begin", q_begin, 1, "CPU"), _ints(w, "k_begin", k_begin, count + 1, "CPU")
-    if q_begin[-1] > n or k_begin[count] > nk:
-        raise ValueError("%s: the prompts end at %d and %d, q and k hold %d and %d rows"
-                         % (w, q_begin[-1], k_begin[count], n, nk))
-    wp, = _devs(w, (workspace, 0, "workspace"))
-    _check(library().hg_prompt_attention(_DTYPES[str(d)], count, hq, heads, io, qb, kb, _lse(w, lse, n, hq),
-                                         1 if causal else 0, softmax_scale, wp, workspace.nbytes, _stream(stream)), w)
+    qb, kb = _ints(w, "q_begin", q_begin, 1, False), _ints(w, "k_begin", k_begin, count + 1, False)
+    q_end, k_end = _Int.from_address(qb + 4 * count).value, _Int.from_address(kb + 4 * count).value
+    if q_end > n or k_end > nk:
+        raise ValueError("%s: the prompts end at %d and %d, q and k hold %d and %d rows" % (w, q_end, k_end, n, nk))
+    _check(library().hg_prompt_attention(code, count, hq, heads, io, qb, kb, _lse(w, lse, n, hq), 1 if causal else 0,
+                                         softmax_scale, *_workspace(w, workspace), _stream(stream)), w)

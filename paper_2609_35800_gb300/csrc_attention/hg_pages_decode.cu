@@ -4,11 +4,13 @@
 // Every key and value is used by G <= 16 queries only, 2 G flop per byte, so the kernel is bound by the reads of the
 // cache; it has to keep enough of them in flight and to spread them evenly.
 //
-// The work is cut into tiles of 64 tokens of one (request, KV head), numbered request by request, head by head.  CTA i
-// of n takes the tiles [T i / n, T (i + 1) / n): the same share for everybody whatever the requests' lengths, which the
-// kernel reads on the device.  A CTA's run of tiles cuts at most two (request, head) items, its first and its last; it
-// leaves their (m, l, o) in the workspace, and the last CTA to arrive at an item (a ticket, no waiting) joins its parts
-// in order, so the result does not depend on who comes last.
+// The work is cut into tiles of 64 tokens of one (request, KV head), numbered request by request, head by head; each
+// such item counts as kItemCost tiles more, ahead of its first, for its queries, sums and result.  CTA i of n takes the
+// units [T i / n, T (i + 1) / n): the same share for everybody whatever the requests' lengths, which the kernel reads on
+// the device.  A CTA's run cuts at most two items, its first and its last; it leaves their (m, l, o) in the workspace,
+// and the last CTA to arrive at an item (a ticket, no waiting) joins its parts in order, so the result does not depend on
+// who comes last.  Where no item is more than kJoinCost units longer than the share, joining would cost more than it
+// gains, and a CTA takes the whole items that begin in its units.
 //
 // A producer warp copies tiles into a ring of three 32 KB stages with TMA, a box per page (swizzled rows; a page id
 // outside the pool reads as zeros).  Each of four consumer warps takes 16 of a tile's 64 tokens, with its own running
@@ -33,16 +35,23 @@ constexpr int kQRowBytes = 272;  // a staged query row: 256 bytes, 16 more so th
 constexpr unsigned kAll = 0xffffffffu;
 constexpr float kRescale = 8.0f;  // log2 of how far a score may pass the running maximum
 
-// Shared memory from a 1024-byte boundary.  The staged queries (8 rows a warp) and the warps' parts that are added up
-// at an item's end (three warps, 8 queries at a time) take turns in one region.
+constexpr int kItemCost = 2;  // an item's fixed costs, in tiles
+constexpr int kJoinCost = 7;  // a ticket and a join, in tiles
+constexpr int kKeptLengths = 88;
+
+// Shared memory, two CTAs an SM.  The staged queries (8 rows a warp) and the warps' parts that are added up at an item's
+// end (8 queries at a time) take turns in one region.
 struct Smem {
   static constexpr int scratch = kStages * kStageBytes;
-  static constexpr int scratch_bytes = 3 * 8 * (kHeadDim + 2) * 4;  // > 4 * 8 * kQRowBytes
-  static constexpr int bars = scratch + ((scratch_bytes + 15) & ~15);
-  static constexpr int misc = bars + 2 * kStages * 8;  // abort flag, start of the CTA's work, scan
-  static constexpr int bytes = misc + 128 + 1024;
+  static constexpr int scratch_bytes = kConsumers * 8 * (kHeadDim + 2) * 4;
+  static constexpr int bars = scratch + scratch_bytes;
+  static constexpr int misc = bars + 2 * kStages * 8;  // abort flag, last part, start of the CTA's work, scan
+  static constexpr int lengths = misc + 128;           // the first requests' lengths
+  static constexpr int bytes = lengths + 4 * kKeptLengths;
 };
 static_assert(Smem::scratch_bytes >= kConsumers * 8 * kQRowBytes, "queries are staged there too");
+static_assert((8 + 17) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
+static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 
 // Where a run of tiles stands.
 struct Cursor {
@@ -56,12 +65,12 @@ __device__ __forceinline__ int request_length(const PagesDecodeParams& p, int b)
 // A request without a token counts as a tile too: its zeros have to be written.
 __device__ __forceinline__ int tiles_of(int len) { return max(1, (len + kTile - 1) / kTile); }
 
-__device__ __forceinline__ void next_item(const PagesDecodeParams& p, Cursor& c) {
+__device__ __forceinline__ void next_item(const PagesDecodeParams& p, const int* kept, Cursor& c) {
   c.t = 0;
   if (++c.h < p.pool.heads) return;
   c.h = 0;
   if (++c.b >= p.batch) return;
-  c.len = request_length(p, c.b);
+  c.len = c.b < kKeptLengths ? kept[c.b] : request_length(p, c.b);
   c.tiles = tiles_of(c.len);
 }
 
@@ -73,76 +82,132 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// The tiles [u0, u1) of the launch's `total` that this CTA, one of `ctas` that have any, takes.
+// The units [u0, u1) of the launch's `total` that this CTA, one of `ctas` that have any, takes.
 struct Work {
   int64_t u0, u1, total, ctas;
+  int first_unit;  // of its item, that u0 is
   __device__ __forceinline__ int cta_of(int64_t u) const { return (int)(((u + 1) * ctas - 1) / total); }
 };
 
-// The CTA's work, and where it begins; false: none.  Every thread adds
-// up the tiles of its share of the requests; the one whose share holds u0 looks for it there.
-__device__ bool find_work(const PagesDecodeParams& p, int* scan, Work& w, Cursor& c) {
+// The CTA's work, the first tile of it and how many there are; 0: none.  Every thread adds up the units of its share of
+// the requests; the one whose share holds u0 looks for it there.
+__device__ int64_t find_work(const PagesDecodeParams& p, int* scan, int* kept, Work& w, Cursor& c) {
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int per = (p.batch + kThreads - 1) / kThreads;
   const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += tiles_of(request_length(p, b));
+  int mine = 0, longest = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int len = request_length(p, b), units = tiles_of(len) + kItemCost;
+    if (b < kKeptLengths) kept[b] = len;
+    mine += units;
+    longest = max(longest, units);
+  }
+  longest = __reduce_max_sync(kAll, longest);
   int sum = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int x = __shfl_up_sync(kAll, sum, o);
     if (lane >= o) sum += x;
   }
-  if (lane == 31) scan[warp] = sum;
+  if (lane == 31) {
+    scan[warp] = sum;
+    scan[12 + warp] = longest;
+  }
   __syncthreads();
   int before = sum - mine, all = 0;
 #pragma unroll
   for (int i = 0; i < kConsumers + 1; ++i) {
     if (i < warp) before += scan[i];
     all += scan[i];
+    longest = max(longest, scan[12 + i]);
   }
   w.total = (int64_t)all * p.pool.heads;
   w.ctas = min((int64_t)gridDim.x, w.total);
-  if (blockIdx.x >= w.ctas) return false;
+  if (blockIdx.x >= w.ctas) return 0;
   w.u0 = w.total * blockIdx.x / w.ctas;
   w.u1 = w.total * (blockIdx.x + 1) / w.ctas;
   const int64_t at = w.u0 - (int64_t)before * p.pool.heads;
   if (at >= 0 && at < (int64_t)mine * p.pool.heads) {
     int64_t left = at;
-    int b = b0, len = 0, tiles = 0;
+    int b = b0, len = 0, units = 0;
     for (;; ++b) {
       len = request_length(p, b);
-      tiles = tiles_of(len);
-      if (left < (int64_t)tiles * p.pool.heads) break;
-      left -= (int64_t)tiles * p.pool.heads;
+      units = tiles_of(len) + kItemCost;
+      if (left < (int64_t)units * p.pool.heads) break;
+      left -= (int64_t)units * p.pool.heads;
     }
     scan[8] = b;
-    scan[9] = (int)(left / tiles);
-    scan[10] = (int)(left % tiles);
+    scan[9] = (int)(left / units);
+    scan[10] = (int)(left % units);
     scan[11] = len;
-    scan[12] = tiles;
   }
   __syncthreads();
-  c = {scan[8], scan[9], scan[10], scan[11], scan[12]};
-  return true;
+  w.first_unit = scan[10];
+  c = {scan[8], scan[9], max(0, w.first_unit - kItemCost), scan[11], tiles_of(scan[11])};
+  if (longest <= w.total / w.ctas + kJoinCost) {
+    // from the first item that begins at u0 or later to the last that begins before u1
+    int64_t at = w.u0;
+    if (w.first_unit > 0) {
+      at += c.tiles + kItemCost - w.first_unit;
+      w.first_unit = 0;
+      if (at < w.u1) next_item(p, kept, c);
+    }
+    w.u0 = at;
+    int64_t tiles = 0;
+    for (Cursor x = c; at < w.u1;) {
+      tiles += x.tiles;
+      at += x.tiles + kItemCost;
+      if (at < w.u1) next_item(p, kept, x);
+    }
+    return tiles;
+  }
+  // the run's units less those that stand for fixed costs
+  int64_t left = w.u1 - w.u0, tiles = 0;
+  int skip = max(0, kItemCost - w.first_unit);
+  for (Cursor x = c; left > skip; skip = kItemCost) {
+    left -= skip;
+    const int64_t n = min(left, (int64_t)(x.tiles - x.t));
+    tiles += n;
+    left -= n;
+    if (left > 0) next_item(p, kept, x);
+  }
+  return tiles;
+}
+
+// Lets the launch's page ids, queries and rotations into L2 before the caches' reads fill the memory's queues: CTA by CTA a request.
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
+__device__ void prefetch_queries(const PagesDecodeParams& p) {
+  for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+    const int heads = p.group * p.pool.heads;
+    for (int i = 32 * threadIdx.x; i < p.table_stride; i += 32 * kThreads) prefetch_l2(p.table + (int64_t)b * p.table_stride + i);
+    for (int i = threadIdx.x; i < 2 * heads; i += kThreads)
+      prefetch_l2(p.q.data + b * p.q.token_stride + (i / 2) * p.q.head_stride + (i % 2) * 64);
+    if (p.rot.table == nullptr) continue;
+    for (int i = threadIdx.x; i < 3 * 4; i += kThreads) {
+      if (i >= 4 && p.rot.position_stride == 0) break;
+      const int pos = min(max(p.rot.positions[(int64_t)(i / 4) * p.rot.position_stride + b], 0), p.rot.table_len - 1);
+      if (i % 4 * 32 < 2 * p.rot.half) prefetch_l2(p.rot.table + (int64_t)pos * (2 * p.rot.half) + i % 4 * 32);
+    }
+  }
 }
 
 // Copies the CTA's tiles into the ring, in order; returns how many it asked for.
-__device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int64_t units, uint32_t stages, uint32_t full, uint32_t empty,
-                        volatile int* abort) {
+__device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int64_t tiles, const int* kept, uint32_t stages, uint32_t full,
+                            uint32_t empty, volatile int* abort) {
   const int lane = threadIdx.x % 32;
   const int rows = min(p.pool.page_size, kTile);  // tokens of a box
   const int boxes = kTile / rows;
   const uint32_t box_bytes = (uint32_t)rows * kHeadDim * 2;
   uint32_t n = 0;
-  for (; units > 0; next_item(p, c)) {
+  // 32 boxes' page ids, a lane each, from box `first` of request `of` on
+  int of = -1, first = 0, id = 0;
+  for (; tiles > 0; next_item(p, kept, c)) {
     const int* ids = p.table + (int64_t)c.b * p.table_stride;
-    // 32 page ids at a time, a lane each: that of the 64-token tiles' first box, second, ...
-    int first = -1, id = 0;
-    for (; c.t < c.tiles && units > 0; ++c.t, --units, ++n) {
+    for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
       const int box0 = c.t * boxes;  // box number in the item
       const int valid = min(boxes, max(0, (c.len - c.t * kTile + rows - 1) / rows));
-      if (first < 0 || box0 + boxes > first + 32) {
+      if (of != c.b || box0 < first || box0 + boxes > first + 32) {
+        of = c.b;
         first = box0;
         const int64_t token = (int64_t)(first + lane) * rows;
         id = token < c.len ? ids[token >> p.pool.page_shift] : -1;
@@ -176,27 +241,45 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
   else mma_bf16(d, a, b0, b1);
 }
 
-// 16 rows of 8 lanes each, rotated: the queries of the item, 8 at a time, as operands of the first product.
-template <bool F16, int NT>
-__device__ __forceinline__ void load_queries(const PagesDecodeParams& p, int b, int h, uint32_t mine, uint32_t (&qf)[NT][16]) {
+// An item's query rows on their way: 8 lanes a row, four rows at a time.
+template <int NT>
+struct Queries {
+  uint4 lo[NT][2], hi[NT][2];
+  LaneAngles angles;
+};
+
+template <int NT>
+__device__ __forceinline__ void fetch_queries(const PagesDecodeParams& p, int b, int h, Queries<NT>& x) {
   const int lane = threadIdx.x % 32, c = lane % 8;
   const LaneChannels at = lane_channels(p.rot, c, p.rot.table != nullptr);
-  LaneAngles g;
-  if (at.turns) g = lane_angles(p.rot, c, b);
+  const uint16_t* row = p.q.data + b * p.q.token_stride + (int64_t)h * p.group * p.q.head_stride;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int q = nt * 8 + lane / 8 + 4 * i;
+      x.lo[nt][i] = x.hi[nt][i] = make_uint4(0u, 0u, 0u, 0u);
+      if (q < p.group) {
+        x.lo[nt][i] = ldg16(row + q * p.q.head_stride + at.lo);
+        x.hi[nt][i] = ldg16(row + q * p.q.head_stride + at.hi);
+      }
+    }
+  if (at.turns) x.angles = lane_angles(p.rot, c, b);
+}
+
+// Rotated, and through shared memory into the first product's operands.
+template <bool F16, int NT>
+__device__ __forceinline__ void stage_queries(const PagesDecodeParams& p, Queries<NT>& x, uint32_t mine, uint32_t (&qf)[NT][16]) {
+  const int lane = threadIdx.x % 32;
+  const LaneChannels at = lane_channels(p.rot, lane % 8, p.rot.table != nullptr);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int r = lane / 8 + 4 * i, q = nt * 8 + r;
-      uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-      if (q < p.group) {
-        const uint16_t* src = p.q.data + b * p.q.token_stride + (int64_t)(h * p.group + q) * p.q.head_stride;
-        lo = ldg16(src + at.lo);
-        hi = ldg16(src + at.hi);
-        if (at.turns) rotate_lane<F16>(lo, hi, g, p.rot.interleaved != 0);
-      }
-      st_shared16(mine + r * kQRowBytes + at.lo * 2, lo);
-      st_shared16(mine + r * kQRowBytes + at.hi * 2, hi);
+      if (at.turns) rotate_lane<F16>(x.lo[nt][i], x.hi[nt][i], x.angles, p.rot.interleaved != 0);
+      const uint32_t row = mine + (lane / 8 + 4 * i) * kQRowBytes;
+      st_shared16(row + at.lo * 2, x.lo[nt][i]);
+      st_shared16(row + at.hi * 2, x.hi[nt][i]);
     }
     __syncwarp();
 #pragma unroll
@@ -312,164 +395,166 @@ __device__ __forceinline__ float* partial_of(const PagesDecodeParams& p, int cta
   return p.partials + ((int64_t)cta * 2 + (begins ? 1 : 0)) * p.group * kPartialFloats;
 }
 
-// out = o / l in the cache's type and the log-sum-exp of a query; a lane has channels 4 lane ..
+// Eight channels of out = o / l in the cache's type, and the query's log-sum-exp.
 template <bool F16>
-__device__ __forceinline__ void write_query(const PagesDecodeParams& p, int b, int h, int q, float m, float l, const float4& o,
-                                            int len, float c) {
-  const int lane = threadIdx.x % 32;
-  const float r = len > 0 ? 1.0f / l : 0.f;
-  const int head = h * p.group + q;
-  uint16_t* out = p.out.data + b * p.out.token_stride + head * p.out.head_stride;
-  *reinterpret_cast<uint2*>(out + 4 * lane) = make_uint2(pack2<F16>(o.x * r, o.y * r), pack2<F16>(o.z * r, o.w * r));
-  if (p.lse && lane == 0) p.lse[(int64_t)b * p.pool.heads * p.group + head] = l == 0.f ? -INFINITY : m * p.scale + logf(l);
+__device__ __forceinline__ void write_query(const PagesDecodeParams& p, const Cursor& c, int q, int channel, float m, float l,
+                                            const float (&o)[8]) {
+  const float r = c.len > 0 ? 1.0f / l : 0.f;
+  const int head = c.h * p.group + q;
+  uint16_t* out = p.out.data + c.b * p.out.token_stride + head * p.out.head_stride;
+  *reinterpret_cast<uint4*>(out + channel) = make_uint4(pack2<F16>(o[0] * r, o[1] * r), pack2<F16>(o[2] * r, o[3] * r),
+                                                        pack2<F16>(o[4] * r, o[5] * r), pack2<F16>(o[6] * r, o[7] * r));
+  if (p.lse && channel == 0)
+    p.lse[(int64_t)c.b * p.pool.heads * p.group + head] = l == 0.f ? -INFINITY : m * p.scale + logf(l);
 }
 
-// The end of the CTA's part of an item: the four warps' sums are added up, 8 queries at a time; a whole item is
-// written, a part goes to the workspace, and the last part's CTA joins them all.
+// Adds a part (m, l, eight channels) to another.
+struct Part {
+  float m, l, o[8];
+};
+__device__ __forceinline__ void join(Part& a, float m, float l, const float4& x, const float4& y, float cs) {
+  const float top = fmaxf(a.m, m), base = top == -INFINITY ? 0.f : top;
+  const float ka = exp2_approx((a.m - base) * cs), kb = exp2_approx((m - base) * cs);
+  a.m = top;
+  a.l = a.l * ka + l * kb;
+  const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a.o[i] = a.o[i] * ka + v[i] * kb;
+}
+
+// Takes a number; what the CTA's threads wrote before their last barrier is visible to whoever takes a later one.
+__device__ __forceinline__ uint32_t take_ticket(uint32_t* counter) {
+  uint32_t n;
+  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;\n" : "=r"(n) : "l"(counter) : "memory");
+  return n;
+}
+
+// The end of the CTA's part of an item: the four warps' sums are added up, 8 queries at a time, 16 threads to a query; a
+// whole item is written, a part goes to the workspace, and the last part's CTA joins them all.
 template <bool F16, int NT>
-__device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cursor& c, bool whole, bool begins,
-                            int64_t item_u0, const Work& w, float* scratch, volatile int* misc, float cs) {
+__device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cursor& c, bool whole, bool begins, int64_t tile_u0,
+                            const Work& w, float* scratch, volatile int* misc, float cs) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, tq = lane % 4;
-  float* slot = partial_of(p, blockIdx.x, begins);
+  const int mine = threadIdx.x / 16, channel = 8 * (threadIdx.x % 16);
+  float* ml = scratch;  // [warp][query] m, l, then 128 channels
+  float* o = scratch + kConsumers * 8 * 2;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) st.l[nt][j] += __shfl_xor_sync(kAll, st.l[nt][j], o);
-    // [warp][query] m, l and 128 channels
-    if (nt > 0) named_barrier<kConsumers * 32>(1);
-    float* ml = scratch;
-    float* o = scratch + 3 * 8 * 2;
-    if (warp > 0) {
+      for (int i = 4; i < 32; i <<= 1) st.l[nt][j] += __shfl_xor_sync(kAll, st.l[nt][j], i);
+    if (nt > 0) named_barrier<kConsumers * 32>(1);  // the first queries' sums are read
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int row = (warp - 1) * 8 + 2 * tq + j;
-        if (g == 0) {
-          ml[2 * row] = st.m[nt][j];
-          ml[2 * row + 1] = st.l[nt][j];
-        }
+    for (int j = 0; j < 2; ++j) {
+      const int row = warp * 8 + 2 * tq + j;
+      if (g == 0) {
+        ml[2 * row] = st.m[nt][j];
+        ml[2 * row + 1] = st.l[nt][j];
+      }
 #pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          o[row * kHeadDim + 16 * d + g] = st.o[nt][d][j];
-          o[row * kHeadDim + 16 * d + 8 + g] = st.o[nt][d][2 + j];
-        }
+      for (int d = 0; d < 8; ++d) {
+        o[row * kHeadDim + 16 * d + g] = st.o[nt][d][j];
+        o[row * kHeadDim + 16 * d + 8 + g] = st.o[nt][d][2 + j];
       }
     }
     named_barrier<kConsumers * 32>(1);
-    if (warp == 0) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float m = st.m[nt][j], l = 0.f;
-        const int q = 2 * tq + j;
-#pragma unroll
-        for (int w = 0; w < 3; ++w) m = fmaxf(m, ml[2 * (8 * w + q)]);
-        const float base = m == -INFINITY ? 0.f : m;
-        const float own = exp2_approx((st.m[nt][j] - base) * cs);
-        l = st.l[nt][j] * own;
-        float e[3];
-#pragma unroll
-        for (int w = 0; w < 3; ++w) {
-          e[w] = exp2_approx((ml[2 * (8 * w + q)] - base) * cs);
-          l += ml[2 * (8 * w + q) + 1] * e[w];
-        }
-        st.m[nt][j] = m;
-        st.l[nt][j] = l;
-#pragma unroll
-        for (int d = 0; d < 8; ++d)
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float x = st.o[nt][d][2 * half + j] * own;
-#pragma unroll
-            for (int w = 0; w < 3; ++w) x += o[(8 * w + q) * kHeadDim + 16 * d + 8 * half + g] * e[w];
-            st.o[nt][d][2 * half + j] = x;
-          }
+    const int q = 8 * nt + mine;
+    if (q < p.group) {
+      Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 1
+      for (int i = 0; i < kConsumers; ++i) {
+        const float4* x = reinterpret_cast<const float4*>(o + (8 * i + mine) * kHeadDim + channel);
+        join(a, ml[2 * (8 * i + mine)], ml[2 * (8 * i + mine) + 1], x[0], x[1], cs);
       }
-      // back through shared memory, so that a query's channels lie side by side
-      __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          o[(2 * tq + j) * kHeadDim + 16 * d + g] = st.o[nt][d][j];
-          o[(2 * tq + j) * kHeadDim + 16 * d + 8 + g] = st.o[nt][d][2 + j];
-        }
-      if (g == 0)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          ml[2 * (2 * tq + j)] = st.m[nt][j];
-          ml[2 * (2 * tq + j) + 1] = st.l[nt][j];
-        }
-    }
-    named_barrier<kConsumers * 32>(1);
-    for (int q = warp; q < 8 && 8 * nt + q < p.group; q += kConsumers) {
-      const float4 x = *reinterpret_cast<const float4*>(o + q * kHeadDim + 4 * lane);
       if (whole) {
-        write_query<F16>(p, c.b, c.h, 8 * nt + q, ml[2 * q], ml[2 * q + 1], x, c.len, cs);
+        write_query<F16>(p, c, q, channel, a.m, a.l, a.o);
       } else {
-        float* row = slot + (8 * nt + q) * kPartialFloats;
-        *reinterpret_cast<float4*>(row + 4 + 4 * lane) = x;
-        if (lane == 0) *reinterpret_cast<float2*>(row) = make_float2(ml[2 * q], ml[2 * q + 1]);
+        float* row = partial_of(p, blockIdx.x, begins) + q * kPartialFloats;
+        *reinterpret_cast<float4*>(row + 4 + channel) = make_float4(a.o[0], a.o[1], a.o[2], a.o[3]);
+        *reinterpret_cast<float4*>(row + 8 + channel) = make_float4(a.o[4], a.o[5], a.o[6], a.o[7]);
+        if (channel == 0) *reinterpret_cast<float2*>(row) = make_float2(a.m, a.l);
       }
     }
   }
-  if (whole) {
-    named_barrier<kConsumers * 32>(1);  // the scratch is free again
-    return;
-  }
-  // ticket: the parts before it are visible to the last one
-  const int cta0 = w.cta_of(item_u0), cta1 = w.cta_of(item_u0 + c.tiles - 1);
-  uint32_t* counter = p.counters + (int64_t)c.b * p.pool.heads + c.h;
-  __threadfence();
-  named_barrier<kConsumers * 32>(1);
+  named_barrier<kConsumers * 32>(1);  // the scratch is free again; the part is written
+  if (whole) return;
+  const int cta0 = w.cta_of(tile_u0), cta1 = w.cta_of(tile_u0 + c.tiles - 1);
   if (threadIdx.x == 0) {
-    const uint32_t before = atomicAdd(counter, 1u);
-    misc[1] = before == (uint32_t)(cta1 - cta0);
-    if (misc[1]) *counter = 0u;
-    __threadfence();
+    uint32_t* counter = p.counters + (int64_t)c.b * p.pool.heads + c.h;
+    const bool last = take_ticket(counter) == (uint32_t)(cta1 - cta0);
+    if (last) *counter = 0u;
+    misc[1] = last;
   }
   named_barrier<kConsumers * 32>(1);
   if (!misc[1]) return;
-  __threadfence();
-  for (int q = warp; q < p.group; q += kConsumers) {
-    float m = -INFINITY;
-    for (int i = cta0 + lane; i <= cta1; i += 32) {
-      m = fmaxf(m, __ldcg(partial_of(p, i, i == cta0) + q * kPartialFloats));
+  // fewer than five queries: several groups of 16 threads take every second, fourth or eighth part of each
+  const int apart = NT > 1 || p.group > 4 ? 8 : p.group > 2 ? 4 : p.group, subs = 8 / apart, sub = mine / apart;
+  for (int q = mine % apart; q < p.group; q += apart) {
+    Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+    constexpr int kBatch = 4;  // parts whose reads are in flight together
+#pragma unroll 1
+    for (int i0 = cta0 + sub; i0 <= cta1; i0 += kBatch * subs) {
+      float2 s[kBatch];
+      float4 x[kBatch], y[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int cta = i0 + i * subs;
+        const float* row = partial_of(p, min(cta, cta1), cta == cta0) + q * kPartialFloats;
+        s[i] = __ldcg(reinterpret_cast<const float2*>(row));
+        x[i] = __ldcg(reinterpret_cast<const float4*>(row + 4 + channel));
+        y[i] = __ldcg(reinterpret_cast<const float4*>(row + 8 + channel));
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (i0 + i * subs <= cta1) join(a, s[i].x, s[i].y, x[i], y[i], cs);
     }
-    m = warp_max(m);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = cta0; i <= cta1; ++i) {
-      const float* row = partial_of(p, i, i == cta0) + q * kPartialFloats;
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(row));
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(row + 4) + lane);
-      const float e = exp2_approx((ml.x - base) * cs);
-      l += ml.y * e;
-      acc.x += x.x * e;
-      acc.y += x.y * e;
-      acc.z += x.z * e;
-      acc.w += x.w * e;
+    if (subs > 1) {  // then there is one round
+      float4* mine_o = reinterpret_cast<float4*>(o + mine * kHeadDim + channel);
+      mine_o[0] = make_float4(a.o[0], a.o[1], a.o[2], a.o[3]);
+      mine_o[1] = make_float4(a.o[4], a.o[5], a.o[6], a.o[7]);
+      if (channel == 0) {
+        ml[2 * mine] = a.m;
+        ml[2 * mine + 1] = a.l;
+      }
+    } else {
+      write_query<F16>(p, c, q, channel, a.m, a.l, a.o);
     }
-    write_query<F16>(p, c.b, c.h, q, m, l, acc, c.len, cs);
   }
+  if (subs == 1) return;
+  named_barrier<kConsumers * 32>(1);
+  if (mine < p.group) {
+    Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+    for (int i = 0; i < subs; ++i) {
+      const int from = i * apart + mine;
+      const float4* x = reinterpret_cast<const float4*>(o + from * kHeadDim + channel);
+      join(a, ml[2 * from], ml[2 * from + 1], x[0], x[1], cs);
+    }
+    write_query<F16>(p, c, mine, channel, a.m, a.l, a.o);
+  }
+  named_barrier<kConsumers * 32>(1);  // the scratch is free again
 }
 
 template <bool F16, int NT>
-__device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, uint32_t base, char* smem, volatile int* misc) {
+__device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int64_t tiles, uint32_t base, char* smem,
+                        volatile int* misc) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t full = base + Smem::bars, empty = full + 8 * kStages;
   const int rows = min(p.pool.page_size, kTile);
   const float cs = p.scale * kLog2e;
   float* scratch = reinterpret_cast<float*>(smem + Smem::scratch);
+  const int* kept = reinterpret_cast<const int*>(smem + Smem::lengths);
   uint32_t n = 0;
   bool alive = true;  // false: a wait ran out, and the warp only keeps up with the others' barriers
-  for (int64_t u = w.u0; u < w.u1; next_item(p, c)) {
-    const int64_t item_u0 = u - c.t;
-    const bool begins = item_u0 >= w.u0, whole = c.t == 0 && u + c.tiles <= w.u1;
+  // unit of the first item's first tile
+  int64_t tile_u0 = w.u0 - w.first_unit + kItemCost;
+  Queries<NT> queries;
+  if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);
+  while (tiles > 0) {
+    if (NT > 1) fetch_queries<NT>(p, c.b, c.h, queries);
+    const bool begins = c.t == 0, whole = begins && c.tiles <= tiles;
     uint32_t qf[NT][16];
-    load_queries<F16, NT>(p, c.b, c.h, base + Smem::scratch + warp * 8 * kQRowBytes, qf);
+    stage_queries<F16, NT>(p, queries, base + Smem::scratch + warp * 8 * kQRowBytes, qf);
     State<NT> st;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -480,7 +565,7 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, uin
 #pragma unroll
         for (int i = 0; i < 4; ++i) st.o[nt][d][i] = 0.f;
     }
-    for (; c.t < c.tiles && u < w.u1; ++c.t, ++u, ++n) {
+    for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
       const int s = n % kStages;
       alive = alive && wait_phase(full + 8 * s, (n / kStages) & 1, misc, p.status);
       const uint32_t kt = base + s * kStageBytes, vt = kt + kStageBytes / 2;
@@ -503,16 +588,20 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, uin
       __syncwarp();
       if (lane == 0) mbar_arrive(empty + 8 * s);
     }
-    --c.t;  // the item's last tile of this run
+    const Cursor done = c;
+    if (tiles > 0) {  // the next item's queries come in meanwhile
+      next_item(p, kept, c);
+      if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);  // (of 16 queries they would take the sums' registers)
+    }
     named_barrier<kConsumers * 32>(1);  // every warp has read its queries from the scratch
-    finish_item<F16, NT>(p, st, c, whole, begins, item_u0, w, scratch, misc, cs);
+    finish_item<F16, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs);
+    tile_u0 += done.tiles + kItemCost;
   }
 }
 
 template <bool F16, int NT>
 __global__ void __launch_bounds__(kThreads, 2) pages_decode_kernel(const __grid_constant__ PagesDecodeParams p) {
-  extern __shared__ char raw[];
-  char* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+  extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_u32(smem), full = base + Smem::bars, empty = full + 8 * kStages;
   volatile int* misc = reinterpret_cast<int*>(smem + Smem::misc);  // [0] abort, [1] last part, [8 ..] scan
   if (threadIdx.x == 0) {
@@ -526,15 +615,18 @@ __global__ void __launch_bounds__(kThreads, 2) pages_decode_kernel(const __grid_
   __syncthreads();
   grid_launch_dependents();
   grid_dependency_wait();
+  prefetch_queries(p);
   Work w;
   Cursor c;
-  if (!find_work(p, const_cast<int*>(misc) + 8, w, c)) return;
+  int* kept = reinterpret_cast<int*>(smem + Smem::lengths);
+  const int64_t tiles = find_work(p, const_cast<int*>(misc) + 8, kept, w, c);
+  if (tiles == 0) return;
   uint32_t asked = 0;
   if (threadIdx.x / 32 == kConsumers) {
     fence_proxy_async_global();  // pages written by ordinary stores of earlier launches
-    asked = produce(p, c, w.u1 - w.u0, base, full, empty, misc);
+    asked = produce(p, c, tiles, kept, base, full, empty, misc);
   } else {
-    consume<F16, NT>(p, c, w, base, smem, misc);
+    consume<F16, NT>(p, c, w, tiles, base, smem, misc);
   }
   __syncthreads();
   if (misc[0]) {  // a CTA that gave up leaves once the copies it asked for have landed

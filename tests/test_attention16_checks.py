@@ -174,6 +174,8 @@ def test_decode_workspace_size(lib, pages):
     (dict(io=None), INVALID), (dict(q=NONE), INVALID), (dict(k=NONE), INVALID), (dict(v=NONE), INVALID), (dict(out=NONE), INVALID),
     (dict(k=_rows(A + 8)), ALIGN), (dict(v=_rows(token=129)), ALIGN), (dict(out=_rows(head=-8)), INVALID),
     (dict(lse=A + 2), ALIGN), (dict(ws=None), INVALID), (dict(ws=A + 8), ALIGN), (dict(ws_bytes=-1), WS_SMALL),
+    (dict(k=_rows(head=0)), UNSUPPORTED), (dict(q=_rows(token=64)), UNSUPPORTED),  # rows that share memory
+    (dict(k=_rows(head=0), ws=None), UNSUPPORTED),
 ])
 def test_prompt(lib, kw, status):
     need = ctypes.c_size_t()
@@ -240,3 +242,5 @@ def test_binding_decode_and_prompt(pool):
     _raises(lambda: hg._lse("f", torch.zeros(3, 8), 3, 8), "CUDA")
     _raises(lambda: hg.hg_prompt_attention(q.float(), k, k, i, i, q, None, True, 0.0, i), "bfloat16 or float16")
     _raises(lambda: hg.hg_prompt_attention(q, k, k, i, i, q, None, True, 0.0, i), "CUDA tensor")
+    _raises(lambda: hg._workspace("f", i), "workspace must be a CUDA tensor")
+    _raises(lambda: hg._workspace("f", None), "workspace must be a tensor")
