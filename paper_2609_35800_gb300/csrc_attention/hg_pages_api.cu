@@ -208,7 +208,11 @@ hg_status pages_decode(const hg_pages* pages, int32_t batch, int32_t num_q_heads
   if (!io || table_stride < 0 || !(softmax_scale == softmax_scale)) return HG_ERR_INVALID_ARG;
   if (batch == 0) return HG_OK;
   if ((table_stride > 0 && !page_table) || !lengths || !ws) return HG_ERR_INVALID_ARG;
-  if ((int64_t)table_stride * pages->pool.page_size > INT32_MAX) return HG_ERR_UNSUPPORTED;
+  // the kernel numbers tokens, and tiles and fixed costs of every request and head, in 32 bits
+  const int64_t capacity = (int64_t)table_stride * pages->pool.page_size;
+  if (capacity > INT32_MAX ||
+      (capacity / kDecodeTile + 1 + kDecodeItemCost) * pages->pool.heads > INT32_MAX / std::max(batch, 1))
+    return HG_ERR_UNSUPPORTED;
   st = store ? check_all({&io->q, &io->k, &io->v, &io->out}) : check_all({&io->q, &io->out});
   if (st != HG_OK) return st;
   st = check_rotation(rotation, positions);

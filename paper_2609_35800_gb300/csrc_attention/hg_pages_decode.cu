@@ -4,7 +4,7 @@
 // Every key and value is used by G <= 16 queries only, 2 G flop per byte, so the kernel is bound by the reads of the
 // cache; it has to keep enough of them in flight and to spread them evenly.
 //
-// The work is cut into tiles of 64 tokens of one (request, KV head), numbered request by request, head by head; each
+// The work is cut into tiles of 32 tokens of one (request, KV head), numbered request by request, head by head; each
 // such item counts as kItemCost tiles more, ahead of its first, for its queries, sums and result.  CTA i of n takes the
 // units [T i / n, T (i + 1) / n): the same share for everybody whatever the requests' lengths, which the kernel reads on
 // the device.  A CTA's run cuts at most two items, its first and its last; it leaves their (m, l, o) in the workspace,
@@ -12,9 +12,11 @@
 // who comes last.  Where no item is more than kJoinCost units longer than the share, joining would cost more than it
 // gains, and a CTA takes the whole items that begin in its units.
 //
-// A producer warp copies tiles into a ring of three 32 KB stages with TMA, a box per page (swizzled rows; a page id
-// outside the pool reads as zeros).  Each of four consumer warps takes 16 of a tile's 64 tokens, with its own running
-// maximum and sums, and computes with mma.sync m16n8k16 (a tcgen05 product would have M = 128 tokens by N = 8 queries
+// A producer warp copies tiles into a ring of six 16 KB stages with TMA, a box per page (swizzled rows; a page id
+// outside the pool reads as zeros).  Three consumer warps take the tiles in turn, each with its own running maximum and
+// sums, so that three tiles' chains of load, product, maximum, exponential and product run side by side (four warps on
+// 16 tokens each of one 64-token tile needed about 1,200 cycles a tile).  Two of the stages belong to each warp: it waits
+// for every phase of their barriers, in order, as a wait by parity needs.  They compute with mma.sync m16n8k16 (a tcgen05 product would have M = 128 tokens by N = 8 queries
 // and its probabilities would pass through TMEM; the tensor work here is a few per cent of what mma.sync gives):
 //   S^T[token][query] = K . q        A = keys (ldmatrix), B = the queries, padded to 8 or 16
 //   O^T[channel][query] += V^T . P^T A = values (ldmatrix.trans), B = P^T (movmatrix of the scores' fragment)
@@ -26,31 +28,34 @@
 namespace hg {
 namespace {
 
-constexpr int kTile = kDecodeTile;
-constexpr int kStages = 3;
+constexpr int kTile = kDecodeTile, kTileShift = 5;
+static_assert(kTile == 1 << kTileShift, "tile");
+constexpr int kStages = 6;
 constexpr int kStageBytes = 2 * kTile * kHeadDim * 2;  // keys, then values
-constexpr int kConsumers = 4;
+constexpr int kConsumers = 3;
 constexpr int kThreads = (kConsumers + 1) * 32;
+static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
 constexpr int kQRowBytes = 272;  // a staged query row: 256 bytes, 16 more so that ldmatrix meets every bank once
 constexpr unsigned kAll = 0xffffffffu;
 constexpr float kRescale = 8.0f;  // log2 of how far a score may pass the running maximum
 
-constexpr int kItemCost = 2;  // an item's fixed costs, in tiles
-constexpr int kJoinCost = 7;  // a ticket and a join, in tiles
-constexpr int kKeptLengths = 88;
+constexpr int kItemCost = kDecodeItemCost;
+constexpr int kJoinCost = 16;  // a ticket and a join, in tiles
+constexpr int kKeptLengths = 72;
+constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l; rows 4 banks apart
 
 // Shared memory, two CTAs an SM.  The staged queries (8 rows a warp) and the warps' parts that are added up at an item's
 // end (8 queries at a time) take turns in one region.
 struct Smem {
   static constexpr int scratch = kStages * kStageBytes;
-  static constexpr int scratch_bytes = kConsumers * 8 * (kHeadDim + 2) * 4;
+  static constexpr int scratch_bytes = kConsumers * 8 * kSumFloats * 4;
   static constexpr int bars = scratch + scratch_bytes;
   static constexpr int misc = bars + 2 * kStages * 8;  // abort flag, last part, start of the CTA's work, scan
   static constexpr int lengths = misc + 128;           // the first requests' lengths
   static constexpr int bytes = lengths + 4 * kKeptLengths;
 };
 static_assert(Smem::scratch_bytes >= kConsumers * 8 * kQRowBytes, "queries are staged there too");
-static_assert((8 + 17) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
+static_assert((8 + 12 + kConsumers + 1) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
 static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 
 // Where a run of tiles stands.
@@ -82,17 +87,22 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// The units [u0, u1) of the launch's `total` that this CTA, one of `ctas` that have any, takes.
+// The launch's units, cut into `ctas` runs of `share` units, the first `more` of them one longer; those of this CTA are
+// [u0, u1).
 struct Work {
-  int64_t u0, u1, total, ctas;
+  int u0, u1, total, ctas, share, more;
   int first_unit;  // of its item, that u0 is
-  __device__ __forceinline__ int cta_of(int64_t u) const { return (int)(((u + 1) * ctas - 1) / total); }
+  __device__ __forceinline__ int start_of(int cta) const { return cta * share + min(cta, more); }
+  __device__ __forceinline__ int cta_of(int u) const {
+    const int longer = more * (share + 1);
+    return u < longer ? u / (share + 1) : more + (u - longer) / share;
+  }
 };
 
 // The CTA's work, the first tile of it and how many there are; 0: none.  Every thread adds up the units of its share of
 // the requests; the one whose share holds u0 looks for it there.
-__device__ int64_t find_work(const PagesDecodeParams& p, int* scan, int* kept, Work& w, Cursor& c) {
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+__device__ int find_work(const PagesDecodeParams& p, int* scan, int* kept, Work& w, Cursor& c) {
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, heads = p.pool.heads;
   const int per = (p.batch + kThreads - 1) / kThreads;
   const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
   int mine = 0, longest = 0;
@@ -121,39 +131,40 @@ __device__ int64_t find_work(const PagesDecodeParams& p, int* scan, int* kept, W
     all += scan[i];
     longest = max(longest, scan[12 + i]);
   }
-  w.total = (int64_t)all * p.pool.heads;
-  w.ctas = min((int64_t)gridDim.x, w.total);
-  if (blockIdx.x >= w.ctas) return 0;
-  w.u0 = w.total * blockIdx.x / w.ctas;
-  w.u1 = w.total * (blockIdx.x + 1) / w.ctas;
-  const int64_t at = w.u0 - (int64_t)before * p.pool.heads;
-  if (at >= 0 && at < (int64_t)mine * p.pool.heads) {
-    int64_t left = at;
+  w.total = all * heads;
+  w.ctas = min((int)gridDim.x, w.total);
+  if ((int)blockIdx.x >= w.ctas) return 0;
+  w.share = w.total / w.ctas;
+  w.more = w.total - w.share * w.ctas;
+  w.u0 = w.start_of(blockIdx.x);
+  w.u1 = w.start_of(blockIdx.x + 1);
+  int left = w.u0 - before * heads;
+  if (left >= 0 && left < mine * heads) {
     int b = b0, len = 0, units = 0;
     for (;; ++b) {
-      len = request_length(p, b);
+      len = b < kKeptLengths ? kept[b] : request_length(p, b);
       units = tiles_of(len) + kItemCost;
-      if (left < (int64_t)units * p.pool.heads) break;
-      left -= (int64_t)units * p.pool.heads;
+      if (left < units * heads) break;
+      left -= units * heads;
     }
     scan[8] = b;
-    scan[9] = (int)(left / units);
-    scan[10] = (int)(left % units);
+    scan[9] = left / units;
+    scan[10] = left - scan[9] * units;
     scan[11] = len;
   }
   __syncthreads();
   w.first_unit = scan[10];
   c = {scan[8], scan[9], max(0, w.first_unit - kItemCost), scan[11], tiles_of(scan[11])};
-  if (longest <= w.total / w.ctas + kJoinCost) {
+  int tiles = 0;
+  if (longest <= w.share + kJoinCost) {
     // from the first item that begins at u0 or later to the last that begins before u1
-    int64_t at = w.u0;
+    int at = w.u0;
     if (w.first_unit > 0) {
       at += c.tiles + kItemCost - w.first_unit;
       w.first_unit = 0;
       if (at < w.u1) next_item(p, kept, c);
     }
     w.u0 = at;
-    int64_t tiles = 0;
     for (Cursor x = c; at < w.u1;) {
       tiles += x.tiles;
       at += x.tiles + kItemCost;
@@ -162,14 +173,13 @@ __device__ int64_t find_work(const PagesDecodeParams& p, int* scan, int* kept, W
     return tiles;
   }
   // the run's units less those that stand for fixed costs
-  int64_t left = w.u1 - w.u0, tiles = 0;
-  int skip = max(0, kItemCost - w.first_unit);
-  for (Cursor x = c; left > skip; skip = kItemCost) {
-    left -= skip;
-    const int64_t n = min(left, (int64_t)(x.tiles - x.t));
+  int rest = w.u1 - w.u0, skip = max(0, kItemCost - w.first_unit);
+  for (Cursor x = c; rest > skip; skip = kItemCost) {
+    rest -= skip;
+    const int n = min(rest, x.tiles - x.t);
     tiles += n;
-    left -= n;
-    if (left > 0) next_item(p, kept, x);
+    rest -= n;
+    if (rest > 0) next_item(p, kept, x);
   }
   return tiles;
 }
@@ -192,11 +202,11 @@ __device__ void prefetch_queries(const PagesDecodeParams& p) {
 }
 
 // Copies the CTA's tiles into the ring, in order; returns how many it asked for.
-__device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int64_t tiles, const int* kept, uint32_t stages, uint32_t full,
+__device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int tiles, const int* kept, uint32_t stages, uint32_t full,
                             uint32_t empty, volatile int* abort) {
   const int lane = threadIdx.x % 32;
-  const int rows = min(p.pool.page_size, kTile);  // tokens of a box
-  const int boxes = kTile / rows;
+  const int shift = min(p.pool.page_shift, kTileShift), rows = 1 << shift;  // tokens of a box
+  const int boxes = kTile >> shift;
   const uint32_t box_bytes = (uint32_t)rows * kHeadDim * 2;
   uint32_t n = 0;
   // 32 boxes' page ids, a lane each, from box `first` of request `of` on
@@ -205,7 +215,7 @@ __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int64_t tiles,
     const int* ids = p.table + (int64_t)c.b * p.table_stride;
     for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
       const int box0 = c.t * boxes;  // box number in the item
-      const int valid = min(boxes, max(0, (c.len - c.t * kTile + rows - 1) / rows));
+      const int valid = min(boxes, max(0, (c.len - c.t * kTile + rows - 1) >> shift));
       if (of != c.b || box0 < first || box0 + boxes > first + 32) {
         of = c.b;
         first = box0;
@@ -214,14 +224,15 @@ __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int64_t tiles,
       }
       const int s = n % kStages;
       if (n >= kStages && !wait_phase(empty + 8 * s, (n / kStages - 1) & 1, abort, p.status)) return n;
-      if (lane == 0) mbar_arrive_expect_tx(full + 8 * s, 2 * valid * box_bytes);
-      __syncwarp();
-      const int page = __shfl_sync(kAll, id, (box0 - first + lane) & 31);
-      if (lane < valid) {
-        const int row = ((box0 + lane) * rows) & (p.pool.page_size - 1);
-        const uint32_t dst = stages + s * kStageBytes + lane * box_bytes;
-        tma_page(dst, &p.k_map, row, c.h, page, full + 8 * s);
-        tma_page(dst + kStageBytes / 2, &p.v_map, row, c.h, page, full + 8 * s);
+      if (elect_one()) mbar_arrive_expect_tx(full + 8 * s, 2 * valid * box_bytes);
+      for (int i = 0; i < valid; ++i) {
+        const int page = __shfl_sync(kAll, id, box0 - first + i);
+        const int row = ((box0 + i) << shift) & (p.pool.page_size - 1);
+        const uint32_t dst = stages + s * kStageBytes + i * box_bytes;
+        if (elect_one()) {  // (lanes that issue side by side take turns, one copy after the other)
+          tma_page(dst, &p.k_map, row, c.h, page, full + 8 * s);
+          tma_page(dst + kStageBytes / 2, &p.v_map, row, c.h, page, full + 8 * s);
+        }
       }
     }
   }
@@ -293,10 +304,16 @@ __device__ __forceinline__ void stage_queries(const PagesDecodeParams& p, Querie
   }
 }
 
+// 16-byte chunk of a tile's row: boxes of `rows` (16 or 32) rows, first halves before second halves.
+__device__ __forceinline__ uint32_t tile_chunk(uint32_t tile, int rows, int r, int chunk) {
+  const int box = r & ~(rows - 1);
+  return tile + box * kHeadDim * 2 + (chunk / 8) * rows * 128 + swizzled(r - box, chunk % 8);
+}
+
 // The new token of a decode step: into its page, and over row r of the stage's tile (which may hold what was there).
 template <bool F16>
-__device__ __forceinline__ void place_new_token(const PagesDecodeParams& p, const Cursor& c, uint32_t kbox, uint32_t vbox,
-                                                int rows, int r) {
+__device__ __forceinline__ void place_new_token(const PagesDecodeParams& p, const Cursor& c, uint32_t kt, uint32_t vt, int rows,
+                                                int r) {
   const int lane = threadIdx.x % 32;
   if (lane < 16) {
     const int i = lane % 8;
@@ -306,9 +323,8 @@ __device__ __forceinline__ void place_new_token(const PagesDecodeParams& p, cons
     const uint16_t* src = in.data + c.b * in.token_stride + c.h * in.head_stride;
     uint4 lo = ldg16(src + at.lo), hi = ldg16(src + at.hi);
     if (at.turns) rotate_lane<F16>(lo, hi, lane_angles(p.rot, i, c.b), p.rot.interleaved != 0);
-    const uint32_t box = is_v ? vbox : kbox;
-    st_shared16(box + (at.lo / 64) * rows * 128 + swizzled(r, at.lo / 8 % 8), lo);
-    st_shared16(box + (at.hi / 64) * rows * 128 + swizzled(r, at.hi / 8 % 8), hi);
+    st_shared16(tile_chunk(is_v ? vt : kt, rows, r, at.lo / 8), lo);
+    st_shared16(tile_chunk(is_v ? vt : kt, rows, r, at.hi / 8), hi);
     const int last = c.len - 1;
     const int page = p.table[(int64_t)c.b * p.table_stride + (last >> p.pool.page_shift)];
     if (page >= 0 && page < p.pool.num_pages) {
@@ -320,36 +336,55 @@ __device__ __forceinline__ void place_new_token(const PagesDecodeParams& p, cons
   __syncwarp();
 }
 
-// 16 tokens of a tile, of which the first `seen` belong to the request.
+// A tile of 32 tokens, of which the first `seen` belong to the request; box(r): where row r's box begins.
 template <bool F16, int NT>
-__device__ __forceinline__ void attend_slice(const PagesDecodeParams& p, State<NT>& st, const uint32_t (&qf)[NT][16], uint32_t kbox,
-                                             uint32_t vbox, int rows, int r0, int seen, float c) {
+__device__ __forceinline__ void attend_tile(State<NT>& st, const uint32_t (&qf)[NT][16], uint32_t kt, uint32_t vt, int rows, int seen,
+                                            float c) {
   const int lane = threadIdx.x % 32;
-  float s[NT][4];
-  float s2[NT][4];  // two chains of products, one for each half of the channels
+  float s[2][NT][4], s2[2][NT][4];  // [16 tokens][query tile]; a chain of products for each half of the channels
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+  for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[nt][i] = s2[nt][i] = 0.f;
-  const int kr = r0 + lane % 16;
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[mt][nt][i] = s2[mt][nt][i] = 0.f;
+  // rows are 16 (a page's 16 tokens a box) or 32: token 16 mt + r lies in box mt, row r, or in the box's row 16 mt + r
+  const uint32_t second = rows == 16 ? 16 * kHeadDim * 2 : 16 * 128, half = rows * 128;
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks) {
-    uint32_t a[4], a2[4];
-    ldsm_x4(a, kbox + swizzled(kr, 2 * ks + lane / 16));
-    ldsm_x4(a2, kbox + rows * 128 + swizzled(kr, 2 * ks + lane / 16));
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      mma16<F16>(s[nt], a, qf[nt][2 * ks], qf[nt][2 * ks + 1]);
-      mma16<F16>(s2[nt], a2, qf[nt][8 + 2 * ks], qf[nt][8 + 2 * ks + 1]);
+    for (int mt = 0; mt < 2; ++mt) {
+      uint32_t a[4], a2[4];
+      const uint32_t at = kt + mt * second + swizzled(lane % 16, 2 * ks + lane / 16);
+      ldsm_x4(a, at);
+      ldsm_x4(a2, at + half);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        mma16<F16>(s[mt][nt], a, qf[nt][2 * ks], qf[nt][2 * ks + 1]);
+        mma16<F16>(s2[mt][nt], a2, qf[nt][8 + 2 * ks], qf[nt][8 + 2 * ks + 1]);
+      }
     }
   }
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[mt][nt][i] += s2[mt][nt][i];
   const int g = lane / 4;
-  uint32_t pf[NT][2];
+  uint32_t pf[2][NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
+    if (seen < kTile) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[nt][i] = g + 8 * (i / 2) < seen ? s[nt][i] + s2[nt][i] : -INFINITY;
-    float top[2] = {fmaxf(s[nt][0], s[nt][2]), fmaxf(s[nt][1], s[nt][3])};
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * mt + g + 8 * (i / 2) >= seen) s[mt][nt][i] = -INFINITY;
+    }
+    float top[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) top[j] = fmaxf(fmaxf(s[0][nt][j], s[0][nt][2 + j]), fmaxf(s[1][nt][j], s[1][nt][2 + j]));
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) {
       top[0] = fmaxf(top[0], __shfl_xor_sync(kAll, top[0], o));
@@ -372,22 +407,26 @@ __device__ __forceinline__ void attend_slice(const PagesDecodeParams& p, State<N
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float m = st.m[nt][i % 2];
-      s[nt][i] = exp2_approx((s[nt][i] - (m == -INFINITY ? 0.f : m)) * c);
-      st.l[nt][i % 2] += s[nt][i];
+    for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float m = st.m[nt][i % 2];
+        s[mt][nt][i] = exp2_approx((s[mt][nt][i] - (m == -INFINITY ? 0.f : m)) * c);
+        st.l[nt][i % 2] += s[mt][nt][i];
+      }
+      pf[mt][nt][0] = movtrans(pack2<F16>(s[mt][nt][0], s[mt][nt][1]));
+      pf[mt][nt][1] = movtrans(pack2<F16>(s[mt][nt][2], s[mt][nt][3]));
     }
-    pf[nt][0] = movtrans(pack2<F16>(s[nt][0], s[nt][1]));
-    pf[nt][1] = movtrans(pack2<F16>(s[nt][2], s[nt][3]));
   }
-  const int vr = r0 + lane % 8 + 8 * (lane / 16);
 #pragma unroll
-  for (int d = 0; d < 8; ++d) {
-    uint32_t a[4];
-    ldsm_x4_trans(a, vbox + (d / 4) * rows * 128 + swizzled(vr, 2 * (d % 4) + lane / 8 % 2));
+  for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) mma16<F16>(st.o[nt][d], a, pf[nt][0], pf[nt][1]);
-  }
+    for (int d = 0; d < 8; ++d) {
+      uint32_t a[4];
+      ldsm_x4_trans(a, vt + mt * second + (d / 4) * half + swizzled(lane % 8 + 8 * (lane / 16), 2 * (d % 4) + lane / 8 % 2));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma16<F16>(st.o[nt][d], a, pf[mt][nt][0], pf[mt][nt][1]);
+    }
 }
 
 // A CTA's part of the item that begins in its run (`begins`), or of the one that began before it.
@@ -395,31 +434,71 @@ __device__ __forceinline__ float* partial_of(const PagesDecodeParams& p, int cta
   return p.partials + ((int64_t)cta * 2 + (begins ? 1 : 0)) * p.group * kPartialFloats;
 }
 
-// Eight channels of out = o / l in the cache's type, and the query's log-sum-exp.
-template <bool F16>
-__device__ __forceinline__ void write_query(const PagesDecodeParams& p, const Cursor& c, int q, int channel, float m, float l,
-                                            const float (&o)[8]) {
-  const float r = c.len > 0 ? 1.0f / l : 0.f;
-  const int head = c.h * p.group + q;
-  uint16_t* out = p.out.data + c.b * p.out.token_stride + head * p.out.head_stride;
-  *reinterpret_cast<uint4*>(out + channel) = make_uint4(pack2<F16>(o[0] * r, o[1] * r), pack2<F16>(o[2] * r, o[3] * r),
-                                                        pack2<F16>(o[4] * r, o[5] * r), pack2<F16>(o[6] * r, o[7] * r));
-  if (p.lse && channel == 0)
-    p.lse[(int64_t)c.b * p.pool.heads * p.group + head] = l == 0.f ? -INFINITY : m * p.scale + logf(l);
-}
-
-// Adds a part (m, l, eight channels) to another.
+// A query's sums, 16 channels of them.
 struct Part {
-  float m, l, o[8];
+  float m = -INFINITY, l = 0.f, o[16] = {};
 };
-__device__ __forceinline__ void join(Part& a, float m, float l, const float4& x, const float4& y, float cs) {
+// Adds a part: 16 channels at `o`, its m and l.
+__device__ __forceinline__ void join(Part& a, float m, float l, const float4 (&o)[4], float cs) {
   const float top = fmaxf(a.m, m), base = top == -INFINITY ? 0.f : top;
   const float ka = exp2_approx((a.m - base) * cs), kb = exp2_approx((m - base) * cs);
   a.m = top;
   a.l = a.l * ka + l * kb;
-  const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a.o[i] = a.o[i] * ka + v[i] * kb;
+  for (int i = 0; i < 4; ++i) {
+    a.o[4 * i] = a.o[4 * i] * ka + o[i].x * kb;
+    a.o[4 * i + 1] = a.o[4 * i + 1] * ka + o[i].y * kb;
+    a.o[4 * i + 2] = a.o[4 * i + 2] * ka + o[i].z * kb;
+    a.o[4 * i + 3] = a.o[4 * i + 3] * ka + o[i].w * kb;
+  }
+}
+// Adds up N rows of sums in shared memory, `apart` floats from one to the next: one maximum, then independent terms.
+template <int N>
+__device__ __forceinline__ Part add_rows(const float* row, int apart, int count, int channel, float cs) {
+  Part a;
+  float2 ml[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    ml[i] = i < count ? *reinterpret_cast<const float2*>(row + i * apart + kHeadDim) : make_float2(-INFINITY, 0.f);
+    a.m = fmaxf(a.m, ml[i].x);
+  }
+  const float base = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i >= count) break;
+    const float e = exp2_approx((ml[i].x - base) * cs);
+    a.l += ml[i].y * e;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(row + i * apart + channel + 4 * k);
+      a.o[4 * k] += x.x * e;
+      a.o[4 * k + 1] += x.y * e;
+      a.o[4 * k + 2] += x.z * e;
+      a.o[4 * k + 3] += x.w * e;
+    }
+  }
+  return a;
+}
+__device__ __forceinline__ void store_part(const Part& a, float* channels, float* ml, int channel) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<float4*>(channels + channel + 4 * i) = make_float4(a.o[4 * i], a.o[4 * i + 1], a.o[4 * i + 2], a.o[4 * i + 3]);
+  if (channel == 0) *reinterpret_cast<float2*>(ml) = make_float2(a.m, a.l);
+}
+
+// out = o / l in the cache's type, and the query's log-sum-exp.
+template <bool F16>
+__device__ __forceinline__ void write_query(const PagesDecodeParams& p, const Cursor& c, int q, int channel, const Part& a) {
+  const float r = c.len > 0 ? 1.0f / a.l : 0.f;
+  const int head = c.h * p.group + q;
+  uint16_t* out = p.out.data + c.b * p.out.token_stride + head * p.out.head_stride + channel;
+  uint32_t x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = pack2<F16>(a.o[2 * i] * r, a.o[2 * i + 1] * r);
+  *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<uint4*>(out + 8) = make_uint4(x[4], x[5], x[6], x[7]);
+  if (p.lse && channel == 0)
+    p.lse[(int64_t)c.b * p.pool.heads * p.group + head] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l);
 }
 
 // Takes a number; what the CTA's threads wrote before their last barrier is visible to whoever takes a later one.
@@ -429,15 +508,14 @@ __device__ __forceinline__ uint32_t take_ticket(uint32_t* counter) {
   return n;
 }
 
-// The end of the CTA's part of an item: the four warps' sums are added up, 8 queries at a time, 16 threads to a query; a
-// whole item is written, a part goes to the workspace, and the last part's CTA joins them all.
+// The end of the CTA's part of an item: the warps' sums are added up, 8 queries at a time, 8 threads to a query; a whole
+// item is written, a part goes to the workspace, and the last part's CTA joins them all.
 template <bool F16, int NT>
-__device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cursor& c, bool whole, bool begins, int64_t tile_u0,
+__device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cursor& c, bool whole, bool begins, int tile_u0,
                             const Work& w, float* scratch, volatile int* misc, float cs) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, tq = lane % 4;
-  const int mine = threadIdx.x / 16, channel = 8 * (threadIdx.x % 16);
-  float* ml = scratch;  // [warp][query] m, l, then 128 channels
-  float* o = scratch + kConsumers * 8 * 2;
+  constexpr int kGroups = kConsumers * 4;
+  const int mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -447,33 +525,23 @@ __device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cur
     if (nt > 0) named_barrier<kConsumers * 32>(1);  // the first queries' sums are read
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int row = warp * 8 + 2 * tq + j;
-      if (g == 0) {
-        ml[2 * row] = st.m[nt][j];
-        ml[2 * row + 1] = st.l[nt][j];
-      }
+      float* row = scratch + (warp * 8 + 2 * tq + j) * kSumFloats;
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
-        o[row * kHeadDim + 16 * d + g] = st.o[nt][d][j];
-        o[row * kHeadDim + 16 * d + 8 + g] = st.o[nt][d][2 + j];
+        row[16 * d + g] = st.o[nt][d][j];
+        row[16 * d + 8 + g] = st.o[nt][d][2 + j];
       }
+      if (g == 0) *reinterpret_cast<float2*>(row + kHeadDim) = make_float2(st.m[nt][j], st.l[nt][j]);
     }
     named_barrier<kConsumers * 32>(1);
     const int q = 8 * nt + mine;
-    if (q < p.group) {
-      Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-#pragma unroll 1
-      for (int i = 0; i < kConsumers; ++i) {
-        const float4* x = reinterpret_cast<const float4*>(o + (8 * i + mine) * kHeadDim + channel);
-        join(a, ml[2 * (8 * i + mine)], ml[2 * (8 * i + mine) + 1], x[0], x[1], cs);
-      }
+    if (mine < 8 && q < p.group) {
+      const Part a = add_rows<kConsumers>(scratch + mine * kSumFloats, 8 * kSumFloats, kConsumers, channel, cs);
       if (whole) {
-        write_query<F16>(p, c, q, channel, a.m, a.l, a.o);
+        write_query<F16>(p, c, q, channel, a);
       } else {
         float* row = partial_of(p, blockIdx.x, begins) + q * kPartialFloats;
-        *reinterpret_cast<float4*>(row + 4 + channel) = make_float4(a.o[0], a.o[1], a.o[2], a.o[3]);
-        *reinterpret_cast<float4*>(row + 8 + channel) = make_float4(a.o[4], a.o[5], a.o[6], a.o[7]);
-        if (channel == 0) *reinterpret_cast<float2*>(row) = make_float2(a.m, a.l);
+        store_part(a, row + 4, row, channel);
       }
     }
   }
@@ -488,55 +556,45 @@ __device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cur
   }
   named_barrier<kConsumers * 32>(1);
   if (!misc[1]) return;
-  // fewer than five queries: several groups of 16 threads take every second, fourth or eighth part of each
-  const int apart = NT > 1 || p.group > 4 ? 8 : p.group > 2 ? 4 : p.group, subs = 8 / apart, sub = mine / apart;
-  for (int q = mine % apart; q < p.group; q += apart) {
-    Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+  // up to six queries: several groups of threads share a query's parts, each takes every `subs`-th
+  const int subs = max(1, kGroups / p.group), sub = mine / p.group;
+  for (int q = subs > 1 ? mine % p.group : mine; q < p.group && (subs == 1 || sub < subs); q += kGroups) {
+    Part a;
     constexpr int kBatch = 4;  // parts whose reads are in flight together
 #pragma unroll 1
-    for (int i0 = cta0 + sub; i0 <= cta1; i0 += kBatch * subs) {
+    for (int i0 = cta0 + (subs > 1 ? sub : 0); i0 <= cta1; i0 += kBatch * subs) {
       float2 s[kBatch];
-      float4 x[kBatch], y[kBatch];
+      float4 o[kBatch][4];
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
         const int cta = i0 + i * subs;
         const float* row = partial_of(p, min(cta, cta1), cta == cta0) + q * kPartialFloats;
         s[i] = __ldcg(reinterpret_cast<const float2*>(row));
-        x[i] = __ldcg(reinterpret_cast<const float4*>(row + 4 + channel));
-        y[i] = __ldcg(reinterpret_cast<const float4*>(row + 8 + channel));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[i][k] = __ldcg(reinterpret_cast<const float4*>(row + 4 + channel + 4 * k));
       }
 #pragma unroll
       for (int i = 0; i < kBatch; ++i)
-        if (i0 + i * subs <= cta1) join(a, s[i].x, s[i].y, x[i], y[i], cs);
+        if (i0 + i * subs <= cta1) join(a, s[i].x, s[i].y, o[i], cs);
     }
-    if (subs > 1) {  // then there is one round
-      float4* mine_o = reinterpret_cast<float4*>(o + mine * kHeadDim + channel);
-      mine_o[0] = make_float4(a.o[0], a.o[1], a.o[2], a.o[3]);
-      mine_o[1] = make_float4(a.o[4], a.o[5], a.o[6], a.o[7]);
-      if (channel == 0) {
-        ml[2 * mine] = a.m;
-        ml[2 * mine + 1] = a.l;
-      }
-    } else {
-      write_query<F16>(p, c, q, channel, a.m, a.l, a.o);
+    if (subs == 1) {
+      write_query<F16>(p, c, q, channel, a);
+    } else {  // then this is the only round
+      float* row = scratch + (sub * p.group + q) * kSumFloats;
+      store_part(a, row, row + kHeadDim, channel);
     }
   }
   if (subs == 1) return;
   named_barrier<kConsumers * 32>(1);
   if (mine < p.group) {
-    Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-    for (int i = 0; i < subs; ++i) {
-      const int from = i * apart + mine;
-      const float4* x = reinterpret_cast<const float4*>(o + from * kHeadDim + channel);
-      join(a, ml[2 * from], ml[2 * from + 1], x[0], x[1], cs);
-    }
-    write_query<F16>(p, c, mine, channel, a.m, a.l, a.o);
+    const Part a = add_rows<kGroups>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
+    write_query<F16>(p, c, mine, channel, a);
   }
   named_barrier<kConsumers * 32>(1);  // the scratch is free again
 }
 
 template <bool F16, int NT>
-__device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int64_t tiles, uint32_t base, char* smem,
+__device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int tiles, uint32_t base, char* smem,
                         volatile int* misc) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t full = base + Smem::bars, empty = full + 8 * kStages;
@@ -547,7 +605,7 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
   uint32_t n = 0;
   bool alive = true;  // false: a wait ran out, and the warp only keeps up with the others' barriers
   // unit of the first item's first tile
-  int64_t tile_u0 = w.u0 - w.first_unit + kItemCost;
+  int tile_u0 = w.u0 - w.first_unit + kItemCost;
   Queries<NT> queries;
   if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);
   while (tiles > 0) {
@@ -566,24 +624,22 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
         for (int i = 0; i < 4; ++i) st.o[nt][d][i] = 0.f;
     }
     for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
+      if (n % kConsumers != warp) continue;
       const int s = n % kStages;
       alive = alive && wait_phase(full + 8 * s, (n / kStages) & 1, misc, p.status);
       const uint32_t kt = base + s * kStageBytes, vt = kt + kStageBytes / 2;
-      const int t0 = 16 * warp, seen = c.len - c.t * kTile - t0;  // of this warp's 16 tokens
+      const int seen = c.len - c.t * kTile;
+      __syncwarp();
       if (alive && seen > 0) {
-        const uint32_t box = (uint32_t)(t0 / rows) * rows * kHeadDim * 2;
-        const int r0 = t0 % rows;
-        if (seen < 16) {
+        if (seen < kTile) {
           // what follows the request's last token may be anything, and 0 times NaN is no 0
-          for (int i = seen * 16 + lane; i < 256; i += 32) {
-            const int r = r0 + i / 16, chunk = i % 16;
-            st_shared16(vt + box + (chunk / 8) * rows * 128 + swizzled(r, chunk % 8), make_uint4(0u, 0u, 0u, 0u));
-          }
+          for (int i = seen * 16 + lane; i < kTile * 16; i += 32)
+            st_shared16(tile_chunk(vt, rows, i / 16, i % 16), make_uint4(0u, 0u, 0u, 0u));
         }
-        if (seen <= 16 && p.store) place_new_token<F16>(p, c, kt + box, vt + box, rows, r0 + seen - 1);
+        if (seen <= kTile && p.store) place_new_token<F16>(p, c, kt, vt, rows, seen - 1);
         __syncwarp();
-        attend_slice<F16, NT>(p, st, qf, kt + box, vt + box, rows, r0, seen, cs);
-        if (seen <= 16) fence_proxy_async_shared();  // TMA writes the stage again
+        attend_tile<F16, NT>(st, qf, kt, vt, rows, seen, cs);
+        if (seen <= kTile) fence_proxy_async_shared();  // TMA writes the stage again
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(empty + 8 * s);
@@ -607,19 +663,23 @@ __global__ void __launch_bounds__(kThreads, 2) pages_decode_kernel(const __grid_
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(full + 8 * i, 1);
-      mbar_init(empty + 8 * i, kConsumers);
+      mbar_init(empty + 8 * i, 1);
     }
     mbar_init_fence();
     misc[0] = 0;
   }
   __syncthreads();
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&p.k_map);
+    prefetch_tensormap(&p.v_map);
+  }
   grid_launch_dependents();
   grid_dependency_wait();
   prefetch_queries(p);
   Work w;
   Cursor c;
   int* kept = reinterpret_cast<int*>(smem + Smem::lengths);
-  const int64_t tiles = find_work(p, const_cast<int*>(misc) + 8, kept, w, c);
+  const int tiles = find_work(p, const_cast<int*>(misc) + 8, kept, w, c);
   if (tiles == 0) return;
   uint32_t asked = 0;
   if (threadIdx.x / 32 == kConsumers) {
