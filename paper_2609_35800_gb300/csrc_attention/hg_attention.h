@@ -49,7 +49,7 @@ struct PagesAppendParams {
 
 // Tokens of a tile of the paged decode; a tensor map's box covers a tile of one page, or the page where that is smaller.
 constexpr int kDecodeTile = 32;
-constexpr int kDecodeItemCost = 4;  // fixed costs of a (request, KV head), in tiles
+constexpr int kDecodeItemCost = 8;  // fixed costs of a (request, KV head), in tiles
 // A query's part in the workspace: m, l, two unused, 128 channels.
 constexpr int kPartialFloats = kHeadDim + 4;
 

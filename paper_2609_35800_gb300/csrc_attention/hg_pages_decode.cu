@@ -40,7 +40,7 @@ constexpr unsigned kAll = 0xffffffffu;
 constexpr float kRescale = 8.0f;  // log2 of how far a score may pass the running maximum
 
 constexpr int kItemCost = kDecodeItemCost;
-constexpr int kJoinCost = 16;  // a ticket and a join, in tiles
+constexpr int kJoinCost = 20;  // a ticket and a join, in tiles
 constexpr int kKeptLengths = 72;
 constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l; rows 4 banks apart
 

@@ -112,22 +112,20 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
 }
 
 // One warp: items from the counter to the others, queries and key blocks into shared memory.  Returns the ring's fills.
-__device__ void load_items(const PromptParams& p, uint32_t base, char* smem, volatile int* misc, uint32_t& fills, uint32_t& queries) {
+__device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t base, char* smem, volatile int* misc,
+                           uint32_t& fills, uint32_t& queries) {
   const int lane = threadIdx.x % 32;
   const uint32_t bars = base + kBarOffset;
   Item* items = reinterpret_cast<Item*>(smem + kItemOffset);
   const uint32_t q_bytes = (uint32_t)p.group * p.tile_tokens * 128;
-  int index = blockIdx.x;
   fills = queries = 0;
-  for (uint32_t n = 0;; ++n) {
-    Item it;
-    it.none = 1;
-    while (index < p.items) {
-      const bool some = item_at(p, index, it);
+  for (uint32_t n = 0;; ++n, some = false) {
+    while (!some) {
+      int index = 0;
       if (lane == 0) index = (int)gridDim.x + (int)atomicAdd(p.counters, 1u);
       index = __shfl_sync(kAll, index, 0);
-      if (some) break;
-      it.none = 1;
+      it.none = index >= p.items;
+      some = it.none || item_at(p, index, it);
     }
     const uint32_t s = n & 1;
     if (n >= 2 && !wait_warp(bars + 8 * (kItemFree + s), ((n >> 1) - 1) & 1, misc, p.status)) return;
@@ -149,18 +147,16 @@ __device__ void load_items(const PromptParams& p, uint32_t base, char* smem, vol
                         it.q0 + it.tok0 + t * p.tile_tokens, bar);
     }
     ++queries;
-    for (int j = 0; j < blocks; ++j) {
-      for (int kv = 0; kv < 2; ++kv, ++fills) {
-        const uint32_t stage = fills % kStages, round = fills / kStages;
-        if (round > 0 && !wait_warp(bars + 8 * (kRingFree + stage), (round - 1) & 1, misc, p.status)) return;
-        if (lane == 0) {
-          const uint32_t bar = bars + 8 * (kRingFull + stage), dst = base + kRingOffset + stage * kTileBytes;
-          mbar_arrive_expect_tx(bar, kTileBytes);
-          for (int half = 0; half < 2; ++half)
-            tma_load_3d(dst + half * kHalfBytes, kv ? &p.v_map : &p.k_map, 64 * half, it.k0 + (it.first + j) * kBlock, it.head, bar);
-        }
-        __syncwarp();
+    for (int j = 0; j < 2 * blocks; ++j, ++fills) {  // K, V of a block
+      const uint32_t stage = fills % kStages, round = fills / kStages;
+      if (round > 0 && !wait_warp(bars + 8 * (kRingFree + stage), (round - 1) & 1, misc, p.status)) return;
+      if (lane == 0) {
+        const uint32_t bar = bars + 8 * (kRingFull + stage), dst = base + kRingOffset + stage * kTileBytes;
+        mbar_arrive_expect_tx(bar, kTileBytes);
+        for (int half = 0; half < 2; ++half)
+          tma_load_3d(dst + half * kHalfBytes, j % 2 ? &p.v_map : &p.k_map, 64 * half, it.k0 + (it.first + j / 2) * kBlock, it.head, bar);
       }
+      __syncwarp();
     }
   }
 }
@@ -214,7 +210,6 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
       for (int t = 0; t < 2; ++t) {
         if (j >= count[t]) continue;
         if (!wait_warp(bars + 8 * (kProbFull + t), probs[t] & 1, misc, p.status)) return;
-        ++probs[t];
         if (t == 0 || j >= count[0]) {  // the first that reads this block's values
           if (!wait_fill(fv)) return;
           const int valid = k_len - (first + j) * kBlock;
@@ -227,18 +222,19 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
             __syncwarp();
           }
         }
+        const uint32_t v = v_operand + (fv % kStages) * (kTileBytes >> 4), o = tmem + kOutColumn + 128 * t;
+        const uint32_t prob = tmem + kScoreColumn + 128 * t;
+        const int steps = j < count[t] - 1 ? kBlock / 16 : (width[t] + 15) / 16;
         tc_fence_after();
+        ++probs[t];
         if (elect_one()) {
-          const uint32_t v = v_operand + (fv % kStages) * (kTileBytes >> 4), o = tmem + kOutColumn + 128 * t;
-          const uint32_t prob = tmem + kScoreColumn + 128 * t;
-          if (j < count[t] - 1) {
+          if (steps == kBlock / 16) {
 #pragma unroll
             for (int i = 0; i < kBlock / 16; ++i) tc_mma_ts(o, prob + 8 * i, v + i * (2048 >> 4), v_shape, i > 0 ? 1u : j > 0);
           } else {
-            const int steps = (width[t] + 15) / 16;
             for (int i = 0; i < steps; ++i) tc_mma_ts(o, prob + 8 * i, v + i * (2048 >> 4), v_shape, j > 0 || i > 0);
-            tc_commit(bars + 8 * (kOutFull + t));
           }
+          if (j == count[t] - 1) tc_commit(bars + 8 * (kOutFull + t));
         }
         __syncwarp();
         if (j + 1 < count[t]) {
@@ -264,6 +260,43 @@ struct RowSum {
 
 __device__ __forceinline__ float residual(float top, float c, float M) {
   return fabsf(M) >= 1048576.f && fabsf(M) < INFINITY ? fmaf(top, c, -M) : 0.f;
+}
+
+__device__ __forceinline__ void st_global32(void* to, const uint32_t (&x)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(to), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]),
+               "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+               : "memory");
+}
+
+// 64 scores of a row to probabilities, two of the type in a word; returns their sum.
+template <bool F16>
+__device__ __forceinline__ float half_probabilities(const uint32_t (&a)[32], const uint32_t (&b)[32], const RowSum& st, float c,
+                                                    uint32_t (&prob)[32]) {
+  const float shift = st.M == -INFINITY ? 0.f : -st.M;
+  const uint64_t c2 = f32x2(__float_as_uint(c), __float_as_uint(c)), shift2 = f32x2(__float_as_uint(shift), __float_as_uint(shift));
+  uint64_t sum[2] = {0, 0};
+  if (__any_sync(kAll, st.r != 0.f)) {
+    const uint64_t r2 = f32x2(__float_as_uint(-st.r), __float_as_uint(-st.r));
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      const uint32_t lo = k < 16 ? a[2 * k & 31] : b[2 * k & 31], hi = k < 16 ? a[(2 * k + 1) & 31] : b[(2 * k + 1) & 31];
+      const uint64_t x = f32x2_add(f32x2_fma(f32x2(lo, hi), c2, shift2), r2);
+      const float e = exp2_approx(__uint_as_float((uint32_t)x)), f = exp2_approx(__uint_as_float((uint32_t)(x >> 32)));
+      sum[k % 2] = f32x2_add(sum[k % 2], f32x2(__float_as_uint(e), __float_as_uint(f)));
+      prob[k] = pack2<F16>(e, f);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      const uint32_t lo = k < 16 ? a[2 * k & 31] : b[2 * k & 31], hi = k < 16 ? a[(2 * k + 1) & 31] : b[(2 * k + 1) & 31];
+      const uint64_t x = f32x2_fma(f32x2(lo, hi), c2, shift2);
+      const float e = exp2_approx(__uint_as_float((uint32_t)x)), f = exp2_approx(__uint_as_float((uint32_t)(x >> 32)));
+      sum[k % 2] = f32x2_add(sum[k % 2], f32x2(__float_as_uint(e), __float_as_uint(f)));
+      prob[k] = pack2<F16>(e, f);
+    }
+  }
+  sum[0] = f32x2_add(sum[0], sum[1]);
+  return __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
 }
 
 // 128 threads, a row each, of tile t.
@@ -336,7 +369,7 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
         __syncwarp();
         if (j > 0) {
           // S of this block is complete, so P V of the one before is, and nothing writes O now
-#pragma unroll
+#pragma unroll 1
           for (int i = 0; i < 4; ++i) {
             uint32_t o[32];
             tmem_load32(o, o_at + 32 * i);
@@ -347,34 +380,11 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
           }
         }
       }
-      float shift = st.M == -INFINITY ? 0.f : -st.M, factor = c;
-      if (__any_sync(kAll, st.r != 0.f)) {
-#pragma unroll
-        for (int i = 0; i < 128; ++i)
-          w[i / 32][i % 32] = __float_as_uint(fmaf(__uint_as_float(w[i / 32][i % 32]), c, shift) - st.r);
-        shift = 0.f;
-        factor = 1.f;
-      }
-      const uint64_t c2 = f32x2(__float_as_uint(factor), __float_as_uint(factor));
-      const uint64_t shift2 = f32x2(__float_as_uint(shift), __float_as_uint(shift));
-      uint64_t sum[2] = {0, 0};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t pw[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const uint64_t x = f32x2_fma(f32x2(w[i][2 * k], w[i][2 * k + 1]), c2, shift2);
-          const float a = exp2_approx(__uint_as_float((uint32_t)x)), b = exp2_approx(__uint_as_float((uint32_t)(x >> 32)));
-          sum[k % 2] = f32x2_add(sum[k % 2], f32x2(__float_as_uint(a), __float_as_uint(b)));
-          pw[k] = pack2<F16>(a, b);
-        }
-#pragma unroll
-        for (int k = 0; k < 16; ++k) w[i / 2][16 * (i % 2) + k] = pw[k];
-      }
-      tmem_store32(s_at, w[0]);
-      tmem_store32(s_at + 32, w[1]);
-      sum[0] = f32x2_add(sum[0], sum[1]);
-      st.l += __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
+      uint32_t prob[32];
+      const float sum = half_probabilities<F16>(w[0], w[1], st, c, prob);
+      tmem_store32(s_at, prob);
+      st.l += sum + half_probabilities<F16>(w[2], w[3], st, c, prob);
+      tmem_store32(s_at + 32, prob);
       tmem_wait_stores();
       tc_fence_before();
       mbar_arrive(bars + 8 * (kProbFull + t));
@@ -393,6 +403,7 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
       p.lse[token * p.q_heads + head] = st.l == 0.f ? -INFINITY : ((st.M + st.r) + log2f(st.l)) * 0.69314718055994531f;
     const float scale = seen > 0 ? 1.0f / st.l : 0.f;
     uint16_t* out = p.out.data + token * p.out.token_stride + head * p.out.head_stride;
+    const bool aligned = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
     float* part = p.parts + (int64_t)it.slot * kPromptPartFloats;
     const int part_row = t * kTileRows + row;
     if (!whole && valid) {
@@ -411,13 +422,20 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
         for (int k = 0; k < 32; ++k) o[k] = 0u;
       }
       if (valid && whole) {
+        // a lane's row lies on lines of its own, and a warp's store takes a cycle a line: 32 bytes a store where they are
+        // aligned (1,460 tokens of 28 heads, all 4 KV heads: 3,100 cycles an item less than in stores of 16)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t x[4];
+        for (int k = 0; k < 2; ++k) {
+          uint32_t x[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[e] = pack2<F16>(__uint_as_float(o[8 * k + 2 * e]) * scale, __uint_as_float(o[8 * k + 2 * e + 1]) * scale);
-          *reinterpret_cast<uint4*>(out + 32 * i + 8 * k) = make_uint4(x[0], x[1], x[2], x[3]);
+          for (int e = 0; e < 8; ++e)
+            x[e] = pack2<F16>(__uint_as_float(o[16 * k + 2 * e]) * scale, __uint_as_float(o[16 * k + 2 * e + 1]) * scale);
+          if (aligned) {
+            st_global32(out + 32 * i + 16 * k, x);
+          } else {
+            *reinterpret_cast<uint4*>(out + 32 * i + 16 * k) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4*>(out + 32 * i + 16 * k + 8) = make_uint4(x[4], x[5], x[6], x[7]);
+          }
         }
       } else if (valid) {
         // [channel / 4][row][4]: a warp's rows lie side by side
@@ -461,6 +479,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = (uint32_t)misc[1];
+  Item mine;  // the first one is known from the launch's parameters alone
+  bool some = false;
+  if (warp == kLoadWarp) {
+    if (threadIdx.x % 32 < 3) prefetch_tensormap(threadIdx.x % 32 == 0 ? &p.q_map : threadIdx.x % 32 == 1 ? &p.k_map : &p.v_map);
+    some = item_at(p, blockIdx.x, mine);
+  }
   grid_launch_dependents();
   grid_dependency_wait();
   uint32_t fills = 0, queries = 0;
@@ -468,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     set_registers_down<kOtherRegisters>();
     if (warp == kLoadWarp) {
       fence_proxy_async_global();  // inputs written by ordinary stores of earlier launches
-      load_items(p, base, smem, misc, fills, queries);
+      load_items(p, mine, some, base, smem, misc, fills, queries);
     } else if (warp == kMmaWarp) {
       issue_products<F16>(p, base, smem, tmem, misc);
     }
@@ -497,12 +521,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   }
 }
 
-// Joins the pieces of an item: a CTA takes 32 of its 256 rows, a warp 16 channels of them, a lane a row.
+// Joins the pieces of an item: a CTA takes 32 of its 256 rows, a lane each, and 32 channels of them, four to a warp.
 template <bool F16>
 __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant__ PromptParams p) {
   grid_launch_dependents();
   grid_dependency_wait();
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int lane = threadIdx.x % 32, quad = blockIdx.y * 8 + threadIdx.x / 32;  // channels 4 quad ..
   const int row = (blockIdx.x % 8) * 32 + lane, index = blockIdx.x / 8;
   Item it;
   item_at(p, index, it);
@@ -517,41 +541,43 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant_
   const int blocks = (seen_by(p, it.q_len, it.k_len, last_tok) + kBlock - 1) / kBlock;
   const int pieces = (blocks + p.chunk - 1) / p.chunk;
   const float* part = p.parts + (int64_t)it.slot * kPromptPartFloats;
-  float M = -INFINITY, r = 0.f;
   const int64_t step = (int64_t)it.slot_step * kPromptPartFloats;
-  for (int i = 0; i < pieces; ++i) {
-    const float m = part[i * step + row], mr = part[i * step + 256 + row];
-    if (m > M) {
-      M = m;
-      r = mr;
+  float M = -INFINITY, r = 0.f, l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kBatch = 6;  // pieces whose reads are in flight together
+#pragma unroll 1
+  for (int i0 = 0; i0 < pieces; i0 += kBatch) {
+    float m[kBatch], mr[kBatch], ml[kBatch];
+    float4 x[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float* from = part + min(i0 + i, pieces - 1) * step;
+      m[i] = i0 + i < pieces ? from[row] : -INFINITY;
+      mr[i] = from[256 + row];
+      ml[i] = from[512 + row];
+      x[i] = *reinterpret_cast<const float4*>(from + 768 + (quad * 256 + row) * 4);
     }
-  }
-  float l = 0.f, acc[16];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) acc[k] = 0.f;
-  for (int i = 0; i < pieces; ++i) {
-    const float* from = part + i * step;
-    const float m = from[row];
-    const float e = m == -INFINITY ? 0.f : exp2_approx((m - M) + (from[256 + row] - r));
-    l += from[512 + row] * e;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(from + 768 + ((4 * warp + k) * 256 + row) * 4);
-      if (m == -INFINITY) continue;
-      acc[4 * k] += x.x * e;
-      acc[4 * k + 1] += x.y * e;
-      acc[4 * k + 2] += x.z * e;
-      acc[4 * k + 3] += x.w * e;
+    for (int i = 0; i < kBatch; ++i) {
+      if (m[i] == -INFINITY) continue;  // the piece has no key that this row sees, or is none
+      float e = 1.f;
+      if (m[i] > M) {
+        const float keep = exp2_approx((M - m[i]) + (r - mr[i]));
+        l *= keep;
+        acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+        M = m[i];
+        r = mr[i];
+      } else {
+        e = exp2_approx((m[i] - M) + (mr[i] - r));
+      }
+      l += ml[i] * e;
+      acc = make_float4(acc.x + x[i].x * e, acc.y + x[i].y * e, acc.z + x[i].z * e, acc.w + x[i].w * e);
     }
   }
   const float scale = seen > 0 ? 1.0f / l : 0.f;
-  uint32_t x[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) x[k] = pack2<F16>(acc[2 * k] * scale, acc[2 * k + 1] * scale);
-  uint16_t* out = p.out.data + token * p.out.token_stride + head * p.out.head_stride + 16 * warp;
-  *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<uint4*>(out + 8) = make_uint4(x[4], x[5], x[6], x[7]);
-  if (p.lse && warp == 0) p.lse[token * p.q_heads + head] = l == 0.f ? -INFINITY : ((M + r) + log2f(l)) * 0.69314718055994531f;
+  uint16_t* out = p.out.data + token * p.out.token_stride + head * p.out.head_stride + 4 * quad;
+  *reinterpret_cast<uint2*>(out) = make_uint2(pack2<F16>(acc.x * scale, acc.y * scale), pack2<F16>(acc.z * scale, acc.w * scale));
+  if (p.lse && quad == 0) p.lse[token * p.q_heads + head] = l == 0.f ? -INFINITY : ((M + r) + log2f(l)) * 0.69314718055994531f;
 }
 
 template <bool F16>
@@ -568,7 +594,7 @@ cudaError_t launch(const PromptParams& p, cudaStream_t s) {
   }
   e = launch_overlapped(prompt_kernel<F16>, dim3((unsigned)std::min(p.items, device_sms())), kThreads, kSmemBytes, s, p);
   if (e != cudaSuccess || !p.split) return e;
-  return launch_overlapped(prompt_join_kernel<F16>, dim3((unsigned)(p.items * 8)), 256, 0, s, p);
+  return launch_overlapped(prompt_join_kernel<F16>, dim3((unsigned)(p.items * 8), 4), 256, 0, s, p);
 }
 
 }  // namespace
