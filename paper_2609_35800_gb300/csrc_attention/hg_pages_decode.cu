@@ -223,7 +223,7 @@ __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int tiles, con
         id = token < c.len ? ids[token >> p.pool.page_shift] : -1;
       }
       const int s = n % kStages;
-      if (n >= kStages && !wait_phase(empty + 8 * s, (n / kStages - 1) & 1, abort, p.status)) return n;
+      if (n >= kStages && !wait_warp(empty + 8 * s, (n / kStages - 1) & 1, abort, p.status)) return n;
       if (elect_one()) mbar_arrive_expect_tx(full + 8 * s, 2 * valid * box_bytes);
       for (int i = 0; i < valid; ++i) {
         const int page = __shfl_sync(kAll, id, box0 - first + i);
@@ -626,7 +626,7 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
     for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
       if (n % kConsumers != warp) continue;
       const int s = n % kStages;
-      alive = alive && wait_phase(full + 8 * s, (n / kStages) & 1, misc, p.status);
+      alive = alive && wait_warp(full + 8 * s, (n / kStages) & 1, misc, p.status);
       const uint32_t kt = base + s * kStageBytes, vt = kt + kStageBytes / 2;
       const int seen = c.len - c.t * kTile;
       __syncwarp();

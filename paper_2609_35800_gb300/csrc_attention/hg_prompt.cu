@@ -29,7 +29,7 @@ constexpr int kBlock = kPromptBlock;        // keys of a block
 constexpr int kTileRows = 128;
 constexpr int kHalfBytes = 128 * 128;       // 64 channels of 128 rows
 constexpr int kTileBytes = 2 * kHalfBytes;  // a tile of queries, a block of keys or of values
-constexpr int kStages = 5;
+constexpr int kStages = 4;
 constexpr int kThreads = 384;  // the last two warps have nothing to do: registers are divided by warpgroups
 // Registers a thread: at launch 65,536 / 384 give 168; the softmax rows need more, the others less.
 constexpr int kRowRegisters = 208, kOtherRegisters = 88;
@@ -106,11 +106,6 @@ __device__ bool item_at(const PromptParams& p, int index, Item& it) {
   return piece == 0 || blocks > it.first;
 }
 
-// Waits of a whole warp, which stays together: all of its threads go on, or none.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
-  return __all_sync(kAll, wait_phase(bar, parity, abort, status));
-}
-
 // One warp: items from the counter to the others, queries and key blocks into shared memory.  Returns the ring's fills.
 __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t base, char* smem, volatile int* misc,
                            uint32_t& fills, uint32_t& queries) {
@@ -180,7 +175,7 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
     if (none) return;
     const int blocks = max(count[0], count[1]);
     if (blocks == 0) continue;
-    if (!wait_warp(bars + 8 * kQueryFull, queries & 1, misc, p.status)) return;
+    wait_data(bars + 8 * kQueryFull, queries & 1, misc, p.status);
     ++queries;
 
     // S of tile t and block j: 128 rows by the block's keys that any of them sees, 16 channels at a time
@@ -197,10 +192,10 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
       tc_commit(bars + 8 * (kScoreFull + t));
       if (j == count[t] - 1 && count[t] == blocks && (t == 1 || count[1] < blocks)) tc_commit(bars + 8 * kQueryFree);
     };
-    auto wait_fill = [&](uint32_t f) { return wait_warp(bars + 8 * (kRingFull + f % kStages), (f / kStages) & 1, misc, p.status); };
+    auto wait_fill = [&](uint32_t f) { wait_data(bars + 8 * (kRingFull + f % kStages), (f / kStages) & 1, misc, p.status); };
 
     // the ring holds K, V of block 0, K, V of block 1, ...: block j's K is fill + 2 j
-    if (!wait_fill(fill)) return;
+    wait_fill(fill);
     scores(0, 0, fill % kStages);
     scores(1, 0, fill % kStages);
     if (elect_one()) tc_commit(bars + 8 * (kRingFree + fill % kStages));
@@ -209,9 +204,9 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if (j >= count[t]) continue;
-        if (!wait_warp(bars + 8 * (kProbFull + t), probs[t] & 1, misc, p.status)) return;
+        wait_data(bars + 8 * (kProbFull + t), probs[t] & 1, misc, p.status);
         if (t == 0 || j >= count[0]) {  // the first that reads this block's values
-          if (!wait_fill(fv)) return;
+          wait_fill(fv);
           const int valid = k_len - (first + j) * kBlock;
           if (valid < kBlock && valid % 16 != 0) {
             // rows past the prompt's last value may be anything, and 0 times NaN is no 0: zeros up to a step's end
@@ -238,7 +233,7 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, const char*
         }
         __syncwarp();
         if (j + 1 < count[t]) {
-          if (!wait_fill(fk)) return;
+          wait_fill(fk);
           scores(t, j + 1, fk % kStages);
         }
       }
@@ -333,7 +328,7 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
     const int least = __reduce_min_sync(kAll, limit);
     RowSum st = {-INFINITY, 0.f, 0.f};
     for (int j = 0; j < blocks; ++j, ++scores) {
-      if (!wait_warp(bars + 8 * (kScoreFull + t), scores & 1, misc, p.status)) return;
+      wait_data(bars + 8 * (kScoreFull + t), scores & 1, misc, p.status);
       tc_fence_after();
       uint32_t w[4][32];
 #pragma unroll
@@ -392,7 +387,7 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
 
     // the tile's end
     if (blocks > 0) {
-      if (!wait_warp(bars + 8 * (kOutFull + t), outs & 1, misc, p.status)) return;
+      wait_data(bars + 8 * (kOutFull + t), outs & 1, misc, p.status);
       ++outs;
       tc_fence_after();
     }

@@ -9,9 +9,10 @@ constexpr uint32_t kAsyncRounds = 20000;   // rounds of up to kAsyncSleepNs each
 constexpr uint32_t kAsyncSleepNs = 50000;
 
 // Wait for a phase of `bar`.  One that runs out flags the workspace's status word and *abort, by which every other
-// wait of the CTA ends too, and returns false: the caller leaves its work.
+// wait of the CTA ends too, and returns false.  (Two plain questions, which the hardware holds back for a while, then
+// suspensions: asking 64 times before the first suspension cost long prompts 5%, suspending at once 12%.)
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
-  for (int i = 0; i < 64; ++i)
+  for (int i = 0; i < 2; ++i)
     if (mbar_try_wait(bar, parity)) return true;
   for (uint32_t i = 0; i < kAsyncRounds; ++i) {
     if (mbar_try_wait_sleep(bar, parity, kAsyncSleepNs)) return true;
@@ -20,6 +21,18 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
   *abort = 1;
   atomicOr(status, kWaitTimeoutBit);
   return false;
+}
+
+// The wait of a whole warp, which stays together: all of its threads go on, or none.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
+  return __all_sync(0xffffffffu, wait_phase(bar, parity, abort, status));
+}
+
+// The same where a vote would lengthen a chain of products and softmax (by 1.5%): the warp goes on in any case, over
+// whatever is there, and finds *abort at its next wait_warp.  For data that no address is made from.
+__device__ __forceinline__ void wait_data(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
+  wait_phase(bar, parity, abort, status);
+  __syncwarp();
 }
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
