@@ -9,11 +9,9 @@ constexpr uint32_t kAsyncRounds = 20000;   // rounds of up to kAsyncSleepNs each
 constexpr uint32_t kAsyncSleepNs = 50000;
 
 // Wait for a phase of `bar`.  One that runs out flags the workspace's status word and *abort, by which every other
-// wait of the CTA ends too, and returns false.  (Two plain questions, which the hardware holds back for a while, then
-// suspensions: asking 64 times before the first suspension cost long prompts 5%, suspending at once 12%.)
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
-  for (int i = 0; i < 2; ++i)
-    if (mbar_try_wait(bar, parity)) return true;
+// wait of the CTA ends too, and returns false.  This one is suspended from the start: for a warp that is ahead of the
+// others, whose questions would only be in their way (prompt attention's loads, 1,541 -> 1,562 TFLOP/s).
+__device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
   for (uint32_t i = 0; i < kAsyncRounds; ++i) {
     if (mbar_try_wait_sleep(bar, parity, kAsyncSleepNs)) return true;
     if (*abort) return false;
@@ -23,9 +21,18 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
   return false;
 }
 
+// The same for those that others wait for: two plain questions, which the hardware holds back for a while, then
+// suspensions.  (Long prompts: 64 questions before the first suspension 5% slower, none 12%.)
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
+  for (int i = 0; i < 2; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  return wait_asleep(bar, parity, abort, status);
+}
+
 // The wait of a whole warp, which stays together: all of its threads go on, or none.
+template <bool ASLEEP = false>
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
-  return __all_sync(0xffffffffu, wait_phase(bar, parity, abort, status));
+  return __all_sync(0xffffffffu, ASLEEP ? wait_asleep(bar, parity, abort, status) : wait_phase(bar, parity, abort, status));
 }
 
 // The same where a vote would lengthen a chain of products and softmax (by 1.5%): the warp goes on in any case, over
