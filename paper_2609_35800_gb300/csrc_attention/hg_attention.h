@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "../../include/headguard.h"
@@ -49,7 +50,9 @@ struct PagesAppendParams {
 
 // Tokens of a tile of the paged decode; a tensor map's box covers a tile of one page, or the page where that is smaller.
 constexpr int kDecodeTile = 32;
-constexpr int kDecodeItemCost = 8;  // fixed costs of a (request, KV head), in tiles
+constexpr int kDecodeItemCost = 12;  // fixed costs of a (request, KV head), in tiles
+// Parts of an item over many CTAs are joined 16 CTAs at a time first; two counters for each 16, ahead of the items' ones.
+constexpr int kDecodeJoinCtas = 16, kDecodeJoinCounters = 128;
 // A query's part in the workspace: m, l, two unused, 128 channels.
 constexpr int kPartialFloats = kHeadDim + 4;
 
@@ -66,7 +69,7 @@ struct PagesDecodeParams {
   float* lse;
   float scale;
   uint32_t* status;
-  uint32_t* counters;  // [batch][heads]
+  uint32_t* counters;  // kDecodeJoinCounters, then [batch][heads]; zero between launches
   float* partials;
 };
 
@@ -131,7 +134,7 @@ inline int device_sms() {
   return n;
 }
 
-// CTAs of a paged decode launch: two to an SM.
-inline int decode_ctas() { return 2 * device_sms(); }
+// CTAs of a paged decode launch: two to an SM (as many as there are counters for).
+inline int decode_ctas() { return std::min(2 * device_sms(), kDecodeJoinCounters / 2 * kDecodeJoinCtas); }
 
 }  // namespace hg

@@ -190,7 +190,8 @@ hg_status map_pages(hg_pages* p) {
 // counters behind them lie at one place for every call), a counter per (request, KV head).
 size_t decode_parts_bytes() { return (size_t)decode_ctas() * 2 * kMaxGroup * kPartialFloats * sizeof(float); }
 size_t decode_workspace_bytes(const hg_pages* p, int batch) {
-  return kAttnHeaderBytes + decode_parts_bytes() + (((size_t)batch * p->pool.heads * sizeof(uint32_t) + 255) & ~size_t(255));
+  const size_t counters = kDecodeJoinCounters + (size_t)batch * p->pool.heads;
+  return kAttnHeaderBytes + decode_parts_bytes() + ((counters * sizeof(uint32_t) + 255) & ~size_t(255));
 }
 
 hg_status decode_batch_ok(const hg_pages* p, int32_t batch, int32_t num_q_heads) {

@@ -8,8 +8,8 @@
 // such item counts as kItemCost tiles more, ahead of its first, for its queries, sums and result.  CTA i of n takes the
 // units [T i / n, T (i + 1) / n): the same share for everybody whatever the requests' lengths, which the kernel reads on
 // the device.  A CTA's run cuts at most two items, its first and its last; it leaves their (m, l, o) in the workspace,
-// and the last CTA to arrive at an item (a ticket, no waiting) joins its parts in order, so the result does not depend on
-// who comes last.  Where no item is more than kJoinCost units longer than the share, joining would cost more than it
+// and the last CTA to arrive at an item (a ticket, no waiting) joins its parts in a fixed order, so the result does not
+// depend on who comes last.  The parts of an item over many CTAs are joined 16 CTAs at a time first.  Where no item is more than kJoinCost units longer than the share, joining would cost more than it
 // gains, and a CTA takes the whole items that begin in its units.
 //
 // A producer warp copies tiles into a ring of six 16 KB stages with TMA, a box per page (swizzled rows; a page id
@@ -36,12 +36,14 @@ constexpr int kConsumers = 3;
 constexpr int kThreads = (kConsumers + 1) * 32;
 static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
 constexpr int kQRowBytes = 272;  // a staged query row: 256 bytes, 16 more so that ldmatrix meets every bank once
+constexpr int kGroups = kConsumers * 4;  // of eight threads
 constexpr unsigned kAll = 0xffffffffu;
 constexpr float kRescale = 8.0f;  // log2 of how far a score may pass the running maximum
 
 constexpr int kItemCost = kDecodeItemCost;
-constexpr int kJoinCost = 20;  // a ticket and a join, in tiles
+constexpr int kJoinCost = 24;  // a ticket and a join, in tiles
 constexpr int kKeptLengths = 72;
+constexpr int kJoinCtas = kDecodeJoinCtas, kJoinCounters = kDecodeJoinCounters;
 constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l; rows 4 banks apart
 
 // Shared memory, two CTAs an SM.  The staged queries (8 rows a warp) and the warps' parts that are added up at an item's
@@ -438,20 +440,6 @@ __device__ __forceinline__ float* partial_of(const PagesDecodeParams& p, int cta
 struct Part {
   float m = -INFINITY, l = 0.f, o[16] = {};
 };
-// Adds a part: 16 channels at `o`, its m and l.
-__device__ __forceinline__ void join(Part& a, float m, float l, const float4 (&o)[4], float cs) {
-  const float top = fmaxf(a.m, m), base = top == -INFINITY ? 0.f : top;
-  const float ka = exp2_approx((a.m - base) * cs), kb = exp2_approx((m - base) * cs);
-  a.m = top;
-  a.l = a.l * ka + l * kb;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    a.o[4 * i] = a.o[4 * i] * ka + o[i].x * kb;
-    a.o[4 * i + 1] = a.o[4 * i + 1] * ka + o[i].y * kb;
-    a.o[4 * i + 2] = a.o[4 * i + 2] * ka + o[i].z * kb;
-    a.o[4 * i + 3] = a.o[4 * i + 3] * ka + o[i].w * kb;
-  }
-}
 // Adds up N rows of sums in shared memory, `apart` floats from one to the next: one maximum, then independent terms.
 template <int N>
 __device__ __forceinline__ Part add_rows(const float* row, int apart, int count, int channel, float cs) {
@@ -488,17 +476,17 @@ __device__ __forceinline__ void store_part(const Part& a, float* channels, float
 
 // out = o / l in the cache's type, and the query's log-sum-exp.
 template <bool F16>
-__device__ __forceinline__ void write_query(const PagesDecodeParams& p, const Cursor& c, int q, int channel, const Part& a) {
-  const float r = c.len > 0 ? 1.0f / a.l : 0.f;
-  const int head = c.h * p.group + q;
-  uint16_t* out = p.out.data + c.b * p.out.token_stride + head * p.out.head_stride + channel;
+__device__ __forceinline__ void write_query(const PagesDecodeParams& p, int b, int h, int len, int q, int channel, const Part& a) {
+  const float r = len > 0 ? 1.0f / a.l : 0.f;
+  const int head = h * p.group + q;
+  uint16_t* out = p.out.data + b * p.out.token_stride + head * p.out.head_stride + channel;
   uint32_t x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = pack2<F16>(a.o[2 * i] * r, a.o[2 * i + 1] * r);
   *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
   *reinterpret_cast<uint4*>(out + 8) = make_uint4(x[4], x[5], x[6], x[7]);
   if (p.lse && channel == 0)
-    p.lse[(int64_t)c.b * p.pool.heads * p.group + head] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l);
+    p.lse[(int64_t)b * p.pool.heads * p.group + head] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l);
 }
 
 // Takes a number; what the CTA's threads wrote before their last barrier is visible to whoever takes a later one.
@@ -508,13 +496,119 @@ __device__ __forceinline__ uint32_t take_ticket(uint32_t* counter) {
   return n;
 }
 
+// The CTA's part of an item over the CTAs [cta0, cta1] is written: whoever comes last joins them.  (Inlined: called, it
+// cost launches of 10 to 30 us up to 5%.)
+template <bool F16>
+__device__ __forceinline__ void join_item(const PagesDecodeParams& p, int b, int h, int len, int cta0, int cta1, float* scratch,
+                                       volatile int* misc, float cs) {
+  const int lane = threadIdx.x % 32, mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
+  // up to six queries: several groups of threads share a query's parts, each takes every `subs`-th
+  const int subs = max(1, kGroups / p.group);
+  const bool two_levels = cta1 - cta0 >= 24 * subs;
+  for (int level = two_levels ? 0 : 1; level < 2; ++level) {
+    // the parts of this level: CTA `first` (level 1 of two: then the first CTA of each further 16), `stride` apart
+    const int round = blockIdx.x & ~(kJoinCtas - 1);
+    const int first = level == 0 ? max(cta0, round) : cta0, stride = two_levels && level == 1 ? kJoinCtas : 1;
+    const int count = level == 0 ? min(cta1, round + kJoinCtas - 1) - first + 1
+                                 : two_levels ? cta1 / kJoinCtas - cta0 / kJoinCtas + 1 : cta1 - cta0 + 1;
+    const auto part = [&](int k) {
+      const int cta = k == 0 ? first : stride == 1 ? first + k : (first & ~(kJoinCtas - 1)) + k * stride;
+      return partial_of(p, cta, cta == cta0);
+    };
+    if (count > 1) {
+      if (threadIdx.x == 0) {
+        uint32_t* counter = level == 0 ? p.counters + blockIdx.x / kJoinCtas * 2 + (cta0 >= round)
+                                       : p.counters + kJoinCounters + (int64_t)b * p.pool.heads + h;
+        const bool last = take_ticket(counter) == (uint32_t)(count - 1);
+        if (last) *counter = 0u;
+        misc[1] = last;
+      }
+      named_barrier<kConsumers * 32>(1);
+      if (!misc[1]) return;
+    }
+    const int sub = mine / p.group, lane8 = lane % 8;
+    const unsigned group_mask = 0xffu << (lane & 24);
+    for (int q = subs > 1 ? mine % p.group : mine; q < p.group && (subs == 1 || sub < subs); q += kGroups) {
+      Part a;
+#pragma unroll 1
+      for (int k0 = subs > 1 ? sub : 0; k0 < count; k0 += 8 * subs) {
+        // eight parts at a time: a lane has one's m and l, all lanes 16 channels of each, of four at once
+        const int k = k0 + lane8 * subs;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (k < count) ml = __ldcg(reinterpret_cast<const float2*>(part(k) + q * kPartialFloats));
+        float e = 0.f;
+#pragma unroll
+        for (int j0 = 0; j0 < 8; j0 += 4) {
+          float4 o[4][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int kj = k0 + (j0 + j) * subs;
+            const float* row = part(kj) + q * kPartialFloats + 4 + channel;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              o[j][i] = kj < count ? __ldcg(reinterpret_cast<const float4*>(row + 4 * i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          if (j0 == 0) {
+            float top = fmaxf(a.m, ml.x);
+#pragma unroll
+            for (int i = 1; i < 8; i <<= 1) top = fmaxf(top, __shfl_xor_sync(group_mask, top, i));
+            const float base = top == -INFINITY ? 0.f : top;
+            const float keep = exp2_approx((a.m - base) * cs);
+            e = exp2_approx((ml.x - base) * cs);
+            float l = ml.y * e;
+#pragma unroll
+            for (int i = 1; i < 8; i <<= 1) l += __shfl_xor_sync(group_mask, l, i);
+            a.m = top;
+            a.l = a.l * keep + l;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) a.o[i] *= keep;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float ej = __shfl_sync(group_mask, e, (lane & 24) + j0 + j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              a.o[4 * i] += o[j][i].x * ej;
+              a.o[4 * i + 1] += o[j][i].y * ej;
+              a.o[4 * i + 2] += o[j][i].z * ej;
+              a.o[4 * i + 3] += o[j][i].w * ej;
+            }
+          }
+          if (k0 + 4 * subs >= count) break;
+        }
+      }
+      if (subs > 1) {  // then this is the only round
+        float* row = scratch + (sub * p.group + q) * kSumFloats;
+        store_part(a, row, row + kHeadDim, channel);
+      } else if (level == 1) {
+        write_query<F16>(p, b, h, len, q, channel, a);
+      } else {
+        float* row = part(0) + q * kPartialFloats;
+        store_part(a, row + 4, row, channel);
+      }
+    }
+    if (subs > 1) {
+      named_barrier<kConsumers * 32>(1);
+      if (mine < p.group) {
+        const Part a = add_rows<kGroups>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
+        if (level == 1) {
+          write_query<F16>(p, b, h, len, mine, channel, a);
+        } else {
+          float* row = part(0) + mine * kPartialFloats;
+          store_part(a, row + 4, row, channel);
+        }
+      }
+    }
+    named_barrier<kConsumers * 32>(1);  // the scratch is free again; the joined part is written
+  }
+}
+
 // The end of the CTA's part of an item: the warps' sums are added up, 8 queries at a time, 8 threads to a query; a whole
 // item is written, a part goes to the workspace, and the last part's CTA joins them all.
 template <bool F16, int NT>
 __device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cursor& c, bool whole, bool begins, int tile_u0,
                             const Work& w, float* scratch, volatile int* misc, float cs) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, tq = lane % 4;
-  constexpr int kGroups = kConsumers * 4;
   const int mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -538,7 +632,7 @@ __device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cur
     if (mine < 8 && q < p.group) {
       const Part a = add_rows<kConsumers>(scratch + mine * kSumFloats, 8 * kSumFloats, kConsumers, channel, cs);
       if (whole) {
-        write_query<F16>(p, c, q, channel, a);
+        write_query<F16>(p, c.b, c.h, c.len, q, channel, a);
       } else {
         float* row = partial_of(p, blockIdx.x, begins) + q * kPartialFloats;
         store_part(a, row + 4, row, channel);
@@ -547,50 +641,7 @@ __device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cur
   }
   named_barrier<kConsumers * 32>(1);  // the scratch is free again; the part is written
   if (whole) return;
-  const int cta0 = w.cta_of(tile_u0), cta1 = w.cta_of(tile_u0 + c.tiles - 1);
-  if (threadIdx.x == 0) {
-    uint32_t* counter = p.counters + (int64_t)c.b * p.pool.heads + c.h;
-    const bool last = take_ticket(counter) == (uint32_t)(cta1 - cta0);
-    if (last) *counter = 0u;
-    misc[1] = last;
-  }
-  named_barrier<kConsumers * 32>(1);
-  if (!misc[1]) return;
-  // up to six queries: several groups of threads share a query's parts, each takes every `subs`-th
-  const int subs = max(1, kGroups / p.group), sub = mine / p.group;
-  for (int q = subs > 1 ? mine % p.group : mine; q < p.group && (subs == 1 || sub < subs); q += kGroups) {
-    Part a;
-    constexpr int kBatch = 4;  // parts whose reads are in flight together
-#pragma unroll 1
-    for (int i0 = cta0 + (subs > 1 ? sub : 0); i0 <= cta1; i0 += kBatch * subs) {
-      float2 s[kBatch];
-      float4 o[kBatch][4];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int cta = i0 + i * subs;
-        const float* row = partial_of(p, min(cta, cta1), cta == cta0) + q * kPartialFloats;
-        s[i] = __ldcg(reinterpret_cast<const float2*>(row));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[i][k] = __ldcg(reinterpret_cast<const float4*>(row + 4 + channel + 4 * k));
-      }
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        if (i0 + i * subs <= cta1) join(a, s[i].x, s[i].y, o[i], cs);
-    }
-    if (subs == 1) {
-      write_query<F16>(p, c, q, channel, a);
-    } else {  // then this is the only round
-      float* row = scratch + (sub * p.group + q) * kSumFloats;
-      store_part(a, row, row + kHeadDim, channel);
-    }
-  }
-  if (subs == 1) return;
-  named_barrier<kConsumers * 32>(1);
-  if (mine < p.group) {
-    const Part a = add_rows<kGroups>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
-    write_query<F16>(p, c, mine, channel, a);
-  }
-  named_barrier<kConsumers * 32>(1);  // the scratch is free again
+  join_item<F16>(p, c.b, c.h, c.len, w.cta_of(tile_u0), w.cta_of(tile_u0 + c.tiles - 1), scratch, misc, cs);
 }
 
 template <bool F16, int NT>
