@@ -35,10 +35,10 @@
  *              launched; a call that returns an error has enqueued nothing and
  *              changed no state.  HG_ERR_CUDA reports a launch error returned
  *              by the CUDA runtime (cudaGetLastError after the launch).
- *              The only polling waits in device code are decode CTAs waiting
- *              on mbarriers for their own tile copies, each bounded: one that runs out
- *              sets the workspace status word (hg_workspace_status) instead
- *              of hanging.
+ *              The only polling waits in device code are CTAs of the attention
+ *              kernels waiting on mbarriers for their own tile copies (and
+ *              products), each bounded: one that runs out sets the workspace
+ *              status word (hg_workspace_status) instead of hanging.
  *   Threads    A hg_cache may be used from one host thread at a time.
  */
 #ifndef HEADGUARD_H
@@ -452,7 +452,9 @@ typedef struct hg_attention_io {
 /* Workspace bytes of hg_pages_decode_attention and hg_pages_decode_step for up to
  * `batch` requests on the current device.  Used as a decode workspace is: zeroed
  * once by hg_workspace_clear, one launch at a time, status by
- * hg_workspace_status; it serves any pool and any smaller batch. */
+ * hg_workspace_status; it serves any pool and any smaller batch.  Before another
+ * kind of call (hg_prompt_attention, hg_decode_*) uses it, it has to be cleared
+ * again. */
 hg_status hg_pages_decode_workspace_size(const hg_pages *pages, int32_t batch, int32_t num_q_heads,
                                          size_t *bytes);
 
@@ -485,9 +487,10 @@ hg_status hg_pages_decode_step(const hg_pages *pages, int32_t batch, int32_t num
                                const int32_t *page_table, int32_t table_stride, const int32_t *lengths, float *lse,
                                float softmax_scale, void *workspace, size_t workspace_bytes, hg_stream_t stream);
 
-/* Workspace bytes of hg_prompt_attention on the current device, for any sizes.
- * Zeroed once by hg_workspace_clear, one launch at a time, status by
- * hg_workspace_status. */
+/* Workspace bytes of hg_prompt_attention, for any sizes (82 MB: the parts of 608
+ * work items, touched only where keys are cut into pieces).  Zeroed once by
+ * hg_workspace_clear, one launch at a time, status by hg_workspace_status; to be
+ * cleared again before another kind of call uses it. */
 hg_status hg_prompt_workspace_size(size_t *bytes);
 
 /* Attention of whole prompts, packed one after the other.  Prompt i has the

@@ -504,6 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     for (uint32_t i = 0; queries > 0 && i < kAsyncRounds && !mbar_try_wait_sleep(bars + 8 * kQueryFull, (queries - 1) & 1, kAsyncSleepNs); ++i) {
     }
   }
+  if (misc[0] && warp == kMmaWarp) __nanosleep(1000000);  // and its products have ended
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();

@@ -23,9 +23,11 @@ class PagedRunner:
         self.per_request = -(-max_tokens // page_size)
         self.table = torch.zeros(max_batch, self.per_request, dtype=torch.int32, device=device)
         self.lens = torch.zeros(max_batch, dtype=torch.int32, device=device)
-        self.ws = torch.empty(max(hg_pages_decode_workspace_size(self.pages, max_batch, q_heads),
-                                  hg_prompt_workspace_size()), dtype=torch.uint8, device=device)
+        # one each: a workspace's counters lie where the other kind of call keeps its parts
+        self.ws, self.prompt_ws = (torch.empty(n, dtype=torch.uint8, device=device) for n in (
+            hg_pages_decode_workspace_size(self.pages, max_batch, q_heads), hg_prompt_workspace_size()))
         hg_workspace_clear(self.ws)
+        hg_workspace_clear(self.prompt_ws)
 
     def _grow(self, request, tokens):
         need = -(-tokens // self.page_size)
@@ -60,7 +62,7 @@ class PagedRunner:
         hg_pages_append(self.pages, q, k, v, self.rotation, positions, slots, q_rot, k_out, v_out)
         begin = torch.tensor([0] + list(prompt_lengths)).cumsum(0).to(torch.int32)
         out = torch.empty_like(q_rot)
-        hg_prompt_attention(q_rot, k_out, v, begin, begin, out, None, True, 0.0, self.ws)
+        hg_prompt_attention(q_rot, k_out, v, begin, begin, out, None, True, 0.0, self.prompt_ws)
         return out
 
     def step(self, q, k, v, positions):

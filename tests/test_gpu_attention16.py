@@ -550,16 +550,47 @@ def test_prompt_on_another_stream():
     _check_prompt(q, k, v, qb, kb, True, out, None)
 
 
+def _apart(shape, dtype, fill=NAN):
+    """A dense tensor that starts 16 bytes past a 32-byte boundary."""
+    n = math.prod(shape)
+    return torch.full((n + 24,), fill, dtype=dtype, device="cuda")[8:8 + n].view(shape)
+
+
+@TYPES
+def test_rows_aligned_to_16_bytes_only(dtype):
+    g = _gen(40)
+    heads, group, lens = 2, 4, [150, 33]
+    hq, n = heads * group, sum(lens)
+    q, k, v, qb, kb = _prompt(g, lens, lens, heads, group, dtype, "tokens")
+    shifted = [_apart(x.shape, dtype) for x in (q, k, v, q)]
+    assert all(x.data_ptr() % 32 == 16 for x in shifted)
+    for to, x in zip(shifted, (q, k, v)):
+        to.copy_(x)
+    ws = _workspace(hg.hg_prompt_workspace_size())
+    hg.hg_prompt_attention(*shifted[:3], qb, kb, shifted[3], None, True, 0.0, ws)
+    _check_prompt(q, k, v, qb, kb, True, shifted[3], None)
+    kp, vp = _apart((20, heads, 16, D), dtype), _apart((20, heads, 16, D), dtype)
+    pool = hg.hg_pages_create(kp, vp)
+    slots = torch.arange(n, dtype=torch.int32, device="cuda") + 16
+    hg.hg_pages_append(pool, *shifted[:3], None, None, slots, shifted[3])
+    assert torch.equal(_bits(shifted[3]), _bits(q))
+    tab = torch.arange(1, 13, dtype=torch.int32, device="cuda")[None].contiguous()
+    out, dws = _apart((1, hq, D), dtype), _workspace(hg.hg_pages_decode_workspace_size(pool, 1, hq))
+    hg.hg_pages_decode_attention(pool, shifted[0][:1], tab, torch.tensor([n], dtype=torch.int32, device="cuda"), out, None,
+                                 0.0, dws)
+    _check_decode(q[:1], kp, vp, tab, [n], 16, out, None)
+
+
 # -- together ----------------------------------------------------------------------------------------------------------
 
-def test_serving_run():
+@pytest.mark.parametrize("heads,group,lens", [(4, 7, [70, 5, 200, 33]), (1, 2, [2500, 40])])  # (whole items; pieces)
+def test_serving_run(heads, group, lens):
     """Prompts admitted together, three tokens each, against one attention over everything in 64 bits."""
     from paper_2609_35800_gb300.paged import PagedRunner
     g = _gen(30)
-    heads, group, lens = 4, 7, [70, 5, 200, 33]
     hq = heads * group
-    tab = table(512, 128, "cuda")
-    run = PagedRunner(64, 16, hq, heads, hg.Rotation(tab), max_batch=8, max_tokens=400)
+    tab = table(max(lens) + 8, 128, "cuda")
+    run = PagedRunner(sum(lens) // 16 + 40, 16, hq, heads, hg.Rotation(tab), max_batch=8, max_tokens=2600)
     for _ in range(2):  # the second time in pages that the first gave back
         n = sum(lens)
         qkv = _randn(g, n, hq + 2 * heads, D)
@@ -587,3 +618,35 @@ def test_serving_run():
                 ref = ref[:3] + (ref[3] + 2.0 ** 17 * 2.0 ** -8 * ref[3],)
                 check(got[i:i + 1], None, ref, BF16, len(keys[i]), 5.0)
         run.release()
+
+
+def test_a_prompt_goes_on_in_the_packed_cache():
+    """Rotated keys and values written heads first are what hg_quantize_kv takes, as they are."""
+    from paper_2609_35800_gb300 import workloads as wl
+    from paper_2609_35800_gb300.runner import config_of, shape_of
+    g = _gen(41)
+    w = wl.custom("prompt", 1, 1, 8, 2, 24, 64, 40, wl.BASE_MINMAX, 4, 0, decode_steps=2, protected=[(0, 1)])
+    n, heads, hq = w.seq_len, 2, 8
+    kp, vp = _pool(g, 12, heads, 16, BF16, False)
+    pool = hg.hg_pages_create(kp, vp)
+    qkv, tab = _randn(g, n, hq + 2 * heads, D), table(n, 128, "cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    k, v = torch.empty(1, heads, n, D, dtype=BF16, device="cuda"), torch.empty(1, heads, n, D, dtype=BF16, device="cuda")
+    q = torch.empty(n, hq, D, dtype=BF16, device="cuda")
+    hg.hg_pages_append(pool, qkv[:, :hq], qkv[:, hq:hq + heads], qkv[:, hq + heads:], hg.Rotation(tab), pos, pos, q,
+                       k[0].transpose(0, 1), v[0].transpose(0, 1))
+    begin = torch.tensor([0, n], dtype=torch.int32)
+    out, lse = _run_prompt(q, k[0].transpose(0, 1), v[0].transpose(0, 1), begin, begin, True)
+    _check_prompt(q, k[0].transpose(0, 1), v[0].transpose(0, 1), begin, begin, True, out, lse)
+    shape, config, mask = shape_of(w), config_of(w), wl.protection_mask(w).numpy()
+    arena = torch.empty(hg.hg_cache_layout(shape, config, mask), dtype=torch.uint8, device="cuda")
+    cache = hg.hg_cache_create(shape, config, mask, arena)
+    hg.hg_quantize_kv(cache, 0, [k], [v])
+    kd, vd = torch.empty_like(k), torch.empty_like(v)
+    hg.hg_dequantize_kv(cache, 0, 1, kd, vd, False)
+    for got, want in ((kd, k), (vd, v)):
+        assert torch.equal(got[:, 1], want[:, 1])  # the protected head, and all text
+        assert torch.equal(got[:, :, :24], want[:, :, :24]) and torch.equal(got[:, :, 88:], want[:, :, 88:])
+        span = want[:, 0, 24:88].float()  # 4-bit codes: at most half a step off, and the rounding to BF16
+        step = (span.amax(-1, keepdim=True) - span.amin(-1, keepdim=True)) / 15
+        assert bool(((got[:, 0, 24:88].float() - span).abs() <= step * 0.501 + span.abs() * 2.0 ** -8).all())
