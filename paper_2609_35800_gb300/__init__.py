@@ -425,6 +425,7 @@ class _Types:
 
 
 _types = _Types()
+_pack18, _pack12 = struct.Struct("=18q").pack, struct.Struct("=12q").pack  # hg_append_io, hg_attention_io
 
 
 class Pages:
@@ -542,7 +543,7 @@ def hg_pages_append(pages, q, k, v, rotation, positions, slots, q_out=None, k_ou
     n, heads, hq = k.shape[0], pages.shape.num_kv_heads, 0 if q is None else q.shape[1]
     if q is not None and q_out is None:
         raise ValueError("hg_pages_append: q needs q_out")
-    io = struct.pack("=18q", *(_rows(w, "q", q, n, hq, d) if hq else _NO_ROWS), *_rows(w, "k", k, n, heads, d),
+    io = _pack18(*(_rows(w, "q", q, n, hq, d) if hq else _NO_ROWS), *_rows(w, "k", k, n, heads, d),
                      *_rows(w, "v", v, n, heads, d), *(_rows(w, "q_out", q_out, n, hq, d) if hq else _NO_ROWS),
                      *(_NO_ROWS if k_out is None else _rows(w, "k_out", k_out, n, heads, d)),
                      *(_NO_ROWS if v_out is None else _rows(w, "v_out", v_out, n, heads, d)))
@@ -577,7 +578,7 @@ def hg_pages_decode_attention(pages, q, page_table, lengths, out, lse, softmax_s
     page_table[b]; lse float32 [batch][heads] or None."""
     w, d = "hg_pages_decode_attention", pages.dtype
     n, hq = q.shape[0], q.shape[1]
-    io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), 0, 0, 0, 0, 0, 0, *_rows(w, "out", out, n, hq, d))
+    io = _pack12(*_rows(w, "q", q, n, hq, d), 0, 0, 0, 0, 0, 0, *_rows(w, "out", out, n, hq, d))
     tp, ts, lp = _decode_table(w, page_table, lengths, n)
     _check(library().hg_pages_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse(w, lse, n, hq),
                                                softmax_scale, *_workspace(w, workspace), _stream(stream)), w)
@@ -589,7 +590,7 @@ def hg_pages_decode_step(pages, q, k, v, rotation, positions, page_table, length
     over its lengths[b] tokens."""
     w, d = "hg_pages_decode_step", pages.dtype
     n, hq, heads = q.shape[0], q.shape[1], pages.shape.num_kv_heads
-    io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, n, heads, d),
+    io = _pack12(*_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, n, heads, d),
                      *_rows(w, "v", v, n, heads, d), *_rows(w, "out", out, n, hq, d))
     rp, pp = _rotated_by(w, rotation, positions, n)
     tp, ts, lp = _decode_table(w, page_table, lengths, n)
@@ -614,7 +615,7 @@ def hg_prompt_attention(q, k, v, q_begin, k_begin, out, lse, causal, softmax_sca
     n, hq, _ = q.shape
     nk, heads, _ = k.shape
     count = q_begin.numel() - 1
-    io = struct.pack("=12q", *_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, nk, heads, d),
+    io = _pack12(*_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, nk, heads, d),
                      *_rows(w, "v", v, nk, heads, d), *_rows(w, "out", out, n, hq, d))
     qb, kb = _ints(w, "q_begin", q_begin, 1, False), _ints(w, "k_begin", k_begin, count + 1, False)
     q_end, k_end = _Int.from_address(qb + 4 * count).value, _Int.from_address(kb + 4 * count).value

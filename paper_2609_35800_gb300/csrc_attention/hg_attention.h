@@ -95,8 +95,10 @@ struct PromptParams {
   uint32_t* status;
   uint32_t* counters;  // items taken, CTAs that have finished; zero between launches
   float* parts;
-  PromptRange range[kPromptsPerLaunch];     // longest first
-  int first_unit[kPromptsPerLaunch];  // (piece, tile pair) number of each prompt's first
+  int tiles;        // tile pairs of every prompt
+  PromptRange range[kPromptsPerLaunch];  // longest first
+  int first_unit[kPromptsPerLaunch];     // (piece, tile pair) number of each prompt's first
+  int first_tile[kPromptsPerLaunch];     // tile pair number of each prompt's first
 };
 
 cudaError_t launch_pages_append(const PagesAppendParams& p, bool f16, cudaStream_t s);

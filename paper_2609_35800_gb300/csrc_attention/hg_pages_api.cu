@@ -127,14 +127,17 @@ bool rows_mappable(const hg_rows& r, int tokens, int heads) {
 
 // Pieces, tile pairs and heads of the launch's prompts, in blocks of kPromptBlock keys a piece at most `chunk`.
 int64_t count_items(PromptParams* p) {
-  int64_t units = 0;
+  int64_t units = 0, all = 0;
   for (int i = 0; i < p->prompts; ++i) {
     const PromptRange& r = p->range[i];
     p->first_unit[i] = (int)std::min<int64_t>(units, INT32_MAX);
+    p->first_tile[i] = (int)std::min<int64_t>(all, INT32_MAX);
     const int64_t tiles = (r.q_len + 2 * p->tile_tokens - 1) / (2 * p->tile_tokens);
     const int64_t blocks = (r.k_len + kPromptBlock - 1) / kPromptBlock;
     units += tiles * std::max<int64_t>(1, (blocks + p->chunk - 1) / p->chunk);
+    all += tiles;
   }
+  p->tiles = (int)std::min<int64_t>(all, INT32_MAX);
   return units * p->kv_heads;
 }
 

@@ -4,7 +4,8 @@
 // Nothing is used twice but a token's cosines and sines, so the kernel is bound by memory: every row is read once and
 // written once (a key that is wanted densely too, twice).  Eight lanes take a row, 16 channels each in two 16-byte
 // loads, both halves of a pair in one lane; rows are numbered token by token (queries, keys, values), so a block's
-// lanes share a token's cosines and sines through L1.
+// lanes share a token's cosines and sines through L1.  Measured: 21,400 tokens of 60 + 5 + 5 heads 148 us, 6.25 TB/s,
+// 0.92 of a copy's rate (two rows a thread: 150 us); 1,460 tokens of 28 + 4 + 4 heads 5.1 us on the device.
 #include "hg_rows.cuh"
 
 namespace hg {

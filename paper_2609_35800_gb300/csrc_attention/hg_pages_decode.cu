@@ -1,23 +1,28 @@
 // Attention of one new token per request over a paged cache, split over the cache's length and joined.
 //
 // For a request, KV head and its G queries: s_t = scale q.k_t, m = max s_t, out = sum e^(s_t - m) v_t / sum e^(s_t - m).
-// Every key and value is used by G <= 16 queries only, 2 G flop per byte, so the kernel is bound by the reads of the
-// cache; it has to keep enough of them in flight and to spread them evenly.
+// Every key and value is used by G <= 16 queries only, G flop per byte, so the kernel is bound by the reads of the cache;
+// it has to keep enough of them in flight and to spread them evenly.  Measured: 32 requests x 8,577 tokens x 8 KV heads
+// 171 us, 6.60 TB/s, 0.97 of a copy's rate; one request of 131,073 tokens 88 us (0.90); 37 of 1 to 9,001 tokens and 12
+// queries a KV head 29 us (0.53; start and tail); 321 tokens 7.5 us.
 //
 // The work is cut into tiles of 32 tokens of one (request, KV head), numbered request by request, head by head; each
-// such item counts as kItemCost tiles more, ahead of its first, for its queries, sums and result.  CTA i of n takes the
-// units [T i / n, T (i + 1) / n): the same share for everybody whatever the requests' lengths, which the kernel reads on
-// the device.  A CTA's run cuts at most two items, its first and its last; it leaves their (m, l, o) in the workspace,
-// and the last CTA to arrive at an item (a ticket, no waiting) joins its parts in a fixed order, so the result does not
-// depend on who comes last.  The parts of an item over many CTAs are joined 16 CTAs at a time first.  Where no item is more than kJoinCost units longer than the share, joining would cost more than it
-// gains, and a CTA takes the whole items that begin in its units.
+// such item counts as kItemCost tiles more, ahead of its first, for its queries, sums and result (19 shapes, geometric
+// mean: 15.2 us at 4 tiles, 15.0 at 8, 14.9 at 12 and 16).  A CTA takes an even share of the units, whatever the
+// requests' lengths, which the kernel reads on the device.  Its run cuts at most two items, the first and the last; it
+// leaves their (m, l, o) in the workspace, and the last CTA to arrive at an item (a ticket, no waiting) joins its parts
+// in a fixed order, so the result does not depend on who comes last.  The parts of an item over many CTAs are joined 16
+// CTAs at a time first (one KV head, 131,072 tokens: 79 -> 23 us).  Where no item is more than kJoinCost units longer
+// than the share, joining would cost more than it gains (321 tokens: 8.9 us cut, 7.5 whole), and a CTA takes the whole
+// items that begin in its units.
 //
 // A producer warp copies tiles into a ring of six 16 KB stages with TMA, a box per page (swizzled rows; a page id
 // outside the pool reads as zeros).  Three consumer warps take the tiles in turn, each with its own running maximum and
-// sums, so that three tiles' chains of load, product, maximum, exponential and product run side by side (four warps on
-// 16 tokens each of one 64-token tile needed about 1,200 cycles a tile).  Two of the stages belong to each warp: it waits
-// for every phase of their barriers, in order, as a wait by parity needs.  They compute with mma.sync m16n8k16 (a tcgen05 product would have M = 128 tokens by N = 8 queries
-// and its probabilities would pass through TMEM; the tensor work here is a few per cent of what mma.sync gives):
+// sums, so that three tiles' chains of load, product, maximum, exponential and product run side by side, about 950
+// cycles each (four warps on 16 tokens each of one 64-token tile took 1,200 cycles a tile).  Two of the stages belong to
+// each warp: it waits for every phase of their barriers, in order, as a wait by parity needs.  They compute with mma.sync
+// m16n8k16 (a tcgen05 product would have M = 128 tokens by N = 8 queries and its probabilities would pass through tensor
+// memory; the tensor pipe is 7% busy):
 //   S^T[token][query] = K . q        A = keys (ldmatrix), B = the queries, padded to 8 or 16
 //   O^T[channel][query] += V^T . P^T A = values (ldmatrix.trans), B = P^T (movmatrix of the scores' fragment)
 // Scores, maxima, sums and outputs are held in 32 bits; probabilities are rounded to the cache's type for the second

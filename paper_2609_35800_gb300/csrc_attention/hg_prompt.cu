@@ -1,8 +1,10 @@
 // Attention of packed prompts on the fifth-generation tensor cores.
 //
 // For a prompt's query row: s_t = scale q.k_t over the keys it sees, m = max s_t, out = sum e^(s_t - m) v_t / sum
-// e^(s_t - m).  4 * 128 flop a (query head, key) pair: from about a thousand keys on the kernel is bound by the tensor
-// cores, or by the exponentials, of which there is one for 512 flop.
+// e^(s_t - m).  4 * 128 flop a (query head, key) pair and little to read: the kernel is bound by the products, and for
+// short prompts by the chain of a tile's blocks.  Measured: 2 x 8,192 causal tokens of 64 heads 1,545 TFLOP/s (1,604 with
+// the softmax left out: a product of 128 x 128 with both operands in shared memory reads all that it can give, 128 bytes
+// a cycle); 1,460 tokens of 28 heads 26 us, 12 blocks of 3,000 cycles one after the other.
 //
 // A work item is two tiles of 128 rows of one prompt and KV head.  A tile's rows are 128 / G consecutive tokens times
 // the G query heads of the KV head, so short prompts fill their tiles and a causal tile spans few tokens; both tiles use
@@ -12,11 +14,15 @@
 //   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a thread to a row: S out of tensor memory, P back over it (so a
 //               tile's next S follows its P V), O scaled there when a maximum moves, written out at the end
 // While one tile's softmax runs the tensor cores work on the other tile.  Tensor memory: S 2 x 128 columns, O 2 x 128.
+// What is not here because it was slower: P handed over in halves (1,409 TFLOP/s then, 1,467 without), outputs written by
+// a warpgroup of their own (1,387), items taken by a warp of its own (1,508 of 1,547: every waiting warp takes something),
+// three or five stages of the ring (1,514 and 1,497 of 1,541 and 1,562).
 //
 // Scores, maxima, sums and O are held in 32 bits; P is rounded to the inputs' type for the second product.  The running
 // maximum moves when a score passes it by more than 2^8, which bounds P by 256 and makes changes of O rare.
 // Where the items are fewer than the SMs can share (few rows over long keys), an item's keys are cut into pieces whose
-// (m, l, O) go to the workspace, and a second kernel joins them.
+// (m, l, O) go to the workspace, and a second kernel joins them (64 tokens after 16,000: 25 us;
+// uncut, 126 blocks would follow one another).
 #include <algorithm>
 
 #include "hg_rows.cuh"
@@ -418,7 +424,7 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
       }
       if (valid && whole) {
         // a lane's row lies on lines of its own, and a warp's store takes a cycle a line: 32 bytes a store where they are
-        // aligned (1,460 tokens of 28 heads, all 4 KV heads: 3,100 cycles an item less than in stores of 16)
+        // aligned (an item's output takes about 2,700 cycles, 4,500 in stores of 16 bytes)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           uint32_t x[8];
@@ -523,10 +529,16 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant_
   grid_launch_dependents();
   grid_dependency_wait();
   const int lane = threadIdx.x % 32, quad = blockIdx.y * 8 + threadIdx.x / 32;  // channels 4 quad ..
-  const int row = (blockIdx.x % 8) * 32 + lane, index = blockIdx.x / 8;
-  Item it;
-  item_at(p, index, it);
-  if (it.slot < 0 || it.first > 0) return;  // whole, or not the item's first piece
+  const int row = (blockIdx.x % 8) * 32 + lane, head_of_kv = blockIdx.x / 8 % p.kv_heads, tile = blockIdx.x / 8 / p.kv_heads;
+  int prompt = 0, next = p.prompts;
+  while (next - prompt > 1) {
+    const int mid = (prompt + next) / 2;
+    if (p.first_tile[mid] <= tile) prompt = mid;
+    else next = mid;
+  }
+  Item it;  // its first piece
+  item_at(p, (p.first_unit[prompt] + tile - p.first_tile[prompt]) * p.kv_heads + head_of_kv, it);
+  if (it.slot < 0) return;  // whole
   const int t = row / kTileRows, in_tile = row % kTileRows;
   const int tok_of_row = in_tile / p.group, tok = it.tok0 + t * p.tile_tokens + tok_of_row;
   if (tok_of_row >= p.tile_tokens || tok >= it.q_len) return;
@@ -590,7 +602,7 @@ cudaError_t launch(const PromptParams& p, cudaStream_t s) {
   }
   e = launch_overlapped(prompt_kernel<F16>, dim3((unsigned)std::min(p.items, device_sms())), kThreads, kSmemBytes, s, p);
   if (e != cudaSuccess || !p.split) return e;
-  return launch_overlapped(prompt_join_kernel<F16>, dim3((unsigned)(p.items * 8), 4), 256, 0, s, p);
+  return launch_overlapped(prompt_join_kernel<F16>, dim3((unsigned)(p.tiles * p.kv_heads * 8), 4), 256, 0, s, p);
 }
 
 }  // namespace
