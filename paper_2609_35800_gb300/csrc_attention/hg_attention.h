@@ -83,7 +83,8 @@ constexpr int kPromptBlock = 128;  // keys of a block
 constexpr int kPromptPartFloats = 3 * 256 + 256 * kHeadDim;
 constexpr int kPromptParts = 608;
 struct PromptParams {
-  CUtensorMap q_map, k_map, v_map;  // [tokens][heads][128] (q), [heads][tokens][128]: boxes of 64 channels
+  CUtensorMap q_map, k_map, v_map, out_map;  // [tokens][heads][128] (q, out), [heads][tokens][128]: boxes of 64 channels
+  int out_mapped;  // out's strides allow a map
   Rows out;
   float* lse;
   int prompts, q_heads, kv_heads, group, causal;

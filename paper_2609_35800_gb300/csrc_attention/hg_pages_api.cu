@@ -398,6 +398,9 @@ hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_
                encode_rows(encode, &p.v_map, io->v.data, num_kv_heads, io->v.head_stride, 1, key_rows, io->v.token_stride,
                            kPromptBlock, f16) != CUDA_SUCCESS))
     return HG_ERR_CUDA;
+  p.out_mapped = rows_mappable(io->out, rows, num_q_heads) &&
+                 encode_rows(encode, &p.out_map, io->out.data, rows, io->out.token_stride, 128 / p.group, num_q_heads,
+                             io->out.head_stride, p.group, f16) == CUDA_SUCCESS;
   for (int done = 0; done < num_prompts; done += kPromptsPerLaunch) {
     const int n = std::min(kPromptsPerLaunch, num_prompts - done);
     p.prompts = p.split = 0;

@@ -48,16 +48,17 @@ constexpr unsigned kAll = 0xffffffffu;
 // Shared memory from a 1024-byte boundary.
 constexpr int kQueryOffset = 0;
 constexpr int kRingOffset = 2 * kTileBytes;
-constexpr int kBarOffset = kRingOffset + kStages * kTileBytes;
+constexpr int kOutOffset = kRingOffset + kStages * kTileBytes;  // half of the channels of each tile, on their way out
+constexpr int kBarOffset = kOutOffset + 2 * kHalfBytes;
 constexpr int kSmemBytes = kBarOffset + 512 + 1024;
 enum Bar { kQueryFull = 0, kQueryFree, kScoreFull, kProbFull = kScoreFull + 2, kOutFull = kProbFull + 2,
-           kItemFull = kOutFull + 2, kItemFree = kItemFull + 2, kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages,
+           kStageFull = kOutFull + 2, kStageFree = kStageFull + 2, kItemFull = kStageFree + 2, kItemFree = kItemFull + 2, kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages,
            kBars = kRingFree + kStages };
 constexpr int kItemOffset = kBarOffset + 256;  // two Items
 constexpr int kMiscOffset = kItemOffset + 2 * 64;  // abort flag, tensor memory address
 static_assert(kBars * 8 <= 256, "barriers");
 
-struct Item {
+struct __align__(16) Item {
   int q0;         // first query row (token of the tensors) of the prompt
   int tok0;       // first token of tile 0, in the prompt
   int q_len, k_len, k0;
@@ -69,10 +70,21 @@ struct Item {
   int slot_step;  // from a piece's slot to the next one's
   int none;       // no further item
 };
-static_assert(sizeof(Item) <= 64, "items");
+static_assert(sizeof(Item) == 64, "items");
 
 __device__ __forceinline__ int seen_by(const PromptParams& p, int q_len, int k_len, int tok) {
   return p.causal ? min(max(tok + 1 + k_len - q_len, 0), k_len) : k_len;
+}
+
+// The item at a shared-memory address.
+__device__ __forceinline__ void read_item(Item& it, uint32_t from) {
+  union {
+    uint4 w[4];
+    Item item;
+  } x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.w[i] = ld_shared16(from + 16 * i);
+  it = x.item;
 }
 
 // Item number -> work: prompt by prompt (longest first), piece by piece, tile pair by tile pair (last tokens first), heads
@@ -137,7 +149,7 @@ __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t b
     if (it.none) return;
     const int blocks = max(it.n[0], it.n[1]);
     if (blocks == 0) continue;
-    if (queries > 0 && !wait_warp<true>(bars + 8 * kQueryFree, (queries - 1) & 1, misc, p.status)) return;
+    if (queries > 0 && !wait_warp(bars + 8 * kQueryFree, (queries - 1) & 1, misc, p.status)) return;
     if (lane == 0) {
       const uint32_t bar = bars + 8 * kQueryFull;
       mbar_arrive_expect_tx(bar, (uint32_t)((it.n[0] > 0) + (it.n[1] > 0)) * 2 * q_bytes);
@@ -164,18 +176,19 @@ __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t b
 
 // One warp, of which one thread issues every product.
 template <bool F16>
-__device__ void issue_products(const PromptParams& p, uint32_t base, const char* smem, uint32_t tmem, volatile int* misc) {
+__device__ void issue_products(const PromptParams& p, uint32_t base, uint32_t tmem, volatile int* misc) {
   const int lane = threadIdx.x % 32;
   const uint32_t bars = base + kBarOffset;
-  const volatile Item* items = reinterpret_cast<const volatile Item*>(smem + kItemOffset);
   const uint32_t q_operand = smem_operand(base + kQueryOffset, 16), k_operand = smem_operand(base + kRingOffset, 16);
   const uint32_t v_operand = smem_operand(base + kRingOffset, kHalfBytes), v_shape = mma_shape(F16, kHeadDim, true);
   uint32_t fill = 0, queries = 0, probs[2] = {0, 0};
   for (uint32_t n = 0;; ++n) {
     const uint32_t slot = n & 1;
     if (!wait_warp(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc, p.status)) return;
-    const int none = items[slot].none, first = items[slot].first, k_len = items[slot].k_len;
-    const int count[2] = {items[slot].n[0], items[slot].n[1]}, width[2] = {items[slot].width[0], items[slot].width[1]};
+    Item it;
+    read_item(it, base + kItemOffset + slot * 64);
+    const int none = it.none, first = it.first, k_len = it.k_len;
+    const int count[2] = {it.n[0], it.n[1]}, width[2] = {it.width[0], it.width[1]};
     __syncwarp();
     if (lane == 0) mbar_arrive(bars + 8 * (kItemFree + slot));
     if (none) return;
@@ -302,28 +315,20 @@ __device__ __forceinline__ float half_probabilities(const uint32_t (&a)[32], con
 
 // 128 threads, a row each, of tile t.
 template <bool F16>
-__device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const char* smem, uint32_t tmem, volatile int* misc) {
+__device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, uint32_t tmem, volatile int* misc) {
   const int lane = threadIdx.x % 32, row = threadIdx.x % kTileRows;
   const uint32_t bars = base + kBarOffset;
-  const volatile Item* items = reinterpret_cast<const volatile Item*>(smem + kItemOffset);
   const uint32_t mine = (uint32_t)(row / 32 * 32) << 16;  // this warp's lanes of tensor memory
   const uint32_t s_at = tmem + mine + kScoreColumn + 128 * t, o_at = tmem + mine + kOutColumn + 128 * t;
   const float c = p.scale * kLog2e;
   const int tok_of_row = row / p.group, head_of_row = row - tok_of_row * p.group;
-  uint32_t scores = 0, outs = 0;
+  uint32_t scores = 0, outs = 0, stores = 0;
   for (uint32_t n = 0;; ++n) {
     const uint32_t slot = n & 1;
     if (!wait_warp(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc, p.status)) return;
     Item it;
-    it.none = items[slot].none;
-    it.q0 = items[slot].q0;
-    it.tok0 = items[slot].tok0;
-    it.q_len = items[slot].q_len;
-    it.k_len = items[slot].k_len;
-    it.head = items[slot].head;
-    it.first = items[slot].first;
-    it.slot = items[slot].slot;
-    const int blocks = items[slot].n[t];
+    read_item(it, base + kItemOffset + slot * 64);
+    const int blocks = t == 0 ? it.n[0] : it.n[1];
     __syncwarp();
     if (lane == 0) mbar_arrive(bars + 8 * (kItemFree + slot));
     if (it.none) return;
@@ -412,6 +417,38 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, const 
       part[256 + part_row] = st.r;
       part[512 + part_row] = st.l;
     }
+    if (whole && blocks > 0 && p.out_mapped && it.tok0 + (t + 1) * p.tile_tokens <= it.q_len) {
+      // every row is somebody's: through shared memory, and one copy for each half of the channels
+      const uint32_t stage = base + kOutOffset + t * kHalfBytes;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half, ++stores) {
+        if (stores > 0) wait_data(bars + 8 * (kStageFree + t), (stores - 1) & 1, misc, p.status);
+        uint32_t o[2][32];
+        tmem_load32(o[0], o_at + 64 * half);
+        tmem_load32(o[1], o_at + 64 * half + 32);
+        tmem_wait_loads();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          uint32_t x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] = pack2<F16>(__uint_as_float(o[k / 4][(8 * k + 2 * e) % 32]) * scale,
+                              __uint_as_float(o[k / 4][(8 * k + 2 * e + 1) % 32]) * scale);
+          st_shared16(stage + swizzled(row, k), make_uint4(x[0], x[1], x[2], x[3]));
+        }
+        fence_proxy_async_shared();
+        mbar_arrive(bars + 8 * (kStageFull + t));
+        if (row == 0) {
+          wait_phase(bars + 8 * (kStageFull + t), stores & 1, misc, p.status);
+          tma_store_3d(&p.out_map, stage, 64 * half, it.head * p.group, it.q0 + it.tok0 + t * p.tile_tokens);
+          bulk_stores_read();
+          mbar_arrive(bars + 8 * (kStageFree + t));
+        }
+        __syncwarp();
+      }
+      tc_fence_before();
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t o[32];
@@ -465,6 +502,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       mbar_init(bars + 8 * (kScoreFull + t), 1);
       mbar_init(bars + 8 * (kProbFull + t), kTileRows);
       mbar_init(bars + 8 * (kOutFull + t), 1);
+      mbar_init(bars + 8 * (kStageFull + t), kTileRows);
+      mbar_init(bars + 8 * (kStageFree + t), 1);
       mbar_init(bars + 8 * (kItemFull + t), 1);
       mbar_init(bars + 8 * (kItemFree + t), 9);  // eight softmax warps and the one that issues
     }
@@ -495,11 +534,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       fence_proxy_async_global();  // inputs written by ordinary stores of earlier launches
       load_items(p, mine, some, base, smem, misc, fills, queries);
     } else if (warp == kMmaWarp) {
-      issue_products<F16>(p, base, smem, tmem, misc);
+      issue_products<F16>(p, base, tmem, misc);
     }
   } else {
     set_registers_up<kRowRegisters>();
-    softmax_rows<F16>(p, warp / 4, base, smem, tmem, misc);
+    softmax_rows<F16>(p, warp / 4, base, tmem, misc);
+    if (threadIdx.x % kTileRows == 0) bulk_stores_done();
   }
   tc_fence_before();
   __syncthreads();
