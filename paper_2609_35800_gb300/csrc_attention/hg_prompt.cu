@@ -2,8 +2,8 @@
 //
 // For a prompt's query row: s_t = scale q.k_t over the keys it sees, m = max s_t, out = sum e^(s_t - m) v_t / sum
 // e^(s_t - m).  4 * 128 flop a (query head, key) pair and little to read: the kernel is bound by the products, and for
-// short prompts by the chain of a tile's blocks.  Measured: 2 x 8,192 causal tokens of 64 heads 1,545 TFLOP/s (1,604 with
-// the softmax left out: a product of 128 x 128 with both operands in shared memory reads all that it can give, 128 bytes
+// short prompts by the chain of a tile's blocks.  Measured: 2 x 8,192 causal tokens of 64 heads 1,579 TFLOP/s (an earlier
+// form 1,461, and 1,604 with the softmax left out: a product of 128 x 128 with both operands in shared memory reads all that it can give, 128 bytes
 // a cycle); 1,460 tokens of 28 heads 26 us, 12 blocks of 3,000 cycles one after the other.
 //
 // A work item is two tiles of 128 rows of one prompt and KV head.  A tile's rows are 128 / G consecutive tokens times
@@ -396,7 +396,7 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, uint32
       mbar_arrive(bars + 8 * (kProbFull + t));
     }
 
-    // the tile's end
+    // the tile's end: about 3,500 cycles, a third of it in the two copies of a whole tile
     if (blocks > 0) {
       wait_data(bars + 8 * (kOutFull + t), outs & 1, misc, p.status);
       ++outs;

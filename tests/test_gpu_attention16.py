@@ -490,6 +490,25 @@ def test_prompt_long(dtype, lens, heads, group, layout):
     _check_prompt(q, k, v, qb, kb, True, out, lse, some=range(min(len(lens), 3)))
 
 
+@TYPES
+@pytest.mark.parametrize("heads,group", [(2, 8), (3, 5), (1, 16), (4, 1)])
+def test_prompt_output_strides(dtype, heads, group):
+    """Outputs heads first, and every second head of a wider tensor: whole tiles and those that end a prompt."""
+    g = _gen(heads * 7 + group)
+    lens = [300, 31, 16, 1, 256, 129]
+    q, k, v, qb, kb = _prompt(g, lens, lens, heads, group, dtype, "tokens")
+    n, hq = q.shape[0], q.shape[1]
+    dense, lse = _run_prompt(q, k, v, qb, kb, True)
+    _check_prompt(q, k, v, qb, kb, True, dense, lse)
+    ws = _workspace(hg.hg_prompt_workspace_size())
+    first = torch.full((hq, n, D), NAN, dtype=dtype, device="cuda").transpose(0, 1)
+    hg.hg_prompt_attention(q, k, v, qb, kb, first, None, True, 0.0, ws)
+    assert torch.equal(_bits(first), _bits(dense))
+    wide = torch.full((n, 2 * hq, D), NAN, dtype=dtype, device="cuda")
+    hg.hg_prompt_attention(q, k, v, qb, kb, wide[:, ::2], None, True, 0.0, ws)
+    assert torch.equal(_bits(wide[:, ::2]), _bits(dense)) and bool(wide[:, 1::2].isnan().all())
+
+
 def test_prompt_many_prompts():
     """More prompts than one launch takes."""
     g = _gen(20)
