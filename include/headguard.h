@@ -400,8 +400,8 @@ typedef struct hg_rotation {
  * page_size) of head h in page p starts at p * page_stride + h * head_stride +
  * t * token_stride elements.  page_size: 16, 32, 64, 128 or 256.  All strides 0:
  * dense [num_pages][num_kv_heads][page_size][128].  Strides are multiples of 8
- * elements below 2^38, at least 128 (page_stride at least 1 where num_pages is
- * 1), and rows must not overlap; num_pages * page_size < 2^31. */
+ * elements below 2^38, token_stride at least 128 and so are those of an axis
+ * longer than 1, and rows must not overlap; num_pages * page_size < 2^31. */
 typedef struct hg_page_shape {
     int32_t dtype;          /* hg_dtype */
     int32_t num_pages;

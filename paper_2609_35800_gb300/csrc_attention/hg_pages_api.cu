@@ -142,10 +142,12 @@ int64_t count_items(PromptParams* p) {
 }
 
 // How the launch's keys are cut.  Uncut, the launch lasts as long as its longest item at least; cut, as long as the
-// SMs' even share of all blocks, and the parts' way through memory besides (a few blocks' time).
+// SMs' even share of all blocks, and the parts' way through memory and the join besides.  64 tokens after 16,000, 28
+// heads: longest 126 blocks, share 6.6, cut 25 us.  1,460 tokens, 28 heads: longest 12, share 6.7, uncut 26 us, cut 49.
 hg_status plan_prompts(PromptParams* p) {
   p->tile_tokens = 128 / p->group;
-  std::stable_sort(p->range, p->range + p->prompts, [](const PromptRange& a, const PromptRange& b) { return a.k_len > b.k_len; });
+  std::sort(p->range, p->range + p->prompts,
+            [](const PromptRange& a, const PromptRange& b) { return a.k_len != b.k_len ? a.k_len > b.k_len : a.q0 < b.q0; });
   p->chunk = INT32_MAX / 2;
   int64_t items = count_items(p);
   double blocks = 0.;

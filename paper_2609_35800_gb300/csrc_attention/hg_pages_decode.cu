@@ -191,12 +191,14 @@ __device__ int find_work(const PagesDecodeParams& p, int* scan, int* kept, Work&
   return tiles;
 }
 
-// Lets the launch's page ids, queries and rotations into L2 before the caches' reads fill the memory's queues: CTA by CTA a request.
+// Lets the launch's page ids, queries and rotations into L2 before the caches' reads fill the memory's queues: a request
+// by each CTA in turn.
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
 __device__ void prefetch_queries(const PagesDecodeParams& p) {
   for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
     const int heads = p.group * p.pool.heads;
-    for (int i = 32 * threadIdx.x; i < p.table_stride; i += 32 * kThreads) prefetch_l2(p.table + (int64_t)b * p.table_stride + i);
+    for (int i = 32 * threadIdx.x; i < p.table_stride; i += 32 * kThreads)
+      prefetch_l2(p.table + (int64_t)b * p.table_stride + i);
     for (int i = threadIdx.x; i < 2 * heads; i += kThreads)
       prefetch_l2(p.q.data + b * p.q.token_stride + (i / 2) * p.q.head_stride + (i % 2) * 64);
     if (p.rot.table == nullptr) continue;
@@ -287,7 +289,8 @@ __device__ __forceinline__ void fetch_queries(const PagesDecodeParams& p, int b,
 
 // Rotated, and through shared memory into the first product's operands.
 template <bool F16, int NT>
-__device__ __forceinline__ void stage_queries(const PagesDecodeParams& p, Queries<NT>& x, uint32_t mine, uint32_t (&qf)[NT][16]) {
+__device__ __forceinline__ void stage_queries(const PagesDecodeParams& p, Queries<NT>& x, uint32_t mine,
+                                              uint32_t (&qf)[NT][16]) {
   const int lane = threadIdx.x % 32;
   const LaneChannels at = lane_channels(p.rot, lane % 8, p.rot.table != nullptr);
 #pragma unroll
@@ -343,10 +346,10 @@ __device__ __forceinline__ void place_new_token(const PagesDecodeParams& p, cons
   __syncwarp();
 }
 
-// A tile of 32 tokens, of which the first `seen` belong to the request; box(r): where row r's box begins.
+// A tile of 32 tokens, of which the first `seen` belong to the request.
 template <bool F16, int NT>
-__device__ __forceinline__ void attend_tile(State<NT>& st, const uint32_t (&qf)[NT][16], uint32_t kt, uint32_t vt, int rows, int seen,
-                                            float c) {
+__device__ __forceinline__ void attend_tile(State<NT>& st, const uint32_t (&qf)[NT][16], uint32_t kt, uint32_t vt, int rows,
+                                            int seen, float c) {
   const int lane = threadIdx.x % 32;
   float s[2][NT][4], s2[2][NT][4];  // [16 tokens][query tile]; a chain of products for each half of the channels
 #pragma unroll
@@ -475,13 +478,15 @@ __device__ __forceinline__ Part add_rows(const float* row, int apart, int count,
 __device__ __forceinline__ void store_part(const Part& a, float* channels, float* ml, int channel) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<float4*>(channels + channel + 4 * i) = make_float4(a.o[4 * i], a.o[4 * i + 1], a.o[4 * i + 2], a.o[4 * i + 3]);
+    *reinterpret_cast<float4*>(channels + channel + 4 * i) =
+        make_float4(a.o[4 * i], a.o[4 * i + 1], a.o[4 * i + 2], a.o[4 * i + 3]);
   if (channel == 0) *reinterpret_cast<float2*>(ml) = make_float2(a.m, a.l);
 }
 
 // out = o / l in the cache's type, and the query's log-sum-exp.
 template <bool F16>
-__device__ __forceinline__ void write_query(const PagesDecodeParams& p, int b, int h, int len, int q, int channel, const Part& a) {
+__device__ __forceinline__ void write_query(const PagesDecodeParams& p, int b, int h, int len, int q, int channel,
+                                            const Part& a) {
   const float r = len > 0 ? 1.0f / a.l : 0.f;
   const int head = h * p.group + q;
   uint16_t* out = p.out.data + b * p.out.token_stride + head * p.out.head_stride + channel;
@@ -747,8 +752,7 @@ __global__ void __launch_bounds__(kThreads, 2) pages_decode_kernel(const __grid_
   __syncthreads();
   if (misc[0]) {  // a CTA that gave up leaves once the copies it asked for have landed
     for (uint32_t n = asked > kStages ? asked - kStages : 0; n < asked; ++n)
-      for (uint32_t i = 0; i < kAsyncRounds && !mbar_try_wait_sleep(full + 8 * (n % kStages), (n / kStages) & 1, kAsyncSleepNs); ++i) {
-      }
+      drain_phase(full + 8 * (n % kStages), (n / kStages) & 1);
   }
 }
 

@@ -3,8 +3,8 @@
 // For a prompt's query row: s_t = scale q.k_t over the keys it sees, m = max s_t, out = sum e^(s_t - m) v_t / sum
 // e^(s_t - m).  4 * 128 flop a (query head, key) pair and little to read: the kernel is bound by the products, and for
 // short prompts by the chain of a tile's blocks.  Measured: 2 x 8,192 causal tokens of 64 heads 1,579 TFLOP/s (an earlier
-// form 1,461, and 1,604 with the softmax left out: a product of 128 x 128 with both operands in shared memory reads all that it can give, 128 bytes
-// a cycle); 1,460 tokens of 28 heads 26 us, 12 blocks of 3,000 cycles one after the other.
+// form 1,461, and 1,604 with the softmax left out: a product of 128 x 128 with both operands in shared memory reads all
+// that it can give, 128 bytes a cycle); 1,460 tokens of 28 heads 26 us, 12 blocks of 3,000 cycles one after the other.
 //
 // A work item is two tiles of 128 rows of one prompt and KV head.  A tile's rows are 128 / G consecutive tokens times
 // the G query heads of the KV head, so short prompts fill their tiles and a causal tile spans few tokens; both tiles use
@@ -52,8 +52,8 @@ constexpr int kOutOffset = kRingOffset + kStages * kTileBytes;  // half of the c
 constexpr int kBarOffset = kOutOffset + 2 * kHalfBytes;
 constexpr int kSmemBytes = kBarOffset + 512 + 1024;
 enum Bar { kQueryFull = 0, kQueryFree, kScoreFull, kProbFull = kScoreFull + 2, kOutFull = kProbFull + 2,
-           kStageFull = kOutFull + 2, kStageFree = kStageFull + 2, kItemFull = kStageFree + 2, kItemFree = kItemFull + 2, kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages,
-           kBars = kRingFree + kStages };
+           kStageFull = kOutFull + 2, kStageFree = kStageFull + 2, kItemFull = kStageFree + 2, kItemFree = kItemFull + 2,
+           kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages, kBars = kRingFree + kStages };
 constexpr int kItemOffset = kBarOffset + 256;  // two Items
 constexpr int kMiscOffset = kItemOffset + 2 * 64;  // abort flag, tensor memory address
 static_assert(kBars * 8 <= 256, "barriers");
@@ -167,7 +167,8 @@ __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t b
         const uint32_t bar = bars + 8 * (kRingFull + stage), dst = base + kRingOffset + stage * kTileBytes;
         mbar_arrive_expect_tx(bar, kTileBytes);
         for (int half = 0; half < 2; ++half)
-          tma_load_3d(dst + half * kHalfBytes, j % 2 ? &p.v_map : &p.k_map, 64 * half, it.k0 + (it.first + j / 2) * kBlock, it.head, bar);
+          tma_load_3d(dst + half * kHalfBytes, j % 2 ? &p.v_map : &p.k_map, 64 * half, it.k0 + (it.first + j / 2) * kBlock,
+                      it.head, bar);
       }
       __syncwarp();
     }
@@ -287,7 +288,8 @@ template <bool F16>
 __device__ __forceinline__ float half_probabilities(const uint32_t (&a)[32], const uint32_t (&b)[32], const RowSum& st, float c,
                                                     uint32_t (&prob)[32]) {
   const float shift = st.M == -INFINITY ? 0.f : -st.M;
-  const uint64_t c2 = f32x2(__float_as_uint(c), __float_as_uint(c)), shift2 = f32x2(__float_as_uint(shift), __float_as_uint(shift));
+  const uint64_t c2 = f32x2(__float_as_uint(c), __float_as_uint(c));
+  const uint64_t shift2 = f32x2(__float_as_uint(shift), __float_as_uint(shift));
   uint64_t sum[2] = {0, 0};
   if (__any_sync(kAll, st.r != 0.f)) {
     const uint64_t r2 = f32x2(__float_as_uint(-st.r), __float_as_uint(-st.r));
@@ -522,7 +524,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   Item mine;  // the first one is known from the launch's parameters alone
   bool some = false;
   if (warp == kLoadWarp) {
-    if (threadIdx.x % 32 < 3) prefetch_tensormap(threadIdx.x % 32 == 0 ? &p.q_map : threadIdx.x % 32 == 1 ? &p.k_map : &p.v_map);
+    const int lane = threadIdx.x % 32;  // (without a key in any prompt, or with an output that has no map, there is none)
+    if (lane == 0) prefetch_tensormap(&p.q_map);
+    if (lane == 1 && p.range[0].k_len > 0) prefetch_tensormap(&p.k_map);
+    if (lane == 2 && p.range[0].k_len > 0) prefetch_tensormap(&p.v_map);
+    if (lane == 3 && p.out_mapped) prefetch_tensormap(&p.out_map);
     some = item_at(p, blockIdx.x, mine);
   }
   grid_launch_dependents();
@@ -545,10 +551,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   __syncthreads();
   if (misc[0] && warp == kLoadWarp) {  // a CTA that gave up leaves once the copies it asked for have landed
     for (uint32_t n = fills > kStages ? fills - kStages : 0; n < fills; ++n)
-      for (uint32_t i = 0; i < kAsyncRounds && !mbar_try_wait_sleep(bars + 8 * (kRingFull + n % kStages), (n / kStages) & 1, kAsyncSleepNs); ++i) {
-      }
-    for (uint32_t i = 0; queries > 0 && i < kAsyncRounds && !mbar_try_wait_sleep(bars + 8 * kQueryFull, (queries - 1) & 1, kAsyncSleepNs); ++i) {
-    }
+      drain_phase(bars + 8 * (kRingFull + n % kStages), (n / kStages) & 1);
+    if (queries > 0) drain_phase(bars + 8 * kQueryFull, (queries - 1) & 1);
   }
   if (misc[0] && warp == kMmaWarp) __nanosleep(1000000);  // and its products have ended
   __syncthreads();
@@ -624,7 +628,8 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant_
   }
   const float scale = seen > 0 ? 1.0f / l : 0.f;
   uint16_t* out = p.out.data + token * p.out.token_stride + head * p.out.head_stride + 4 * quad;
-  *reinterpret_cast<uint2*>(out) = make_uint2(pack2<F16>(acc.x * scale, acc.y * scale), pack2<F16>(acc.z * scale, acc.w * scale));
+  *reinterpret_cast<uint2*>(out) =
+      make_uint2(pack2<F16>(acc.x * scale, acc.y * scale), pack2<F16>(acc.z * scale, acc.w * scale));
   if (p.lse && quad == 0) p.lse[token * p.q_heads + head] = l == 0.f ? -INFINITY : ((M + r) + log2f(l)) * 0.69314718055994531f;
 }
 

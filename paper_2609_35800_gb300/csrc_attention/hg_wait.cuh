@@ -42,6 +42,12 @@ __device__ __forceinline__ void wait_data(uint32_t bar, uint32_t parity, volatil
   __syncwarp();
 }
 
+// For a CTA that gave up: until the copies that complete this phase have landed, or a second has passed.
+__device__ __forceinline__ void drain_phase(uint32_t bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kAsyncRounds && !mbar_try_wait_sleep(bar, parity, kAsyncSleepNs); ++i) {
+  }
+}
+
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
 }

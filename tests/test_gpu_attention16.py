@@ -490,6 +490,18 @@ def test_prompt_long(dtype, lens, heads, group, layout):
     _check_prompt(q, k, v, qb, kb, True, out, lse, some=range(min(len(lens), 3)))
 
 
+def test_prompts_without_any_key_and_an_empty_batch():
+    g = _gen(25)
+    q = _randn(g, 70, 6, D)
+    none = torch.empty(0, 2, D, dtype=BF16, device="cuda")
+    qb, kb = torch.tensor([0, 40, 70], dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for causal in (True, False):
+        out, lse = _run_prompt(q, none, none, qb, kb, causal)
+        assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    out, lse = _run_prompt(q, none, none, qb[:1], kb[:1], True)  # no prompt
+    assert bool(out.isnan().all())
+
+
 @TYPES
 @pytest.mark.parametrize("heads,group", [(2, 8), (3, 5), (1, 16), (4, 1)])
 def test_prompt_output_strides(dtype, heads, group):
