@@ -5,7 +5,8 @@ Thin ctypes marshalling over ``libheadguard.so`` (declared in
 converts its arguments (torch tensors -> device pointers, streams -> handles)
 and raises :class:`HGError` on a non-zero status (and ValueError, before the
 call, when a tensor argument is not a dense CUDA tensor holding the bytes the
-call reads or writes through it).  All computation happens in
+call reads or writes through it; the calls of the 16-bit caches also take
+strided rows of dense channels).  All computation happens in
 the library's CUDA kernels; there is no Python or CPU fallback, and importing
 the compute functions without the built library raises.
 """
