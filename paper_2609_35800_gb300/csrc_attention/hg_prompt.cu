@@ -149,7 +149,7 @@ __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t b
     if (it.none) return;
     const int blocks = max(it.n[0], it.n[1]);
     if (blocks == 0) continue;
-    if (queries > 0 && !wait_warp(bars + 8 * kQueryFree, (queries - 1) & 1, misc, p.status)) return;
+    if (queries > 0 && !wait_to_fill(bars + 8 * kQueryFree, (queries - 1) & 1, misc, p.status)) return;
     if (lane == 0) {
       const uint32_t bar = bars + 8 * kQueryFull;
       mbar_arrive_expect_tx(bar, (uint32_t)((it.n[0] > 0) + (it.n[1] > 0)) * 2 * q_bytes);
@@ -162,7 +162,7 @@ __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t b
     ++queries;
     for (int j = 0; j < 2 * blocks; ++j, ++fills) {  // K, V of a block
       const uint32_t stage = fills % kStages, round = fills / kStages;
-      if (round > 0 && !wait_warp<true>(bars + 8 * (kRingFree + stage), (round - 1) & 1, misc, p.status)) return;
+      if (round > 0 && !wait_to_fill<true>(bars + 8 * (kRingFree + stage), (round - 1) & 1, misc, p.status)) return;
       if (lane == 0) {
         const uint32_t bar = bars + 8 * (kRingFull + stage), dst = base + kRingOffset + stage * kTileBytes;
         mbar_arrive_expect_tx(bar, kTileBytes);

@@ -35,8 +35,17 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, ASLEEP ? wait_asleep(bar, parity, abort, status) : wait_phase(bar, parity, abort, status));
 }
 
-// The same where a vote would lengthen a chain of products and softmax (by 1.5%): the warp goes on in any case, over
-// whatever is there, and finds *abort at its next wait_warp.  For data that no address is made from.
+// The wait of a warp that fills the place it waited for.  A warp that gave up on a copy may have handed the place on all
+// the same, and one more arrival on a barrier whose bytes are still expected is an error: nothing is filled once *abort
+// is set (which it was before the place was handed on).
+template <bool ASLEEP = false>
+__device__ __forceinline__ bool wait_to_fill(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
+  const bool there = ASLEEP ? wait_asleep(bar, parity, abort, status) : wait_phase(bar, parity, abort, status);
+  return __all_sync(0xffffffffu, there && !*abort);
+}
+
+// The same as wait_warp where a vote would lengthen a chain of products and softmax (by 1.5%): the warp goes on in any
+// case, over whatever is there, and finds *abort at its next wait_warp.  For data that no address is made from.
 __device__ __forceinline__ void wait_data(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
   wait_phase(bar, parity, abort, status);
   __syncwarp();

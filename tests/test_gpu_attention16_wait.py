@@ -1,0 +1,35 @@
+"""The give-up paths of the 16-bit kernels: their waits run on barriers that nobody completes, end within their limit and
+leave a status; nothing is filled, and no tensor memory freed, over what was given up on."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2609_35800_gb300 import build
+
+pytestmark = pytest.mark.gpu
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def probe(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("probe") / "attention_wait_probe.so")
+    subprocess.run([build.nvcc()] + build.ARCH + build.NVCC_FLAGS + ["-shared", os.path.join(HERE, "attention_wait_probe.cu"),
+                                                                     "-o", so], check=True)
+    lib = ctypes.CDLL(so)
+    for f in (lib.run_ring,):
+        f.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
+    return lib
+
+
+def test_a_place_is_not_filled_over_a_copy_that_was_given_up_on(probe):
+    for _ in range(2):
+        status = torch.zeros(4, dtype=torch.int32, device="cuda")
+        result = torch.full((5,), 7, dtype=torch.int32, device="cuda")
+        assert probe.run_ring(status.data_ptr(), result.data_ptr()) == 0
+        torch.cuda.synchronize()
+        # nobody's wait was met, nothing was filled again, and everybody left
+        assert result.tolist() == [0, 0, 0, 0, 1]
+        assert status.tolist() == [1, 0, 0, 0]
