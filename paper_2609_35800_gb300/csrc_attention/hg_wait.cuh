@@ -5,7 +5,7 @@
 namespace hg {
 
 constexpr uint32_t kWaitTimeoutBit = 1;    // status word: a wait ran out
-constexpr uint32_t kAsyncRounds = 20000;   // rounds of up to kAsyncSleepNs each: about a second
+constexpr uint32_t kAsyncRounds = 1 << 18;  // rounds of 3.8 us each as measured, whatever longer time is asked for: a second
 constexpr uint32_t kAsyncSleepNs = 50000;
 
 // Wait for a phase of `bar`.  One that runs out flags the workspace's status word and *abort, by which every other

@@ -3,6 +3,7 @@ leave a status; nothing is filled, and no tensor memory freed, over what was giv
 import ctypes
 import os
 import subprocess
+import time
 
 import pytest
 import torch
@@ -33,3 +34,15 @@ def test_a_place_is_not_filled_over_a_copy_that_was_given_up_on(probe):
         # nobody's wait was met, nothing was filled again, and everybody left
         assert result.tolist() == [0, 0, 0, 0, 1]
         assert status.tolist() == [1, 0, 0, 0]
+
+
+def test_a_wait_lasts_about_a_second(probe):
+    """Long enough for a copy behind anything that the memory may be busy with, and the end of a launch that is stuck."""
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    result = torch.zeros(5, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    begin = time.perf_counter()
+    assert probe.run_ring(status.data_ptr(), result.data_ptr()) == 0
+    torch.cuda.synchronize()
+    waits = (time.perf_counter() - begin) / 2  # a wait, then a drain
+    assert 0.5 <= waits <= 4.0
