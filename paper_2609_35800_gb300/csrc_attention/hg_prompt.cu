@@ -55,7 +55,7 @@ enum Bar { kQueryFull = 0, kQueryFree, kScoreFull, kProbFull = kScoreFull + 2, k
            kStageFull = kOutFull + 2, kStageFree = kStageFull + 2, kItemFull = kStageFree + 2, kItemFree = kItemFull + 2,
            kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages, kBars = kRingFree + kStages };
 constexpr int kItemOffset = kBarOffset + 256;  // two Items
-constexpr int kMiscOffset = kItemOffset + 2 * 64;  // abort flag, tensor memory address
+constexpr int kMiscOffset = kItemOffset + 2 * 64;  // abort flag, tensor memory address, copies asked for
 static_assert(kBars * 8 <= 256, "barriers");
 
 struct __align__(16) Item {
@@ -164,6 +164,7 @@ __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t b
       const uint32_t stage = fills % kStages, round = fills / kStages;
       if (round > 0 && !wait_to_fill<true>(bars + 8 * (kRingFree + stage), (round - 1) & 1, misc, p.status)) return;
       if (lane == 0) {
+        misc[2] = (int)fills;
         const uint32_t bar = bars + 8 * (kRingFull + stage), dst = base + kRingOffset + stage * kTileBytes;
         mbar_arrive_expect_tx(bar, kTileBytes);
         for (int half = 0; half < 2; ++half)
@@ -327,7 +328,8 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, uint32
   uint32_t scores = 0, outs = 0, stores = 0;
   for (uint32_t n = 0;; ++n) {
     const uint32_t slot = n & 1;
-    if (!wait_warp(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc, p.status)) return;
+    // (a tile without rows waits for as long as the other tile's keys take)
+    if (!wait_for_others(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc + 2, misc, p.status)) return;
     Item it;
     read_item(it, base + kItemOffset + slot * 64);
     const int blocks = t == 0 ? it.n[0] : it.n[1];
@@ -514,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       mbar_init(bars + 8 * (kRingFree + i), 1);
     }
     mbar_init_fence();
-    misc[0] = 0;
+    misc[0] = misc[2] = 0;
   }
   if (warp == kMmaWarp) tmem_alloc(base + kMiscOffset + 4, 512);
   tc_fence_before();

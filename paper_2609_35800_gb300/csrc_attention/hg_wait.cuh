@@ -23,10 +23,11 @@ __device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volat
 
 // The same for those that others wait for: two plain questions, which the hardware holds back for a while, then
 // suspensions.  (Long prompts: 64 questions before the first suspension 5% slower, none 12%.)
+__device__ __forceinline__ bool wait_phase_briefly(uint32_t bar, uint32_t parity) {
+  return mbar_try_wait(bar, parity) || mbar_try_wait(bar, parity);
+}
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
-  for (int i = 0; i < 2; ++i)
-    if (mbar_try_wait(bar, parity)) return true;
-  return wait_asleep(bar, parity, abort, status);
+  return wait_phase_briefly(bar, parity) || wait_asleep(bar, parity, abort, status);
 }
 
 // The wait of a whole warp, which stays together: all of its threads go on, or none.
@@ -42,6 +43,26 @@ template <bool ASLEEP = false>
 __device__ __forceinline__ bool wait_to_fill(uint32_t bar, uint32_t parity, volatile int* abort, uint32_t* status) {
   const bool there = ASLEEP ? wait_asleep(bar, parity, abort, status) : wait_phase(bar, parity, abort, status);
   return __all_sync(0xffffffffu, there && !*abort);
+}
+
+// The wait of a whole warp that may have nothing to do for as long as others have: it runs out once *progress, which they
+// move, has stood still for as long as a wait lasts.
+__device__ __forceinline__ bool wait_for_others(uint32_t bar, uint32_t parity, volatile int* progress, volatile int* abort,
+                                                uint32_t* status) {
+  bool there = wait_phase_briefly(bar, parity);
+  for (uint32_t i = 0, last = *progress; !there; ++i) {
+    there = mbar_try_wait_sleep(bar, parity, kAsyncSleepNs);
+    const uint32_t now = *progress;
+    if (now != last) i = 0;
+    last = now;
+    if (there || *abort) break;
+    if (i >= kAsyncRounds) {
+      *abort = 1;
+      atomicOr(status, kWaitTimeoutBit);
+      break;
+    }
+  }
+  return __all_sync(0xffffffffu, there);
 }
 
 // The same as wait_warp where a vote would lengthen a chain of products and softmax (by 1.5%): the warp goes on in any

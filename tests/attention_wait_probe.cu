@@ -39,8 +39,42 @@ __global__ void ring_kernel(uint32_t* status, int* result) {
   if (threadIdx.x == 0) result[4] = abort;
 }
 
+// Warp 0 waits for warp 1, which takes `ns` and moves what they share all the while, or not.
+__global__ void slow_kernel(uint32_t* status, int* result, uint64_t ns, bool moves) {
+  __shared__ __align__(8) uint64_t bar;
+  __shared__ volatile int abort, progress;
+  const uint32_t done = smem_u32(&bar);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (threadIdx.x == 0) {
+    mbar_init(done, 1);
+    mbar_init_fence();
+    abort = progress = 0;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    const bool there = wait_for_others(done, 0, &progress, &abort, status);
+    if (lane == 0) result[0] = there;
+  } else if (lane == 0) {
+    uint64_t begin, now;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(begin));
+    for (int i = 0; i < 100000; ++i) {
+      __nanosleep(100000);
+      if (moves) progress = i + 1;
+      asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+      if (now - begin > ns) break;
+    }
+    mbar_arrive(done);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) result[1] = abort;
+}
+
 }  // namespace
 
+extern "C" int run_slow(uint32_t* status, int* result, uint64_t ns, int moves) {
+  slow_kernel<<<1, 64>>>(status, result, ns, moves != 0);
+  return (int)cudaGetLastError();
+}
 extern "C" int run_ring(uint32_t* status, int* result) {
   ring_kernel<<<1, 128>>>(status, result);
   return (int)cudaGetLastError();

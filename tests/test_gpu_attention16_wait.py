@@ -20,8 +20,8 @@ def probe(tmp_path_factory):
     subprocess.run([build.nvcc()] + build.ARCH + build.NVCC_FLAGS + ["-shared", os.path.join(HERE, "attention_wait_probe.cu"),
                                                                      "-o", so], check=True)
     lib = ctypes.CDLL(so)
-    for f in (lib.run_ring,):
-        f.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
+    lib.run_ring.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
+    lib.run_slow.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int]
     return lib
 
 
@@ -46,3 +46,13 @@ def test_a_wait_lasts_about_a_second(probe):
     torch.cuda.synchronize()
     waits = (time.perf_counter() - begin) / 2  # a wait, then a drain
     assert 0.5 <= waits <= 4.0
+
+
+@pytest.mark.parametrize("moves", [1, 0])
+def test_whoever_has_nothing_to_do_waits_as_long_as_others_move(probe, moves):
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    result = torch.full((2,), 7, dtype=torch.int32, device="cuda")
+    assert probe.run_slow(status.data_ptr(), result.data_ptr(), 3_000_000_000, moves) == 0
+    torch.cuda.synchronize()
+    assert result.tolist() == [moves, 1 - moves]
+    assert status.tolist() == [1 - moves, 0, 0, 0]
