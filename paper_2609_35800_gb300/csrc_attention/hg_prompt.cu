@@ -53,7 +53,8 @@ constexpr int kBarOffset = kOutOffset + 2 * kHalfBytes;
 constexpr int kSmemBytes = kBarOffset + 512 + 1024;
 enum Bar { kQueryFull = 0, kQueryFree, kScoreFull, kProbFull = kScoreFull + 2, kOutFull = kProbFull + 2,
            kStageFull = kOutFull + 2, kStageFree = kStageFull + 2, kItemFull = kStageFree + 2, kItemFree = kItemFull + 2,
-           kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages, kBars = kRingFree + kStages };
+           kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages, kProductsEnded = kRingFree + kStages,
+           kBars = kProductsEnded + 1 };
 constexpr int kItemOffset = kBarOffset + 256;  // two Items
 constexpr int kMiscOffset = kItemOffset + 2 * 64;  // abort flag, tensor memory address, copies asked for
 static_assert(kBars * 8 <= 256, "barriers");
@@ -515,6 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       mbar_init(bars + 8 * (kRingFull + i), 1);
       mbar_init(bars + 8 * (kRingFree + i), 1);
     }
+    mbar_init(bars + 8 * kProductsEnded, 1);
     mbar_init_fence();
     misc[0] = misc[2] = 0;
   }
@@ -556,7 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       drain_phase(bars + 8 * (kRingFull + n % kStages), (n / kStages) & 1);
     if (queries > 0) drain_phase(bars + 8 * kQueryFull, (queries - 1) & 1);
   }
-  if (misc[0] && warp == kMmaWarp) __nanosleep(1000000);  // and its products have ended
+  if (misc[0] && warp == kMmaWarp) drain_products(bars + 8 * kProductsEnded);  // and its products have ended
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();

@@ -1,5 +1,5 @@
 // The bounded waits of the 16-bit kernels, run out on purpose: on barriers that nobody completes, with no copy in flight.
-#include "hg_wait.cuh"
+#include "hg_tcgen05.cuh"
 
 using namespace hg;
 
@@ -69,8 +69,70 @@ __global__ void slow_kernel(uint32_t* status, int* result, uint64_t ns, bool mov
   if (threadIdx.x == 0) result[1] = abort;
 }
 
+// A wait that runs out; products issued all the same (128 x 128 x 16 `steps` times over operands of ones, one after the
+// other); the drain, and then tensor memory is read and freed.  result: whether the wait was met, whether the products had ended when
+// the drain returned, and how many of the 128 x 128 sums are right.
+constexpr int kOperandBytes = 128 * 128;
+__global__ void products_kernel(uint32_t* status, int* result, int steps) {
+  extern __shared__ char raw[];
+  __shared__ __align__(8) uint64_t bars[2];
+  __shared__ volatile int abort;
+  __shared__ int address;
+  const uint32_t base = (smem_u32(raw) + 1023) & ~1023u, never = smem_u32(bars), ended = never + 8;
+  const int warp = threadIdx.x / 32;
+  if (threadIdx.x == 0) {
+    mbar_init(never, 1);
+    mbar_init(ended, 1);
+    mbar_init_fence();
+    abort = 0;
+  }
+  for (int i = threadIdx.x; i < 2 * kOperandBytes / 16; i += blockDim.x)
+    st_shared16(base + 16 * i, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));  // BF16 ones
+  fence_proxy_async_shared();
+  if (warp == 0) tmem_alloc(smem_u32(&address), 128);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)address;
+  if (warp == 0) {
+    const bool there = wait_warp(never, 0, &abort, status);
+    if (elect_one()) {
+      const uint32_t a = smem_operand(base, 16), b = smem_operand(base + kOperandBytes, 16), shape = mma_shape(false, 128, false);
+      for (int i = 0; i < steps; ++i) tc_mma_ss(tmem, a, b, shape, i > 0);
+    }
+    __syncwarp();
+    drain_products(ended);
+    if (threadIdx.x == 0) {
+      result[0] = there;
+      result[1] = mbar_try_wait(ended, 0);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  int right = 0;
+  for (int i = 0; i < 4; ++i) {
+    uint32_t d[32];
+    tmem_load32(d, tmem + ((uint32_t)(warp * 32) << 16) + 32 * i);
+    tmem_wait_loads();
+    for (int k = 0; k < 32; ++k) right += __uint_as_float(d[k]) == 16.f * steps;
+  }
+  atomicAdd(result + 2, right);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_free(tmem, 128);
+  }
+}
+
 }  // namespace
 
+extern "C" int run_products(uint32_t* status, int* result, int steps) {
+  constexpr int bytes = 2 * kOperandBytes + 1024;
+  products_kernel<<<1, 128, bytes>>>(status, result, steps);
+  return (int)cudaGetLastError();
+}
 extern "C" int run_slow(uint32_t* status, int* result, uint64_t ns, int moves) {
   slow_kernel<<<1, 64>>>(status, result, ns, moves != 0);
   return (int)cudaGetLastError();

@@ -22,6 +22,7 @@ def probe(tmp_path_factory):
     lib = ctypes.CDLL(so)
     lib.run_ring.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
     lib.run_slow.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int]
+    lib.run_products.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int]
     return lib
 
 
@@ -56,3 +57,13 @@ def test_whoever_has_nothing_to_do_waits_as_long_as_others_move(probe, moves):
     torch.cuda.synchronize()
     assert result.tolist() == [moves, 1 - moves]
     assert status.tolist() == [1 - moves, 0, 0, 0]
+
+
+def test_products_have_ended_before_tensor_memory_is_freed(probe):
+    for steps in (1, 2000, 8):  # (and a launch after one that gave up has its tensor memory)
+        status = torch.zeros(4, dtype=torch.int32, device="cuda")
+        result = torch.zeros(3, dtype=torch.int32, device="cuda")
+        assert probe.run_products(status.data_ptr(), result.data_ptr(), steps) == 0
+        torch.cuda.synchronize()
+        assert result.tolist() == [0, 1, 128 * 128]
+        assert status.tolist() == [1, 0, 0, 0]
