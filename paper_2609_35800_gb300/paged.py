@@ -39,6 +39,22 @@ class PagedRunner:
             self.owned[request].append(page)
         self.lengths[request] = tokens
 
+    def _pages_for(self, owned, tokens):
+        """The free pages that requests which own these would get next, up to these tokens each; nothing is changed."""
+        need = [-(-n // self.page_size) - len(have) for n, have in zip(tokens, owned)]
+        if any(n + len(have) > self.per_request for n, have in zip(need, owned)):
+            raise RuntimeError("PagedRunner: a request of %d tokens, the table holds %d" % (
+                max(tokens), self.per_request * self.page_size))
+        if sum(need) > len(self.free):
+            raise RuntimeError("PagedRunner: %d pages wanted, %d left" % (sum(need), len(self.free)))
+        ids = iter(reversed(self.free))
+        return [[next(ids) for _ in range(n)] for n in need]
+
+    def _take(self, pages):
+        """The pages of _pages_for are no longer free."""
+        count = sum(len(ids) for ids in pages)
+        del self.free[len(self.free) - count:]
+
     def admit(self, q, k, v, prompt_lengths, positions, k_out=None, v_out=None):
         """Prompts one after the other, q / k / v [tokens][heads][128] not yet rotated: their attention
         [tokens][q_heads][128].  k_out / v_out: where the rotated keys and the values go as dense tensors as well (a
@@ -66,14 +82,29 @@ class PagedRunner:
         return out
 
     def step(self, q, k, v, positions):
-        """One new token of every request: q [requests][q_heads][128], k, v [requests][kv_heads][128]."""
+        """One new token of every request: q [requests][q_heads][128], k, v [requests][kv_heads][128].  A step that is
+        refused (no page left, arguments that do not fit) leaves the requests as they were."""
         n = len(self.owned)
-        for i in range(n):
-            self._grow(i, self.lengths[i] + 1)
-        self.lens[:n] += 1
+        if q.shape[0] != n:
+            raise ValueError("PagedRunner.step: q holds %d rows, there are %d requests" % (q.shape[0], n))
+        grown = [tokens + 1 for tokens in self.lengths]
+        pages = self._pages_for(self.owned, grown)
+        for i, ids in enumerate(pages):
+            if ids:  # (past a request's length the table is not read)
+                at = len(self.owned[i])
+                self.table[i, at:at + len(ids)] = torch.tensor(ids, dtype=torch.int32)
         out = torch.empty(n, self.q_heads, 128, dtype=self.dtype, device=self.device)
-        hg_pages_decode_step(self.pages, q, k, v, self.rotation, positions, self.table[:n], self.lens, out, None, 0.0,
-                             self.ws)
+        self.lens[:n] += 1
+        try:
+            hg_pages_decode_step(self.pages, q, k, v, self.rotation, positions, self.table[:n], self.lens, out, None, 0.0,
+                                 self.ws)
+        except BaseException:
+            self.lens[:n] -= 1
+            raise
+        self.lengths = grown
+        for owned, ids in zip(self.owned, pages):
+            owned += ids
+        self._take(pages)
         return out
 
     def release(self):
