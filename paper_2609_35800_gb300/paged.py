@@ -29,16 +29,6 @@ class PagedRunner:
         hg_workspace_clear(self.ws)
         hg_workspace_clear(self.prompt_ws)
 
-    def _grow(self, request, tokens):
-        need = -(-tokens // self.page_size)
-        if need > self.per_request or need - len(self.owned[request]) > len(self.free):
-            raise RuntimeError("no page left for request %d" % request)
-        while len(self.owned[request]) < need:
-            page = self.free.pop()
-            self.table[request, len(self.owned[request])] = page
-            self.owned[request].append(page)
-        self.lengths[request] = tokens
-
     def _pages_for(self, owned, tokens):
         """The free pages that requests which own these would get next, up to these tokens each; nothing is changed."""
         need = [-(-n // self.page_size) - len(have) for n, have in zip(tokens, owned)]
@@ -58,27 +48,32 @@ class PagedRunner:
     def admit(self, q, k, v, prompt_lengths, positions, k_out=None, v_out=None):
         """Prompts one after the other, q / k / v [tokens][heads][128] not yet rotated: their attention
         [tokens][q_heads][128].  k_out / v_out: where the rotated keys and the values go as dense tensors as well (a
-        request that goes on in the packed cache takes hg_quantize_kv's layout from there)."""
-        first = len(self.owned)
-        if first + len(prompt_lengths) > self.table.shape[0]:
-            raise RuntimeError("more requests than the batch holds")
-        slots = []
-        for i, n in enumerate(prompt_lengths):
-            self.owned.append([])
-            self.lengths.append(0)
-            self._grow(first + i, n)
-            at = torch.arange(n)
-            pages = torch.tensor(self.owned[first + i], dtype=torch.int64)
-            slots.append(pages[at // self.page_size] * self.page_size + at % self.page_size)
-        slots = torch.cat(slots).to(torch.int32).to(self.device)
-        self.lens[first:first + len(prompt_lengths)] = torch.tensor(prompt_lengths, dtype=torch.int32)
+        request that goes on in the packed cache takes hg_quantize_kv's layout from there).  Prompts that are refused (no
+        page or place left, arguments that do not fit) are not admitted, none of the call's, and the others stay."""
+        lens, first = list(prompt_lengths), len(self.owned)
+        if first + len(lens) > self.table.shape[0]:
+            raise RuntimeError("PagedRunner: more requests than the batch holds")
+        if any(n < 0 for n in lens) or any(x.shape[0] != sum(lens) for x in (q, k, v)):
+            raise ValueError("PagedRunner.admit: q, k and v hold %d, %d and %d rows, the prompts %d"
+                             % (q.shape[0], k.shape[0], v.shape[0], sum(lens)))
+        pages = self._pages_for([[]] * len(lens), lens)
+        slots = [torch.empty(0, dtype=torch.int32)]
+        for i, (n, ids) in enumerate(zip(lens, pages)):
+            at, ids = torch.arange(n, dtype=torch.int32), torch.tensor(ids, dtype=torch.int32)
+            slots.append(ids[at // self.page_size] * self.page_size + at % self.page_size)
+            self.table[first + i, :len(ids)] = ids
+        slots = torch.cat(slots).to(self.device)
         q_rot = torch.empty(q.shape, dtype=self.dtype, device=self.device)
         if k_out is None:
             k_out = torch.empty(k.shape, dtype=self.dtype, device=self.device)
         hg_pages_append(self.pages, q, k, v, self.rotation, positions, slots, q_rot, k_out, v_out)
-        begin = torch.tensor([0] + list(prompt_lengths)).cumsum(0).to(torch.int32)
+        begin = torch.tensor([0] + lens).cumsum(0).to(torch.int32)
         out = torch.empty_like(q_rot)
         hg_prompt_attention(q_rot, k_out, v, begin, begin, out, None, True, 0.0, self.prompt_ws)
+        self.lens[first:first + len(lens)] = torch.tensor(lens, dtype=torch.int32)
+        self.owned += pages
+        self.lengths += lens
+        self._take(pages)
         return out
 
     def step(self, q, k, v, positions):

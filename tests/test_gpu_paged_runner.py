@@ -39,7 +39,7 @@ class Requests:
 
     def admit(self, lens):
         q, k, v = self.rows(sum(lens))
-        pos = torch.cat([torch.arange(n) for n in lens]).to(torch.int32).cuda()
+        pos = torch.cat([torch.arange(0)] + [torch.arange(n) for n in lens]).to(torch.int32).cuda()
         out = self.run.admit(q, k, v, lens, pos)
         q, k = self.rotated(q, pos), self.rotated(k, pos)
         at = 0
@@ -112,3 +112,39 @@ def test_a_step_past_the_table_changes_nothing():
     with pytest.raises(RuntimeError):
         r.run.step(*r.rows(2), torch.tensor([32, 10], dtype=torch.int32, device="cuda"))
     assert r.state() == before
+
+
+def test_refused_prompts_are_not_admitted():
+    """Without pages in the middle of the call, without a place in the batch, past the table, with arguments that do not
+    fit: no request of the call is there, no page is gone, and the others go on."""
+    r = Requests(4, 12, max_batch=4, max_tokens=100)
+    r.admit([40, 5])
+    r.step()
+    before = r.state()
+    positions = lambda lens: torch.cat([torch.arange(n) for n in lens]).to(torch.int32).cuda()  # noqa: E731
+    for lens in ([60, 90], [10, 10, 10], [113], [20, -1]):
+        with pytest.raises((RuntimeError, ValueError)):
+            r.run.admit(*r.rows(max(0, sum(lens))), lens, positions([max(0, n) for n in lens]))
+        assert r.state() == before
+    q, k, v = r.rows(30)
+    for args in ((q, k, v, [20, 11], positions([20, 11])), (q, k, v, [20, 9], positions([20, 9])),
+                 (q[:-1], k, v, [20, 10], positions([20, 10])), (q, k, v, [20, 10], positions([20, 9])),
+                 (q, k, v.half(), [20, 10], positions([20, 10])), (q, k, v, [20, 10], positions([20, 10]).cpu()),
+                 (q, k.cpu(), v, [20, 10], positions([20, 10])), (q, k, v, [20, 10], positions([20, 10]), k[:, :1]),
+                 # what only the attention refuses, after the append: heads whose values are the same memory
+                 (q, k, v[:, :1].expand(30, HEADS, D), [20, 10], positions([20, 10]))):
+        with pytest.raises((ValueError, hg.HGError)):
+            r.run.admit(*args)
+        assert r.state() == before
+    r.step()
+    r.admit([33, 70])
+    r.step()
+
+
+def test_no_prompt_and_empty_prompts():
+    r = Requests(5, 8)
+    r.admit([])
+    r.admit([0, 17, 0])
+    for _ in range(2):
+        r.step()
+    assert r.run.lengths == [2, 19, 2]
