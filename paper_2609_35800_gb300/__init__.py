@@ -448,7 +448,7 @@ class Pages:
 class Rotation:
     """Position rotation of queries and keys: `table` float32 [positions][rot_dim] on the GPU, cosines of the
     rot_dim / 2 pairs, then sines; `sections`: the pairs that turn by each of a token's three positions (None: one
-    position a token).  See hg_rotation."""
+    position a token).  A call's positions are then [3][tokens], else [tokens].  See hg_rotation."""
 
     def __init__(self, table, interleaved=False, sections=None):
         import torch
@@ -506,7 +506,11 @@ def _lse(where, x, tokens, heads):
 def _rotated_by(where, rotation, positions, tokens):
     if rotation is None:
         return None, None
-    return rotation.pointer, _ints(where, "positions", positions, rotation.positions * tokens)
+    parts = rotation.positions
+    if parts > 1 and positions.shape != (parts, tokens) and positions.shape != (parts * tokens,):
+        # (their distance is the call's tokens: a longer row would be read from the wrong places)
+        raise ValueError("%s: positions are %s, the call takes [%d][%d]" % (where, list(positions.shape), parts, tokens))
+    return rotation.pointer, _ints(where, "positions", positions, parts * tokens)
 
 
 def hg_pages_create(k_pages, v_pages):

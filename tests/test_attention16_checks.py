@@ -244,3 +244,21 @@ def test_binding_decode_and_prompt(pool):
     _raises(lambda: hg.hg_prompt_attention(q, k, k, i, i, q, None, True, 0.0, i), "CUDA tensor")
     _raises(lambda: hg._workspace("f", i), "workspace must be a CUDA tensor")
     _raises(lambda: hg._workspace("f", None), "workspace must be a tensor")
+
+
+class _Turn:
+    """Stands for a Rotation of three positions a token; the checks come before its table is read."""
+    pointer, positions = 0, 3
+
+
+@pytest.mark.parametrize("shape", [(3, 64), (64, 3), (3, 4), (5, 3), (192,), (4, 5), (1, 15), (15, 1)])
+def test_three_positions_have_the_calls_own_layout(shape):
+    """Positions are read as [3][tokens]: a buffer of more tokens, or one of tokens first, holds enough entries, elsewhere."""
+    positions = torch.zeros(shape, dtype=torch.int32)
+    _raises(lambda: hg._rotated_by("f", _Turn, positions, 5), "f: positions are %s, the call takes [3][5]" % list(shape))
+
+
+@pytest.mark.parametrize("shape", [(3, 5), (15,)])
+def test_three_positions_as_the_call_takes_them(shape):
+    _raises(lambda: hg._rotated_by("f", _Turn, torch.zeros(shape, dtype=torch.int32), 5), "must be a CUDA tensor")
+    _raises(lambda: hg._rotated_by("f", _Turn, torch.zeros(shape), 5), "contiguous int32")
