@@ -457,7 +457,7 @@ class Rotation:
         if not table.is_cuda:
             raise ValueError("Rotation: table must be a CUDA tensor")
         self.table = table
-        self.positions = 3 if sections is not None else 1
+        self.positions = 3 if sections is not None and any(sections) else 1  # (all 0: one, as in hg_rotation)
         self.raw = _Rotation(table.data_ptr(), table.shape[0], table.shape[1], int(interleaved),
                              (ctypes.c_int32 * 3)(*(sections or (0, 0, 0))))
         self.pointer = ctypes.addressof(self.raw)

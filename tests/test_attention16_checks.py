@@ -262,3 +262,19 @@ def test_three_positions_have_the_calls_own_layout(shape):
 def test_three_positions_as_the_call_takes_them(shape):
     _raises(lambda: hg._rotated_by("f", _Turn, torch.zeros(shape, dtype=torch.int32), 5), "must be a CUDA tensor")
     _raises(lambda: hg._rotated_by("f", _Turn, torch.zeros(shape), 5), "contiguous int32")
+
+
+class _Table:
+    """A table on no GPU in particular: the rotation keeps its address."""
+    dtype, is_cuda, shape = torch.float32, True, (10, 128)
+    dim = staticmethod(lambda: 2)
+    is_contiguous = staticmethod(lambda: True)
+    data_ptr = staticmethod(lambda: A)
+
+
+@pytest.mark.parametrize("sections,positions", [(None, 1), ((0, 0, 0), 1), ((16, 24, 24), 3), ((0, 0, 64), 3)])
+def test_positions_of_a_rotation(sections, positions):
+    """Sections that are all 0 are one position a token, in the library and in the binding."""
+    rotation = hg.Rotation(_Table, sections=sections)
+    assert rotation.positions == positions
+    assert tuple(rotation.raw.sections) == (sections or (0, 0, 0))
