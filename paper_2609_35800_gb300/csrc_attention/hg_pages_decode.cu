@@ -232,7 +232,7 @@ __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int tiles, con
         id = token < c.len ? ids[token >> p.pool.page_shift] : -1;
       }
       const int s = n % kStages;
-      if (n >= kStages && !wait_to_fill(empty + 8 * s, (n / kStages - 1) & 1, abort, p.status)) return n;
+      if (n >= kStages && !wait_warp(empty + 8 * s, (n / kStages - 1) & 1, abort, p.status)) return n;
       if (elect_one()) mbar_arrive_expect_tx(full + 8 * s, 2 * valid * box_bytes);
       for (int i = 0; i < valid; ++i) {
         const int page = __shfl_sync(kAll, id, box0 - first + i);
@@ -703,7 +703,8 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
         if (seen <= kTile) fence_proxy_async_shared();  // TMA writes the stage again
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(empty + 8 * s);
+      // (not after a wait that ran out: the stage would be filled over a copy whose bytes are still expected)
+      if (alive && lane == 0) mbar_arrive(empty + 8 * s);
     }
     const Cursor done = c;
     if (tiles > 0) {  // the next item's queries come in meanwhile

@@ -6,7 +6,7 @@ using namespace hg;
 namespace {
 
 // Warp 1 fills a place whose copy never comes (the bytes are expected, no copy is issued) and waits to fill it again;
-// warp 0 waits for the copy, gives up, and hands the place on all the same, as the decode's consumers do.  Warps 2 and 3
+// warp 0 waits for the copy, gives up, and hands the place on all the same, as a warp does that goes on.  Warps 2 and 3
 // wait for something else that does not come either.  result: what each warp's wait said, then the abort flag.
 __global__ void ring_kernel(uint32_t* status, int* result) {
   __shared__ __align__(8) uint64_t bars[4];
