@@ -480,8 +480,10 @@ hg_status hg_pages_decode_attention(const hg_pages *pages, int32_t batch, int32_
  * 1 of request b, and attends over the lengths[b] tokens, the new one included
  * (rounded to the cache's type as it is stored).  io: q, k, v, out; none of q, k,
  * v is changed.  A request of length 0 stores nothing; one whose last page is
- * outside the pool neither, and attends to its new token all the same.  The other
- * arguments as for hg_pages_decode_attention. */
+ * outside the pool neither, and attends to its new token all the same.  One whose
+ * length is beyond table_stride * page_size has no place for its new token: it
+ * stores nothing and attends over the cached tokens of its whole table.  The
+ * other arguments as for hg_pages_decode_attention. */
 hg_status hg_pages_decode_step(const hg_pages *pages, int32_t batch, int32_t num_q_heads,
                                const hg_attention_io *io, const hg_rotation *rotation, const int32_t *positions,
                                const int32_t *page_table, int32_t table_stride, const int32_t *lengths, float *lse,

@@ -320,7 +320,8 @@ __device__ __forceinline__ uint32_t tile_chunk(uint32_t tile, int rows, int r, i
   return tile + box * kHeadDim * 2 + (chunk / 8) * rows * 128 + swizzled(r - box, chunk % 8);
 }
 
-// The new token of a decode step: into its page, and over row r of the stage's tile (which may hold what was there).
+// The new token of a decode step: into its page, and over row r of the stage's tile (which may hold what was there).  Not
+// where the request has grown past its table: its new token has no place there, and the last row is a token's own.
 template <bool F16>
 __device__ __forceinline__ void place_new_token(const PagesDecodeParams& p, const Cursor& c, uint32_t kt, uint32_t vt, int rows,
                                                 int r) {
@@ -331,16 +332,18 @@ __device__ __forceinline__ void place_new_token(const PagesDecodeParams& p, cons
     const Rows& in = is_v ? p.v : p.k;
     const LaneChannels at = lane_channels(p.rot, i, p.rot.table != nullptr && !is_v);
     const uint16_t* src = in.data + c.b * in.token_stride + c.h * in.head_stride;
+    const int given = p.lengths[c.b], last = c.len - 1;
     uint4 lo = ldg16(src + at.lo), hi = ldg16(src + at.hi);
     if (at.turns) rotate_lane<F16>(lo, hi, lane_angles(p.rot, i, c.b), p.rot.interleaved != 0);
-    st_shared16(tile_chunk(is_v ? vt : kt, rows, r, at.lo / 8), lo);
-    st_shared16(tile_chunk(is_v ? vt : kt, rows, r, at.hi / 8), hi);
-    const int last = c.len - 1;
-    const int page = p.table[(int64_t)c.b * p.table_stride + (last >> p.pool.page_shift)];
-    if (page >= 0 && page < p.pool.num_pages) {
-      uint16_t* dst = (is_v ? p.pool.v : p.pool.k) + page_row(p.pool, page, last & (p.pool.page_size - 1), c.h);
-      *reinterpret_cast<uint4*>(dst + at.lo) = lo;
-      *reinterpret_cast<uint4*>(dst + at.hi) = hi;
+    if (given == c.len) {
+      st_shared16(tile_chunk(is_v ? vt : kt, rows, r, at.lo / 8), lo);
+      st_shared16(tile_chunk(is_v ? vt : kt, rows, r, at.hi / 8), hi);
+      const int page = p.table[(int64_t)c.b * p.table_stride + (last >> p.pool.page_shift)];
+      if (page >= 0 && page < p.pool.num_pages) {
+        uint16_t* dst = (is_v ? p.pool.v : p.pool.k) + page_row(p.pool, page, last & (p.pool.page_size - 1), c.h);
+        *reinterpret_cast<uint4*>(dst + at.lo) = lo;
+        *reinterpret_cast<uint4*>(dst + at.hi) = hi;
+      }
     }
   }
   __syncwarp();

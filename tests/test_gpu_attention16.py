@@ -681,3 +681,32 @@ def test_a_prompt_goes_on_in_the_packed_cache():
         span = want[:, 0, 24:88].float()  # 4-bit codes: at most half a step off, and the rounding to BF16
         step = (span.amax(-1, keepdim=True) - span.amin(-1, keepdim=True)) / 15
         assert bool(((got[:, 0, 24:88].float() - span).abs() <= step * 0.501 + span.abs() * 2.0 ** -8).all())
+
+
+@TYPES
+@pytest.mark.parametrize("heads,group,size,rotated", [(2, 4, 16, True), (1, 12, 64, False), (3, 1, 32, True)])
+def test_step_of_requests_longer_than_their_table(dtype, heads, group, size, rotated):
+    """No place for the new token: nothing is stored, and the table's last token stays what it was."""
+    g = _gen(50 + heads)
+    hq, per = heads * group, 5
+    cap = per * size
+    given = [cap, cap + 1, cap + 2, 2 ** 31 - 1, cap - 1, 0, -5]
+    n, kept = len(given), [cap, cap, cap, cap, cap - 1, 0, 0]
+    tab, pages = _tables(g, [cap] * n, size)
+    kp, vp = _pool(g, pages, heads, size, dtype, False)
+    pool = hg.hg_pages_create(kp, vp)
+    q, k, v = (_randn(g, n, h, D, dtype=dtype) for h in (hq, heads, heads))
+    rot = hg.Rotation(table(64, D, "cuda")) if rotated else None
+    pos = torch.randint(0, 64, (n,), generator=g, device="cuda", dtype=torch.int32)
+    kq, vq, q_rot = kp.clone(), vp.clone(), torch.empty_like(q)
+    slots = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    for b in (0, 4):  # the two that have a place
+        slots[b] = tab[b, (given[b] - 1) // size] * size + (given[b] - 1) % size
+    hg.hg_pages_append(hg.hg_pages_create(kq, vq), q, k, v, rot, pos, slots, q_rot)
+    ws = _workspace(hg.hg_pages_decode_workspace_size(pool, n, hq))
+    out, lse = torch.full((n, hq, D), NAN, dtype=dtype, device="cuda"), torch.full((n, hq), NAN, device="cuda")
+    lens = torch.tensor(given, dtype=torch.int32, device="cuda")
+    hg.hg_pages_decode_step(pool, q, k, v, rot, pos, tab, lens, out, lse, 0.0, ws)
+    assert hg.hg_workspace_status(ws) == 0
+    assert torch.equal(_bits(kp), _bits(kq)) and torch.equal(_bits(vp), _bits(vq))
+    _check_decode(q_rot, kp, vp, tab, kept, size, out, lse)
