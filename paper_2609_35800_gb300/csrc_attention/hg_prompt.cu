@@ -53,8 +53,7 @@ constexpr int kBarOffset = kOutOffset + 2 * kHalfBytes;
 constexpr int kSmemBytes = kBarOffset + 512 + 1024;
 enum Bar { kQueryFull = 0, kQueryFree, kScoreFull, kProbFull = kScoreFull + 2, kOutFull = kProbFull + 2,
            kStageFull = kOutFull + 2, kStageFree = kStageFull + 2, kItemFull = kStageFree + 2, kItemFree = kItemFull + 2,
-           kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages, kProductsEnded = kRingFree + kStages,
-           kBars = kProductsEnded + 1 };
+           kRingFull = kItemFree + 2, kRingFree = kRingFull + kStages, kBars = kRingFree + kStages };
 constexpr int kItemOffset = kBarOffset + 256;  // two Items
 constexpr int kMiscOffset = kItemOffset + 2 * 64;  // abort flag, tensor memory address, copies asked for
 static_assert(kBars * 8 <= 256, "barriers");
@@ -177,9 +176,9 @@ __device__ void load_items(const PromptParams& p, Item it, bool some, uint32_t b
   }
 }
 
-// One warp, of which one thread issues every product.
+// One warp, of which one thread issues every product.  Returns how many of the ring's blocks they have used.
 template <bool F16>
-__device__ void issue_products(const PromptParams& p, uint32_t base, uint32_t tmem, volatile int* misc) {
+__device__ uint32_t issue_products(const PromptParams& p, uint32_t base, uint32_t tmem, volatile int* misc) {
   const int lane = threadIdx.x % 32;
   const uint32_t bars = base + kBarOffset;
   const uint32_t q_operand = smem_operand(base + kQueryOffset, 16), k_operand = smem_operand(base + kRingOffset, 16);
@@ -187,14 +186,14 @@ __device__ void issue_products(const PromptParams& p, uint32_t base, uint32_t tm
   uint32_t fill = 0, queries = 0, probs[2] = {0, 0};
   for (uint32_t n = 0;; ++n) {
     const uint32_t slot = n & 1;
-    if (!wait_warp(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc, p.status)) return;
+    if (!wait_warp(bars + 8 * (kItemFull + slot), (n >> 1) & 1, misc, p.status)) return fill;
     Item it;
     read_item(it, base + kItemOffset + slot * 64);
     const int none = it.none, first = it.first, k_len = it.k_len;
     const int count[2] = {it.n[0], it.n[1]}, width[2] = {it.width[0], it.width[1]};
     __syncwarp();
     if (lane == 0) mbar_arrive(bars + 8 * (kItemFree + slot));
-    if (none) return;
+    if (none) return fill;
     const int blocks = max(count[0], count[1]);
     if (blocks == 0) continue;
     wait_data(bars + 8 * kQueryFull, queries & 1, misc, p.status);
@@ -516,7 +515,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       mbar_init(bars + 8 * (kRingFull + i), 1);
       mbar_init(bars + 8 * (kRingFree + i), 1);
     }
-    mbar_init(bars + 8 * kProductsEnded, 1);
     mbar_init_fence();
     misc[0] = misc[2] = 0;
   }
@@ -544,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       fence_proxy_async_global();  // inputs written by ordinary stores of earlier launches
       load_items(p, mine, some, base, smem, misc, fills, queries);
     } else if (warp == kMmaWarp) {
-      issue_products<F16>(p, base, tmem, misc);
+      fills = issue_products<F16>(p, base, tmem, misc);
     }
   } else {
     set_registers_up<kRowRegisters>();
@@ -558,7 +556,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       drain_phase(bars + 8 * (kRingFull + n % kStages), (n / kStages) & 1);
     if (queries > 0) drain_phase(bars + 8 * kQueryFull, (queries - 1) & 1);
   }
-  if (misc[0] && warp == kMmaWarp) drain_products(bars + 8 * kProductsEnded);  // and its products have ended
+  if (misc[0] && warp == kMmaWarp && fills > 0)  // and its products have ended: the last commit gave a place back
+    drain_phase(bars + 8 * (kRingFree + (fills - 1) % kStages), ((fills - 1) / kStages) & 1);
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();
@@ -615,7 +614,8 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant_
     }
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      if (m[i] == -INFINITY) continue;  // the piece has no key that this row sees, or is none
+      // the piece has no key that this row sees, or is none (one whose scores are all NaN has no maximum either, and counts)
+      if (m[i] == -INFINITY) continue;
       float e = 1.f;
       if (m[i] > M) {
         const float keep = exp2_approx((M - m[i]) + (r - mr[i]));

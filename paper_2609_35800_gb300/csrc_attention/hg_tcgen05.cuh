@@ -22,14 +22,6 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
 }
 
-// For a CTA that gave up, by the whole warp that issued its products (from the lane that elect_one names): until they have
-// ended, or a drain's limit has passed.  `bar`: an mbarrier of one arrival that nothing else uses.
-__device__ __forceinline__ void drain_products(uint32_t bar) {
-  if (elect_one()) tc_commit(bar);
-  __syncwarp();
-  drain_phase(bar, 0);
-}
-
 // Shared-memory operands under the 128-byte swizzle.  The descriptor's low word holds the address and the byte stride of
 // the outer axis along M or N (of B with N contiguous: from 64 channels to the next 64), the high one that of 8 rows to
 // the next 8, 1024 bytes in every operand here, and the swizzle.  Addresses advance by adding to the low word.

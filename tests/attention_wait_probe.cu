@@ -101,7 +101,9 @@ __global__ void products_kernel(uint32_t* status, int* result, int steps) {
       for (int i = 0; i < steps; ++i) tc_mma_ss(tmem, a, b, shape, i > 0);
     }
     __syncwarp();
-    drain_products(ended);
+    if (elect_one()) tc_commit(ended);
+    __syncwarp();
+    drain_phase(ended, 0);
     if (threadIdx.x == 0) {
       result[0] = there;
       result[1] = mbar_try_wait(ended, 0);
