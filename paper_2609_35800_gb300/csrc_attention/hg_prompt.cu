@@ -417,7 +417,7 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, uint32
     float* part = p.parts + (int64_t)it.slot * kPromptPartFloats;
     const int part_row = t * kTileRows + row;
     if (!whole && valid) {
-      part[part_row] = st.M;
+      part[part_row] = isnan(st.l) ? 0.f : st.M;  // (a piece whose scores are all NaN has no maximum, and counts)
       part[256 + part_row] = st.r;
       part[512 + part_row] = st.l;
     }

@@ -710,3 +710,24 @@ def test_step_of_requests_longer_than_their_table(dtype, heads, group, size, rot
     assert hg.hg_workspace_status(ws) == 0
     assert torch.equal(_bits(kp), _bits(kq)) and torch.equal(_bits(vp), _bits(vq))
     _check_decode(q_rot, kp, vp, tab, kept, size, out, lse)
+
+
+@TYPES
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompt_keys_that_are_nan_over_whole_pieces(dtype, causal):
+    """Few rows over long keys are joined from pieces: one whose scores are all NaN makes its rows NaN like any other."""
+    g = _gen(60)
+    nq, nk, heads, group = 40, 9000, 4, 7
+    q, k, v, qb, kb = _prompt(g, [nq, 30], [nk, 30], heads, group, dtype, "tokens")
+    k[1000:3100, 1] = NAN
+    q[7, 3] = NAN
+    out, lse = _run_prompt(q, k, v, qb, kb, causal)
+    sick = torch.zeros(nq + 30, heads * group, dtype=torch.bool, device="cuda")
+    sick[:nq, group:2 * group] = True
+    sick[7, 3] = True
+    assert bool(out[sick].isnan().all()) and bool(lse[sick].isnan().all())
+    assert bool(out[~sick].isfinite().all()) and bool(lse[~sick].isfinite().all())
+    whole = [h for h in range(heads * group) if h // group != 1 and h != 3]
+    for h in whole[::5]:
+        kv = h // group
+        _check_prompt(q[:, h:h + 1], k[:, kv:kv + 1], v[:, kv:kv + 1], qb, kb, causal, out[:, h:h + 1], lse[:, h:h + 1])
