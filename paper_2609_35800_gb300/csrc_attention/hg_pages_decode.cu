@@ -26,7 +26,7 @@
 //   S^T[token][query] = K . q        A = keys (ldmatrix), B = the queries, padded to 8 or 16
 //   O^T[channel][query] += V^T . P^T A = values (ldmatrix.trans), B = P^T (movmatrix of the scores' fragment)
 // Scores, maxima, sums and outputs are held in 32 bits; probabilities are rounded to the cache's type for the second
-// product only.  The running maximum moves when a score passes it by more than 2^8, so probabilities stay below 256.
+// product only, lifted in FP16 (kLift).  The running maximum moves when a score passes it by more than 2^8.
 #include "hg_rows.cuh"
 #include "hg_wait.cuh"
 
@@ -43,7 +43,6 @@ static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
 constexpr int kQRowBytes = 272;  // a staged query row: 256 bytes, 16 more so that ldmatrix meets every bank once
 constexpr int kGroups = kConsumers * 4;  // of eight threads
 constexpr unsigned kAll = 0xffffffffu;
-constexpr float kRescale = 8.0f;  // log2 of how far a score may pass the running maximum
 
 constexpr int kItemCost = kDecodeItemCost;
 constexpr int kJoinCost = 24;  // a ticket and a join, in tiles
@@ -424,7 +423,7 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, const uint32_t (&qf)[
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float m = st.m[nt][i % 2];
-        s[mt][nt][i] = exp2_approx((s[mt][nt][i] - (m == -INFINITY ? 0.f : m)) * c);
+        s[mt][nt][i] = exp2_approx(fmaf(s[mt][nt][i] - (m == -INFINITY ? 0.f : m), c, kLift<F16>));
         st.l[nt][i % 2] += s[mt][nt][i];
       }
       pf[mt][nt][0] = movtrans(pack2<F16>(s[mt][nt][0], s[mt][nt][1]));
@@ -486,7 +485,7 @@ __device__ __forceinline__ void store_part(const Part& a, float* channels, float
   if (channel == 0) *reinterpret_cast<float2*>(ml) = make_float2(a.m, a.l);
 }
 
-// out = o / l in the cache's type, and the query's log-sum-exp.
+// out = o / l in the cache's type, and the query's log-sum-exp (o and l are lifted alike).
 template <bool F16>
 __device__ __forceinline__ void write_query(const PagesDecodeParams& p, int b, int h, int len, int q, int channel,
                                             const Part& a) {
@@ -499,7 +498,7 @@ __device__ __forceinline__ void write_query(const PagesDecodeParams& p, int b, i
   *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
   *reinterpret_cast<uint4*>(out + 8) = make_uint4(x[4], x[5], x[6], x[7]);
   if (p.lse && channel == 0)
-    p.lse[(int64_t)b * p.pool.heads * p.group + head] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l);
+    p.lse[(int64_t)b * p.pool.heads * p.group + head] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l * (F16 ? 0x1p-7f : 1.f));
 }
 
 // Takes a number; what the CTA's threads wrote before their last barrier is visible to whoever takes a later one.

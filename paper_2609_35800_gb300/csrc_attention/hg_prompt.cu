@@ -18,8 +18,8 @@
 // a warpgroup of their own (1,387), items taken by a warp of its own (1,508 of 1,547: every waiting warp takes something),
 // three or five stages of the ring (1,514 and 1,497 of 1,541 and 1,562).
 //
-// Scores, maxima, sums and O are held in 32 bits; P is rounded to the inputs' type for the second product.  The running
-// maximum moves when a score passes it by more than 2^8, which bounds P by 256 and makes changes of O rare.
+// Scores, maxima, sums and O are held in 32 bits; P is rounded to the inputs' type for the second product, lifted in FP16
+// (kLift).  The running maximum moves when a score passes it by more than 2^8, which bounds P and makes changes of O rare.
 // Where the items are fewer than the SMs can share (few rows over long keys), an item's keys are cut into pieces whose
 // (m, l, O) go to the workspace, and a second kernel joins them (64 tokens after 16,000: 25 us;
 // uncut, 126 blocks would follow one another).
@@ -41,7 +41,6 @@ constexpr int kThreads = 384;  // the last two warps have nothing to do: registe
 constexpr int kRowRegisters = 208, kOtherRegisters = 88;
 static_assert(256 * kRowRegisters + 128 * kOtherRegisters <= kThreads * 168, "what the launch has");
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
-constexpr float kRescale = 8.0f;
 constexpr uint32_t kScoreColumn = 0, kOutColumn = 256;  // + 128 for tile 1
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -268,14 +267,15 @@ __device__ uint32_t issue_products(const PromptParams& p, uint32_t base, uint32_
   }
 }
 
-// A row's softmax so far.  Its probabilities are 2^(s c - (M + r)), c = scale log2(e): M is the maximum times c, rounded;
-// r, what the rounding took, where M is so large that it shows, else 0.
+// A row's softmax so far.  Its probabilities are 2^(s c - (M + r)), c = scale log2(e): M is the maximum times c less the
+// lift, rounded; r, what the rounding took, where M is so large that it shows, else 0.
 struct RowSum {
   float M, r, l;
 };
 
+template <bool F16>
 __device__ __forceinline__ float residual(float top, float c, float M) {
-  return fabsf(M) >= 1048576.f && fabsf(M) < INFINITY ? fmaf(top, c, -M) : 0.f;
+  return fabsf(M) >= 1048576.f && fabsf(M) < INFINITY ? fmaf(top, c, -M) - kLift<F16> : 0.f;
 }
 
 __device__ __forceinline__ void st_global32(void* to, const uint32_t (&x)[8]) {
@@ -364,13 +364,13 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, uint32
         top[i] = fmaxf(top[i], __uint_as_float(w[i][31]));
       }
       const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      const float M = best * c;
+      const float M = fmaf(best, c, -kLift<F16>);
       // each row by itself (rows of nobody hold what shared memory held, and must not change the others' rounding)
       const bool moves = valid && M - st.M > kRescale;
       if (__any_sync(kAll, moves)) {
         float keep = 1.f;
         if (moves) {
-          const float r = residual(best, c, M);
+          const float r = residual<F16>(best, c, M);
           keep = exp2_approx((st.M - M) + (st.r - r));
           st.M = M;
           st.r = r;

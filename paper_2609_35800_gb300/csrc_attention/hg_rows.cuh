@@ -21,6 +21,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return F16 ? pack_half2(lo, hi) : pack_bf16x2(lo, hi);
 }
 
+// Probabilities are held as 2^kLift e^(s - m) for the second product; a running maximum m may stay 2^kRescale behind, so the
+// largest are 2^(kLift + kRescale).  FP16 ends at 2^-25: lifted by 2^7, below 65,504 still, terms down to 2^-32 of the
+// largest are kept, where many small ones make up a part of a row.  BF16 reaches down to 2^-133 as it is.
+constexpr float kRescale = 8.0f;
+template <bool F16>
+constexpr float kLift = F16 ? 7.0f : 0.0f;
+
 // A row's 128 channels are divided among 8 lanes, 16 channels each, so that a lane holds whole pairs: with `half` =
 // rot_dim / 2, lane c < half / 8 has the pairs [8c, 8c + 8), the others 16 channels that pass.  The lane's channels are
 // [lo, lo + 8) and [hi, hi + 8).

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2609_35800_gb300 as hg
-from attention16 import attend, check, check_turned, table, turned
+from attention16 import ROUNDOFF, attend, check, check_turned, table, turned
 
 pytestmark = pytest.mark.gpu
 D = 128
@@ -731,3 +731,60 @@ def test_prompt_keys_that_are_nan_over_whole_pieces(dtype, causal):
     for h in whole[::5]:
         kv = h // group
         _check_prompt(q[:, h:h + 1], k[:, kv:kv + 1], v[:, kv:kv + 1], qb, kb, causal, out[:, h:h + 1], lse[:, h:h + 1])
+
+
+def _small_terms(keys, heads, at, dtype):
+    """Keys at `at` whose probability is 1, all the others' about 2^-25.4 each; the others' values alone are not 0."""
+    g = _gen(keys)
+    k, v = (torch.zeros(keys, heads, D, dtype=dtype, device="cuda") for _ in range(2))
+    k[:, :, 0] = (torch.rand((keys, heads), generator=g, device="cuda") * 0.6 - 0.3).to(dtype)
+    v[:] = (1000.0 + 10.0 * torch.randn((keys, heads, D), generator=g, device="cuda")).to(dtype)
+    k[at, :, 0], v[at] = 17.59375, 0.0
+    return k, v
+
+
+def _check_small_terms(out, lse, q, k, v, seen, scale):
+    """As `check`, with what FP16 cannot hold of a probability 2^7 times larger: half of 2^-24, times 2^-7."""
+    ref, rlse, mean, big = attend(q, k, v, seen, scale)
+    u, delta = ROUNDOFF[q.dtype], 2.0 ** -17 * big + 2.0 ** -20
+    tol = u * ref.abs() + (u + 2.0 * delta[..., None]) * mean * 1.01 + 2.0 ** -25
+    if q.dtype == F16:
+        tol = tol + 2.0 ** -32 * k.shape[0] * float(v.double().abs().max())
+    assert float(ref.min()) > 8.0 * float(tol.max())  # the terms show: 2^6.6 over the largest keys' number (3 to 8)
+    assert bool(((out.double() - ref).abs() <= tol).all())
+    assert bool(((lse.double() - rlse).abs() <= delta + 2.0 ** -22 * rlse.abs() + 2.0 ** -20).all())
+
+
+@TYPES
+@pytest.mark.parametrize("heads,group", [(8, 4), (8, 12)])
+def test_decode_many_small_terms(dtype, heads, group):
+    """Requests that are not cut: the first tiles of every warp hold the largest score, thousands of keys follow."""
+    size, n, length = 64, 48, 8000
+    tab, pages = _tables(_gen(70), [length] * n, size)
+    kp, vp = (torch.zeros((pages, heads, size, D), dtype=dtype, device="cuda") for _ in range(2))
+    k, v = _small_terms(length, heads, torch.tensor([0, 32, 64]), dtype)
+    for pool, x in ((kp, k), (vp, v)):
+        pool[tab.long()] = x.view(length // size, size, heads, D).transpose(1, 2)
+    q = torch.zeros(n, heads * group, D, dtype=dtype, device="cuda")
+    q[:, :, 0] = 1.0
+    pool = hg.hg_pages_create(kp, vp)
+    ws = _workspace(hg.hg_pages_decode_workspace_size(pool, n, heads * group))
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    lens = torch.full((n,), length, dtype=torch.int32, device="cuda")
+    hg.hg_pages_decode_attention(pool, q, tab, lens, out, lse, 1.0, ws)
+    for b in (0, 17, n - 1):
+        _check_small_terms(out[b:b + 1], lse[b:b + 1], q[b:b + 1], k, v, lens[b:b + 1].long(), 1.0)
+
+
+@TYPES
+@pytest.mark.parametrize("nq,nk,copies", [(300, 60000, 1), (16, 9000, 40)])  # (cut in pieces; and not)
+def test_prompt_many_small_terms(dtype, nq, nk, copies):
+    heads, group = 4, 8
+    k, v = _small_terms(nk, heads, torch.arange(0, nk, 8192), dtype)
+    q = torch.zeros(nq * copies, heads * group, D, dtype=dtype, device="cuda")
+    q[:, :, 0] = 1.0
+    qb, kb = (torch.arange(copies + 1, dtype=torch.int32) * n for n in (nq, nk))
+    out, lse = _run_prompt(q, k.repeat(copies, 1, 1), v.repeat(copies, 1, 1), qb, kb, False, scale=1.0)
+    for i in {0, copies // 2, copies - 1}:
+        rows = slice(i * nq, i * nq + 8)
+        _check_small_terms(out[rows], lse[rows], q[rows], k, v, torch.full((8,), nk, device="cuda"), 1.0)
