@@ -507,7 +507,10 @@ hg_status hg_prompt_workspace_size(size_t *bytes);
  * and values of other prompts are never used, whatever their bits; a prompt's
  * own V rows that are later than a query (masked) must be finite.  num_q_heads at
  * most 16 times num_kv_heads (1..64).  Strides of q, k and v along an axis
- * longer than 1 are at least 128 (HG_ERR_UNSUPPORTED). */
+ * longer than 1 are at least 128 (HG_ERR_UNSUPPORTED).  A call is one launch for
+ * every 256 prompts, and one more each where keys are cut into pieces; every
+ * other error is found before the first, but HG_ERR_CUDA of a later one leaves
+ * those before it enqueued. */
 hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_heads, int32_t num_kv_heads,
                               const hg_attention_io *io, const int32_t *q_begin, const int32_t *k_begin, float *lse,
                               int32_t causal, float softmax_scale, void *workspace, size_t workspace_bytes,

@@ -177,6 +177,16 @@ hg_status plan_prompts(PromptParams* p) {
   return HG_OK;
 }
 
+// The launch of prompts [done, done + kPromptsPerLaunch) of a call: none of them may have a query, then there is none.
+hg_status plan_launch(PromptParams* p, const int32_t* q_begin, const int32_t* k_begin, int num_prompts, int done) {
+  const int end = std::min(num_prompts - done, kPromptsPerLaunch) + done;
+  p->prompts = p->split = 0;
+  for (int i = done; i < end; ++i)
+    if (q_begin[i + 1] > q_begin[i])  // a prompt without a query has nothing to write
+      p->range[p->prompts++] = {q_begin[i], q_begin[i + 1] - q_begin[i], k_begin[i], k_begin[i + 1] - k_begin[i]};
+  return p->prompts == 0 ? HG_OK : plan_prompts(p);
+}
+
 hg_status map_pages(hg_pages* p) {
   if (p->mapped.load(std::memory_order_acquire)) return HG_OK;
   const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
@@ -389,6 +399,10 @@ hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_
   p.status = reinterpret_cast<uint32_t*>(w);
   p.counters = reinterpret_cast<uint32_t*>(w + 256);
   p.parts = reinterpret_cast<float*>(w + kAttnHeaderBytes);
+  for (int done = 0; done < num_prompts; done += kPromptsPerLaunch) {  // what the last launch would refuse is refused here
+    st = plan_launch(&p, q_begin, k_begin, num_prompts, done);
+    if (st != HG_OK) return st;
+  }
   const bool f16 = dtype == HG_DTYPE_F16;
   const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
   if (!encode ||
@@ -404,16 +418,8 @@ hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_
                  encode_rows(encode, &p.out_map, io->out.data, rows, io->out.token_stride, 128 / p.group, num_q_heads,
                              io->out.head_stride, p.group, f16) == CUDA_SUCCESS;
   for (int done = 0; done < num_prompts; done += kPromptsPerLaunch) {
-    const int n = std::min(kPromptsPerLaunch, num_prompts - done);
-    p.prompts = p.split = 0;
-    for (int i = 0; i < n; ++i) {
-      const int j = done + i;
-      if (q_begin[j + 1] > q_begin[j])  // a prompt without a query has nothing to write
-        p.range[p.prompts++] = {q_begin[j], q_begin[j + 1] - q_begin[j], k_begin[j], k_begin[j + 1] - k_begin[j]};
-    }
-    if (p.prompts == 0) continue;
-    st = plan_prompts(&p);
-    if (st == HG_OK) st = of_cuda(launch_prompt(p, f16, reinterpret_cast<cudaStream_t>(stream)));
+    if (num_prompts > kPromptsPerLaunch) st = plan_launch(&p, q_begin, k_begin, num_prompts, done);
+    if (st == HG_OK && p.prompts > 0) st = of_cuda(launch_prompt(p, f16, reinterpret_cast<cudaStream_t>(stream)));
     if (st != HG_OK) return st;
   }
   return HG_OK;

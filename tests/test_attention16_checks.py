@@ -278,3 +278,16 @@ def test_positions_of_a_rotation(sections, positions):
     rotation = hg.Rotation(_Table, sections=sections)
     assert rotation.positions == positions
     assert tuple(rotation.raw.sections) == (sections or (0, 0, 0))
+
+
+@pytest.mark.parametrize("before", [0, 255, 256, 600])
+def test_prompts_are_planned_before_the_first_launch(lib, before):
+    """2^30 tokens of 64 heads are more than one launch numbers: refused as such, whatever comes before them."""
+    need = ctypes.c_size_t()
+    assert lib.hg_prompt_workspace_size(ctypes.byref(need)) == OK
+    q_begin = list(range(before + 1)) + [before + (1 << 30)]
+    k_begin = list(range(before + 2))
+    ints = lambda x: (ctypes.c_int32 * len(x))(*x)  # noqa: E731
+    io = _io(*[_rows(token=64 * 128)] * 4)
+    got = lib.hg_prompt_attention(0, before + 1, 64, 64, io, ints(q_begin), ints(k_begin), None, 1, 0.0, A, need.value, None)
+    assert got == UNSUPPORTED
