@@ -467,9 +467,10 @@ hg_status hg_pages_decode_workspace_size(const hg_pages *pages, int32_t batch, i
  * unused.  lse (or NULL): device float [batch][num_q_heads], the natural
  * logarithm of the sum of exp(score).  A request of length 0 gets out = 0, lse =
  * -inf.  page_table, lengths: device int32, read by the launch; a page outside
- * the pool reads as zeros.  batch * num_kv_heads * (table_stride * page_size / 32
- * + 5) is below 2^31 (HG_ERR_UNSUPPORTED).  Everything is read in stream order, so the call can
- * be captured in a graph and replayed with other lengths. */
+ * the pool reads as zeros.  batch * num_kv_heads * (table_stride * page_size / 32 +
+ * 13) is below 2^31, and table_stride * page_size too (HG_ERR_UNSUPPORTED).
+ * Everything is read in stream order, so the call can be captured in a graph and
+ * replayed with other lengths. */
 hg_status hg_pages_decode_attention(const hg_pages *pages, int32_t batch, int32_t num_q_heads,
                                     const hg_attention_io *io, const int32_t *page_table, int32_t table_stride,
                                     const int32_t *lengths, float *lse, float softmax_scale, void *workspace,

@@ -1,6 +1,8 @@
 """Refusals of the paged and prompt attention entry points, on CPU: the C ABI's (status codes, nothing enqueued) and
 the Python binding's (ValueError before the library is entered)."""
 import ctypes
+import os
+import re
 import struct
 
 import pytest
@@ -291,3 +293,25 @@ def test_prompts_are_planned_before_the_first_launch(lib, before):
     io = _io(*[_rows(token=64 * 128)] * 4)
     got = lib.hg_prompt_attention(0, before + 1, 64, 64, io, ints(q_begin), ints(k_begin), None, 1, 0.0, A, need.value, None)
     assert got == UNSUPPORTED
+
+
+@pytest.mark.parametrize("batch,heads,page_size", [(1 << 10, 4, 16), (1 << 17, 64, 16), (1 << 20, 2, 32)])
+def test_decode_takes_tables_up_to_the_headers_limit(lib, batch, heads, page_size):
+    """Of a table that the header allows only the workspace, which is too small, is refused."""
+    text = open(os.path.join(build.INCLUDE, "headguard.h")).read()
+    more = int(re.search(r"table_stride \* page_size / 32[\s*]*\+[\s*]*(\d+)", text).group(1))
+    h = ctypes.c_void_p()
+    assert lib.hg_pages_create(ctypes.byref(_shape(num_kv_heads=heads, page_size=page_size)), A, A, ctypes.byref(h)) == OK
+    try:
+        tiles = (1 << 31) // (batch * heads) - more  # the first number of tiles that is not allowed
+        for over in (False, True):
+            stride = max(0, (tiles if over else tiles - 1) * 32 // page_size)
+            if over and stride * page_size // 32 < tiles:
+                stride += 1
+            if stride * page_size >= 1 << 31:
+                continue
+            got = lib.hg_pages_decode_attention(h, batch, heads, _io(_rows(), NONE, NONE, _rows()), A, stride, A, None, 0.0, A,
+                                                0, None)
+            assert got == (UNSUPPORTED if over else WS_SMALL)
+    finally:
+        lib.hg_pages_destroy(h)
