@@ -202,10 +202,11 @@ hg_status map_pages(hg_pages* p) {
 }
 
 // Decode workspace: header, the parts that CTAs leave (two each, at the largest group whatever the call's, so that the
-// counters behind them lie at one place for every call), a counter per (request, KV head).
+// counters behind them lie at one place for every call), a counter per (request, KV head): of the most KV heads that a
+// pool may have, so that a workspace serves every pool (256 bytes a request).
 size_t decode_parts_bytes() { return (size_t)decode_ctas() * 2 * kMaxGroup * kPartialFloats * sizeof(float); }
-size_t decode_workspace_bytes(const hg_pages* p, int batch) {
-  const size_t counters = kDecodeJoinCounters + (size_t)batch * p->pool.heads;
+size_t decode_workspace_bytes(int batch) {
+  const size_t counters = kDecodeJoinCounters + (size_t)batch * kMaxKvHeads;
   return kAttnHeaderBytes + decode_parts_bytes() + ((counters * sizeof(uint32_t) + 255) & ~size_t(255));
 }
 
@@ -234,7 +235,7 @@ hg_status pages_decode(const hg_pages* pages, int32_t batch, int32_t num_q_heads
   st = check_rotation(rotation, positions);
   if (st != HG_OK) return st;
   if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(lse) || !aligned16(ws)) return HG_ERR_ALIGNMENT;
-  if (ws_bytes < decode_workspace_bytes(pages, batch)) return HG_ERR_WORKSPACE_TOO_SMALL;
+  if (ws_bytes < decode_workspace_bytes(batch)) return HG_ERR_WORKSPACE_TOO_SMALL;
   st = map_pages(const_cast<hg_pages*>(pages));
   if (st != HG_OK) return st;
   PagesDecodeParams p;
@@ -333,7 +334,7 @@ hg_status hg_pages_decode_workspace_size(const hg_pages* pages, int32_t batch, i
   if (!bytes) return HG_ERR_INVALID_ARG;
   const hg_status st = decode_batch_ok(pages, batch, num_q_heads);
   if (st != HG_OK) return st;
-  *bytes = decode_workspace_bytes(pages, batch);
+  *bytes = decode_workspace_bytes(batch);
   return HG_OK;
 }
 

@@ -788,3 +788,20 @@ def test_prompt_many_small_terms(dtype, nq, nk, copies):
     for i in {0, copies // 2, copies - 1}:
         rows = slice(i * nq, i * nq + 8)
         _check_small_terms(out[rows], lse[rows], q[rows], k, v, torch.full((8,), nk, device="cuda"), 1.0)
+
+
+def test_decode_workspace_of_another_pool():
+    """A workspace made for a pool of one KV head serves a pool of many, at the same batch and below."""
+    g = _gen(80)
+    small = hg.hg_pages_create(*_pool(g, 2, 1, 16, BF16, False))
+    ws = _workspace(hg.hg_pages_decode_workspace_size(small, 37, 1))
+    for heads, group, lens in [(64, 1, [5, 900] * 18 + [3]), (1, 16, [4000] * 37), (32, 2, [20000])]:
+        tab, pages = _tables(g, lens, 32)
+        kp, vp = _pool(g, pages, heads, 32, BF16, False)
+        pool = hg.hg_pages_create(kp, vp)
+        q = _randn(g, len(lens), heads * group, D)
+        for _ in range(2):
+            out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+            hg.hg_pages_decode_attention(pool, q, tab, torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse, 0.0, ws)
+            _check_decode(q[:3], kp, vp, tab[:3], lens[:3], 32, out[:3], lse[:3])
+    assert hg.hg_workspace_status(ws) == 0
