@@ -470,7 +470,11 @@ hg_status hg_pages_decode_workspace_size(const hg_pages *pages, int32_t batch, i
  * the pool reads as zeros.  batch * num_kv_heads * (table_stride * page_size / 32 +
  * 13) is below 2^31, and table_stride * page_size too (HG_ERR_UNSUPPORTED).
  * Everything is read in stream order, so the call can be captured in a graph and
- * replayed with other lengths. */
+ * replayed with other lengths.
+ * Scores, maxima, sums and outputs are binary32 until the output's one rounding;
+ * the probabilities are rounded to the cache's type for their product with the
+ * values (2^-8 of each in BF16, 2^-11 in FP16, where terms below 2^-32 of the
+ * largest are lost to that product).  hg_prompt_attention does the same. */
 hg_status hg_pages_decode_attention(const hg_pages *pages, int32_t batch, int32_t num_q_heads,
                                     const hg_attention_io *io, const int32_t *page_table, int32_t table_stride,
                                     const int32_t *lengths, float *lse, float softmax_scale, void *workspace,

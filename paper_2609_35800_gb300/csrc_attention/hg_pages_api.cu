@@ -144,6 +144,8 @@ int64_t count_items(PromptParams* p) {
 // How the launch's keys are cut.  Uncut, the launch lasts as long as its longest item at least; cut, as long as the
 // SMs' even share of all blocks, and the parts' way through memory and the join besides.  64 tokens after 16,000, 28
 // heads: longest 126 blocks, share 6.6, cut 25 us.  1,460 tokens, 28 heads: longest 12, share 6.7, uncut 26 us, cut 49.
+// Left out is that whole items come in rounds: 20 prompts of 8 tokens after 8,000 of 64 heads are 160 items on 152 SMs and
+// take 179 us, 18 of them (144 items) 96.
 hg_status plan_prompts(PromptParams* p) {
   p->tile_tokens = 128 / p->group;
   std::sort(p->range, p->range + p->prompts,

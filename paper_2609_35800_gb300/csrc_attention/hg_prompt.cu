@@ -2,9 +2,11 @@
 //
 // For a prompt's query row: s_t = scale q.k_t over the keys it sees, m = max s_t, out = sum e^(s_t - m) v_t / sum
 // e^(s_t - m).  4 * 128 flop a (query head, key) pair and little to read: the kernel is bound by the products, and for
-// short prompts by the chain of a tile's blocks.  Measured: 2 x 8,192 causal tokens of 64 heads 1,579 TFLOP/s (an earlier
-// form 1,461, and 1,604 with the softmax left out: a product of 128 x 128 with both operands in shared memory reads all
-// that it can give, 128 bytes a cycle); 1,460 tokens of 28 heads 26 us, 12 blocks of 3,000 cycles one after the other.
+// short prompts by the chain of a tile's blocks.  Measured: 2 x 8,192 causal tokens of 64 heads 1,551-1,565 TFLOP/s in short
+// runs, 1,462 over seconds under the power limit (at 1,950 MHz: 4,930 flop a cycle and SM, of 7,780 that a large matrix
+// product reaches).  An earlier form ran at 1,461, at 1,604 with the softmax left out and at 1,641 without loads either, so
+// most of the rest is in the products as they are issued here; what holds them back is not known (shared memory's pipe is
+// 42% busy with their operands).  1,460 tokens of 28 heads 25.5 us, 12 blocks of 3,000 cycles one after the other.
 //
 // A work item is two tiles of 128 rows of one prompt and KV head.  A tile's rows are 128 / G consecutive tokens times
 // the G query heads of the KV head, so short prompts fill their tiles and a causal tile spans few tokens; both tiles use
@@ -14,9 +16,10 @@
 //   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a thread to a row: S out of tensor memory, P back over it (so a
 //               tile's next S follows its P V), O scaled there when a maximum moves, written out at the end
 // While one tile's softmax runs the tensor cores work on the other tile.  Tensor memory: S 2 x 128 columns, O 2 x 128.
-// What is not here because it was slower: P handed over in halves (1,409 TFLOP/s then, 1,467 without), outputs written by
-// a warpgroup of their own (1,387), items taken by a warp of its own (1,508 of 1,547: every waiting warp takes something),
-// three or five stages of the ring (1,514 and 1,497 of 1,541 and 1,562).
+// What is not here because it was slower at 2 x 8,192 tokens (on short items none of it was measured): P handed over in
+// halves (1,409 TFLOP/s then, 1,467 without), outputs written by a warpgroup of their own (1,387), items taken by a warp of
+// its own (1,508 of 1,547: every waiting warp takes something), three or five stages of the ring (1,514 and 1,497 of 1,541
+// and 1,562).
 //
 // Scores, maxima, sums and O are held in 32 bits; P is rounded to the inputs' type for the second product, lifted in FP16
 // (kLift).  The running maximum moves when a score passes it by more than 2^8, which bounds P and makes changes of O rare.
