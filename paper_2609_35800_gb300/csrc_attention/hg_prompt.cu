@@ -369,11 +369,12 @@ __device__ void softmax_rows(const PromptParams& p, int t, uint32_t base, uint32
       const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
       const float M = fmaf(best, c, -kLift<F16>);
       // each row by itself (rows of nobody hold what shared memory held, and must not change the others' rounding)
-      const bool moves = valid && M - st.M > kRescale;
+      // (by the unrounded maxima: of scores in the millions the rounded ones may be near where these are far apart)
+      const float r = residual<F16>(best, c, M);
+      const bool moves = valid && (M - st.M) + (r - st.r) > kRescale;
       if (__any_sync(kAll, moves)) {
         float keep = 1.f;
         if (moves) {
-          const float r = residual<F16>(best, c, M);
           keep = exp2_approx((st.M - M) + (st.r - r));
           st.M = M;
           st.r = r;

@@ -805,3 +805,34 @@ def test_decode_workspace_of_another_pool():
             hg.hg_pages_decode_attention(pool, q, tab, torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse, 0.0, ws)
             _check_decode(q[:3], kp, vp, tab[:3], lens[:3], 32, out[:3], lse[:3])
     assert hg.hg_workspace_status(ws) == 0
+
+
+@TYPES
+@pytest.mark.parametrize("top", [22, 24, 26, 28, 30])
+def test_prompt_scores_whose_maxima_round_alike(dtype, top):
+    """Scores 2^k apart around 2^`top` in units of the exponent, where binary32 holds their scaled maxima half as finely as
+    the scores themselves: keys far above the maximum so far are found all the same, whatever the maxima round to."""
+    # score = 2^15 * 65024 + 128 j exactly (binary32 holds it); times scale log2(e) just above 2^top
+    heads, group, n = 2, 4, 4
+    base, step = 32768.0 * 65024.0, 128.0
+    keys = 128 * (n + 1)
+    g = _gen(top)
+    for i in range(12):
+        scale = float(torch.tensor(2.0 ** top * (1.001 + 0.0007 * i) / base * math.log(2.0), dtype=torch.float32))
+        j = torch.zeros(keys, dtype=torch.float64, device="cuda")
+        for b in range(1, n + 1):  # each block's first key a few steps above the block before
+            j[128 * b:] += (i + b) % 4
+        q, k = torch.zeros(32, heads * group, D, dtype=dtype, device="cuda"), torch.zeros(keys, heads, D, dtype=dtype, device="cuda")
+        q[:, :, 0], q[:, :, 1], k[:, :, 0], k[:, :, 1] = 32768.0, step, 65024.0, j.to(dtype)[:, None]
+        v = _randn(g, keys, heads, D, dtype=dtype)
+        begin = [torch.tensor([0, x], dtype=torch.int32) for x in (32, keys)]
+        out, lse = _run_prompt(q, k, v, *begin, False, scale=scale)
+        s = (base + step * j) * scale
+        w = torch.softmax(s, 0)
+        ref = torch.einsum("k,khd->hd", w, v.double()).repeat_interleave(group, 0)
+        mean = torch.einsum("k,khd->hd", w, v.double().abs()).repeat_interleave(group, 0)
+        u = ROUNDOFF[dtype]
+        # (a term's exponent is a difference of at most 64 units, 2^-23 of which its factors' roundings move)
+        tol = u * ref.abs() + (u + 2.0 ** -16) * mean * 1.01 + 2.0 ** -25 + 2.0 ** -32 * keys * float(v.abs().max())
+        assert bool(((out.double() - ref).abs() <= tol).all())
+        assert bool(((lse.double() - torch.logsumexp(s, 0)).abs() <= 2.0 ** -21 * float(s.max())).all())
