@@ -521,6 +521,139 @@ hg_status hg_prompt_attention(int32_t dtype, int32_t num_prompts, int32_t num_q_
                               int32_t causal, float softmax_scale, void *workspace, size_t workspace_bytes,
                               hg_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged caches held in 8 bits, and page tables built on the GPU (no counterpart
+ * in the paper): half the bytes of the 16-bit pages, for requests whose cache is
+ * not packed into 2 to 4 bits.  Rows are hg_rows of 16-bit channels, as above.
+ * ------------------------------------------------------------------------ */
+
+/* Tokens that share a scale: blocks of a page, from its first token on. */
+#define HG_PAGES8_BLOCK 16
+
+/* Opaque host-side descriptor of an 8-bit page pool; the pool's memory stays the
+ * caller's.  It never changes after its creation: any number of host threads and
+ * streams may use one. */
+typedef struct hg_pages8 hg_pages8;
+
+/* Descriptor of the pool whose keys start at k_pages and values at v_pages
+ * (device, 16-byte aligned, the same geometry): e4m3 codes, a byte each (sign, 4
+ * exponent bits of bias 7, 3 mantissa bits; 0x7f and 0xff are NaN), in the
+ * geometry of hg_page_shape with strides in bytes, multiples of 16; dtype is the
+ * type of the rows that calls take and give.  k_scales, v_scales: device float
+ * [num_pages][num_kv_heads][page_size / 16], dense, 4-byte aligned; an entry
+ * stands for its code times its block's scale, which is finite and not negative.
+ * Nothing needs initialisation: codes and scales past a request's length are
+ * never used, whatever their bits.  Host only; no CUDA call. */
+hg_status hg_pages8_create(const hg_page_shape *shape, void *k_pages, void *v_pages, float *k_scales,
+                           float *v_scales, hg_pages8 **out);
+void hg_pages8_destroy(hg_pages8 *pages);
+
+/* New tokens into an 8-bit paged cache.  Request r's new tokens are the rows
+ * [begin[r], begin[r + 1]) (device int32 [num_requests + 1], not decreasing,
+ * within [0, num_tokens]) and become its tokens lengths[r] - (begin[r + 1] -
+ * begin[r]) .. lengths[r] - 1 (device int32 [num_requests]: what hg_pages_plan
+ * leaves there), token t in page page_table[r * table_stride + t / page_size] at
+ * t % page_size.  Queries and keys are rotated as by hg_pages_append; the rotated
+ * q goes to q_out, the rotated k and the v in 16 bits to k_out / v_out where
+ * these are given (for hg_prompt_attention).  An output may be its own input.
+ *
+ * A block's scale is a power of two: the least s with |x| <= 448 s for its new
+ * tokens' entries x (binary32 after the rotation), at least 2^-126 -- e4m3 keeps
+ * four significant bits at any scale, so a power of two costs none -- and not
+ * below that of the tokens that the block has already (a scale of another
+ * writer's is first raised to a power of two).  An entry is stored as e4m3(x /
+ * s), rounded to nearest even: off by 2^-4 of its value at most, or 2^-10 s where
+ * it is below 2^-6 s.  Where the scale rises, the block's tokens so far are
+ * stored again as e4m3(code * old / new), exactly except below 2^-6 of the new.
+ * NaN and infinities are stored as NaN and do not count for the scale.
+ *
+ * Rows outside [begin[0], begin[num_requests]) are neither read nor written.  A
+ * token whose page is outside the pool, or whose place is outside the table, is
+ * rotated and not stored.  What lies behind a request's last token stays as it
+ * is.  No two requests may write to the same block. */
+hg_status hg_pages8_append(const hg_pages8 *pages, int32_t num_tokens, int32_t num_requests, int32_t num_q_heads,
+                           const hg_append_io *io, const hg_rotation *rotation, const int32_t *positions,
+                           const int32_t *begin, const int32_t *page_table, int32_t table_stride,
+                           const int32_t *lengths, hg_stream_t stream);
+
+/* Tokens of an 8-bit paged cache as dense 16-bit rows: row begin[r] + t of k_out
+ * and v_out is token t of request r, for every t below begin[r + 1] - begin[r]
+ * (begin as for hg_pages8_append; rows [num_rows][num_kv_heads], one of the two
+ * may be absent), each entry code * scale rounded once and, beyond the type's
+ * range, its largest value.  A page outside the pool, or a place outside the
+ * table, reads as zeros.  Other rows are not written.  So hg_prompt_attention
+ * takes a prompt's next tokens after cached ones. */
+hg_status hg_pages8_dequantize(const hg_pages8 *pages, int32_t num_rows, int32_t num_requests,
+                               const int32_t *begin, const int32_t *page_table, int32_t table_stride,
+                               const hg_rows *k_out, const hg_rows *v_out, hg_stream_t stream);
+
+/* Workspace bytes of hg_pages8_decode_attention and hg_pages8_decode_step: the
+ * same as hg_pages_decode_workspace_size's, and a workspace serves both kinds of
+ * pool. */
+hg_status hg_pages8_decode_workspace_size(const hg_pages8 *pages, int32_t batch, int32_t num_q_heads,
+                                          size_t *bytes);
+
+/* Attention of one new token per request over the 8-bit paged cache: arguments
+ * and limits of hg_pages_decode_attention, keys and values code * scale.  Scores,
+ * maxima, sums and outputs are binary32 until the output's one rounding (beyond
+ * FP16's range: its largest value).  Queries and codes meet as FP16, exactly
+ * (a BF16 query row is first multiplied by a power of two that brings its
+ * largest entry to [2^14, 2^15); entries below 2^-39 of that lose bits).
+ * Probabilities times the value block's scale are rounded to FP16 (2^-11 of
+ * each; terms below 2^-32 of the largest such product are lost). */
+hg_status hg_pages8_decode_attention(const hg_pages8 *pages, int32_t batch, int32_t num_q_heads,
+                                     const hg_attention_io *io, const int32_t *page_table, int32_t table_stride,
+                                     const int32_t *lengths, float *lse, float softmax_scale, void *workspace,
+                                     size_t workspace_bytes, hg_stream_t stream);
+
+/* One decode step on the 8-bit paged cache: as hg_pages_decode_step, the new
+ * token's k and v stored as by hg_pages8_append and attended to as stored.  One
+ * whose page is outside the pool is attended to with a scale of its own. */
+hg_status hg_pages8_decode_step(const hg_pages8 *pages, int32_t batch, int32_t num_q_heads,
+                                const hg_attention_io *io, const hg_rotation *rotation, const int32_t *positions,
+                                const int32_t *page_table, int32_t table_stride, const int32_t *lengths, float *lse,
+                                float softmax_scale, void *workspace, size_t workspace_bytes, hg_stream_t stream);
+
+/* What hg_pages_plan leaves in counts. */
+typedef enum hg_plan_count {
+    HG_PLAN_FREE = 0,     /* free pages afterwards */
+    HG_PLAN_REFUSED = 1,  /* 0: planned; n > 0: n pages are missing; -1: a request outgrows its row of the
+                             table; -2: more new tokens than max_tokens; -3: the free list has no room */
+    HG_PLAN_TOKENS = 2,   /* new tokens placed */
+    HG_PLAN_LONGEST = 3   /* length of the longest request afterwards */
+} hg_plan_count;
+
+/* Page tables and slots of a batch's new tokens, on the GPU, for 16-bit and 8-bit
+ * pools alike.  All arrays are device int32.
+ *   page_table   [batch][table_stride], in and out: request r has ceil(cached[r] /
+ *                page_size) pages; those that its new tokens need are taken from
+ *                the free list and written behind them
+ *   cached       [batch]: tokens that each request has (below 0: taken as 0)
+ *   new_tokens   [batch]: tokens that come; below 0: the request ends, and its
+ *                pages go back to the free list, for this call's other requests first
+ *   free_pages   [free_capacity]: page ids, the first free_count[0] of them free.
+ *                Pages are taken from the list's end, request by request; pages
+ *                given back go behind the free ones, the last one taken first.
+ *                Entries below free_count[0] are not changed.
+ *   lengths      [batch], out: cached + new tokens, 0 for a request that ended; may
+ *                be cached itself
+ *   begin        [batch + 1], out: the new tokens of request r are the rows
+ *                [begin[r], begin[r + 1])
+ *   slots        [max_tokens], out: slot of every new token, as hg_pages_append
+ *                takes it; -1 behind the last
+ *   positions    [max_tokens], out: each new token's number in its request, 0
+ *                behind the last; may be NULL
+ *   counts       [4], out: hg_plan_count; counts[0] may be free_count itself
+ * All requests are planned or none: a call that is refused (counts[1]) changes
+ * neither table nor free list, leaves lengths as cached, and places no token
+ * (begin all 0, slots all -1).  Page ids are not looked at.  batch up to 16,384;
+ * page_size 16, 32, 64, 128 or 256.  Everything is read in stream order, so the
+ * call can be captured in a graph and replayed with other lengths. */
+hg_status hg_pages_plan(int32_t batch, int32_t page_size, int32_t *page_table, int32_t table_stride,
+                        const int32_t *cached, const int32_t *new_tokens, int32_t *free_pages, int32_t free_capacity,
+                        const int32_t *free_count, int32_t max_tokens, int32_t *lengths, int32_t *begin,
+                        int32_t *slots, int32_t *positions, int32_t *counts, hg_stream_t stream);
+
 /* Static description of a status code (no counterpart in the paper). */
 const char *hg_status_string(hg_status status);
 

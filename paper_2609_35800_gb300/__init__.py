@@ -5,7 +5,7 @@ Thin ctypes marshalling over ``libheadguard.so`` (declared in
 converts its arguments (torch tensors -> device pointers, streams -> handles)
 and raises :class:`HGError` on a non-zero status (and ValueError, before the
 call, when a tensor argument is not a dense CUDA tensor holding the bytes the
-call reads or writes through it; the calls of the 16-bit caches also take
+call reads or writes through it; the calls of the paged caches also take
 strided rows of dense channels).  All computation happens in
 the library's CUDA kernels; there is no Python or CPU fallback, and importing
 the compute functions without the built library raises.
@@ -30,6 +30,9 @@ __all__ = [
     "HG_DTYPE_BF16", "HG_DTYPE_F16", "PageShape", "Pages", "Rotation",
     "hg_pages_create", "hg_pages_destroy", "hg_pages_append", "hg_pages_decode_workspace_size",
     "hg_pages_decode_attention", "hg_pages_decode_step", "hg_prompt_workspace_size", "hg_prompt_attention",
+    "HG_PAGES8_BLOCK", "HG_PLAN_FREE", "HG_PLAN_REFUSED", "HG_PLAN_TOKENS", "HG_PLAN_LONGEST", "Pages8",
+    "hg_pages8_create", "hg_pages8_destroy", "hg_pages8_append", "hg_pages8_dequantize",
+    "hg_pages8_decode_workspace_size", "hg_pages8_decode_attention", "hg_pages8_decode_step", "hg_pages_plan",
     "library", "library_path",
 ]
 
@@ -41,6 +44,11 @@ HG_HEAD_KEYS_ONLY = 1
 HG_HEAD_PROTECTED = 2
 HG_DTYPE_BF16 = 0
 HG_DTYPE_F16 = 1
+HG_PAGES8_BLOCK = 16
+HG_PLAN_FREE = 0
+HG_PLAN_REFUSED = 1
+HG_PLAN_TOKENS = 2
+HG_PLAN_LONGEST = 3
 NONE_OFFSET = (1 << 64) - 1
 
 STATUS = {
@@ -135,6 +143,14 @@ def library():
         "hg_pages_decode_step": ([P, i32, i32, P, P, P, P, i32, P, P, ctypes.c_float, P, sz, P], st),
         "hg_prompt_workspace_size": ([ctypes.POINTER(sz)], st),
         "hg_prompt_attention": ([i32, i32, i32, i32, P, P, P, P, i32, ctypes.c_float, P, sz, P], st),
+        "hg_pages8_create": ([P, P, P, P, P, ctypes.POINTER(P)], st),
+        "hg_pages8_destroy": ([P], None),
+        "hg_pages8_append": ([P, i32, i32, i32, P, P, P, P, P, i32, P, P], st),
+        "hg_pages8_dequantize": ([P, i32, i32, P, P, i32, P, P, P], st),
+        "hg_pages8_decode_workspace_size": ([P, i32, i32, ctypes.POINTER(sz)], st),
+        "hg_pages8_decode_attention": ([P, i32, i32, P, P, i32, P, P, ctypes.c_float, P, sz, P], st),
+        "hg_pages8_decode_step": ([P, i32, i32, P, P, P, P, i32, P, P, ctypes.c_float, P, sz, P], st),
+        "hg_pages_plan": ([i32, i32, P, i32, P, P, P, i32, P, i32, P, P, P, P, P, P], st),
         "hg_status_string": ([st], ctypes.c_char_p),
     }
     for name, (args, res) in sigs.items():
@@ -421,12 +437,13 @@ class _Types:
     def __getattr__(self, name):
         import torch
         self.code = {torch.bfloat16: HG_DTYPE_BF16, torch.float16: HG_DTYPE_F16}
-        self.int32, self.float32 = torch.int32, torch.float32
+        self.int32, self.float32, self.codes = torch.int32, torch.float32, (torch.float8_e4m3fn, torch.uint8)
         return self.__dict__[name]
 
 
 _types = _Types()
 _pack18, _pack12 = struct.Struct("=18q").pack, struct.Struct("=12q").pack  # hg_append_io, hg_attention_io
+_pack3 = struct.Struct("=3q").pack  # hg_rows
 
 
 class Pages:
@@ -628,3 +645,177 @@ def hg_prompt_attention(q, k, v, q_begin, k_begin, out, lse, causal, softmax_sca
         raise ValueError("%s: the prompts end at %d and %d, q and k hold %d and %d rows" % (w, q_end, k_end, n, nk))
     _check(library().hg_prompt_attention(code, count, hq, heads, io, qb, kb, _lse(w, lse, n, hq), 1 if causal else 0,
                                          softmax_scale, *_workspace(w, workspace), _stream(stream)), w)
+
+
+# ---------------------------------------------------------------------------
+# Paged caches in 8 bits, page tables built on the GPU
+# ---------------------------------------------------------------------------
+
+
+class Pages8:
+    """Owning handle of an hg_pages8 descriptor (the pool's tensors stay the caller's)."""
+
+    def __init__(self, handle, k_pages, v_pages, k_scales, v_scales, shape, dtype):
+        self.handle = handle
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.k_scales, self.v_scales = k_scales, v_scales
+        self.shape = shape
+        self.dtype = dtype  # of the rows that calls take and give
+        self.device = k_pages.get_device()
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.hg_pages8_destroy(self.handle)
+            self.handle = None
+
+
+def _on_device(where, device, *tensors):
+    """All of a call's tensors on one device, which is the current one (a launch goes to no other)."""
+    for x in tensors:
+        if x is not None and x.get_device() != device:
+            raise ValueError("%s: tensors on %s and on cuda:%d" % (where, x.device, device))
+    import torch
+    if torch.cuda.current_device() != device:
+        raise ValueError("%s: tensors on cuda:%d, the current device is cuda:%d"
+                         % (where, device, torch.cuda.current_device()))
+
+
+def hg_pages8_create(k_pages, v_pages, k_scales, v_scales, dtype=None):
+    """Descriptor of the 8-bit page pool whose codes are these tensors (float8_e4m3fn, or their bytes as uint8), each
+    seen as [pages][kv heads][page size][128] (any strides), and whose scales are float32 [pages][kv heads][page size /
+    16].  dtype: of the rows that calls take and give (bfloat16, the default, or float16)."""
+    w = "hg_pages8_create"
+    if dtype is None:
+        import torch
+        dtype = torch.bfloat16
+    if dtype not in _types.code:
+        raise ValueError("%s: dtype must be bfloat16 or float16" % w)
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
+        raise ValueError("%s: k_pages and v_pages must be [pages][heads][tokens][128] of one type" % w)
+    if k_pages.dtype not in _types.codes:
+        raise ValueError("%s: pages must be float8_e4m3fn or uint8" % w)
+    n, heads, size, dim = k_pages.shape
+    # the stride of an axis of length 1 is never taken: a dense one stands for it
+    strides = [tuple(s if d > 1 else dim for s, d in zip(x.stride(), x.shape)) for x in (k_pages, v_pages)]
+    if strides[0] != strides[1] or k_pages.stride(3) != 1:
+        raise ValueError("%s: k_pages and v_pages must have the same strides and dense channels" % w)
+    for x in (k_scales, v_scales):
+        if x.dtype != _types.float32 or x.shape != (n, heads, size // HG_PAGES8_BLOCK) or not x.is_contiguous():
+            raise ValueError("%s: scales must be contiguous float32 [%d][%d][%d]" % (w, n, heads, size // HG_PAGES8_BLOCK))
+    pool = (k_pages, v_pages, k_scales, v_scales)
+    if not all(x.is_cuda for x in pool):
+        raise ValueError("%s: pages and scales must be CUDA tensors" % w)
+    if len({x.get_device() for x in pool}) > 1:
+        raise ValueError("%s: pages and scales must be on one device" % w)
+    shape = PageShape(_types.code[dtype], n, size, heads, dim, *strides[0][:3])
+    h = ctypes.c_void_p()
+    _check(library().hg_pages8_create(ctypes.byref(shape), *(x.data_ptr() for x in pool), ctypes.byref(h)), w)
+    return Pages8(h, *pool, shape, dtype)
+
+
+def hg_pages8_destroy(pages):
+    if pages.handle:
+        library().hg_pages8_destroy(pages.handle)
+        pages.handle = None
+
+
+def _requests(where, begin, page_table, lengths=None):
+    """Number of requests, and what says where their tokens lie."""
+    n = max(begin.numel() - 1, 0)
+    if page_table.dim() != 2 or page_table.shape[0] < n:
+        raise ValueError("%s: page_table must be [%d][pages]" % (where, n))
+    per = page_table.shape[1]
+    bp, tp = _ints(where, "begin", begin, 1), _ints(where, "page_table", page_table, n * per)
+    return n, bp, tp, per, None if lengths is None else _ints(where, "lengths", lengths, n)
+
+
+def hg_pages8_append(pages, q, k, v, rotation, positions, begin, page_table, lengths, q_out=None, k_out=None, v_out=None,
+                     stream=None):
+    """Rotate q and k ([tokens][heads][128], any token and head strides; q None: no queries) and store k and v in 8 bits:
+    rows begin[r]..begin[r + 1] are the last of the lengths[r] tokens of request r, whose pages are page_table[r].  The
+    rotated rows also go to q_out and, where given, k_out; v to v_out."""
+    w, d = "hg_pages8_append", pages.dtype
+    n, heads, hq = k.shape[0], pages.shape.num_kv_heads, 0 if q is None else q.shape[1]
+    if q is not None and q_out is None:
+        raise ValueError("hg_pages8_append: q needs q_out")
+    io = _pack18(*(_rows(w, "q", q, n, hq, d) if hq else _NO_ROWS), *_rows(w, "k", k, n, heads, d),
+                     *_rows(w, "v", v, n, heads, d), *(_rows(w, "q_out", q_out, n, hq, d) if hq else _NO_ROWS),
+                     *(_NO_ROWS if k_out is None else _rows(w, "k_out", k_out, n, heads, d)),
+                     *(_NO_ROWS if v_out is None else _rows(w, "v_out", v_out, n, heads, d)))
+    rp, pp = _rotated_by(w, rotation, positions, n)
+    count, bp, tp, per, lp = _requests(w, begin, page_table, lengths)
+    _on_device(w, pages.device, q, k, v, q_out, k_out, v_out, begin, page_table, lengths,
+               *(() if rotation is None else (rotation.table, positions)))
+    _check(library().hg_pages8_append(pages.handle, n, count, hq, io, rp, pp, bp, tp, per, lp, _stream(stream)), w)
+
+
+def hg_pages8_dequantize(pages, begin, page_table, k_out, v_out=None, stream=None):
+    """The first begin[r + 1] - begin[r] tokens of each request as dense rows begin[r].. of k_out and v_out
+    ([rows][kv heads][128] of the pool's row type, any token and head strides; either may be None)."""
+    w, d, heads = "hg_pages8_dequantize", pages.dtype, pages.shape.num_kv_heads
+    if k_out is None and v_out is None:
+        raise ValueError("%s: neither k_out nor v_out is given" % w)
+    n = (v_out if k_out is None else k_out).shape[0]
+    kp = None if k_out is None else _pack3(*_rows(w, "k_out", k_out, n, heads, d))
+    vp = None if v_out is None else _pack3(*_rows(w, "v_out", v_out, n, heads, d))
+    count, bp, tp, per, _ = _requests(w, begin, page_table)
+    _on_device(w, pages.device, begin, page_table, k_out, v_out)
+    _check(library().hg_pages8_dequantize(pages.handle, n, count, bp, tp, per, kp, vp, _stream(stream)), w)
+
+
+def hg_pages8_decode_workspace_size(pages, batch, num_q_heads):
+    out = ctypes.c_size_t(0)
+    _check(library().hg_pages8_decode_workspace_size(pages.handle, batch, num_q_heads, ctypes.byref(out)),
+           "hg_pages8_decode_workspace_size")
+    return out.value
+
+
+def hg_pages8_decode_attention(pages, q, page_table, lengths, out, lse, softmax_scale, workspace, stream=None):
+    """Attention of one token per request (q, out [batch][heads][128]) over the first lengths[b] tokens of its 8-bit
+    pages page_table[b]; lse float32 [batch][heads] or None."""
+    w, d = "hg_pages8_decode_attention", pages.dtype
+    n, hq = q.shape[0], q.shape[1]
+    io = _pack12(*_rows(w, "q", q, n, hq, d), 0, 0, 0, 0, 0, 0, *_rows(w, "out", out, n, hq, d))
+    tp, ts, lp = _decode_table(w, page_table, lengths, n)
+    ws = _workspace(w, workspace)
+    _on_device(w, pages.device, q, out, page_table, lengths, lse, workspace)
+    _check(library().hg_pages8_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse(w, lse, n, hq), softmax_scale,
+                                                *ws, _stream(stream)), w)
+
+
+def hg_pages8_decode_step(pages, q, k, v, rotation, positions, page_table, lengths, out, lse, softmax_scale, workspace,
+                          stream=None):
+    """One decode step on the 8-bit pages: q and the new token's k rotated, k and v stored as token lengths[b] - 1 of
+    request b, attention over its lengths[b] tokens."""
+    w, d = "hg_pages8_decode_step", pages.dtype
+    n, hq, heads = q.shape[0], q.shape[1], pages.shape.num_kv_heads
+    io = _pack12(*_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, n, heads, d),
+                     *_rows(w, "v", v, n, heads, d), *_rows(w, "out", out, n, hq, d))
+    rp, pp = _rotated_by(w, rotation, positions, n)
+    tp, ts, lp = _decode_table(w, page_table, lengths, n)
+    ws = _workspace(w, workspace)
+    _on_device(w, pages.device, q, k, v, out, page_table, lengths, lse, workspace,
+               *(() if rotation is None else (rotation.table, positions)))
+    _check(library().hg_pages8_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse(w, lse, n, hq),
+                                           softmax_scale, *ws, _stream(stream)), w)
+
+
+def hg_pages_plan(page_table, cached, new_tokens, free_pages, free_count, page_size, lengths, begin, slots, positions,
+                  counts, stream=None):
+    """Pages, rows and slots of a batch's new tokens, on the GPU (all int32): request r has cached[r] tokens in the pages
+    page_table[r], new_tokens[r] come (negative: it ends, and gives its pages back); pages are taken from the end of
+    free_pages[:free_count[0]].  Leaves lengths [batch] (may be cached itself), begin [batch + 1], slots and positions (or
+    None), one entry for each token there is room for, and counts [4] (HG_PLAN_*; counts[:1] may be free_count)."""
+    w = "hg_pages_plan"
+    n = cached.numel()
+    if page_table.dim() != 2 or page_table.shape[0] < n:
+        raise ValueError("%s: page_table must be [%d][pages]" % (w, n))
+    per, room = page_table.shape[1], slots.numel()
+    _on = (page_table, cached, new_tokens, free_pages, free_count, lengths, begin, slots, positions, counts)
+    args = (n, int(page_size), _ints(w, "page_table", page_table, n * per), per, _ints(w, "cached", cached, n),
+            _ints(w, "new_tokens", new_tokens, n), _ints(w, "free_pages", free_pages, 0), free_pages.numel(),
+            _ints(w, "free_count", free_count, 1), room, _ints(w, "lengths", lengths, n), _ints(w, "begin", begin, n + 1),
+            _ints(w, "slots", slots, 0), None if positions is None else _ints(w, "positions", positions, room),
+            _ints(w, "counts", counts, 4))
+    _on_device(w, counts.get_device(), *_on)
+    _check(library().hg_pages_plan(*args, _stream(stream)), w)

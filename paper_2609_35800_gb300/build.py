@@ -14,7 +14,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-CSRC_ATTENTION = os.path.join(HERE, "csrc_attention")  # caches that stay 16-bit, prompt attention
+CSRC_ATTENTION = os.path.join(HERE, "csrc_attention")  # paged caches in 16 and 8 bits, prompt attention
 INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB_NAME = "libheadguard.so"
@@ -22,7 +22,9 @@ LIB = os.path.join(OUT_DIR, LIB_NAME)
 SOURCES = [os.path.join(CSRC, f) for f in ("hg_api.cu", "hg_quantize.cu", "hg_decode.cu", "hg_decode_m16.cu",
                                             "hg_noalloc.cu")]
 SOURCES += [os.path.join(CSRC_ATTENTION, f) for f in ("hg_pages_api.cu", "hg_pages_append.cu", "hg_pages_decode.cu",
-                                                      "hg_prompt.cu")]
+                                                      "hg_prompt.cu", "hg_pages8_api.cu", "hg_pages8_append.cu",
+                                                      "hg_pages8_decode.cu", "hg_pages8_dequantize.cu",
+                                                      "hg_pages_plan.cu")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
               "-I" + INCLUDE, "-I" + CSRC, "-I" + CSRC_ATTENTION]

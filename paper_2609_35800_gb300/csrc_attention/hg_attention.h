@@ -34,10 +34,20 @@ struct Rotation {
   int position_stride;  // tokens: distance between a token's first, second and third position
 };
 
-struct PagePool {
-  uint16_t *k, *v;
+struct PoolShape {
   int num_pages, page_size, page_shift, heads;
-  int64_t page_stride, head_stride, token_stride;
+  int64_t page_stride, head_stride, token_stride;  // elements
+};
+struct PagePool : PoolShape {
+  uint16_t *k, *v;
+};
+
+// An 8-bit pool: codes of a byte (strides in bytes), a scale for each block of kBlock8 tokens and head.
+constexpr int kBlock8 = HG_PAGES8_BLOCK, kBlock8Shift = 4;
+static_assert(kBlock8 == 1 << kBlock8Shift, "block");
+struct PagePool8 : PoolShape {
+  uint8_t *k, *v;
+  float *k_scales, *v_scales;  // [pages][heads][page_size / kBlock8]
 };
 
 struct PagesAppendParams {
@@ -47,6 +57,45 @@ struct PagesAppendParams {
   Rows q, k, v, q_out, k_out, v_out;
   const int* slots;
 };
+
+struct Pages8AppendParams {
+  PagePool8 pool;
+  Rotation rot;
+  int tokens, requests, q_heads;
+  int kv_ctas;  // CTAs that store keys and values, ahead of those that turn queries
+  Rows q, k, v, q_out, k_out, v_out;
+  const int* begin;
+  const int* table;
+  int table_stride;
+  const int* lengths;
+};
+
+struct Pages8DequantizeParams {
+  PagePool8 pool;
+  int tokens, requests;
+  Rows k_out, v_out;
+  const int* begin;
+  const int* table;
+  int table_stride;
+};
+
+struct PagesPlanParams {
+  int batch, page_shift;
+  int* table;
+  int table_stride;
+  const int* cached;
+  const int* new_tokens;
+  int* free_pages;
+  int free_capacity;
+  const int* free_count;
+  int tokens;  // room for new ones
+  int* lengths;
+  int* begin;
+  int* slots;
+  int* positions;
+  int* counts;
+};
+constexpr int kPlanMaxBatch = 16384;
 
 // Tokens of a tile of the paged decode; a tensor map's box covers a tile of one page, or the page where that is smaller.
 constexpr int kDecodeTile = 32;
@@ -70,6 +119,22 @@ struct PagesDecodeParams {
   float scale;
   uint32_t* status;
   uint32_t* counters;  // kDecodeJoinCounters, then [batch][heads]; zero between launches
+  float* partials;
+};
+
+struct Pages8DecodeParams {
+  PagePool8 pool;
+  Rotation rot;
+  int batch, group;
+  int store;  // a decode step: k, v hold the new token, which is stored
+  Rows q, k, v, out;
+  const int* table;
+  int table_stride;
+  const int* lengths;
+  float* lse;
+  float scale;
+  uint32_t* status;
+  uint32_t* counters;
   float* partials;
 };
 
@@ -104,6 +169,10 @@ struct PromptParams {
 
 cudaError_t launch_pages_append(const PagesAppendParams& p, bool f16, cudaStream_t s);
 cudaError_t launch_pages_decode(const PagesDecodeParams& p, bool f16, cudaStream_t s);
+cudaError_t launch_pages8_append(const Pages8AppendParams& p, bool f16, cudaStream_t s);
+cudaError_t launch_pages8_dequantize(const Pages8DequantizeParams& p, bool f16, cudaStream_t s);
+cudaError_t launch_pages8_decode(const Pages8DecodeParams& p, bool f16, cudaStream_t s);
+cudaError_t launch_pages_plan(const PagesPlanParams& p, cudaStream_t s);
 cudaError_t launch_prompt(const PromptParams& p, bool f16, cudaStream_t s);
 
 // A launch that may be scheduled while the kernel before it on the stream still runs (the kernel waits itself).

@@ -1,0 +1,109 @@
+// Device helpers for 8-bit pages: e4m3 codes, the blocks' scales, addresses.
+#pragma once
+#include <cuda_fp8.h>
+
+#include "hg_rows.cuh"
+
+namespace hg {
+
+// Powers of two are compared and inverted by their exponent field.  448, e4m3's largest, is 1.75 * 2^8.
+constexpr int kLeastField = 1, kMostField = 253;  // 2^-126 and 2^126: their inverses are normal too
+
+// Exponent field of the least power of two s with |x| <= 448 s for the largest |x|, given by its bits (finite).
+__device__ __forceinline__ int needed_field(uint32_t amax_bits) {
+  const int e = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return max(e, kLeastField);
+}
+// That of a stored scale, raised to a power of two.
+__device__ __forceinline__ int stored_field(float s) {
+  return min(max((int)((__float_as_uint(s) & 0x7fffffffu) + 0x7fffffu >> 23), kLeastField), kMostField);
+}
+__device__ __forceinline__ float power_of_field(int field) { return __uint_as_float((uint32_t)field << 23); }
+__device__ __forceinline__ float inverse_of_field(int field) { return __uint_as_float((uint32_t)(254 - field) << 23); }
+
+// |x| as it counts for a scale: NaN and infinities do not.
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+  return b < 0x7f800000u ? b : 0u;
+}
+
+// Codes of (a, b) * inv; an infinity becomes NaN, which stays one.
+__device__ __forceinline__ uint32_t encode2(float a, float b, float inv) {
+  a = fabsf(a) < INFINITY ? a * inv : NAN;
+  b = fabsf(b) < INFINITY ? b * inv : NAN;
+  return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ uint2 encode8(const float* x, float inv) {
+  return make_uint2(encode2(x[0], x[1], inv) | encode2(x[2], x[3], inv) << 16,
+                    encode2(x[4], x[5], inv) | encode2(x[6], x[7], inv) << 16);
+}
+
+// Two codes as FP16, exactly.
+__device__ __forceinline__ uint32_t decode2(uint32_t codes) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
+  return (uint32_t)h.x | (uint32_t)h.y << 16;
+}
+__device__ __forceinline__ void decode8(uint2 codes, float* x) {
+  const uint32_t w[2] = {codes.x, codes.y};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = half2_bits_to_float2(decode2(w[i / 2] >> 16 * (i % 2) & 0xffffu));
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+// Codes times `ratio`, as codes again.
+__device__ __forceinline__ uint2 recode8(uint2 codes, float ratio) {
+  float x[8];
+  decode8(codes, x);
+  return encode8(x, ratio);
+}
+
+// A lane's 16 channels of a row in binary32: lo's eight, then hi's; turned where `g` is given.
+template <bool F16>
+__device__ __forceinline__ void row_values(const uint4& lo, const uint4& hi, const LaneAngles* g, bool interleaved,
+                                           float (&x)[16]) {
+  const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 f = unpack2<F16>(w[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+  if (!g) return;
+  const float cs[8] = {g->cos[0].x, g->cos[0].y, g->cos[0].z, g->cos[0].w, g->cos[1].x, g->cos[1].y, g->cos[1].z, g->cos[1].w};
+  const float sn[8] = {g->sin[0].x, g->sin[0].y, g->sin[0].z, g->sin[0].w, g->sin[1].x, g->sin[1].y, g->sin[1].z, g->sin[1].w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (interleaved) turn(x[2 * i], x[2 * i + 1], cs[i], sn[i]);
+    else turn(x[i], x[8 + i], cs[i], sn[i]);
+  }
+}
+template <bool F16>
+__device__ __forceinline__ uint4 pack8(const float* x) {
+  return make_uint4(pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3]), pack2<F16>(x[4], x[5]), pack2<F16>(x[6], x[7]));
+}
+
+// x, or the 16-bit type's largest value where it is beyond; NaN stays.
+template <bool F16>
+__device__ __forceinline__ float in_range(float x) {
+  constexpr float kMost = F16 ? 65504.f : 0x1.fep127f;
+  return x > kMost ? kMost : x < -kMost ? -kMost : x;
+}
+
+// Byte offset of a token's codes in the pool; index of its block's scale.
+__device__ __forceinline__ int64_t code_row(const PagePool8& p, int page, int in_page, int head) {
+  return page * p.page_stride + head * p.head_stride + in_page * p.token_stride;
+}
+__device__ __forceinline__ int64_t scale_at(const PagePool8& p, int page, int in_page, int head) {
+  return (((int64_t)page * p.heads + head) << (p.page_shift - kBlock8Shift)) + (in_page >> kBlock8Shift);
+}
+// Page of a request's token; -1 where its place is outside the table or the page outside the pool.
+__device__ __forceinline__ int page_of(const PagePool8& p, const int* table_row, int table_stride, int token) {
+  const int at = token >> p.page_shift;
+  if (token < 0 || at >= table_stride) return -1;
+  const int page = table_row[at];
+  return page >= 0 && page < p.num_pages ? page : -1;
+}
+
+}  // namespace hg

@@ -1,14 +1,11 @@
 // C ABI of the 16-bit caches: page pools, append, paged decode attention, prompt attention.  Every argument is checked
 // here, on the host, before anything is enqueued.
 #include <algorithm>
-#include <cmath>
 #include <cstring>
 #include <mutex>
 #include <new>
 
-#include <cudaTypedefs.h>
-
-#include "hg_attention.h"
+#include "hg_checks.h"
 
 struct hg_pages {
   hg::PagePool pool;
@@ -25,75 +22,6 @@ using namespace hg;
 
 constexpr double kPromptSplitGain = 8;  // blocks by which the longest item has to pass the even share
 constexpr int kPromptLeastChunk = 4;
-constexpr int64_t kMaxStride = int64_t(1) << 38;  // elements; a tensor map's strides are below 2^40 bytes
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-hg_status of_cuda(cudaError_t e) { return e == cudaSuccess ? HG_OK : HG_ERR_CUDA; }
-
-// One set of rows: present, aligned, strides in range.
-hg_status check_rows(const hg_rows& r) {
-  if (!r.data || r.token_stride < 0 || r.head_stride < 0 || r.token_stride >= kMaxStride || r.head_stride >= kMaxStride)
-    return HG_ERR_INVALID_ARG;
-  return aligned16(r.data) && r.token_stride % 8 == 0 && r.head_stride % 8 == 0 ? HG_OK : HG_ERR_ALIGNMENT;
-}
-
-hg_status check_all(std::initializer_list<const hg_rows*> rows) {
-  hg_status first = HG_OK;
-  for (const hg_rows* r : rows) {
-    const hg_status st = check_rows(*r);
-    if (st == HG_ERR_INVALID_ARG) return st;
-    if (first == HG_OK) first = st;
-  }
-  return first;
-}
-
-hg_status check_rotation(const hg_rotation* r, const int32_t* positions) {
-  if (!r) return HG_OK;
-  if (!r->table || !positions || r->table_len < 1 || r->interleaved < 0 || r->interleaved > 1) return HG_ERR_INVALID_ARG;
-  if (!aligned16(r->table) || !aligned4(positions)) return HG_ERR_ALIGNMENT;
-  if (r->rot_dim < 16 || r->rot_dim > kHeadDim || r->rot_dim % 16 != 0) return HG_ERR_UNSUPPORTED;
-  const int32_t* s = r->sections;
-  if (s[0] < 0 || s[1] < 0 || s[2] < 0) return HG_ERR_INVALID_ARG;
-  if (s[0] || s[1] || s[2]) {
-    if (s[0] > 64 || s[1] > 64 || s[2] > 64 || s[0] + s[1] + s[2] != r->rot_dim / 2) return HG_ERR_INVALID_ARG;
-    if (s[0] % 8 || s[1] % 8 || s[2] % 8) return HG_ERR_UNSUPPORTED;
-  }
-  return HG_OK;
-}
-
-Rotation rotation_of(const hg_rotation* r, const int32_t* positions, int tokens) {
-  Rotation o = {};
-  if (!r) return o;
-  o.table = r->table;
-  o.table_len = r->table_len;
-  o.half = r->rot_dim / 2;
-  o.interleaved = r->interleaved;
-  const bool three = r->sections[0] || r->sections[1] || r->sections[2];
-  o.end0 = three ? r->sections[0] : o.half;
-  o.end1 = three ? r->sections[0] + r->sections[1] : o.half;
-  o.positions = positions;
-  o.position_stride = three ? tokens : 0;
-  return o;
-}
-
-float scale_of(float softmax_scale) { return softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)kHeadDim); }
-
-// cuTensorMapEncodeTiled through the runtime (no link against the driver library).
-PFN_cuTensorMapEncodeTiled_v12000 map_encoder() {
-  static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> cached{nullptr};
-  PFN_cuTensorMapEncodeTiled_v12000 fn = cached.load(std::memory_order_acquire);
-  if (!fn) {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
-    cached.store(fn, std::memory_order_release);
-  }
-  return fn;
-}
-
 // A page pool as [pages][heads][2][page_size][64]: both halves of a row's channels as rows of 128 bytes, the span of
 // the swizzle.  A box is a tile's tokens of one page and head: first halves, then second halves.
 CUresult encode_pages(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map, void* data, const PagePool& p, bool f16) {
@@ -203,35 +131,17 @@ hg_status map_pages(hg_pages* p) {
   return HG_OK;
 }
 
-// Decode workspace: header, the parts that CTAs leave (two each, at the largest group whatever the call's, so that the
-// counters behind them lie at one place for every call), a counter per (request, KV head): of the most KV heads that a
-// pool may have, so that a workspace serves every pool (256 bytes a request).
-size_t decode_parts_bytes() { return (size_t)decode_ctas() * 2 * kMaxGroup * kPartialFloats * sizeof(float); }
-size_t decode_workspace_bytes(int batch) {
-  const size_t counters = kDecodeJoinCounters + (size_t)batch * kMaxKvHeads;
-  return kAttnHeaderBytes + decode_parts_bytes() + ((counters * sizeof(uint32_t) + 255) & ~size_t(255));
-}
-
-hg_status decode_batch_ok(const hg_pages* p, int32_t batch, int32_t num_q_heads) {
-  if (!p || batch < 0 || num_q_heads < 1 || num_q_heads % p->pool.heads != 0) return HG_ERR_INVALID_ARG;
-  if (num_q_heads / p->pool.heads > kMaxGroup || batch > (1 << 20)) return HG_ERR_UNSUPPORTED;
-  return HG_OK;
-}
-
 hg_status pages_decode(const hg_pages* pages, int32_t batch, int32_t num_q_heads, const hg_attention_io* io,
                        const hg_rotation* rotation, const int32_t* positions, const int32_t* page_table,
                        int32_t table_stride, const int32_t* lengths, float* lse, float softmax_scale, void* ws,
                        size_t ws_bytes, bool store, cudaStream_t stream) {
-  hg_status st = decode_batch_ok(pages, batch, num_q_heads);
+  if (!pages) return HG_ERR_INVALID_ARG;
+  hg_status st = decode_batch_ok(pages->pool.heads, batch, num_q_heads);
   if (st != HG_OK) return st;
   if (!io || table_stride < 0 || !(softmax_scale == softmax_scale)) return HG_ERR_INVALID_ARG;
   if (batch == 0) return HG_OK;
   if ((table_stride > 0 && !page_table) || !lengths || !ws) return HG_ERR_INVALID_ARG;
-  // the kernel numbers tokens, and tiles and fixed costs of every request and head, in 32 bits
-  const int64_t capacity = (int64_t)table_stride * pages->pool.page_size;
-  if (capacity > INT32_MAX ||
-      (capacity / kDecodeTile + 1 + kDecodeItemCost) * pages->pool.heads > INT32_MAX / std::max(batch, 1))
-    return HG_ERR_UNSUPPORTED;
+  if (!decode_table_ok(pages->pool, batch, table_stride)) return HG_ERR_UNSUPPORTED;
   st = store ? check_all({&io->q, &io->k, &io->v, &io->out}) : check_all({&io->q, &io->out});
   if (st != HG_OK) return st;
   st = check_rotation(rotation, positions);
@@ -273,28 +183,15 @@ extern "C" {
 
 hg_status hg_pages_create(const hg_page_shape* s, void* k_pages, void* v_pages, hg_pages** out) {
   if (!s || !k_pages || !v_pages || !out) return HG_ERR_INVALID_ARG;
-  if (s->dtype != HG_DTYPE_BF16 && s->dtype != HG_DTYPE_F16) return HG_ERR_INVALID_ARG;
-  if (s->num_pages < 1 || s->num_kv_heads < 1 || s->page_size < 1) return HG_ERR_INVALID_ARG;
-  if (s->page_stride < 0 || s->head_stride < 0 || s->token_stride < 0) return HG_ERR_INVALID_ARG;
-  if (s->head_dim != kHeadDim || s->num_kv_heads > kMaxKvHeads) return HG_ERR_UNSUPPORTED;
-  if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1))) return HG_ERR_UNSUPPORTED;
-  if ((int64_t)s->num_pages * s->page_size > INT32_MAX) return HG_ERR_UNSUPPORTED;
-  int64_t token = s->token_stride, head = s->head_stride, page = s->page_stride;
-  if (token == 0 && head == 0 && page == 0) {
-    token = kHeadDim;
-    head = token * s->page_size;
-    page = head * s->num_kv_heads;
-  }
-  if (token < kHeadDim || (s->num_kv_heads > 1 && head < kHeadDim) || (s->num_pages > 1 && page < kHeadDim))
-    return HG_ERR_INVALID_ARG;
-  if (token >= kMaxStride || head >= kMaxStride || page >= kMaxStride) return HG_ERR_UNSUPPORTED;
-  if (!aligned16(k_pages) || !aligned16(v_pages) || token % 8 || head % 8 || page % 8) return HG_ERR_ALIGNMENT;
+  PoolShape shape;
+  const hg_status st = check_shape(s, 8, &shape);
+  if (st != HG_OK && st != HG_ERR_ALIGNMENT) return st;
+  if (st != HG_OK || !aligned16(k_pages) || !aligned16(v_pages)) return HG_ERR_ALIGNMENT;
   hg_pages* p = new (std::nothrow) hg_pages();
   if (!p) return HG_ERR_CUDA;
-  int shift = 0;
-  while ((1 << shift) < s->page_size) ++shift;
-  p->pool = {static_cast<uint16_t*>(k_pages), static_cast<uint16_t*>(v_pages), s->num_pages, s->page_size, shift,
-             s->num_kv_heads, page, head, token};
+  static_cast<PoolShape&>(p->pool) = shape;
+  p->pool.k = static_cast<uint16_t*>(k_pages);
+  p->pool.v = static_cast<uint16_t*>(v_pages);
   p->dtype = s->dtype;
   *out = p;
   return HG_OK;
@@ -333,8 +230,8 @@ hg_status hg_pages_append(const hg_pages* pages, int32_t num_tokens, int32_t num
 }
 
 hg_status hg_pages_decode_workspace_size(const hg_pages* pages, int32_t batch, int32_t num_q_heads, size_t* bytes) {
-  if (!bytes) return HG_ERR_INVALID_ARG;
-  const hg_status st = decode_batch_ok(pages, batch, num_q_heads);
+  if (!bytes || !pages) return HG_ERR_INVALID_ARG;
+  const hg_status st = decode_batch_ok(pages->pool.heads, batch, num_q_heads);
   if (st != HG_OK) return st;
   *bytes = decode_workspace_bytes(batch);
   return HG_OK;
