@@ -123,6 +123,7 @@ struct PagesDecodeParams {
 };
 
 struct Pages8DecodeParams {
+  CUtensorMap k_map, v_map;  // the pool as [pages][heads][page_size][128 bytes]
   PagePool8 pool;
   Rotation rot;
   int batch, group;

@@ -1,6 +1,7 @@
 // C ABI of the 8-bit paged caches and of page tables built on the GPU.  Every argument is checked here, on the host,
 // before anything is enqueued.
 #include <cstring>
+#include <mutex>
 #include <new>
 
 #include "hg_checks.h"
@@ -8,6 +9,10 @@
 struct hg_pages8 {
   hg::PagePool8 pool;
   int dtype;
+  // tensor maps, encoded by the first decode call
+  std::mutex mutex;
+  std::atomic<bool> mapped{false};
+  CUtensorMap k_map, v_map;
 };
 
 namespace {
@@ -22,6 +27,31 @@ hg_status check_places(int32_t requests, const int32_t* begin, const int32_t* pa
   if (!begin || table_stride < 0 || (table_stride > 0 && !page_table)) return HG_ERR_INVALID_ARG;
   if (!aligned4(begin) || !aligned4(page_table)) return HG_ERR_ALIGNMENT;
   return (int64_t)table_stride * pool.page_size > INT32_MAX ? HG_ERR_UNSUPPORTED : HG_OK;
+}
+
+// A pool as [pages][heads][page_size][128]: a box is a tile's tokens of one page and head, a row the swizzle's span.
+CUresult encode_pages8(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map, void* data, const PagePool8& p) {
+  const cuuint64_t dims[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)p.page_size, (cuuint64_t)p.heads, (cuuint64_t)p.num_pages};
+  // the stride of an axis of length 1 is never taken
+  const cuuint64_t strides[3] = {(cuuint64_t)p.token_stride, p.heads > 1 ? (cuuint64_t)p.head_stride : 128,
+                                 p.num_pages > 1 ? (cuuint64_t)p.page_stride : 128};
+  const cuuint32_t box[4] = {kHeadDim, (cuuint32_t)std::min(p.page_size, kDecodeTile), 1, 1};
+  const cuuint32_t steps[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, data, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+hg_status map_pages8(hg_pages8* p) {
+  if (p->mapped.load(std::memory_order_acquire)) return HG_OK;
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
+  if (!encode) return HG_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(p->mutex);
+  if (p->mapped.load(std::memory_order_relaxed)) return HG_OK;
+  if (encode_pages8(encode, &p->k_map, p->pool.k, p->pool) != CUDA_SUCCESS ||
+      encode_pages8(encode, &p->v_map, p->pool.v, p->pool) != CUDA_SUCCESS)
+    return HG_ERR_CUDA;
+  p->mapped.store(true, std::memory_order_release);
+  return HG_OK;
 }
 
 hg_status pages8_decode(const hg_pages8* pages, int32_t batch, int32_t num_q_heads, const hg_attention_io* io,
@@ -41,8 +71,12 @@ hg_status pages8_decode(const hg_pages8* pages, int32_t batch, int32_t num_q_hea
   if (st != HG_OK) return st;
   if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(lse) || !aligned16(ws)) return HG_ERR_ALIGNMENT;
   if (ws_bytes < decode_workspace_bytes(batch)) return HG_ERR_WORKSPACE_TOO_SMALL;
+  st = map_pages8(const_cast<hg_pages8*>(pages));
+  if (st != HG_OK) return st;
   Pages8DecodeParams p;
   std::memset(&p, 0, sizeof p);
+  p.k_map = pages->k_map;
+  p.v_map = pages->v_map;
   p.pool = pages->pool;
   p.rot = rotation_of(rotation, positions, batch);
   p.batch = batch;

@@ -17,10 +17,8 @@ namespace {
 constexpr int kThreads = 128;  // 16 rows
 constexpr unsigned kAll = 0xffffffffu;
 
-// begin[r], whatever lies there, within the call's rows; without begin a request has one row.
-__device__ __forceinline__ int begin_of(const Pages8AppendParams& p, int r) {
-  return p.begin ? min(max(p.begin[r], 0), p.tokens) : r;
-}
+// begin[r], whatever lies there, within the call's rows.
+__device__ __forceinline__ int begin_of(const Pages8AppendParams& p, int r) { return min(max(p.begin[r], 0), p.tokens); }
 
 // The request that unit u belongs to: the last whose first unit is not above it.  32 candidates a round, a lane each.
 __device__ int request_of(const Pages8AppendParams& p, int u, int begin0) {

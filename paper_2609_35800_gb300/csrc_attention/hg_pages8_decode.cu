@@ -1,130 +1,509 @@
-// Attention of one new token per request over an 8-bit paged cache.
+// Attention of one new token per request over an 8-bit paged cache, split over the cache's length and joined.
 //
 // For a request, KV head and its G queries: S_t = scale ks q.c_t with the key block's scale ks, m = max S_t, out = sum e^(S_t
-// - m) vs c'_t / sum e^(S_t - m) with the value block's scale vs.  A warp takes a request's query head and goes through its
-// tokens one by one with a running maximum and sum, four channels a lane.
+// - m) vs c'_t / sum e^(S_t - m) with the value block's scale vs.  A block is 16 tokens, the height of a product's tile, so
+// a scale is one factor of a fragment.  The work is divided and joined as over 16-bit pages (hg_pages_split.cuh).
+//
+// A producer warp copies tiles of 32 tokens into a ring of stages with TMA, a box per page (swizzled rows of 128 bytes; a
+// page outside the pool reads as zeros), and their scales beside them with four-byte asynchronous copies that arrive on the
+// same barrier.  Three consumer warps take the tiles in turn, each with its own running maximum and sums, and turn codes
+// into FP16 in registers, exactly (e4m3 is a subset), for mma.sync m16n8k16:
+//   S^T[token][query] = K . q        A = keys.  A 16-byte chunk of a row is a product's 16 channels; ldmatrix leaves
+//                                    channels 4i .. 4i + 3 in a lane, where the product wants 2i, 2i + 1, 2i + 8, 2i + 9:
+//                                    the queries' fragments have the same order, and a sum's order is free
+//   O^T[channel][query] += V^T . P^T A = values, by ldmatrix.trans on pairs of channels; a byte permutation parts them,
+//                                    rows i and i + 8 of the product are channels 2i and 2i + 1
+// A BF16 query is multiplied by a power of two that brings its largest entry below 2^15, so that FP16 holds it (and 2^39
+// downwards); the factor comes back with ks.  P is e^(S - m) 2^7 vs / u, where u is the largest vs so far, to a power of two:
+// at most 2^15, the sums O stay in units of u and are moved when u grows.  So terms below 2^-32 of the largest are lost to
+// the second product.  Scores, maxima, sums and outputs are held in 32 bits.
 #include "hg_pages8.cuh"
+#include "hg_pages_split.cuh"
 
 namespace hg {
 namespace {
 
-constexpr int kThreads = 128;
-constexpr unsigned kAll = 0xffffffffu;
+constexpr int kStages = 6;
+static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
+constexpr int kHalfBytes = kTile * kHeadDim;   // keys; then values
+constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kQRowBytes = 288;  // a staged query row: 256 bytes and its factor; 8 banks on, so that four rows meet all
+constexpr int kTileBlocks = kTile / kBlock8;
+constexpr int kScaleLanes = 2 * kTileBlocks;
 
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kAll, x, o);
-  return x;
+// Shared memory, two CTAs an SM.  The staged queries (8 rows a warp) and the warps' parts that are added up at an item's
+// end (8 queries at a time) take turns in one region.
+struct Smem {
+  static constexpr int scales = kStages * kStageBytes;  // of each stage: its keys' blocks, its values' blocks
+  static constexpr int scratch = scales + kStages * kScaleLanes * 4;
+  static constexpr int scratch_bytes = kConsumers * 8 * kSumFloats * 4;
+  static constexpr int bars = scratch + scratch_bytes;
+  static constexpr int misc = bars + 2 * kStages * 8;  // abort flag, last part, start of the CTA's work, scan
+  static constexpr int lengths = misc + 128;           // the first requests' lengths
+  static constexpr int bytes = lengths + 4 * kKeptLengths;
+};
+static_assert(Smem::scratch_bytes >= kConsumers * 8 * kQRowBytes, "queries are staged there too");
+static_assert(Smem::scratch % 16 == 0 && Smem::bars % 8 == 0, "alignment");
+static_assert((8 + 12 + kConsumers + 1) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
+static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
+
+template <bool F16>
+struct Kind {
+  static constexpr bool kF16 = F16;
+  static constexpr float kUnlift = 0x1p-7f;
+  static __device__ __forceinline__ float result(float x) { return in_range<F16>(x); }
+  static __device__ __forceinline__ void place(float* row, int g, float first, float second) {
+    *reinterpret_cast<float2*>(row + 2 * g) = make_float2(first, second);
+  }
+};
+
+__device__ __forceinline__ void tma_page8(uint32_t dst, const CUtensorMap* map, int row, int head, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
+      "[%6];\n" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(head), "r"(page), "r"(bar)
+      : "memory");
+}
+// Four bytes, or zeros where `bytes` is 0.
+__device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// An arrival on `bar`, one of those it counts, once this thread's copies so far have landed.
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(bar) : "memory");
 }
 
-// The row of a head, turned, four channels a lane, through shared memory; 16 channels of it in lanes below 8.
-template <bool F16>
-__device__ __forceinline__ void load_row(const Rows& rows, const Rotation& rot, bool turns, int b, int head, float* staged,
-                                         bool rounded, float (&x)[4]) {
+// Copies the CTA's tiles into the ring, in order; returns how many it asked for.
+__device__ uint32_t produce(const Pages8DecodeParams& p, Cursor c, int tiles, const int* kept, uint32_t stages, uint32_t full,
+                            uint32_t empty, volatile int* abort) {
   const int lane = threadIdx.x % 32;
-  if (lane < 8) {
-    const LaneChannels at = lane_channels(rot, lane, turns && rot.table != nullptr);
-    const uint16_t* src = rows.data + b * rows.token_stride + head * rows.head_stride;
-    const uint4 lo = ldg16(src + at.lo), hi = ldg16(src + at.hi);
-    LaneAngles angles;
-    if (at.turns) angles = lane_angles(rot, lane, b);
-    float v[16];
-    row_values<F16>(lo, hi, at.turns ? &angles : nullptr, rot.interleaved != 0, v);
-    for (int i = 0; i < 16; ++i) {
-      if (rounded) {
-        const float2 f = unpack2<F16>(pack2<F16>(v[i], 0.f));
-        v[i] = f.x;
+  const int shift = min(p.pool.page_shift, kTileShift), rows = 1 << shift;  // tokens of a box
+  const int boxes = kTile >> shift;
+  const uint32_t box_bytes = (uint32_t)rows * kHeadDim;
+  // the lane's scale of a tile
+  const float* scales = lane < kTileBlocks ? p.pool.k_scales : p.pool.v_scales;
+  const int block_row = lane % kTileBlocks * kBlock8;
+  uint32_t n = 0;
+  // 32 boxes' page ids, a lane each, from box `first` of request `of` on
+  int of = -1, first = 0, id = 0;
+  for (; tiles > 0; next_item(p, kept, c)) {
+    const int* ids = p.table + (int64_t)c.b * p.table_stride;
+    for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
+      const int box0 = c.t * boxes;  // box number in the item
+      const int valid = min(boxes, max(0, (c.len - c.t * kTile + rows - 1) >> shift));
+      if (of != c.b || box0 < first || box0 + boxes > first + 32) {
+        of = c.b;
+        first = box0;
+        const int64_t token = (int64_t)(first + lane) * rows;
+        id = token < c.len ? ids[token >> p.pool.page_shift] : -1;
       }
-      staged[(i < 8 ? at.lo + i : at.hi + i - 8)] = v[i];
+      const int s = n % kStages;
+      if (n >= kStages && !wait_warp(empty + 8 * s, (n / kStages - 1) & 1, abort, p.status)) return n;
+      if (elect_one()) mbar_arrive_expect_tx(full + 8 * s, 2 * valid * box_bytes);
+      for (int i = 0; i < valid; ++i) {
+        const int page = __shfl_sync(kAll, id, box0 - first + i);
+        const int row = ((box0 + i) << shift) & (p.pool.page_size - 1);
+        const uint32_t dst = stages + s * kStageBytes + i * box_bytes;
+        if (elect_one()) {  // (lanes that issue side by side take turns, one copy after the other)
+          tma_page8(dst, &p.k_map, row, c.h, page, full + 8 * s);
+          tma_page8(dst + kHalfBytes, &p.v_map, row, c.h, page, full + 8 * s);
+        }
+      }
+      const int page = __shfl_sync(kAll, id, box0 - first + (block_row >> shift));
+      if (lane < kScaleLanes) {
+        const int token = c.t * kTile + block_row;
+        const bool there = token < c.len && page >= 0 && page < p.pool.num_pages;
+        const float* src = there ? scales + scale_at(p.pool, page, token & (p.pool.page_size - 1), c.h) : scales;
+        cp_async4(stages + Smem::scales + (s * kScaleLanes + lane) * 4, src, there ? 4 : 0);
+        cp_async_arrive(full + 8 * s);
+      }
+    }
+  }
+  return n;
+}
+
+// Rotated, as FP16, and through shared memory into the first product's operands; `back`: what undoes each query's factor.
+template <bool F16, int NT>
+__device__ __forceinline__ void stage_queries(const Pages8DecodeParams& p, Queries<NT>& x, uint32_t mine, uint32_t (&qf)[NT][16],
+                                              float (&back)[NT][2]) {
+  const int lane = threadIdx.x % 32;
+  const LaneChannels at = lane_channels(p.rot, lane % 8, p.rot.table != nullptr);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (at.turns) rotate_lane<F16>(x.lo[nt][i], x.hi[nt][i], x.angles, p.rot.interleaved != 0);
+      const uint32_t row = mine + (lane / 8 + 4 * i) * kQRowBytes;
+      if (!F16) {
+        float v[16];
+        row_values<F16>(x.lo[nt][i], x.hi[nt][i], nullptr, false, v);
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) top = max(top, finite_bits(v[k]));
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(kAll, top, o));
+        // 2^(14 - e) for a largest entry in [2^e, 2^(e + 1)), 2^126 at most
+        const int field = min(127 + 14 + 127 - (int)(top >> 23), kMostField);
+        const float factor = power_of_field(field);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] *= factor;
+        x.lo[nt][i] = pack8<true>(v);
+        x.hi[nt][i] = pack8<true>(v + 8);
+        if (lane % 8 == 0) st_shared16(row + 256, make_uint4(__float_as_uint(inverse_of_field(field)), 0u, 0u, 0u));
+      }
+      st_shared16(row + at.lo * 2, x.lo[nt][i]);
+      st_shared16(row + at.hi * 2, x.hi[nt][i]);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {  // a product's 16 channels, four a lane
+      const uint32_t a = mine + (lane / 4) * kQRowBytes + (16 * j + 4 * (lane % 4)) * 2;
+      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];\n" : "=r"(qf[nt][2 * j]), "=r"(qf[nt][2 * j + 1]) : "r"(a) : "memory");
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      back[nt][j] = 1.f;
+      if (!F16) back[nt][j] = __uint_as_float(ld_shared16(mine + (2 * (lane % 4) + j) * kQRowBytes + 256).x);
+    }
+    __syncwarp();
+  }
+}
+
+// Byte `channel` of row r of a tile; boxes lie one after the other, so that a row's place depends on its number alone.
+__device__ __forceinline__ uint32_t tile_byte(uint32_t tile, int r, int channel) {
+  return tile + swizzled(r, channel / 16) + channel % 16;
+}
+__device__ __forceinline__ uint2 ld_shared8(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared8(uint32_t addr, uint2 v) {
+  asm volatile("st.shared.v2.b32 [%0], {%1,%2};\n" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
+}
+
+// The new token of a decode step, row r of the tile: its block is brought to the scale that it needs, in the pool and over
+// what the stage holds.  Not where the request has grown past its table: its new token has no place there, and the last
+// row is a token's own.  ks, vs: the tile's scales, which may rise.
+template <bool F16>
+__device__ __forceinline__ void place_new_token(const Pages8DecodeParams& p, const Cursor& c, uint32_t kt, uint32_t vt, int r,
+                                                float (&ks)[kTileBlocks], float (&vs)[kTileBlocks]) {
+  if (p.lengths[c.b] != c.len) return;
+  const int lane = threadIdx.x % 32, i = lane % 8;
+  const bool is_v = lane / 8 == 1;
+  const int last = c.len - 1, block = r / kBlock8, before = r % kBlock8;  // tokens that the block has
+  const int page = page_of(p.pool, p.table + (int64_t)c.b * p.table_stride, p.table_stride, last);
+  const int in_page = last & (p.pool.page_size - 1);
+  const Rows& in = is_v ? p.v : p.k;
+  const LaneChannels at = lane_channels(p.rot, i, p.rot.table != nullptr && !is_v);
+  const uint16_t* src = in.data + c.b * in.token_stride + c.h * in.head_stride;
+  float x[16];
+  LaneAngles angles;
+  if (at.turns) angles = lane_angles(p.rot, i, c.b);
+  row_values<F16>(ldg16(src + at.lo), ldg16(src + at.hi), at.turns ? &angles : nullptr, p.rot.interleaved != 0, x);
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) top = max(top, finite_bits(x[k]));
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(kAll, top, o));
+  float old = 0.f;
+#pragma unroll
+  for (int k = 0; k < kTileBlocks; ++k)
+    if (k == block) old = is_v ? vs[k] : ks[k];
+  int field = needed_field(top);
+  if (before > 0) field = max(field, stored_field(old));
+  const float scale = power_of_field(field), inv = inverse_of_field(field);
+  uint8_t* row = (is_v ? p.pool.v : p.pool.k) + code_row(p.pool, max(page, 0), in_page, c.h);
+  if (lane < 16) {  // keys by the first eight lanes, values by the next
+    const uint32_t tile = is_v ? vt : kt;
+    const uint2 lo = encode8(x, inv), hi = encode8(x + 8, inv);
+    st_shared8(tile_byte(tile, r, at.lo), lo);
+    st_shared8(tile_byte(tile, r, at.hi), hi);
+    if (page >= 0) {
+      *reinterpret_cast<uint2*>(row + at.lo) = lo;
+      *reinterpret_cast<uint2*>(row + at.hi) = hi;
+      if (i == 0) (is_v ? p.pool.v_scales : p.pool.k_scales)[scale_at(p.pool, page, in_page, c.h)] = scale;
+    }
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {  // the block's tokens so far, a lane 8 bytes
+    const float from = __shfl_sync(kAll, old, 8 * which), to = __shfl_sync(kAll, scale, 8 * which);
+#pragma unroll
+    for (int k = 0; k < kTileBlocks; ++k)
+      if (k == block) (which ? vs : ks)[k] = to;
+    if (before == 0 || from == to) continue;
+    uint8_t* first = (which ? p.pool.v : p.pool.k) + code_row(p.pool, max(page, 0), in_page - before, c.h);
+    const uint32_t tile = which ? vt : kt;
+    for (int k = lane; k < before * 16; k += 32) {
+      const uint32_t a = tile_byte(tile, r - before + k / 16, k % 16 * 8);
+      const uint2 codes = recode8(ld_shared8(a), from / to);
+      st_shared8(a, codes);
+      if (page >= 0) *reinterpret_cast<uint2*>(first + (k / 16) * p.pool.token_stride + k % 16 * 8) = codes;
     }
   }
   __syncwarp();
-  for (int i = 0; i < 4; ++i) x[i] = staged[4 * lane + i];
-  __syncwarp();
 }
 
-// The row as a block of its own holds it.
-__device__ __forceinline__ void held(float (&x)[4]) {
-  uint32_t top = 0;
-  for (int i = 0; i < 4; ++i) top = max(top, finite_bits(x[i]));
-  const int field = needed_field(__reduce_max_sync(kAll, top));
-  const float inv = inverse_of_field(field), s = power_of_field(field);
-  for (int i = 0; i < 4; i += 2) {
-    const float2 f = half2_bits_to_float2(decode2(encode2(x[i], x[i + 1], inv)));
-    x[i] = f.x * s;
-    x[i + 1] = f.y * s;
+// Two codes of a word's lower and of its upper half as FP16.
+__device__ __forceinline__ uint32_t lower2(uint32_t w) { return decode2(w & 0xffffu); }
+__device__ __forceinline__ uint32_t upper2(uint32_t w) { return decode2(w >> 16); }
+
+// What a warp keeps of its item beside its sums: the exponent field of u.
+template <bool F16, int NT>
+__device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint32_t (&qf)[NT][16], const float (&back)[NT][2],
+                                            uint32_t kt, uint32_t vt, const float (&ks)[kTileBlocks],
+                                            const float (&vs)[kTileBlocks], int seen, float c) {
+  const int lane = threadIdx.x % 32;
+  float s[kTileBlocks][NT][4];
+#pragma unroll
+  for (int mt = 0; mt < kTileBlocks; ++mt) {
+    float s2[NT][4];  // a chain of products for each half of the chunks
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[mt][nt][i] = s2[nt][i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t r[4];
+      ldsm_x4(r, kt + mt * kBlock8 * kHeadDim + swizzled(lane % 16, 2 * j + lane / 16));
+      const uint32_t a[4] = {lower2(r[0]), lower2(r[1]), upper2(r[0]), upper2(r[1])};
+      const uint32_t b[4] = {lower2(r[2]), lower2(r[3]), upper2(r[2]), upper2(r[3])};
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        mma_f16(s[mt][nt], a, qf[nt][4 * j], qf[nt][4 * j + 1]);
+        mma_f16(s2[nt], b, qf[nt][4 * j + 2], qf[nt][4 * j + 3]);
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[mt][nt][i] = (s[mt][nt][i] + s2[nt][i]) * (ks[mt] * back[nt][i % 2]);
+  }
+  // a first scale of the values, or one past the old: the sums so far count that much less
+  float top_scale = vs[0];
+#pragma unroll
+  for (int mt = 1; mt < kTileBlocks; ++mt) top_scale = fmaxf(top_scale, vs[mt]);
+  const int field = stored_field(top_scale);
+  if (field > unit) {
+    const float keep = unit > 0 ? power_of_field(unit) * inverse_of_field(field) : 0.f;
+    unit = field;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[nt][d][i] *= keep;
+  }
+  float share[kTileBlocks];
+#pragma unroll
+  for (int mt = 0; mt < kTileBlocks; ++mt) share[mt] = vs[mt] * inverse_of_field(unit);
+  const int g = lane / 4;
+  uint32_t pf[kTileBlocks][NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    if (seen < kTile) {
+#pragma unroll
+      for (int mt = 0; mt < kTileBlocks; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * mt + g + 8 * (i / 2) >= seen) s[mt][nt][i] = -INFINITY;
+    }
+    float top[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      top[j] = fmaxf(s[0][nt][j], s[0][nt][2 + j]);
+#pragma unroll
+      for (int mt = 1; mt < kTileBlocks; ++mt) top[j] = fmaxf(top[j], fmaxf(s[mt][nt][j], s[mt][nt][2 + j]));
+    }
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      top[0] = fmaxf(top[0], __shfl_xor_sync(kAll, top[0], o));
+      top[1] = fmaxf(top[1], __shfl_xor_sync(kAll, top[1], o));
+    }
+    // a first maximum, or one far past the old: the sums so far count that much less (the same in all lanes of a column)
+    const bool moved = (top[0] - st.m[nt][0]) * c > kRescale || (top[1] - st.m[nt][1]) * c > kRescale;
+    if (__any_sync(kAll, moved)) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float m = fmaxf(st.m[nt][j], top[j]);
+        const float keep = m == st.m[nt][j] ? 1.f : exp2_approx((st.m[nt][j] - m) * c);
+        st.m[nt][j] = m;
+        st.l[nt][j] *= keep;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          st.o[nt][d][j] *= keep;
+          st.o[nt][d][2 + j] *= keep;
+        }
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < kTileBlocks; ++mt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float m = st.m[nt][i % 2];
+        s[mt][nt][i] = exp2_approx(fmaf(s[mt][nt][i] - (m == -INFINITY ? 0.f : m), c, kLift<true>));
+        st.l[nt][i % 2] += s[mt][nt][i];
+        s[mt][nt][i] *= share[mt];
+      }
+      pf[mt][nt][0] = movtrans(pack2<true>(s[mt][nt][0], s[mt][nt][1]));
+      pf[mt][nt][1] = movtrans(pack2<true>(s[mt][nt][2], s[mt][nt][3]));
+    }
+  }
+#pragma unroll
+  for (int mt = 0; mt < kTileBlocks; ++mt)
+#pragma unroll
+    for (int d = 0; d < 8; d += 2) {
+      uint32_t r[4];
+      ldsm_x4_trans(r, vt + mt * kBlock8 * kHeadDim + swizzled(lane % 16, d + lane / 16));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = prmt(r[i], 0u, 0x3120u);  // two tokens of a channel side by side
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t a[4] = {lower2(r[2 * e]), upper2(r[2 * e]), lower2(r[2 * e + 1]), upper2(r[2 * e + 1])};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) mma_f16(st.o[nt][d + e], a, pf[mt][nt][0], pf[mt][nt][1]);
+      }
+    }
+}
+
+template <bool F16, int NT>
+__device__ void consume(const Pages8DecodeParams& p, Cursor c, const Work& w, int tiles, uint32_t base, char* smem,
+                        volatile int* misc) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t full = base + Smem::bars, empty = full + 8 * kStages;
+  const float cs = p.scale * kLog2e;
+  float* scratch = reinterpret_cast<float*>(smem + Smem::scratch);
+  const int* kept = reinterpret_cast<const int*>(smem + Smem::lengths);
+  const volatile float* scales = reinterpret_cast<const volatile float*>(smem + Smem::scales);
+  uint32_t n = 0;
+  bool alive = true;  // false: a wait ran out, and the warp only keeps up with the others' barriers
+  // unit of the first item's first tile
+  int tile_u0 = w.u0 - w.first_unit + kItemCost;
+  Queries<NT> queries;
+  if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);
+  while (tiles > 0) {
+    if (NT > 1) fetch_queries<NT>(p, c.b, c.h, queries);
+    const bool begins = c.t == 0, whole = begins && c.tiles <= tiles;
+    uint32_t qf[NT][16];
+    float back[NT][2];
+    stage_queries<F16, NT>(p, queries, base + Smem::scratch + warp * 8 * kQRowBytes, qf, back);
+    State<NT> st;
+    int unit = 0;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      st.m[nt][0] = st.m[nt][1] = -INFINITY;
+      st.l[nt][0] = st.l[nt][1] = 0.f;
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[nt][d][i] = 0.f;
+    }
+    for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
+      if (n % kConsumers != warp) continue;
+      const int s = n % kStages;
+      alive = alive && wait_warp(full + 8 * s, (n / kStages) & 1, misc, p.status);
+      const uint32_t kt = base + s * kStageBytes, vt = kt + kHalfBytes;
+      const int seen = c.len - c.t * kTile;
+      __syncwarp();
+      if (alive && seen > 0) {
+        float ks[kTileBlocks], vs[kTileBlocks];
+#pragma unroll
+        for (int i = 0; i < kTileBlocks; ++i) {
+          ks[i] = scales[s * kScaleLanes + i];
+          vs[i] = scales[s * kScaleLanes + kTileBlocks + i];
+        }
+        if (seen < kTile) {
+          // what follows the request's last token may be anything, and 0 times NaN is no 0
+          for (int i = seen * 8 + lane; i < kTile * 8; i += 32)
+            st_shared16(vt + swizzled(i / 8, i % 8), make_uint4(0u, 0u, 0u, 0u));
+        }
+        if (seen <= kTile && p.store) place_new_token<F16>(p, c, kt, vt, seen - 1, ks, vs);
+        __syncwarp();
+        attend_tile<F16, NT>(st, unit, qf, back, kt, vt, ks, vs, seen, cs);
+        if (seen <= kTile) fence_proxy_async_shared();  // TMA writes the stage again
+      }
+      __syncwarp();
+      // (not after a wait that ran out: the stage would be filled over a copy whose bytes are still expected)
+      if (alive && lane == 0) mbar_arrive(empty + 8 * s);
+    }
+    const Cursor done = c;
+    if (tiles > 0) {  // the next item's queries come in meanwhile
+      next_item(p, kept, c);
+      if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);  // (of 16 queries they would take the sums' registers)
+    }
+    const float in_full = unit > 0 ? power_of_field(unit) : 0.f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[nt][d][i] *= in_full;
+    named_barrier<kConsumers * 32>(1);  // every warp has read its queries from the scratch
+    finish_item<Kind<F16>, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs);
+    tile_u0 += done.tiles + kItemCost;
   }
 }
 
-template <bool F16>
-__global__ void __launch_bounds__(kThreads) pages8_decode_kernel(const __grid_constant__ Pages8DecodeParams p) {
-  __shared__ float staged[kThreads / 32][128];
+template <bool F16, int NT>
+__global__ void __launch_bounds__(kThreads, 2) pages8_decode_kernel(const __grid_constant__ Pages8DecodeParams p) {
+  extern __shared__ __align__(1024) char smem[];
+  const uint32_t base = smem_u32(smem), full = base + Smem::bars, empty = full + 8 * kStages;
+  volatile int* misc = reinterpret_cast<int*>(smem + Smem::misc);  // [0] abort, [1] last part, [8 ..] scan
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(full + 8 * i, 1 + kScaleLanes);
+      mbar_init(empty + 8 * i, 1);
+    }
+    mbar_init_fence();
+    misc[0] = 0;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&p.k_map);
+    prefetch_tensormap(&p.v_map);
+  }
   grid_launch_dependents();
   grid_dependency_wait();
-  const int item = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int heads = p.group * p.pool.heads;
-  const int b = item / heads, qh = item - b * heads, h = qh / p.group;
-  if (b >= p.batch) return;
-  float* mine = staged[threadIdx.x / 32];
-  const int cap = p.table_stride << p.pool.page_shift, given = p.lengths[b], len = min(max(given, 0), cap);
-  const int* table = p.table + (int64_t)b * p.table_stride;
-  float q[4];
-  load_row<F16>(p.q, p.rot, true, b, qh, mine, true, q);
-  float m = -INFINITY, l = 0.f, o[4] = {};
-  for (int t = 0; t < len; ++t) {
-    const int page = page_of(p.pool, table, p.table_stride, t), at = t & (p.pool.page_size - 1);
-    float k[4] = {}, v[4] = {};
-    if (page >= 0) {
-      const int64_t row = code_row(p.pool, page, at, h) + 4 * lane, block = scale_at(p.pool, page, at, h);
-      const uint32_t kc = *reinterpret_cast<const uint32_t*>(p.pool.k + row), vc = *reinterpret_cast<const uint32_t*>(p.pool.v + row);
-      const float ks = p.pool.k_scales[block], vs = p.pool.v_scales[block];
-      for (int i = 0; i < 4; i += 2) {
-        const float2 a = half2_bits_to_float2(decode2(kc >> 8 * i & 0xffffu)), c = half2_bits_to_float2(decode2(vc >> 8 * i & 0xffffu));
-        k[i] = a.x * ks;
-        k[i + 1] = a.y * ks;
-        v[i] = c.x * vs;
-        v[i + 1] = c.y * vs;
-      }
-    } else if (p.store && t == given - 1) {  // it has no block to be in
-      load_row<F16>(p.k, p.rot, true, b, h, mine, false, k);
-      load_row<F16>(p.v, p.rot, false, b, h, mine, false, v);
-      held(k);
-      held(v);
-    }
-    const float s = warp_sum(q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3]) * p.scale;
-    const float top = fmaxf(m, s), keep = expf(m - top), e = expf(s - top);
-    m = top;
-    l = l * keep + e;
-    for (int i = 0; i < 4; ++i) o[i] = o[i] * keep + e * v[i];
+  prefetch_queries(p);
+  Work w;
+  Cursor c;
+  int* kept = reinterpret_cast<int*>(smem + Smem::lengths);
+  const int tiles = find_work(p, const_cast<int*>(misc) + 8, kept, w, c);
+  if (tiles == 0) return;
+  uint32_t asked = 0;
+  if (threadIdx.x / 32 == kConsumers) {
+    fence_proxy_async_global();  // pages written by ordinary stores of earlier launches
+    asked = produce(p, c, tiles, kept, base, full, empty, misc);
+  } else {
+    consume<F16, NT>(p, c, w, tiles, base, smem, misc);
   }
-  const float r = len > 0 ? 1.f / l : 0.f;
-  uint16_t* out = p.out.data + b * p.out.token_stride + qh * p.out.head_stride + 4 * lane;
-  for (int i = 0; i < 4; ++i) o[i] = in_range<F16>(o[i] * r);
-  *reinterpret_cast<uint2*>(out) = make_uint2(pack2<F16>(o[0], o[1]), pack2<F16>(o[2], o[3]));
-  if (p.lse && lane == 0) p.lse[(int64_t)b * heads + qh] = len > 0 ? m + logf(l) : -INFINITY;
+  __syncthreads();
+  if (misc[0]) {  // a CTA that gave up leaves once the copies it asked for have landed
+    for (uint32_t n = asked > kStages ? asked - kStages : 0; n < asked; ++n)
+      drain_phase(full + 8 * (n % kStages), (n / kStages) & 1);
+  }
+}
+
+template <bool F16, int NT>
+cudaError_t launch(const Pages8DecodeParams& p, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};  // devices whose shared-memory limit is raised
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(pages8_decode_kernel<F16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem::bytes);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch_overlapped(pages8_decode_kernel<F16, NT>, dim3((unsigned)decode_ctas()), kThreads, Smem::bytes, s, p);
 }
 
 }  // namespace
 
 cudaError_t launch_pages8_decode(const Pages8DecodeParams& p, bool f16, cudaStream_t s) {
-  if (p.store) {
-    Pages8AppendParams a = {};
-    a.pool = p.pool;
-    a.rot = p.rot;
-    a.tokens = a.requests = p.batch;
-    a.k = p.k;
-    a.v = p.v;
-    a.table = p.table;
-    a.table_stride = p.table_stride;
-    a.lengths = p.lengths;
-    const cudaError_t e = launch_pages8_append(a, f16, s);
-    if (e != cudaSuccess) return e;
-  }
-  const int64_t warps = (int64_t)p.batch * p.group * p.pool.heads, blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
-  if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-  const dim3 grid((unsigned)blocks);
-  return f16 ? launch_overlapped(pages8_decode_kernel<true>, grid, kThreads, 0, s, p)
-             : launch_overlapped(pages8_decode_kernel<false>, grid, kThreads, 0, s, p);
+  if (p.group <= 8) return f16 ? launch<true, 1>(p, s) : launch<false, 1>(p, s);
+  return f16 ? launch<true, 2>(p, s) : launch<false, 2>(p, s);
 }
 
 }  // namespace hg

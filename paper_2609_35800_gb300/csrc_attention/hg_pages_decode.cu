@@ -28,28 +28,15 @@
 //   O^T[channel][query] += V^T . P^T A = values (ldmatrix.trans), B = P^T (movmatrix of the scores' fragment)
 // Scores, maxima, sums and outputs are held in 32 bits; probabilities are rounded to the cache's type for the second
 // product only, lifted in FP16 (kLift).  The running maximum moves when a score passes it by more than 2^8.
-#include "hg_rows.cuh"
-#include "hg_wait.cuh"
+#include "hg_pages_split.cuh"
 
 namespace hg {
 namespace {
 
-constexpr int kTile = kDecodeTile, kTileShift = 5;
-static_assert(kTile == 1 << kTileShift, "tile");
 constexpr int kStages = 6;
-constexpr int kStageBytes = 2 * kTile * kHeadDim * 2;  // keys, then values
-constexpr int kConsumers = 3;
-constexpr int kThreads = (kConsumers + 1) * 32;
 static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
+constexpr int kStageBytes = 2 * kTile * kHeadDim * 2;  // keys, then values
 constexpr int kQRowBytes = 272;  // a staged query row: 256 bytes, 16 more so that ldmatrix meets every bank once
-constexpr int kGroups = kConsumers * 4;  // of eight threads
-constexpr unsigned kAll = 0xffffffffu;
-
-constexpr int kItemCost = kDecodeItemCost;
-constexpr int kJoinCost = 24;  // a ticket and a join, in tiles
-constexpr int kKeptLengths = 72;
-constexpr int kJoinCtas = kDecodeJoinCtas, kJoinCounters = kDecodeJoinCounters;
-constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l; rows 4 banks apart
 
 // Shared memory, two CTAs an SM.  The staged queries (8 rows a warp) and the warps' parts that are added up at an item's
 // end (8 queries at a time) take turns in one region.
@@ -65,27 +52,6 @@ static_assert(Smem::scratch_bytes >= kConsumers * 8 * kQRowBytes, "queries are s
 static_assert((8 + 12 + kConsumers + 1) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
 static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 
-// Where a run of tiles stands.
-struct Cursor {
-  int b, h, t;     // request, KV head, tile of its item
-  int len, tiles;  // of request b
-};
-
-__device__ __forceinline__ int request_length(const PagesDecodeParams& p, int b) {
-  return min(max(p.lengths[b], 0), p.table_stride << p.pool.page_shift);
-}
-// A request without a token counts as a tile too: its zeros have to be written.
-__device__ __forceinline__ int tiles_of(int len) { return max(1, (len + kTile - 1) / kTile); }
-
-__device__ __forceinline__ void next_item(const PagesDecodeParams& p, const int* kept, Cursor& c) {
-  c.t = 0;
-  if (++c.h < p.pool.heads) return;
-  c.h = 0;
-  if (++c.b >= p.batch) return;
-  c.len = c.b < kKeptLengths ? kept[c.b] : request_length(p, c.b);
-  c.tiles = tiles_of(c.len);
-}
-
 __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int row, int head, int page, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], "
@@ -94,121 +60,16 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// The launch's units, cut into `ctas` runs of `share` units, the first `more` of them one longer; those of this CTA are
-// [u0, u1).
-struct Work {
-  int u0, u1, total, ctas, share, more;
-  int first_unit;  // of its item, that u0 is
-  __device__ __forceinline__ int start_of(int cta) const { return cta * share + min(cta, more); }
-  __device__ __forceinline__ int cta_of(int u) const {
-    const int longer = more * (share + 1);
-    return u < longer ? u / (share + 1) : more + (u - longer) / share;
+template <bool F16>
+struct Kind {
+  static constexpr bool kF16 = F16;
+  static constexpr float kUnlift = F16 ? 0x1p-7f : 1.f;
+  static __device__ __forceinline__ float result(float x) { return x; }
+  static __device__ __forceinline__ void place(float* row, int g, float first, float second) {
+    row[g] = first;
+    row[8 + g] = second;
   }
 };
-
-// The CTA's work, the first tile of it and how many there are; 0: none.  Every thread adds up the units of its share of
-// the requests; the one whose share holds u0 looks for it there.
-__device__ int find_work(const PagesDecodeParams& p, int* scan, int* kept, Work& w, Cursor& c) {
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, heads = p.pool.heads;
-  const int per = (p.batch + kThreads - 1) / kThreads;
-  const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
-  int mine = 0, longest = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int len = request_length(p, b), units = tiles_of(len) + kItemCost;
-    if (b < kKeptLengths) kept[b] = len;
-    mine += units;
-    longest = max(longest, units);
-  }
-  longest = __reduce_max_sync(kAll, longest);
-  int sum = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(kAll, sum, o);
-    if (lane >= o) sum += x;
-  }
-  if (lane == 31) {
-    scan[warp] = sum;
-    scan[12 + warp] = longest;
-  }
-  __syncthreads();
-  int before = sum - mine, all = 0;
-#pragma unroll
-  for (int i = 0; i < kConsumers + 1; ++i) {
-    if (i < warp) before += scan[i];
-    all += scan[i];
-    longest = max(longest, scan[12 + i]);
-  }
-  w.total = all * heads;
-  w.ctas = min((int)gridDim.x, w.total);
-  if ((int)blockIdx.x >= w.ctas) return 0;
-  w.share = w.total / w.ctas;
-  w.more = w.total - w.share * w.ctas;
-  w.u0 = w.start_of(blockIdx.x);
-  w.u1 = w.start_of(blockIdx.x + 1);
-  int left = w.u0 - before * heads;
-  if (left >= 0 && left < mine * heads) {
-    int b = b0, len = 0, units = 0;
-    for (;; ++b) {
-      len = b < kKeptLengths ? kept[b] : request_length(p, b);
-      units = tiles_of(len) + kItemCost;
-      if (left < units * heads) break;
-      left -= units * heads;
-    }
-    scan[8] = b;
-    scan[9] = left / units;
-    scan[10] = left - scan[9] * units;
-    scan[11] = len;
-  }
-  __syncthreads();
-  w.first_unit = scan[10];
-  c = {scan[8], scan[9], max(0, w.first_unit - kItemCost), scan[11], tiles_of(scan[11])};
-  int tiles = 0;
-  if (longest <= w.share + kJoinCost) {
-    // from the first item that begins at u0 or later to the last that begins before u1
-    int at = w.u0;
-    if (w.first_unit > 0) {
-      at += c.tiles + kItemCost - w.first_unit;
-      w.first_unit = 0;
-      if (at < w.u1) next_item(p, kept, c);
-    }
-    w.u0 = at;
-    for (Cursor x = c; at < w.u1;) {
-      tiles += x.tiles;
-      at += x.tiles + kItemCost;
-      if (at < w.u1) next_item(p, kept, x);
-    }
-    return tiles;
-  }
-  // the run's units less those that stand for fixed costs
-  int rest = w.u1 - w.u0, skip = max(0, kItemCost - w.first_unit);
-  for (Cursor x = c; rest > skip; skip = kItemCost) {
-    rest -= skip;
-    const int n = min(rest, x.tiles - x.t);
-    tiles += n;
-    rest -= n;
-    if (rest > 0) next_item(p, kept, x);
-  }
-  return tiles;
-}
-
-// Lets the launch's page ids, queries and rotations into L2 before the caches' reads fill the memory's queues: a request
-// by each CTA in turn.
-__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
-__device__ void prefetch_queries(const PagesDecodeParams& p) {
-  for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
-    const int heads = p.group * p.pool.heads;
-    for (int i = 32 * threadIdx.x; i < p.table_stride; i += 32 * kThreads)
-      prefetch_l2(p.table + (int64_t)b * p.table_stride + i);
-    for (int i = threadIdx.x; i < 2 * heads; i += kThreads)
-      prefetch_l2(p.q.data + b * p.q.token_stride + (i / 2) * p.q.head_stride + (i % 2) * 64);
-    if (p.rot.table == nullptr) continue;
-    for (int i = threadIdx.x; i < 3 * 4; i += kThreads) {
-      if (i >= 4 && p.rot.position_stride == 0) break;
-      const int pos = min(max(p.rot.positions[(int64_t)(i / 4) * p.rot.position_stride + b], 0), p.rot.table_len - 1);
-      if (i % 4 * 32 < 2 * p.rot.half) prefetch_l2(p.rot.table + (int64_t)pos * (2 * p.rot.half) + i % 4 * 32);
-    }
-  }
-}
 
 // Copies the CTA's tiles into the ring, in order; returns how many it asked for.
 __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int tiles, const int* kept, uint32_t stages, uint32_t full,
@@ -248,43 +109,10 @@ __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int tiles, con
   return n;
 }
 
-// What a consumer warp keeps of its item: queries 8 nt + 2 (lane % 4) and the next one (rows of S^T, columns of O^T).
-template <int NT>
-struct State {
-  float m[NT][2], l[NT][2];  // l: this lane's own tokens
-  float o[NT][8][4];         // [query tile][16 channels][fragment]
-};
-
 template <bool F16>
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if (F16) mma_f16(d, a, b0, b1);
   else mma_bf16(d, a, b0, b1);
-}
-
-// An item's query rows on their way: 8 lanes a row, four rows at a time.
-template <int NT>
-struct Queries {
-  uint4 lo[NT][2], hi[NT][2];
-  LaneAngles angles;
-};
-
-template <int NT>
-__device__ __forceinline__ void fetch_queries(const PagesDecodeParams& p, int b, int h, Queries<NT>& x) {
-  const int lane = threadIdx.x % 32, c = lane % 8;
-  const LaneChannels at = lane_channels(p.rot, c, p.rot.table != nullptr);
-  const uint16_t* row = p.q.data + b * p.q.token_stride + (int64_t)h * p.group * p.q.head_stride;
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int q = nt * 8 + lane / 8 + 4 * i;
-      x.lo[nt][i] = x.hi[nt][i] = make_uint4(0u, 0u, 0u, 0u);
-      if (q < p.group) {
-        x.lo[nt][i] = ldg16(row + q * p.q.head_stride + at.lo);
-        x.hi[nt][i] = ldg16(row + q * p.q.head_stride + at.hi);
-      }
-    }
-  if (at.turns) x.angles = lane_angles(p.rot, c, b);
 }
 
 // Rotated, and through shared memory into the first product's operands.
@@ -442,221 +270,6 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, const uint32_t (&qf)[
     }
 }
 
-// A CTA's part of the item that begins in its run (`begins`), or of the one that began before it.
-__device__ __forceinline__ float* partial_of(const PagesDecodeParams& p, int cta, bool begins) {
-  return p.partials + ((int64_t)cta * 2 + (begins ? 1 : 0)) * p.group * kPartialFloats;
-}
-
-// A query's sums, 16 channels of them.
-struct Part {
-  float m = -INFINITY, l = 0.f, o[16] = {};
-};
-// Adds up N rows of sums in shared memory, `apart` floats from one to the next: one maximum, then independent terms.
-template <int N>
-__device__ __forceinline__ Part add_rows(const float* row, int apart, int count, int channel, float cs) {
-  Part a;
-  float2 ml[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    ml[i] = i < count ? *reinterpret_cast<const float2*>(row + i * apart + kHeadDim) : make_float2(-INFINITY, 0.f);
-    a.m = fmaxf(a.m, ml[i].x);
-  }
-  const float base = a.m == -INFINITY ? 0.f : a.m;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (i >= count) break;
-    const float e = exp2_approx((ml[i].x - base) * cs);
-    a.l += ml[i].y * e;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(row + i * apart + channel + 4 * k);
-      a.o[4 * k] += x.x * e;
-      a.o[4 * k + 1] += x.y * e;
-      a.o[4 * k + 2] += x.z * e;
-      a.o[4 * k + 3] += x.w * e;
-    }
-  }
-  return a;
-}
-__device__ __forceinline__ void store_part(const Part& a, float* channels, float* ml, int channel) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<float4*>(channels + channel + 4 * i) =
-        make_float4(a.o[4 * i], a.o[4 * i + 1], a.o[4 * i + 2], a.o[4 * i + 3]);
-  if (channel == 0) *reinterpret_cast<float2*>(ml) = make_float2(a.m, a.l);
-}
-
-// out = o / l in the cache's type, and the query's log-sum-exp (o and l are lifted alike).
-template <bool F16>
-__device__ __forceinline__ void write_query(const PagesDecodeParams& p, int b, int h, int len, int q, int channel,
-                                            const Part& a) {
-  const float r = len > 0 ? 1.0f / a.l : 0.f;
-  const int head = h * p.group + q;
-  uint16_t* out = p.out.data + b * p.out.token_stride + head * p.out.head_stride + channel;
-  uint32_t x[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = pack2<F16>(a.o[2 * i] * r, a.o[2 * i + 1] * r);
-  *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<uint4*>(out + 8) = make_uint4(x[4], x[5], x[6], x[7]);
-  if (p.lse && channel == 0)
-    p.lse[(int64_t)b * p.pool.heads * p.group + head] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l * (F16 ? 0x1p-7f : 1.f));
-}
-
-// Takes a number; what the CTA's threads wrote before their last barrier is visible to whoever takes a later one.
-__device__ __forceinline__ uint32_t take_ticket(uint32_t* counter) {
-  uint32_t n;
-  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;\n" : "=r"(n) : "l"(counter) : "memory");
-  return n;
-}
-
-// The CTA's part of an item over the CTAs [cta0, cta1] is written: whoever comes last joins them.  (Inlined: called, it
-// cost launches of 10 to 30 us up to 5%.)
-template <bool F16>
-__device__ __forceinline__ void join_item(const PagesDecodeParams& p, int b, int h, int len, int cta0, int cta1, float* scratch,
-                                       volatile int* misc, float cs) {
-  const int lane = threadIdx.x % 32, mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
-  // up to six queries: several groups of threads share a query's parts, each takes every `subs`-th
-  const int subs = max(1, kGroups / p.group);
-  const bool two_levels = cta1 - cta0 >= 24 * subs;
-  for (int level = two_levels ? 0 : 1; level < 2; ++level) {
-    // the parts of this level: CTA `first` (level 1 of two: then the first CTA of each further 16), `stride` apart
-    const int round = blockIdx.x & ~(kJoinCtas - 1);
-    const int first = level == 0 ? max(cta0, round) : cta0, stride = two_levels && level == 1 ? kJoinCtas : 1;
-    const int count = level == 0 ? min(cta1, round + kJoinCtas - 1) - first + 1
-                                 : two_levels ? cta1 / kJoinCtas - cta0 / kJoinCtas + 1 : cta1 - cta0 + 1;
-    const auto part = [&](int k) {
-      const int cta = k == 0 ? first : stride == 1 ? first + k : (first & ~(kJoinCtas - 1)) + k * stride;
-      return partial_of(p, cta, cta == cta0);
-    };
-    if (count > 1) {
-      if (threadIdx.x == 0) {
-        uint32_t* counter = level == 0 ? p.counters + blockIdx.x / kJoinCtas * 2 + (cta0 >= round)
-                                       : p.counters + kJoinCounters + (int64_t)b * p.pool.heads + h;
-        const bool last = take_ticket(counter) == (uint32_t)(count - 1);
-        if (last) *counter = 0u;
-        misc[1] = last;
-      }
-      named_barrier<kConsumers * 32>(1);
-      if (!misc[1]) return;
-    }
-    const int sub = mine / p.group, lane8 = lane % 8;
-    const unsigned group_mask = 0xffu << (lane & 24);
-    for (int q = subs > 1 ? mine % p.group : mine; q < p.group && (subs == 1 || sub < subs); q += kGroups) {
-      Part a;
-#pragma unroll 1
-      for (int k0 = subs > 1 ? sub : 0; k0 < count; k0 += 8 * subs) {
-        // eight parts at a time: a lane has one's m and l, all lanes 16 channels of each, of four at once
-        const int k = k0 + lane8 * subs;
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (k < count) ml = __ldcg(reinterpret_cast<const float2*>(part(k) + q * kPartialFloats));
-        float e = 0.f;
-#pragma unroll
-        for (int j0 = 0; j0 < 8; j0 += 4) {
-          float4 o[4][4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int kj = k0 + (j0 + j) * subs;
-            const float* row = part(kj) + q * kPartialFloats + 4 + channel;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              o[j][i] = kj < count ? __ldcg(reinterpret_cast<const float4*>(row + 4 * i)) : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-          if (j0 == 0) {
-            float top = fmaxf(a.m, ml.x);
-#pragma unroll
-            for (int i = 1; i < 8; i <<= 1) top = fmaxf(top, __shfl_xor_sync(group_mask, top, i));
-            const float base = top == -INFINITY ? 0.f : top;
-            const float keep = exp2_approx((a.m - base) * cs);
-            e = exp2_approx((ml.x - base) * cs);
-            float l = ml.y * e;
-#pragma unroll
-            for (int i = 1; i < 8; i <<= 1) l += __shfl_xor_sync(group_mask, l, i);
-            a.m = top;
-            a.l = a.l * keep + l;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) a.o[i] *= keep;
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float ej = __shfl_sync(group_mask, e, (lane & 24) + j0 + j);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              a.o[4 * i] += o[j][i].x * ej;
-              a.o[4 * i + 1] += o[j][i].y * ej;
-              a.o[4 * i + 2] += o[j][i].z * ej;
-              a.o[4 * i + 3] += o[j][i].w * ej;
-            }
-          }
-          if (k0 + 4 * subs >= count) break;
-        }
-      }
-      if (subs > 1) {  // then this is the only round
-        float* row = scratch + (sub * p.group + q) * kSumFloats;
-        store_part(a, row, row + kHeadDim, channel);
-      } else if (level == 1) {
-        write_query<F16>(p, b, h, len, q, channel, a);
-      } else {
-        float* row = part(0) + q * kPartialFloats;
-        store_part(a, row + 4, row, channel);
-      }
-    }
-    if (subs > 1) {
-      named_barrier<kConsumers * 32>(1);
-      if (mine < p.group) {
-        const Part a = add_rows<kGroups>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
-        if (level == 1) {
-          write_query<F16>(p, b, h, len, mine, channel, a);
-        } else {
-          float* row = part(0) + mine * kPartialFloats;
-          store_part(a, row + 4, row, channel);
-        }
-      }
-    }
-    named_barrier<kConsumers * 32>(1);  // the scratch is free again; the joined part is written
-  }
-}
-
-// The end of the CTA's part of an item: the warps' sums are added up, 8 queries at a time, 8 threads to a query; a whole
-// item is written, a part goes to the workspace, and the last part's CTA joins them all.
-template <bool F16, int NT>
-__device__ void finish_item(const PagesDecodeParams& p, State<NT>& st, const Cursor& c, bool whole, bool begins, int tile_u0,
-                            const Work& w, float* scratch, volatile int* misc, float cs) {
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, tq = lane % 4;
-  const int mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 4; i < 32; i <<= 1) st.l[nt][j] += __shfl_xor_sync(kAll, st.l[nt][j], i);
-    if (nt > 0) named_barrier<kConsumers * 32>(1);  // the first queries' sums are read
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float* row = scratch + (warp * 8 + 2 * tq + j) * kSumFloats;
-#pragma unroll
-      for (int d = 0; d < 8; ++d) {
-        row[16 * d + g] = st.o[nt][d][j];
-        row[16 * d + 8 + g] = st.o[nt][d][2 + j];
-      }
-      if (g == 0) *reinterpret_cast<float2*>(row + kHeadDim) = make_float2(st.m[nt][j], st.l[nt][j]);
-    }
-    named_barrier<kConsumers * 32>(1);
-    const int q = 8 * nt + mine;
-    if (mine < 8 && q < p.group) {
-      const Part a = add_rows<kConsumers>(scratch + mine * kSumFloats, 8 * kSumFloats, kConsumers, channel, cs);
-      if (whole) {
-        write_query<F16>(p, c.b, c.h, c.len, q, channel, a);
-      } else {
-        float* row = partial_of(p, blockIdx.x, begins) + q * kPartialFloats;
-        store_part(a, row + 4, row, channel);
-      }
-    }
-  }
-  named_barrier<kConsumers * 32>(1);  // the scratch is free again; the part is written
-  if (whole) return;
-  join_item<F16>(p, c.b, c.h, c.len, w.cta_of(tile_u0), w.cta_of(tile_u0 + c.tiles - 1), scratch, misc, cs);
-}
-
 template <bool F16, int NT>
 __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int tiles, uint32_t base, char* smem,
                         volatile int* misc) {
@@ -715,7 +328,7 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
       if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);  // (of 16 queries they would take the sums' registers)
     }
     named_barrier<kConsumers * 32>(1);  // every warp has read its queries from the scratch
-    finish_item<F16, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs);
+    finish_item<Kind<F16>, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs);
     tile_u0 += done.tiles + kItemCost;
   }
 }
