@@ -98,7 +98,7 @@ struct PagesPlanParams {
 constexpr int kPlanMaxBatch = 16384;
 
 // Tokens of a tile of the paged decode; a tensor map's box covers a tile of one page, or the page where that is smaller.
-constexpr int kDecodeTile = 32;
+constexpr int kDecodeTile = 32, kDecodeTile8 = 64;  // (of 16-bit and of 8-bit pages: 16 KB either way)
 constexpr int kDecodeItemCost = 12;  // fixed costs of a (request, KV head), in tiles
 // Parts of an item over many CTAs are joined 16 CTAs at a time first; two counters for each 16, ahead of the items' ones.
 constexpr int kDecodeJoinCtas = 16, kDecodeJoinCounters = 128;

@@ -38,18 +38,25 @@ __device__ __forceinline__ uint2 encode8(const float* x, float inv) {
                     encode2(x[4], x[5], inv) | encode2(x[6], x[7], inv) << 16);
 }
 
-// Two codes as FP16, exactly.
-__device__ __forceinline__ uint32_t decode2(uint32_t codes) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
+// The two codes of a word's lower half, and of its upper half, as FP16, exactly.  (One instruction each: through the
+// conversion functions of the headers, halves taken apart and put together again, a tile of the decode took 925
+// instructions, XXX this way.)
+__device__ __forceinline__ void decode4(uint32_t w, uint32_t& lower, uint32_t& upper) {
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}\n"
+      : "=r"(lower), "=r"(upper)
+      : "r"(w));
 }
 __device__ __forceinline__ void decode8(uint2 codes, float* x) {
   const uint32_t w[2] = {codes.x, codes.y};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = half2_bits_to_float2(decode2(w[i / 2] >> 16 * (i % 2) & 0xffffu));
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
+  for (int i = 0; i < 2; ++i) {
+    uint32_t lower, upper;
+    decode4(w[i], lower, upper);
+    const float2 a = half2_bits_to_float2(lower), b = half2_bits_to_float2(upper);
+    x[4 * i] = a.x;
+    x[4 * i + 1] = a.y;
+    x[4 * i + 2] = b.x;
+    x[4 * i + 3] = b.y;
   }
 }
 // Codes times `ratio`, as codes again.

@@ -35,7 +35,7 @@ CUresult encode_pages8(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* ma
   // the stride of an axis of length 1 is never taken
   const cuuint64_t strides[3] = {(cuuint64_t)p.token_stride, p.heads > 1 ? (cuuint64_t)p.head_stride : 128,
                                  p.num_pages > 1 ? (cuuint64_t)p.page_stride : 128};
-  const cuuint32_t box[4] = {kHeadDim, (cuuint32_t)std::min(p.page_size, kDecodeTile), 1, 1};
+  const cuuint32_t box[4] = {kHeadDim, (cuuint32_t)std::min(p.page_size, kDecodeTile8), 1, 1};
   const cuuint32_t steps[4] = {1, 1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, data, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);

@@ -24,6 +24,9 @@ namespace hg {
 namespace {
 
 constexpr int kStages = 6;
+constexpr int kTile = kDecodeTile8, kTileShift = 6;
+static_assert(kTile == 1 << kTileShift, "tile");
+constexpr int kConsumers = 3;
 static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
 constexpr int kHalfBytes = kTile * kHeadDim;   // keys; then values
 constexpr int kStageBytes = 2 * kHalfBytes;
@@ -49,6 +52,7 @@ static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 
 template <bool F16>
 struct Kind {
+  static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = 0x1p-7f;
   static __device__ __forceinline__ float result(float x) { return in_range<F16>(x); }
@@ -74,6 +78,7 @@ __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
 }
 
 // Copies the CTA's tiles into the ring, in order; returns how many it asked for.
+template <class K>
 __device__ uint32_t produce(const Pages8DecodeParams& p, Cursor c, int tiles, const int* kept, uint32_t stages, uint32_t full,
                             uint32_t empty, volatile int* abort) {
   const int lane = threadIdx.x % 32;
@@ -86,7 +91,7 @@ __device__ uint32_t produce(const Pages8DecodeParams& p, Cursor c, int tiles, co
   uint32_t n = 0;
   // 32 boxes' page ids, a lane each, from box `first` of request `of` on
   int of = -1, first = 0, id = 0;
-  for (; tiles > 0; next_item(p, kept, c)) {
+  for (; tiles > 0; next_item<K>(p, kept, c)) {
     const int* ids = p.table + (int64_t)c.b * p.table_stride;
     for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
       const int box0 = c.t * boxes;  // box number in the item
@@ -244,10 +249,6 @@ __device__ __forceinline__ void place_new_token(const Pages8DecodeParams& p, con
   __syncwarp();
 }
 
-// Two codes of a word's lower and of its upper half as FP16.
-__device__ __forceinline__ uint32_t lower2(uint32_t w) { return decode2(w & 0xffffu); }
-__device__ __forceinline__ uint32_t upper2(uint32_t w) { return decode2(w >> 16); }
-
 // What a warp keeps of its item beside its sums: the exponent field of u.
 template <bool F16, int NT>
 __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint32_t (&qf)[NT][16], const float (&back)[NT][2],
@@ -266,8 +267,11 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint
     for (int j = 0; j < 4; ++j) {
       uint32_t r[4];
       ldsm_x4(r, kt + mt * kBlock8 * kHeadDim + swizzled(lane % 16, 2 * j + lane / 16));
-      const uint32_t a[4] = {lower2(r[0]), lower2(r[1]), upper2(r[0]), upper2(r[1])};
-      const uint32_t b[4] = {lower2(r[2]), lower2(r[3]), upper2(r[2]), upper2(r[3])};
+      uint32_t a[4], b[4];
+      decode4(r[0], a[0], a[2]);
+      decode4(r[1], a[1], a[3]);
+      decode4(r[2], b[0], b[2]);
+      decode4(r[3], b[1], b[3]);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         mma_f16(s[mt][nt], a, qf[nt][4 * j], qf[nt][4 * j + 1]);
@@ -359,7 +363,9 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint
       for (int i = 0; i < 4; ++i) r[i] = prmt(r[i], 0u, 0x3120u);  // two tokens of a channel side by side
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t a[4] = {lower2(r[2 * e]), upper2(r[2 * e]), lower2(r[2 * e + 1]), upper2(r[2 * e + 1])};
+        uint32_t a[4];
+        decode4(r[2 * e], a[0], a[1]);
+        decode4(r[2 * e + 1], a[2], a[3]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) mma_f16(st.o[nt][d + e], a, pf[mt][nt][0], pf[mt][nt][1]);
       }
@@ -428,7 +434,7 @@ __device__ void consume(const Pages8DecodeParams& p, Cursor c, const Work& w, in
     }
     const Cursor done = c;
     if (tiles > 0) {  // the next item's queries come in meanwhile
-      next_item(p, kept, c);
+      next_item<Kind<F16>>(p, kept, c);
       if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);  // (of 16 queries they would take the sums' registers)
     }
     const float in_full = unit > 0 ? power_of_field(unit) : 0.f;
@@ -445,7 +451,7 @@ __device__ void consume(const Pages8DecodeParams& p, Cursor c, const Work& w, in
 }
 
 template <bool F16, int NT>
-__global__ void __launch_bounds__(kThreads, 2) pages8_decode_kernel(const __grid_constant__ Pages8DecodeParams p) {
+__global__ void __launch_bounds__(kThreads<Kind<F16>>, 2) pages8_decode_kernel(const __grid_constant__ Pages8DecodeParams p) {
   extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_u32(smem), full = base + Smem::bars, empty = full + 8 * kStages;
   volatile int* misc = reinterpret_cast<int*>(smem + Smem::misc);  // [0] abort, [1] last part, [8 ..] scan
@@ -464,16 +470,16 @@ __global__ void __launch_bounds__(kThreads, 2) pages8_decode_kernel(const __grid
   }
   grid_launch_dependents();
   grid_dependency_wait();
-  prefetch_queries(p);
+  prefetch_queries<Kind<F16>>(p);
   Work w;
   Cursor c;
   int* kept = reinterpret_cast<int*>(smem + Smem::lengths);
-  const int tiles = find_work(p, const_cast<int*>(misc) + 8, kept, w, c);
+  const int tiles = find_work<Kind<F16>>(p, const_cast<int*>(misc) + 8, kept, w, c);
   if (tiles == 0) return;
   uint32_t asked = 0;
   if (threadIdx.x / 32 == kConsumers) {
     fence_proxy_async_global();  // pages written by ordinary stores of earlier launches
-    asked = produce(p, c, tiles, kept, base, full, empty, misc);
+    asked = produce<Kind<F16>>(p, c, tiles, kept, base, full, empty, misc);
   } else {
     consume<F16, NT>(p, c, w, tiles, base, smem, misc);
   }
@@ -496,7 +502,7 @@ cudaError_t launch(const Pages8DecodeParams& p, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
-  return launch_overlapped(pages8_decode_kernel<F16, NT>, dim3((unsigned)decode_ctas()), kThreads, Smem::bytes, s, p);
+  return launch_overlapped(pages8_decode_kernel<F16, NT>, dim3((unsigned)decode_ctas()), kThreads<Kind<F16>>, Smem::bytes, s, p);
 }
 
 }  // namespace

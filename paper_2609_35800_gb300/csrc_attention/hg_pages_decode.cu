@@ -34,6 +34,9 @@ namespace hg {
 namespace {
 
 constexpr int kStages = 6;
+constexpr int kTile = kDecodeTile, kTileShift = 5;
+static_assert(kTile == 1 << kTileShift, "tile");
+constexpr int kConsumers = 3;
 static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
 constexpr int kStageBytes = 2 * kTile * kHeadDim * 2;  // keys, then values
 constexpr int kQRowBytes = 272;  // a staged query row: 256 bytes, 16 more so that ldmatrix meets every bank once
@@ -62,6 +65,7 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
 
 template <bool F16>
 struct Kind {
+  static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = F16 ? 0x1p-7f : 1.f;
   static __device__ __forceinline__ float result(float x) { return x; }
@@ -72,6 +76,7 @@ struct Kind {
 };
 
 // Copies the CTA's tiles into the ring, in order; returns how many it asked for.
+template <class K>
 __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int tiles, const int* kept, uint32_t stages, uint32_t full,
                             uint32_t empty, volatile int* abort) {
   const int lane = threadIdx.x % 32;
@@ -81,7 +86,7 @@ __device__ uint32_t produce(const PagesDecodeParams& p, Cursor c, int tiles, con
   uint32_t n = 0;
   // 32 boxes' page ids, a lane each, from box `first` of request `of` on
   int of = -1, first = 0, id = 0;
-  for (; tiles > 0; next_item(p, kept, c)) {
+  for (; tiles > 0; next_item<K>(p, kept, c)) {
     const int* ids = p.table + (int64_t)c.b * p.table_stride;
     for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
       const int box0 = c.t * boxes;  // box number in the item
@@ -324,7 +329,7 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
     }
     const Cursor done = c;
     if (tiles > 0) {  // the next item's queries come in meanwhile
-      next_item(p, kept, c);
+      next_item<Kind<F16>>(p, kept, c);
       if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);  // (of 16 queries they would take the sums' registers)
     }
     named_barrier<kConsumers * 32>(1);  // every warp has read its queries from the scratch
@@ -334,7 +339,7 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
 }
 
 template <bool F16, int NT>
-__global__ void __launch_bounds__(kThreads, 2) pages_decode_kernel(const __grid_constant__ PagesDecodeParams p) {
+__global__ void __launch_bounds__(kThreads<Kind<F16>>, 2) pages_decode_kernel(const __grid_constant__ PagesDecodeParams p) {
   extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_u32(smem), full = base + Smem::bars, empty = full + 8 * kStages;
   volatile int* misc = reinterpret_cast<int*>(smem + Smem::misc);  // [0] abort, [1] last part, [8 ..] scan
@@ -353,16 +358,16 @@ __global__ void __launch_bounds__(kThreads, 2) pages_decode_kernel(const __grid_
   }
   grid_launch_dependents();
   grid_dependency_wait();
-  prefetch_queries(p);
+  prefetch_queries<Kind<F16>>(p);
   Work w;
   Cursor c;
   int* kept = reinterpret_cast<int*>(smem + Smem::lengths);
-  const int tiles = find_work(p, const_cast<int*>(misc) + 8, kept, w, c);
+  const int tiles = find_work<Kind<F16>>(p, const_cast<int*>(misc) + 8, kept, w, c);
   if (tiles == 0) return;
   uint32_t asked = 0;
   if (threadIdx.x / 32 == kConsumers) {
     fence_proxy_async_global();  // pages written by ordinary stores of earlier launches
-    asked = produce(p, c, tiles, kept, base, full, empty, misc);
+    asked = produce<Kind<F16>>(p, c, tiles, kept, base, full, empty, misc);
   } else {
     consume<F16, NT>(p, c, w, tiles, base, smem, misc);
   }
@@ -385,7 +390,7 @@ cudaError_t launch(const PagesDecodeParams& p, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
-  return launch_overlapped(pages_decode_kernel<F16, NT>, dim3((unsigned)decode_ctas()), kThreads, Smem::bytes, s, p);
+  return launch_overlapped(pages_decode_kernel<F16, NT>, dim3((unsigned)decode_ctas()), kThreads<Kind<F16>>, Smem::bytes, s, p);
 }
 
 }  // namespace

@@ -1,7 +1,7 @@
 // The paged decode kernels' division of work and what becomes of its parts: an even share of a launch's tiles for every
 // CTA whatever the requests' lengths, parts of an item joined by the last CTA to arrive, results written.  What a tile
-// holds, and how it is computed, is the kernels' own.  P: their launch parameters; K: kF16 (the rows' type), kUnlift (1 /
-// the factor that probabilities are lifted by), result (what an output entry becomes before it is rounded), place (a fragment's two
+// holds, and how it is computed, is the kernels' own.  P: their launch parameters; K: kTile (tokens of a tile), kConsumers
+// (warps, ahead of the producer's), kF16 (the rows' type), kUnlift (1 / the factor that probabilities are lifted by), result (what an output entry becomes before it is rounded), place (a fragment's two
 // channels into a row of sums).
 #pragma once
 #include "hg_rows.cuh"
@@ -10,18 +10,17 @@
 namespace hg {
 namespace {
 
-constexpr int kTile = kDecodeTile, kTileShift = 5;
-static_assert(kTile == 1 << kTileShift, "tile");
-constexpr int kConsumers = 3;
-constexpr int kThreads = (kConsumers + 1) * 32;
-constexpr int kGroups = kConsumers * 4;  // of eight threads
 constexpr unsigned kAll = 0xffffffffu;
-
 constexpr int kItemCost = kDecodeItemCost;
 constexpr int kJoinCost = 24;  // a ticket and a join, in tiles
 constexpr int kKeptLengths = 72;
 constexpr int kJoinCtas = kDecodeJoinCtas, kJoinCounters = kDecodeJoinCounters;
 constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l; rows 4 banks apart
+
+template <class K>
+constexpr int kThreads = (K::kConsumers + 1) * 32;
+template <class K>
+constexpr int kGroups = K::kConsumers * 4;  // of eight threads
 
 // Where a run of tiles stands.
 struct Cursor {
@@ -34,16 +33,19 @@ __device__ __forceinline__ int request_length(const P& p, int b) {
   return min(max(p.lengths[b], 0), p.table_stride << p.pool.page_shift);
 }
 // A request without a token counts as a tile too: its zeros have to be written.
-__device__ __forceinline__ int tiles_of(int len) { return max(1, (len + kTile - 1) / kTile); }
+template <class K>
+__device__ __forceinline__ int tiles_of(int len) {
+  return max(1, (len + K::kTile - 1) / K::kTile);
+}
 
-template <class P>
+template <class K, class P>
 __device__ __forceinline__ void next_item(const P& p, const int* kept, Cursor& c) {
   c.t = 0;
   if (++c.h < p.pool.heads) return;
   c.h = 0;
   if (++c.b >= p.batch) return;
   c.len = c.b < kKeptLengths ? kept[c.b] : request_length(p, c.b);
-  c.tiles = tiles_of(c.len);
+  c.tiles = tiles_of<K>(c.len);
 }
 
 // The launch's units, cut into `ctas` runs of `share` units, the first `more` of them one longer; those of this CTA are
@@ -60,14 +62,14 @@ struct Work {
 
 // The CTA's work, the first tile of it and how many there are; 0: none.  Every thread adds up the units of its share of
 // the requests; the one whose share holds u0 looks for it there.
-template <class P>
+template <class K, class P>
 __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, heads = p.pool.heads;
-  const int per = (p.batch + kThreads - 1) / kThreads;
+  const int per = (p.batch + kThreads<K> - 1) / kThreads<K>;
   const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
   int mine = 0, longest = 0;
   for (int b = b0; b < b1; ++b) {
-    const int len = request_length(p, b), units = tiles_of(len) + kItemCost;
+    const int len = request_length(p, b), units = tiles_of<K>(len) + kItemCost;
     if (b < kKeptLengths) kept[b] = len;
     mine += units;
     longest = max(longest, units);
@@ -86,7 +88,7 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
   __syncthreads();
   int before = sum - mine, all = 0;
 #pragma unroll
-  for (int i = 0; i < kConsumers + 1; ++i) {
+  for (int i = 0; i < K::kConsumers + 1; ++i) {
     if (i < warp) before += scan[i];
     all += scan[i];
     longest = max(longest, scan[12 + i]);
@@ -103,7 +105,7 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
     int b = b0, len = 0, units = 0;
     for (;; ++b) {
       len = b < kKeptLengths ? kept[b] : request_length(p, b);
-      units = tiles_of(len) + kItemCost;
+      units = tiles_of<K>(len) + kItemCost;
       if (left < units * heads) break;
       left -= units * heads;
     }
@@ -114,7 +116,7 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
   }
   __syncthreads();
   w.first_unit = scan[10];
-  c = {scan[8], scan[9], max(0, w.first_unit - kItemCost), scan[11], tiles_of(scan[11])};
+  c = {scan[8], scan[9], max(0, w.first_unit - kItemCost), scan[11], tiles_of<K>(scan[11])};
   int tiles = 0;
   if (longest <= w.share + kJoinCost) {
     // from the first item that begins at u0 or later to the last that begins before u1
@@ -122,13 +124,13 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
     if (w.first_unit > 0) {
       at += c.tiles + kItemCost - w.first_unit;
       w.first_unit = 0;
-      if (at < w.u1) next_item(p, kept, c);
+      if (at < w.u1) next_item<K>(p, kept, c);
     }
     w.u0 = at;
     for (Cursor x = c; at < w.u1;) {
       tiles += x.tiles;
       at += x.tiles + kItemCost;
-      if (at < w.u1) next_item(p, kept, x);
+      if (at < w.u1) next_item<K>(p, kept, x);
     }
     return tiles;
   }
@@ -139,7 +141,7 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
     const int n = min(rest, x.tiles - x.t);
     tiles += n;
     rest -= n;
-    if (rest > 0) next_item(p, kept, x);
+    if (rest > 0) next_item<K>(p, kept, x);
   }
   return tiles;
 }
@@ -147,16 +149,16 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
 // Lets the launch's page ids, queries and rotations into L2 before the caches' reads fill the memory's queues: a request
 // by each CTA in turn.
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
-template <class P>
+template <class K, class P>
 __device__ void prefetch_queries(const P& p) {
   for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
     const int heads = p.group * p.pool.heads;
-    for (int i = 32 * threadIdx.x; i < p.table_stride; i += 32 * kThreads)
+    for (int i = 32 * threadIdx.x; i < p.table_stride; i += 32 * kThreads<K>)
       prefetch_l2(p.table + (int64_t)b * p.table_stride + i);
-    for (int i = threadIdx.x; i < 2 * heads; i += kThreads)
+    for (int i = threadIdx.x; i < 2 * heads; i += kThreads<K>)
       prefetch_l2(p.q.data + b * p.q.token_stride + (i / 2) * p.q.head_stride + (i % 2) * 64);
     if (p.rot.table == nullptr) continue;
-    for (int i = threadIdx.x; i < 3 * 4; i += kThreads) {
+    for (int i = threadIdx.x; i < 3 * 4; i += kThreads<K>) {
       if (i >= 4 && p.rot.position_stride == 0) break;
       const int pos = min(max(p.rot.positions[(int64_t)(i / 4) * p.rot.position_stride + b], 0), p.rot.table_len - 1);
       if (i % 4 * 32 < 2 * p.rot.half) prefetch_l2(p.rot.table + (int64_t)pos * (2 * p.rot.half) + i % 4 * 32);
@@ -273,7 +275,7 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
                                        volatile int* misc, float cs) {
   const int lane = threadIdx.x % 32, mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
   // up to six queries: several groups of threads share a query's parts, each takes every `subs`-th
-  const int subs = max(1, kGroups / p.group);
+  const int subs = max(1, kGroups<K> / p.group);
   const bool two_levels = cta1 - cta0 >= 24 * subs;
   for (int level = two_levels ? 0 : 1; level < 2; ++level) {
     // the parts of this level: CTA `first` (level 1 of two: then the first CTA of each further 16), `stride` apart
@@ -293,12 +295,12 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
         if (last) *counter = 0u;
         misc[1] = last;
       }
-      named_barrier<kConsumers * 32>(1);
+      named_barrier<K::kConsumers * 32>(1);
       if (!misc[1]) return;
     }
     const int sub = mine / p.group, lane8 = lane % 8;
     const unsigned group_mask = 0xffu << (lane & 24);
-    for (int q = subs > 1 ? mine % p.group : mine; q < p.group && (subs == 1 || sub < subs); q += kGroups) {
+    for (int q = subs > 1 ? mine % p.group : mine; q < p.group && (subs == 1 || sub < subs); q += kGroups<K>) {
       Part a;
 #pragma unroll 1
       for (int k0 = subs > 1 ? sub : 0; k0 < count; k0 += 8 * subs) {
@@ -358,9 +360,9 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
       }
     }
     if (subs > 1) {
-      named_barrier<kConsumers * 32>(1);
+      named_barrier<K::kConsumers * 32>(1);
       if (mine < p.group) {
-        const Part a = add_rows<kGroups>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
+        const Part a = add_rows<kGroups<K>>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
         if (level == 1) {
           write_query<K>(p, b, h, len, mine, channel, a);
         } else {
@@ -369,7 +371,7 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
         }
       }
     }
-    named_barrier<kConsumers * 32>(1);  // the scratch is free again; the joined part is written
+    named_barrier<K::kConsumers * 32>(1);  // the scratch is free again; the joined part is written
   }
 }
 
@@ -386,7 +388,7 @@ __device__ void finish_item(const P& p, State<NT>& st, const Cursor& c, bool who
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int i = 4; i < 32; i <<= 1) st.l[nt][j] += __shfl_xor_sync(kAll, st.l[nt][j], i);
-    if (nt > 0) named_barrier<kConsumers * 32>(1);  // the first queries' sums are read
+    if (nt > 0) named_barrier<K::kConsumers * 32>(1);  // the first queries' sums are read
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       float* row = scratch + (warp * 8 + 2 * tq + j) * kSumFloats;
@@ -394,10 +396,10 @@ __device__ void finish_item(const P& p, State<NT>& st, const Cursor& c, bool who
       for (int d = 0; d < 8; ++d) K::place(row + 16 * d, g, st.o[nt][d][j], st.o[nt][d][2 + j]);
       if (g == 0) *reinterpret_cast<float2*>(row + kHeadDim) = make_float2(st.m[nt][j], st.l[nt][j]);
     }
-    named_barrier<kConsumers * 32>(1);
+    named_barrier<K::kConsumers * 32>(1);
     const int q = 8 * nt + mine;
     if (mine < 8 && q < p.group) {
-      const Part a = add_rows<kConsumers>(scratch + mine * kSumFloats, 8 * kSumFloats, kConsumers, channel, cs);
+      const Part a = add_rows<K::kConsumers>(scratch + mine * kSumFloats, 8 * kSumFloats, K::kConsumers, channel, cs);
       if (whole) {
         write_query<K>(p, c.b, c.h, c.len, q, channel, a);
       } else {
@@ -406,7 +408,7 @@ __device__ void finish_item(const P& p, State<NT>& st, const Cursor& c, bool who
       }
     }
   }
-  named_barrier<kConsumers * 32>(1);  // the scratch is free again; the part is written
+  named_barrier<K::kConsumers * 32>(1);  // the scratch is free again; the part is written
   if (whole) return;
   join_item<K>(p, c.b, c.h, c.len, w.cta_of(tile_u0), w.cta_of(tile_u0 + c.tiles - 1), scratch, misc, cs);
 }
