@@ -438,6 +438,10 @@ class _Types:
         import torch
         self.code = {torch.bfloat16: HG_DTYPE_BF16, torch.float16: HG_DTYPE_F16}
         self.int32, self.float32, self.codes = torch.int32, torch.float32, (torch.float8_e4m3fn, torch.uint8)
+        # the current device and a device's current stream, by their numbers alone; not part of torch's public interface
+        self.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
         return self.__dict__[name]
 
 
@@ -669,15 +673,59 @@ class Pages8:
             self.handle = None
 
 
-def _on_device(where, device, *tensors):
-    """All of a call's tensors on one device, which is the current one (a launch goes to no other)."""
-    for x in tensors:
-        if x is not None and x.get_device() != device:
-            raise ValueError("%s: tensors on %s and on cuda:%d" % (where, x.device, device))
-    import torch
-    if torch.cuda.current_device() != device:
-        raise ValueError("%s: tensors on cuda:%d, the current device is cuda:%d"
-                         % (where, device, torch.cuda.current_device()))
+def _elsewhere(where, name, x, device):
+    raise ValueError("%s: %s is on %s, the call's tensors are on cuda:%d" % (where, name, x.device, device))
+
+
+def _rows_on(where, name, x, tokens, heads, dtype, device):
+    """_rows of a tensor on this device."""
+    if x.dtype is dtype and x.shape == (tokens, heads, 128) and x.get_device() == device:
+        ts, hs, cs = x.stride()
+        if cs == 1:
+            return x.data_ptr(), ts if tokens > 1 else 0, hs if heads > 1 else 0
+    _rows(where, name, x, tokens, heads, dtype)
+    _elsewhere(where, name, x, device)
+
+
+def _ints_on(where, name, x, need, device):
+    """_ints of a tensor on this device."""
+    if x.dtype is _types.int32 and x.is_contiguous() and x.numel() >= need and x.get_device() == device:
+        return x.data_ptr()
+    _ints(where, name, x, need)
+    _elsewhere(where, name, x, device)
+
+
+def _lse_on(where, x, tokens, heads, device):
+    at = _lse(where, x, tokens, heads)
+    if at is not None and x.get_device() != device:
+        _elsewhere(where, "lse", x, device)
+    return at
+
+
+def _workspace_on(where, x, device):
+    at = _workspace(where, x)
+    if x.get_device() != device:
+        _elsewhere(where, "workspace", x, device)
+    return at
+
+
+def _rotated_on(where, rotation, positions, tokens, device):
+    if rotation is None:
+        return None, None
+    if rotation.table.get_device() != device:
+        _elsewhere(where, "the rotation's table", rotation.table, device)
+    parts = rotation.positions
+    if parts > 1 and positions.shape != (parts, tokens):
+        _rotated_by(where, rotation, positions, tokens)
+    return rotation.pointer, _ints_on(where, "positions", positions, parts * tokens, device)
+
+
+def _stream_on(where, stream, device):
+    """_stream for tensors of this device, which has to be the current one: a launch goes to no other."""
+    current = _types.device()
+    if current != device:
+        raise ValueError("%s: the call's tensors are on cuda:%d, the current device is cuda:%d" % (where, device, current))
+    return _types.stream(device) if stream is None else _stream(stream)
 
 
 def hg_pages8_create(k_pages, v_pages, k_scales, v_scales, dtype=None):
@@ -719,14 +767,21 @@ def hg_pages8_destroy(pages):
         pages.handle = None
 
 
-def _requests(where, begin, page_table, lengths=None):
-    """Number of requests, and what says where their tokens lie."""
+def _requests(where, begin, page_table, device):
+    """Number of requests, addresses of what says where their tokens lie, and the table's columns."""
     n = max(begin.numel() - 1, 0)
     if page_table.dim() != 2 or page_table.shape[0] < n:
         raise ValueError("%s: page_table must be [%d][pages]" % (where, n))
     per = page_table.shape[1]
-    bp, tp = _ints(where, "begin", begin, 1), _ints(where, "page_table", page_table, n * per)
-    return n, bp, tp, per, None if lengths is None else _ints(where, "lengths", lengths, n)
+    return (n, _ints_on(where, "begin", begin, 1, device), _ints_on(where, "page_table", page_table, n * per, device), per)
+
+
+def _lengths_table(where, page_table, lengths, batch, device):
+    if page_table.dim() != 2 or page_table.shape[0] < batch:
+        raise ValueError("%s: page_table must be [%d][pages]" % (where, batch))
+    per = page_table.shape[1]
+    return (_ints_on(where, "page_table", page_table, batch * per, device), per,
+            _ints_on(where, "lengths", lengths, batch, device))
 
 
 def hg_pages8_append(pages, q, k, v, rotation, positions, begin, page_table, lengths, q_out=None, k_out=None, v_out=None,
@@ -734,33 +789,31 @@ def hg_pages8_append(pages, q, k, v, rotation, positions, begin, page_table, len
     """Rotate q and k ([tokens][heads][128], any token and head strides; q None: no queries) and store k and v in 8 bits:
     rows begin[r]..begin[r + 1] are the last of the lengths[r] tokens of request r, whose pages are page_table[r].  The
     rotated rows also go to q_out and, where given, k_out; v to v_out."""
-    w, d = "hg_pages8_append", pages.dtype
+    w, d, at = "hg_pages8_append", pages.dtype, pages.device
     n, heads, hq = k.shape[0], pages.shape.num_kv_heads, 0 if q is None else q.shape[1]
     if q is not None and q_out is None:
         raise ValueError("hg_pages8_append: q needs q_out")
-    io = _pack18(*(_rows(w, "q", q, n, hq, d) if hq else _NO_ROWS), *_rows(w, "k", k, n, heads, d),
-                     *_rows(w, "v", v, n, heads, d), *(_rows(w, "q_out", q_out, n, hq, d) if hq else _NO_ROWS),
-                     *(_NO_ROWS if k_out is None else _rows(w, "k_out", k_out, n, heads, d)),
-                     *(_NO_ROWS if v_out is None else _rows(w, "v_out", v_out, n, heads, d)))
-    rp, pp = _rotated_by(w, rotation, positions, n)
-    count, bp, tp, per, lp = _requests(w, begin, page_table, lengths)
-    _on_device(w, pages.device, q, k, v, q_out, k_out, v_out, begin, page_table, lengths,
-               *(() if rotation is None else (rotation.table, positions)))
-    _check(library().hg_pages8_append(pages.handle, n, count, hq, io, rp, pp, bp, tp, per, lp, _stream(stream)), w)
+    io = _pack18(*(_rows_on(w, "q", q, n, hq, d, at) if hq else _NO_ROWS), *_rows_on(w, "k", k, n, heads, d, at),
+                     *_rows_on(w, "v", v, n, heads, d, at), *(_rows_on(w, "q_out", q_out, n, hq, d, at) if hq else _NO_ROWS),
+                     *(_NO_ROWS if k_out is None else _rows_on(w, "k_out", k_out, n, heads, d, at)),
+                     *(_NO_ROWS if v_out is None else _rows_on(w, "v_out", v_out, n, heads, d, at)))
+    rp, pp = _rotated_on(w, rotation, positions, n, at)
+    count, bp, tp, per = _requests(w, begin, page_table, at)
+    _check(library().hg_pages8_append(pages.handle, n, count, hq, io, rp, pp, bp, tp, per,
+                                      _ints_on(w, "lengths", lengths, count, at), _stream_on(w, stream, at)), w)
 
 
 def hg_pages8_dequantize(pages, begin, page_table, k_out, v_out=None, stream=None):
     """The first begin[r + 1] - begin[r] tokens of each request as dense rows begin[r].. of k_out and v_out
     ([rows][kv heads][128] of the pool's row type, any token and head strides; either may be None)."""
-    w, d, heads = "hg_pages8_dequantize", pages.dtype, pages.shape.num_kv_heads
+    w, d, at, heads = "hg_pages8_dequantize", pages.dtype, pages.device, pages.shape.num_kv_heads
     if k_out is None and v_out is None:
         raise ValueError("%s: neither k_out nor v_out is given" % w)
     n = (v_out if k_out is None else k_out).shape[0]
-    kp = None if k_out is None else _pack3(*_rows(w, "k_out", k_out, n, heads, d))
-    vp = None if v_out is None else _pack3(*_rows(w, "v_out", v_out, n, heads, d))
-    count, bp, tp, per, _ = _requests(w, begin, page_table)
-    _on_device(w, pages.device, begin, page_table, k_out, v_out)
-    _check(library().hg_pages8_dequantize(pages.handle, n, count, bp, tp, per, kp, vp, _stream(stream)), w)
+    kp = None if k_out is None else _pack3(*_rows_on(w, "k_out", k_out, n, heads, d, at))
+    vp = None if v_out is None else _pack3(*_rows_on(w, "v_out", v_out, n, heads, d, at))
+    count, bp, tp, per = _requests(w, begin, page_table, at)
+    _check(library().hg_pages8_dequantize(pages.handle, n, count, bp, tp, per, kp, vp, _stream_on(w, stream, at)), w)
 
 
 def hg_pages8_decode_workspace_size(pages, batch, num_q_heads):
@@ -773,31 +826,27 @@ def hg_pages8_decode_workspace_size(pages, batch, num_q_heads):
 def hg_pages8_decode_attention(pages, q, page_table, lengths, out, lse, softmax_scale, workspace, stream=None):
     """Attention of one token per request (q, out [batch][heads][128]) over the first lengths[b] tokens of its 8-bit
     pages page_table[b]; lse float32 [batch][heads] or None."""
-    w, d = "hg_pages8_decode_attention", pages.dtype
+    w, d, at = "hg_pages8_decode_attention", pages.dtype, pages.device
     n, hq = q.shape[0], q.shape[1]
-    io = _pack12(*_rows(w, "q", q, n, hq, d), 0, 0, 0, 0, 0, 0, *_rows(w, "out", out, n, hq, d))
-    tp, ts, lp = _decode_table(w, page_table, lengths, n)
-    ws = _workspace(w, workspace)
-    _on_device(w, pages.device, q, out, page_table, lengths, lse, workspace)
-    _check(library().hg_pages8_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse(w, lse, n, hq), softmax_scale,
-                                                *ws, _stream(stream)), w)
+    io = _pack12(*_rows_on(w, "q", q, n, hq, d, at), 0, 0, 0, 0, 0, 0, *_rows_on(w, "out", out, n, hq, d, at))
+    tp, ts, lp = _lengths_table(w, page_table, lengths, n, at)
+    _check(library().hg_pages8_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse_on(w, lse, n, hq, at),
+                                                softmax_scale, *_workspace_on(w, workspace, at),
+                                                _stream_on(w, stream, at)), w)
 
 
 def hg_pages8_decode_step(pages, q, k, v, rotation, positions, page_table, lengths, out, lse, softmax_scale, workspace,
                           stream=None):
     """One decode step on the 8-bit pages: q and the new token's k rotated, k and v stored as token lengths[b] - 1 of
     request b, attention over its lengths[b] tokens."""
-    w, d = "hg_pages8_decode_step", pages.dtype
+    w, d, at = "hg_pages8_decode_step", pages.dtype, pages.device
     n, hq, heads = q.shape[0], q.shape[1], pages.shape.num_kv_heads
-    io = _pack12(*_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, n, heads, d),
-                     *_rows(w, "v", v, n, heads, d), *_rows(w, "out", out, n, hq, d))
-    rp, pp = _rotated_by(w, rotation, positions, n)
-    tp, ts, lp = _decode_table(w, page_table, lengths, n)
-    ws = _workspace(w, workspace)
-    _on_device(w, pages.device, q, k, v, out, page_table, lengths, lse, workspace,
-               *(() if rotation is None else (rotation.table, positions)))
-    _check(library().hg_pages8_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse(w, lse, n, hq),
-                                           softmax_scale, *ws, _stream(stream)), w)
+    io = _pack12(*_rows_on(w, "q", q, n, hq, d, at), *_rows_on(w, "k", k, n, heads, d, at),
+                     *_rows_on(w, "v", v, n, heads, d, at), *_rows_on(w, "out", out, n, hq, d, at))
+    rp, pp = _rotated_on(w, rotation, positions, n, at)
+    tp, ts, lp = _lengths_table(w, page_table, lengths, n, at)
+    _check(library().hg_pages8_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse_on(w, lse, n, hq, at),
+                                           softmax_scale, *_workspace_on(w, workspace, at), _stream_on(w, stream, at)), w)
 
 
 def hg_pages_plan(page_table, cached, new_tokens, free_pages, free_count, page_size, lengths, begin, slots, positions,
@@ -810,12 +859,11 @@ def hg_pages_plan(page_table, cached, new_tokens, free_pages, free_count, page_s
     n = cached.numel()
     if page_table.dim() != 2 or page_table.shape[0] < n:
         raise ValueError("%s: page_table must be [%d][pages]" % (w, n))
-    per, room = page_table.shape[1], slots.numel()
-    _on = (page_table, cached, new_tokens, free_pages, free_count, lengths, begin, slots, positions, counts)
-    args = (n, int(page_size), _ints(w, "page_table", page_table, n * per), per, _ints(w, "cached", cached, n),
-            _ints(w, "new_tokens", new_tokens, n), _ints(w, "free_pages", free_pages, 0), free_pages.numel(),
-            _ints(w, "free_count", free_count, 1), room, _ints(w, "lengths", lengths, n), _ints(w, "begin", begin, n + 1),
-            _ints(w, "slots", slots, 0), None if positions is None else _ints(w, "positions", positions, room),
-            _ints(w, "counts", counts, 4))
-    _on_device(w, counts.get_device(), *_on)
-    _check(library().hg_pages_plan(*args, _stream(stream)), w)
+    per, room, at = page_table.shape[1], slots.numel(), max(counts.get_device(), 0)  # (the CPU's is -1, and refused)
+    _check(library().hg_pages_plan(
+        n, page_size, _ints_on(w, "page_table", page_table, n * per, at), per, _ints_on(w, "cached", cached, n, at),
+        _ints_on(w, "new_tokens", new_tokens, n, at), _ints_on(w, "free_pages", free_pages, 0, at), free_pages.numel(),
+        _ints_on(w, "free_count", free_count, 1, at), room, _ints_on(w, "lengths", lengths, n, at),
+        _ints_on(w, "begin", begin, n + 1, at), _ints_on(w, "slots", slots, 0, at),
+        None if positions is None else _ints_on(w, "positions", positions, room, at),
+        _ints_on(w, "counts", counts, 4, at), _stream_on(w, stream, at)), w)

@@ -26,7 +26,7 @@ namespace {
 constexpr int kStages = 6;
 constexpr int kTile = kDecodeTile8, kTileShift = 6;
 static_assert(kTile == 1 << kTileShift, "tile");
-constexpr int kConsumers = 3;
+constexpr int kConsumers = 3, kItemCost = 6, kJoinCost = 12;
 static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
 constexpr int kHalfBytes = kTile * kHeadDim;   // keys; then values
 constexpr int kStageBytes = 2 * kHalfBytes;
@@ -46,13 +46,15 @@ struct Smem {
   static constexpr int bytes = lengths + 4 * kKeptLengths;
 };
 static_assert(Smem::scratch_bytes >= kConsumers * 8 * kQRowBytes, "queries are staged there too");
+static_assert(Smem::scratch_bytes >= ((kConsumers + 1) * 32 + kDecodeJoinCounters / 2 * kDecodeJoinCtas + 2) * 4, "runs' starts too");
 static_assert(Smem::scratch % 16 == 0 && Smem::bars % 8 == 0, "alignment");
 static_assert((8 + 12 + kConsumers + 1) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
 static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 
 template <bool F16>
 struct Kind {
-  static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers;
+  static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers, kItemCost = hg::kItemCost, kJoinCost = hg::kJoinCost;
+  static constexpr bool kWeighsWhole = true;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = 0x1p-7f;
   static __device__ __forceinline__ float result(float x) { return in_range<F16>(x); }
@@ -474,7 +476,7 @@ __global__ void __launch_bounds__(kThreads<Kind<F16>>, 2) pages8_decode_kernel(c
   Work w;
   Cursor c;
   int* kept = reinterpret_cast<int*>(smem + Smem::lengths);
-  const int tiles = find_work<Kind<F16>>(p, const_cast<int*>(misc) + 8, kept, w, c);
+  const int tiles = find_work<Kind<F16>>(p, const_cast<int*>(misc) + 8, kept, reinterpret_cast<int*>(smem + Smem::scratch), w, c);
   if (tiles == 0) return;
   uint32_t asked = 0;
   if (threadIdx.x / 32 == kConsumers) {

@@ -36,7 +36,8 @@ namespace {
 constexpr int kStages = 6;
 constexpr int kTile = kDecodeTile, kTileShift = 5;
 static_assert(kTile == 1 << kTileShift, "tile");
-constexpr int kConsumers = 3;
+constexpr int kConsumers = 3, kItemCost = kDecodeItemCost;
+constexpr int kJoinCost = 24;  // a ticket and a join, in tiles
 static_assert(kStages % kConsumers == 0, "a stage belongs to one warp");
 constexpr int kStageBytes = 2 * kTile * kHeadDim * 2;  // keys, then values
 constexpr int kQRowBytes = 272;  // a staged query row: 256 bytes, 16 more so that ldmatrix meets every bank once
@@ -65,7 +66,8 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
 
 template <bool F16>
 struct Kind {
-  static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers;
+  static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers, kItemCost = hg::kItemCost, kJoinCost = hg::kJoinCost;
+  static constexpr bool kWeighsWhole = false;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = F16 ? 0x1p-7f : 1.f;
   static __device__ __forceinline__ float result(float x) { return x; }
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(kThreads<Kind<F16>>, 2) pages_decode_kernel(co
   Work w;
   Cursor c;
   int* kept = reinterpret_cast<int*>(smem + Smem::lengths);
-  const int tiles = find_work<Kind<F16>>(p, const_cast<int*>(misc) + 8, kept, w, c);
+  const int tiles = find_work<Kind<F16>>(p, const_cast<int*>(misc) + 8, kept, reinterpret_cast<int*>(smem + Smem::scratch), w, c);
   if (tiles == 0) return;
   uint32_t asked = 0;
   if (threadIdx.x / 32 == kConsumers) {

@@ -1,7 +1,8 @@
 // The paged decode kernels' division of work and what becomes of its parts: an even share of a launch's tiles for every
 // CTA whatever the requests' lengths, parts of an item joined by the last CTA to arrive, results written.  What a tile
-// holds, and how it is computed, is the kernels' own.  P: their launch parameters; K: kTile (tokens of a tile), kConsumers
-// (warps, ahead of the producer's), kF16 (the rows' type), kUnlift (1 / the factor that probabilities are lifted by), result (what an output entry becomes before it is rounded), place (a fragment's two
+// holds, and how it is computed, is the kernels' own.  P: their launch parameters; K: kTile (tokens of a tile), kItemCost
+// (an item's fixed costs, in tiles), kJoinCost (a ticket and a join, in tiles), kWeighsWhole (whether the
+// fullest CTA counts, not the longest item alone), kConsumers (warps, ahead of the producer's), kF16 (the rows' type), kUnlift (1 / the factor that probabilities are lifted by), result (what an output entry becomes before it is rounded), place (a fragment's two
 // channels into a row of sums).
 #pragma once
 #include "hg_rows.cuh"
@@ -11,8 +12,6 @@ namespace hg {
 namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr int kItemCost = kDecodeItemCost;
-constexpr int kJoinCost = 24;  // a ticket and a join, in tiles
 constexpr int kKeptLengths = 72;
 constexpr int kJoinCtas = kDecodeJoinCtas, kJoinCounters = kDecodeJoinCounters;
 constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l; rows 4 banks apart
@@ -60,16 +59,59 @@ struct Work {
   }
 };
 
+// Units of the CTA that would get the most if each took the whole items that begin in its run.  Every thread looks for the
+// first item at or behind some of the runs' starts, in the requests of the thread whose units hold it.  `room`: words of
+// shared memory, kThreads + the CTAs + 2.
+template <class K, class P>
+__device__ int fullest_of_whole(const P& p, const int* kept, int* room, const Work& w, int units_before) {
+  const int tid = threadIdx.x, heads = p.pool.heads, per = (p.batch + kThreads<K> - 1) / kThreads<K>;
+  int *ahead = room, *firsts = room + kThreads<K>, *most = firsts + w.ctas + 1;
+  ahead[tid] = units_before;
+  if (tid == 0) *most = 0;
+  __syncthreads();
+  for (int j = tid; j <= w.ctas; j += kThreads<K>) {
+    const int u = w.start_of(j);
+    int at = u;
+    if (u < w.total) {
+      int t = 0;  // the last thread with requests whose units begin at u or before
+      for (int n = min(kThreads<K>, (p.batch + per - 1) / per); n > 1;) {
+        const int half = n / 2;
+        const bool right = ahead[t + half] <= u;
+        t += right ? half : 0;
+        n = right ? n - half : half;
+      }
+      int left = u - ahead[t];
+      for (int b = t * per; b < p.batch; ++b) {
+        const int units = tiles_of<K>(b < kKeptLengths ? kept[b] : request_length(p, b)) + K::kItemCost;
+        if (left < units * heads) {
+          const int in_item = left % units;
+          at = u + (in_item > 0 ? units - in_item : 0);
+          break;
+        }
+        left -= units * heads;
+      }
+    }
+    firsts[j] = at;
+  }
+  __syncthreads();
+  int mine = 0;
+  for (int j = tid; j < w.ctas; j += kThreads<K>) mine = max(mine, firsts[j + 1] - firsts[j]);
+  mine = __reduce_max_sync(kAll, mine);
+  if (tid % 32 == 0) atomicMax(most, mine);
+  __syncthreads();
+  return *most;
+}
+
 // The CTA's work, the first tile of it and how many there are; 0: none.  Every thread adds up the units of its share of
 // the requests; the one whose share holds u0 looks for it there.
 template <class K, class P>
-__device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
+__device__ int find_work(const P& p, int* scan, int* kept, int* room, Work& w, Cursor& c) {
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, heads = p.pool.heads;
   const int per = (p.batch + kThreads<K> - 1) / kThreads<K>;
   const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
   int mine = 0, longest = 0;
   for (int b = b0; b < b1; ++b) {
-    const int len = request_length(p, b), units = tiles_of<K>(len) + kItemCost;
+    const int len = request_length(p, b), units = tiles_of<K>(len) + K::kItemCost;
     if (b < kKeptLengths) kept[b] = len;
     mine += units;
     longest = max(longest, units);
@@ -105,7 +147,7 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
     int b = b0, len = 0, units = 0;
     for (;; ++b) {
       len = b < kKeptLengths ? kept[b] : request_length(p, b);
-      units = tiles_of<K>(len) + kItemCost;
+      units = tiles_of<K>(len) + K::kItemCost;
       if (left < units * heads) break;
       left -= units * heads;
     }
@@ -116,27 +158,34 @@ __device__ int find_work(const P& p, int* scan, int* kept, Work& w, Cursor& c) {
   }
   __syncthreads();
   w.first_unit = scan[10];
-  c = {scan[8], scan[9], max(0, w.first_unit - kItemCost), scan[11], tiles_of<K>(scan[11])};
+  c = {scan[8], scan[9], max(0, w.first_unit - K::kItemCost), scan[11], tiles_of<K>(scan[11])};
   int tiles = 0;
-  if (longest <= w.share + kJoinCost) {
+  bool whole = longest <= w.share + K::kJoinCost;
+  if (K::kWeighsWhole) {
+    if ((int64_t)p.batch * heads <= w.ctas) whole = 2 * (int64_t)longest <= 3 * (int64_t)w.share + 2 * K::kJoinCost;
+    else if (longest > 2 * K::kJoinCost)
+      whole = whole && fullest_of_whole<K>(p, kept, room, w, before * heads) <= w.share + K::kJoinCost;
+    else whole = true;
+  }
+  if (whole) {
     // from the first item that begins at u0 or later to the last that begins before u1
     int at = w.u0;
     if (w.first_unit > 0) {
-      at += c.tiles + kItemCost - w.first_unit;
+      at += c.tiles + K::kItemCost - w.first_unit;
       w.first_unit = 0;
       if (at < w.u1) next_item<K>(p, kept, c);
     }
     w.u0 = at;
     for (Cursor x = c; at < w.u1;) {
       tiles += x.tiles;
-      at += x.tiles + kItemCost;
+      at += x.tiles + K::kItemCost;
       if (at < w.u1) next_item<K>(p, kept, x);
     }
     return tiles;
   }
   // the run's units less those that stand for fixed costs
-  int rest = w.u1 - w.u0, skip = max(0, kItemCost - w.first_unit);
-  for (Cursor x = c; rest > skip; skip = kItemCost) {
+  int rest = w.u1 - w.u0, skip = max(0, K::kItemCost - w.first_unit);
+  for (Cursor x = c; rest > skip; skip = K::kItemCost) {
     rest -= skip;
     const int n = min(rest, x.tiles - x.t);
     tiles += n;

@@ -198,7 +198,9 @@ def _t(*shape, dtype=torch.bfloat16):
 @pytest.fixture
 def pool(pages):
     c, s = _t(10, 4, 16, 128, dtype=torch.uint8), _t(10, 4, 1, dtype=torch.float32)
-    return hg.Pages8(None, c, c, s, s, _shape(), torch.bfloat16)
+    pages8 = hg.Pages8(None, c, c, s, s, _shape(), torch.bfloat16)
+    pages8.device = 0
+    return pages8
 
 
 def test_binding_create(lib):
@@ -226,9 +228,9 @@ def test_binding_append_and_dequantize(pool):
     _raises(lambda: hg.hg_pages8_dequantize(pool, i, tab, k.half()), "k_out is")
     _raises(lambda: hg.hg_pages8_dequantize(pool, i, tab, None, q), "v_out is")
     _raises(lambda: hg.hg_pages8_dequantize(pool, i, tab, k), "must be a CUDA tensor")
-    _raises(lambda: hg._requests("f", i, tab[:1]), "page_table must be [2]")
-    _raises(lambda: hg._requests("f", i.long(), tab), "begin must be contiguous int32")
-    _raises(lambda: hg._requests("f", i, tab), "begin must be a CUDA tensor")
+    _raises(lambda: hg._requests("f", i, tab[:1], 0), "page_table must be [2]")
+    _raises(lambda: hg._requests("f", i.long(), tab, 0), "begin must be contiguous int32")
+    _raises(lambda: hg._requests("f", i, tab, 0), "begin must be a CUDA tensor")
 
 
 def test_binding_decode(pool):
@@ -249,17 +251,53 @@ def test_binding_plan(lib):
 
 class _Tensor:
     """A tensor on a GPU that this machine may not have."""
+    is_cuda = True
 
-    def __init__(self, index):
-        self.index, self.device = index, "cuda:%d" % index
+    def __init__(self, index, dtype, *shape):
+        self.index, self.device, self.dtype, self.shape, self.nbytes = index, "cuda:%d" % index, dtype, shape, 99
+        self.size = torch.Size(shape)
 
     def get_device(self):
         return self.index
 
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return self.size.numel()
+
+    def stride(self):
+        return 128 * self.shape[1], 128, 1
+
+    def data_ptr(self):
+        return A
+
 
 def test_one_device(monkeypatch):
     """A launch goes to the current device: tensors of another are refused, as are those of several."""
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    hg._on_device("f", 0, _Tensor(0), None, _Tensor(0))
-    _raises(lambda: hg._on_device("f", 0, _Tensor(0), _Tensor(1)), "f: tensors on cuda:1 and on cuda:0")
-    _raises(lambda: hg._on_device("f", 1, _Tensor(1)), "the current device is cuda:0")
+    rows, ints, floats = (_Tensor(1, d, *s) for d, s in ((torch.bfloat16, (3, 4, 128)), (torch.int32, (3,)), (torch.float32, (3, 4))))
+    assert hg._rows_on("f", "x", rows, 3, 4, torch.bfloat16, 1) == (A, 512, 128)
+    assert hg._ints_on("f", "x", ints, 3, 1) == A and hg._lse_on("f", floats, 3, 4, 1) == A
+    assert hg._workspace_on("f", floats, 1) == (A, 99) and hg._lse_on("f", None, 3, 4, 1) is None
+    what = "x is on cuda:1, the call's tensors are on cuda:0"
+    _raises(lambda: hg._rows_on("f", "x", rows, 3, 4, torch.bfloat16, 0), what)
+    _raises(lambda: hg._ints_on("f", "x", ints, 3, 0), what)
+    _raises(lambda: hg._lse_on("f", floats, 3, 4, 0), "lse is on cuda:1")
+    _raises(lambda: hg._workspace_on("f", floats, 0), "workspace is on cuda:1")
+
+    class Turn:
+        pointer, positions, table = 5, 1, floats
+    assert hg._rotated_on("f", Turn, ints, 3, 1) == (5, A)
+    _raises(lambda: hg._rotated_on("f", Turn, ints, 3, 0), "the rotation's table is on cuda:1")
+    monkeypatch.setattr(hg._types, "device", lambda: 0, raising=False)
+    monkeypatch.setattr(hg._types, "stream", lambda device: 77 + device, raising=False)
+    assert hg._stream_on("f", None, 0) == 77 and hg._stream_on("f", 5, 0) == 5
+    _raises(lambda: hg._stream_on("f", None, 1), "the call's tensors are on cuda:1, the current device is cuda:0")
+
+
+@pytest.mark.parametrize("shape", [(3, 64), (64, 3), (5, 3), (192,), (1, 15)])
+def test_three_positions_have_the_calls_own_layout(shape):
+    class Turn:
+        pointer, positions, table = 0, 3, _Tensor(0, torch.float32, 9, 128)
+    _raises(lambda: hg._rotated_on("f", Turn, torch.zeros(shape, dtype=torch.int32), 5, 0),
+            "f: positions are %s, the call takes [3][5]" % list(shape))
