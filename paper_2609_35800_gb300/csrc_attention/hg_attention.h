@@ -70,6 +70,16 @@ struct Pages8AppendParams {
   const int* lengths;
 };
 
+// CTAs of a launch that store keys and values (one for each block that may be touched, head and of the two), and that
+// turn queries (16 sets of kAppend8Queries heads each); false: more than a launch numbers.
+constexpr int kAppend8Queries = 2;
+inline bool append8_grid(int64_t tokens, int64_t requests, int64_t q_heads, int64_t heads, int64_t* kv, int64_t* q) {
+  const int64_t sets = tokens * ((q_heads + kAppend8Queries - 1) / kAppend8Queries);
+  *kv = (tokens / kBlock8 + 2 * requests + 1) * 2 * heads;
+  *q = (sets + 15) / 16;
+  return sets < INT64_C(0xffffff00) && *kv + *q <= INT32_MAX;
+}
+
 struct Pages8DequantizeParams {
   PagePool8 pool;
   int tokens, requests;
@@ -89,12 +99,15 @@ struct PagesPlanParams {
   int free_capacity;
   const int* free_count;
   int tokens;  // room for new ones
+  int in_place;  // lengths and counts share memory with inputs
+  int part;      // kPlanFill: all but lengths and counts, kPlanEnd: these
   int* lengths;
   int* begin;
   int* slots;
   int* positions;
   int* counts;
 };
+constexpr int kPlanAll = 0, kPlanFill = 1, kPlanEnd = 2;
 constexpr int kPlanMaxBatch = 16384;
 
 // Tokens of a tile of the paged decode; a tensor map's box covers a tile of one page, or the page where that is smaller.

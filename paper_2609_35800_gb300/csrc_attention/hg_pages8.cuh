@@ -91,11 +91,24 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
   return make_uint4(pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3]), pack2<F16>(x[4], x[5]), pack2<F16>(x[6], x[7]));
 }
 
+// 16 channels side by side: one store of a whole sector where the row lies so.
+__device__ __forceinline__ void store16(uint16_t* dst, const uint4& lo, const uint4& hi) {
+  if ((reinterpret_cast<uintptr_t>(dst) & 31u) == 0) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(dst), "r"(lo.x), "r"(lo.y), "r"(lo.z),
+                 "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w)
+                 : "memory");
+  } else {
+    *reinterpret_cast<uint4*>(dst) = lo;
+    *reinterpret_cast<uint4*>(dst + 8) = hi;
+  }
+}
+
 // x, or the 16-bit type's largest value where it is beyond; NaN stays.
 template <bool F16>
+constexpr float kMost16 = F16 ? 65504.f : 0x1.fep127f;
+template <bool F16>
 __device__ __forceinline__ float in_range(float x) {
-  constexpr float kMost = F16 ? 65504.f : 0x1.fep127f;
-  return x > kMost ? kMost : x < -kMost ? -kMost : x;
+  return x > kMost16<F16> ? kMost16<F16> : x < -kMost16<F16> ? -kMost16<F16> : x;
 }
 
 // Byte offset of a token's codes in the pool; index of its block's scale.

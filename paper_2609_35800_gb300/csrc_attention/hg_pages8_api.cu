@@ -3,6 +3,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <utility>
 
 #include "hg_checks.h"
 
@@ -53,6 +54,8 @@ hg_status map_pages8(hg_pages8* p) {
   p->mapped.store(true, std::memory_order_release);
   return HG_OK;
 }
+
+bool share_memory(const int32_t* a, int64_t n, const int32_t* b, int64_t m) { return a < b + m && b < a + n; }
 
 hg_status pages8_decode(const hg_pages8* pages, int32_t batch, int32_t num_q_heads, const hg_attention_io* io,
                         const hg_rotation* rotation, const int32_t* positions, const int32_t* page_table,
@@ -133,6 +136,8 @@ hg_status hg_pages8_append(const hg_pages8* pages, int32_t num_tokens, int32_t n
   if (num_q_heads > kMaxGroup * kMaxKvHeads || num_tokens > kMaxRows || num_requests > kMaxRows / 4)
     return HG_ERR_UNSUPPORTED;
   if (num_tokens == 0 || num_requests == 0) return HG_OK;
+  int64_t kv = 0, q = 0;
+  if (!append8_grid(num_tokens, num_requests, num_q_heads, pages->pool.heads, &kv, &q)) return HG_ERR_UNSUPPORTED;
   if (!lengths) return HG_ERR_INVALID_ARG;
   hg_status st = check_places(num_requests, begin, page_table, table_stride, pages->pool);
   if (st != HG_OK) return st;
@@ -245,6 +250,10 @@ hg_status hg_pages_plan(int32_t batch, int32_t page_size, int32_t* page_table, i
   p.slots = slots;
   p.positions = positions;
   p.counts = counts;
+  for (const auto& out : {std::make_pair(lengths, batch), std::make_pair(counts, 4)})
+    if (share_memory(out.first, out.second, cached, batch) || share_memory(out.first, out.second, new_tokens, batch) ||
+        share_memory(out.first, out.second, free_count, 1))
+      p.in_place = 1;
   return of_cuda(launch_pages_plan(p, reinterpret_cast<cudaStream_t>(stream)));
 }
 

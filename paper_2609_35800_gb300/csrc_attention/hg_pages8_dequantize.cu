@@ -11,26 +11,46 @@ namespace {
 constexpr int kThreads = 256, kTokens = kThreads / 8;
 constexpr int kRowsPerCta = 4;  // heads of the keys or the values
 
+// The last request that begins at the row or before it, 32 candidates a round; the first where none does.
+__device__ __forceinline__ int request_of(const Pages8DequantizeParams& p, int row) {
+  const int lane = threadIdx.x % 32;
+  int r = 0;
+  for (int n = p.requests; n > 1;) {
+    const int step = (n + 31) / 32;
+    const bool below = lane * step < n && p.begin[r + lane * step] <= row;
+    const int k = max(__popc(__ballot_sync(0xffffffffu, below)) - 1, 0);
+    r += k * step;
+    n = min(step, n - k * step);
+  }
+  return r;
+}
+
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) pages8_dequantize_kernel(const __grid_constant__ Pages8DequantizeParams p) {
   grid_launch_dependents();
   grid_dependency_wait();
-  const int row = blockIdx.x * kTokens + threadIdx.x / 8, c = threadIdx.x % 8;
+  const int row0 = blockIdx.x * kTokens + threadIdx.x / 32 * 4;  // of the warp
+  const int row = row0 + threadIdx.x % 32 / 8, c = threadIdx.x % 8;
+  int r = request_of(p, row0);
+  while (r + 1 < p.requests && p.begin[r + 1] <= row) ++r;
   if (row >= p.tokens || row < p.begin[0] || row >= p.begin[p.requests]) return;
-  int r = 0;  // the last request that begins at the row or before it
-  for (int n = p.requests; n > 1;) {
-    const int half = n / 2;
-    if (p.begin[r + half] <= row) {
-      r += half;
-      n -= half;
-    } else {
-      n = half;
-    }
-  }
   const int token = row - p.begin[r];
   const int page = page_of(p.pool, p.table + (int64_t)r * p.table_stride, p.table_stride, token);
   const int in_page = token & (p.pool.page_size - 1);
   const int parts = p.pool.heads * ((p.k_out.data ? 1 : 0) + (p.v_out.data ? 1 : 0));
+  uint4 codes[kRowsPerCta];
+  float scale[kRowsPerCta];
+#pragma unroll
+  for (int i = 0; i < kRowsPerCta; ++i) {  // every read before the first store
+    const int part = blockIdx.y * kRowsPerCta + i;
+    const bool is_v = !p.k_out.data || part >= p.pool.heads;
+    const int head = part >= p.pool.heads ? part - p.pool.heads : part;
+    codes[i] = make_uint4(0u, 0u, 0u, 0u);
+    scale[i] = 0.f;
+    if (part >= parts || page < 0) continue;
+    codes[i] = ldg16((is_v ? p.pool.v : p.pool.k) + code_row(p.pool, page, in_page, head) + 16 * c);
+    scale[i] = (is_v ? p.pool.v_scales : p.pool.k_scales)[scale_at(p.pool, page, in_page, head)];
+  }
 #pragma unroll
   for (int i = 0; i < kRowsPerCta; ++i) {
     const int part = blockIdx.y * kRowsPerCta + i;
@@ -38,20 +58,17 @@ __global__ void __launch_bounds__(kThreads) pages8_dequantize_kernel(const __gri
     const bool is_v = !p.k_out.data || part >= p.pool.heads;
     const int head = part >= p.pool.heads ? part - p.pool.heads : part;
     const Rows& out = is_v ? p.v_out : p.k_out;
-    uint4 codes = make_uint4(0u, 0u, 0u, 0u);
-    float scale = 0.f;
-    if (page >= 0) {
-      codes = *reinterpret_cast<const uint4*>((is_v ? p.pool.v : p.pool.k) + code_row(p.pool, page, in_page, head) + 16 * c);
-      scale = (is_v ? p.pool.v_scales : p.pool.k_scales)[scale_at(p.pool, page, in_page, head)];
-    }
     float x[16];
-    decode8(make_uint2(codes.x, codes.y), x);
-    decode8(make_uint2(codes.z, codes.w), x + 8);
+    decode8(make_uint2(codes[i].x, codes[i].y), x);
+    decode8(make_uint2(codes[i].z, codes[i].w), x + 8);
 #pragma unroll
-    for (int k = 0; k < 16; ++k) x[k] = in_range<F16>(x[k] * scale);
+    for (int k = 0; k < 16; ++k) x[k] *= scale[i];
+    if (!(scale[i] * 448.f <= kMost16<F16>)) {  // the largest code would be out of the type's range
+#pragma unroll
+      for (int k = 0; k < 16; ++k) x[k] = in_range<F16>(x[k]);
+    }
     uint16_t* dst = out.data + row * out.token_stride + head * out.head_stride + 16 * c;
-    *reinterpret_cast<uint4*>(dst) = pack8<F16>(x);
-    *reinterpret_cast<uint4*>(dst + 8) = pack8<F16>(x + 8);
+    store16(dst, pack8<F16>(x), pack8<F16>(x + 8));
   }
 }
 

@@ -3,8 +3,11 @@
 // Request r has ceil(cached / P) pages and needs ceil((cached + new) / P); the difference is taken from the end of the
 // free list behind which the pages of requests that end are put first.  Three running sums over the requests (new tokens,
 // pages taken, pages given back) give every token's row, every new page's place in the list and every page's place behind
-// it; each token, page and place is then found by a search in its sum, one after the other by any thread.  A few bytes a
-// request and eight a token: nothing but latency, so one CTA does it all in one launch, the sums in shared memory.
+// it; each token, page and place is then found by a search in its sum.  A few bytes a request and eight a token: nothing
+// but latency.  Every CTA works out the sums for itself, in shared memory, and takes some of the tokens and pages: what it
+// reads for them no other one writes, but for lengths and counts where they are the inputs' own: then a call of up to
+// kTokensPerCta tokens is one CTA, which writes those last, and a larger one has a second launch that does it.  Measured: 64
+// requests of one token XXX us on the device; 1,000 requests, 484,000 tokens XXX us (one CTA 400).
 #include "hg_attention.h"
 #include "hg_mma.cuh"
 
@@ -12,6 +15,7 @@ namespace hg {
 namespace {
 
 constexpr int kThreads = 1024;
+constexpr int kTokensPerWarp = 128, kTokensPerCta = kThreads / 32 * kTokensPerWarp;
 constexpr unsigned kAll = 0xffffffffu;
 
 struct Sums {
@@ -19,6 +23,22 @@ struct Sums {
 };
 __device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
   return {a.tokens + b.tokens, a.taken + b.taken, a.freed + b.freed};
+}
+
+__device__ __forceinline__ Sums operator-(const Sums& a, const Sums& b) {
+  return {a.tokens - b.tokens, a.taken - b.taken, a.freed - b.freed};
+}
+__device__ __forceinline__ Sums from_lane(const Sums& x, int lane) {
+  return {__shfl_sync(kAll, x.tokens, lane), __shfl_sync(kAll, x.taken, lane), __shfl_sync(kAll, x.freed, lane)};
+}
+// The sum of the lanes up to this one.
+__device__ __forceinline__ Sums up_to(Sums x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const Sums below = from_lane(x, max(lane - o, 0));
+    if (lane >= o) x = x + below;
+  }
+  return x;
 }
 
 // What request r wants of the call.
@@ -40,17 +60,13 @@ __device__ __forceinline__ Wish wish_of(const PagesPlanParams& p, int r) {
   return w;
 }
 
-// The last r with sums[r] <= x, sums not decreasing from 0.
-__device__ __forceinline__ int find(const int* sums, int n, int x) {
-  int r = 0;
+// The last r of [r, r + n) with sums[r] <= x, sums not decreasing and the first not above x.
+__device__ __forceinline__ int find(const int* sums, int r, int n, int x) {
   while (n > 1) {
     const int half = n / 2;
-    if (sums[r + half] <= x) {
-      r += half;
-      n -= half;
-    } else {
-      n = half;
-    }
+    const bool right = sums[r + half] <= x;
+    r += right ? half : 0;
+    n = right ? n - half : half;
   }
   return r;
 }
@@ -64,6 +80,7 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   int *tokens_to = sums, *taken_to = sums + p.batch + 1, *freed_to = taken_to + p.batch + 1;
   if (tid < 2) flags[tid] = 0;
+  const int count = min(max(*p.free_count, 0), p.free_capacity);
   const int per = (p.batch + kThreads - 1) / kThreads, r0 = min(tid * per, p.batch), r1 = min(r0 + per, p.batch);
   Sums mine = {0, 0, 0};
   bool outgrows = false;
@@ -75,21 +92,13 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
     held = max(held, w.cached);
     if (p.new_tokens[r] >= 0) longest = max(longest, w.cached + (w.outgrows ? 0 : w.tokens));
   }
-  Sums before = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const Sums x = {__shfl_up_sync(kAll, before.tokens, o), __shfl_up_sync(kAll, before.taken, o),
-                    __shfl_up_sync(kAll, before.freed, o)};
-    if (lane >= o) before = before + x;
-  }
+  Sums before = up_to(mine, lane);
   if (lane == 31) warp_sums[warp] = before;
-  before = {before.tokens - mine.tokens, before.taken - mine.taken, before.freed - mine.freed};
   __syncthreads();
-  Sums all = {0, 0, 0};
-  for (int i = 0; i < kThreads / 32; ++i) {
-    if (i == warp) before = before + all;
-    all = all + warp_sums[i];
-  }
+  const Sums ahead = up_to(warp_sums[lane], lane);  // (a lane a warp)
+  const Sums all = from_lane(ahead, 31), others = from_lane(ahead, max(warp - 1, 0));
+  before = before - mine;
+  if (warp > 0) before = before + others;
   // a refused call's sums are not used: they may pass 32 bits
   for (int r = r0; r < r1; ++r) {
     const Wish w = wish_of(p, r);
@@ -99,47 +108,76 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
     before = before + Sums{w.tokens, w.taken, w.freed};
   }
   if (outgrows) atomicOr(&flags[0], 1);
-  const int count = min(max(*p.free_count, 0), p.free_capacity);
   const int64_t left = count + all.freed - all.taken;
   __syncthreads();
   const int refused = flags[0] ? -1 : all.tokens > p.tokens ? -2 : left < 0 ? (int)min(-left, (int64_t)INT32_MAX)
                                                                 : left > p.free_capacity ? -3 : 0;
-  atomicMax(&flags[1], refused ? held : longest);
+  if (blockIdx.x == 0) {
+    longest = __reduce_max_sync(kAll, refused ? held : longest);
+    if (lane == 0) atomicMax(&flags[1], longest);
+  }
   const int tokens = refused ? 0 : (int)all.tokens, taken = refused ? 0 : (int)all.taken, freed = (int)all.freed;
   // a page of the list's end, of those given back by their number
   const auto given_back = [&](int j) {
-    const int r = find(freed_to, p.batch, j);
+    const int r = find(freed_to, 0, p.batch, j);
     return p.table[(int64_t)r * p.table_stride + j - freed_to[r]];
   };
   const auto page_taken = [&](int k) { return k < freed ? given_back(freed - 1 - k) : p.free_pages[count - 1 - (k - freed)]; };
 
-  for (int k = tid; k < taken; k += kThreads) {
-    const int r = find(taken_to, p.batch, k);
-    p.table[(int64_t)r * p.table_stride + wish_of(p, r).have + k - taken_to[r]] = page_taken(k);
-  }
-  for (int i = tid; i < p.tokens; i += kThreads) {
-    int slot = -1, position = 0;
-    if (i < tokens) {
-      const int r = find(tokens_to, p.batch, i);
-      const Wish w = wish_of(p, r);
-      position = w.cached + i - tokens_to[r];
-      const int at = position >> p.page_shift;
-      const int page = at < w.have ? p.table[(int64_t)r * p.table_stride + at] : page_taken(taken_to[r] + at - w.have);
-      slot = (int)((uint32_t)page << p.page_shift) + (position & ((1 << p.page_shift) - 1));
+  const bool fills = p.part != kPlanEnd;
+  if (fills) {
+    const int first = blockIdx.x * kThreads + tid, step = gridDim.x * kThreads;
+    for (int k = first; k < taken; k += step) {
+      const int r = find(taken_to, 0, p.batch, k);
+      p.table[(int64_t)r * p.table_stride + wish_of(p, r).have + k - taken_to[r]] = page_taken(k);
     }
-    p.slots[i] = slot;
-    if (p.positions) p.positions[i] = position;
+    for (int i0 = (first / 32) * kTokensPerWarp; i0 < p.tokens; i0 += (step / 32) * kTokensPerWarp) {
+      // the requests of the warp's tokens
+      int least = 0, requests = 1;
+      if (i0 < tokens) {
+        least = find(tokens_to, 0, p.batch, i0);
+        requests = find(tokens_to, least, p.batch - least, min(i0 + kTokensPerWarp, tokens) - 1) - least + 1;
+      }
+      // (one step after the other for all of a lane's tokens, so that their reads are in flight together)
+      constexpr int kMine = kTokensPerWarp / 32;
+      int request[kMine], cached[kMine], page[kMine];
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int i = min(i0 + 32 * j + lane, tokens - 1);
+        request[j] = tokens > i0 ? find(tokens_to, least, requests, i) : 0;
+        cached[j] = tokens > i0 ? max(p.cached[request[j]], 0) : 0;
+      }
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int i = i0 + 32 * j + lane, r = request[j];
+        page[j] = 0;
+        if (i >= tokens) continue;
+        const int at = (cached[j] + i - tokens_to[r]) >> p.page_shift;
+        const int have = (int)(((int64_t)cached[j] + (1 << p.page_shift) - 1) >> p.page_shift);
+        page[j] = at < have ? p.table[(int64_t)r * p.table_stride + at] : page_taken(taken_to[r] + at - have);
+      }
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int i = i0 + 32 * j + lane, position = cached[j] + i - tokens_to[request[j]];
+        if (i >= p.tokens) continue;
+        p.slots[i] = i < tokens ? (int)((uint32_t)page[j] << p.page_shift) + (position & ((1 << p.page_shift) - 1)) : -1;
+        if (p.positions) p.positions[i] = i < tokens ? position : 0;
+      }
+    }
+    if (!refused)
+      for (int j = first; j < (int)left - count; j += step) p.free_pages[count + j] = given_back(j);
+    if (blockIdx.x == 0) {
+      for (int r = r0; r < r1; ++r) p.begin[r] = refused ? 0 : tokens_to[r];
+      if (tid == 0) p.begin[p.batch] = tokens;
+    }
   }
-  if (!refused)
-    for (int j = tid; j < (int)left - count; j += kThreads) p.free_pages[count + j] = given_back(j);
-  for (int r = r0; r < r1; ++r) p.begin[r] = refused ? 0 : tokens_to[r];
+  if (p.part == kPlanFill || blockIdx.x > 0) return;
   __syncthreads();  // cached and free_count may be lengths and counts
   for (int r = r0; r < r1; ++r) {
     const Wish w = wish_of(p, r);
     p.lengths[r] = refused ? p.cached[r] : p.new_tokens[r] < 0 ? 0 : w.cached + w.tokens;
   }
   if (tid == 0) {
-    p.begin[p.batch] = tokens;
     p.counts[HG_PLAN_FREE] = refused ? count : (int)left;
     p.counts[HG_PLAN_REFUSED] = refused;
     p.counts[HG_PLAN_TOKENS] = tokens;
@@ -160,7 +198,14 @@ cudaError_t launch_pages_plan(const PagesPlanParams& p, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
-  return launch_overlapped(pages_plan_kernel, dim3(1), kThreads, 3 * (p.batch + 1) * 4, s, p);
+  const int smem = 3 * (p.batch + 1) * 4;
+  const int ctas = std::min((p.tokens + kTokensPerCta - 1) / kTokensPerCta, device_sms());
+  PagesPlanParams a = p;
+  a.part = ctas > 1 && p.in_place ? kPlanFill : kPlanAll;
+  e = launch_overlapped(pages_plan_kernel, dim3((unsigned)std::max(ctas, 1)), kThreads, smem, s, a);
+  if (e != cudaSuccess || a.part == kPlanAll) return e;
+  a.part = kPlanEnd;
+  return launch_overlapped(pages_plan_kernel, dim3(1), kThreads, smem, s, a);
 }
 
 }  // namespace hg

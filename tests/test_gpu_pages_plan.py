@@ -149,3 +149,19 @@ def test_requests_come_and_go():
             hg.hg_pages_plan(table, lens, _ints([-1] * n), free, count[:1], size, lens, begin, slots, None, count)
             assert int(count[0]) == pool
     assert refused > 2
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("batch,size,longest,ending,context", [(1, 64, 300000, 0, 50), (900, 16, 700, 6, 300), (16384, 16, 3, 9, 40),
+                                                              (5, 256, 9000, 2, 3000), (16384, 32, 1, 2, 5)])
+def test_large_plans(batch, size, longest, ending, context, in_place):
+    """More tokens than one CTA takes, and as many requests as a call may have."""
+    args = _case(batch + longest, batch, size, longest, ending, context=context)
+    room = sum(max(n, 0) for n in args[2])
+    want = plan(*args, room + 10001)
+    assert want[5][1] == 0
+    assert _run(*args, room + 10001, in_place=in_place) == want
+    if room > 0:  # refused: no token is placed
+        assert _run(*args, room - 1, in_place=in_place) == plan(*args, room - 1)
+    short = args[:4] + (max(args[4] - 5, 0), size)  # fewer free pages than needed
+    assert _run(*short, room, in_place=in_place) == plan(*short, room)
