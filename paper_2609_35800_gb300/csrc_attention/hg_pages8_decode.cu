@@ -33,8 +33,11 @@ constexpr int kStageBytes = 2 * kHalfBytes;
 constexpr int kQRowBytes = 288;  // a staged query row: 256 bytes and its factor; 8 banks on, so that four rows meet all
 constexpr int kTileBlocks = kTile / kBlock8;
 constexpr int kScaleLanes = 2 * kTileBlocks;
+// A tile with no more tokens than this goes block by block (one token: 3.6 -> 3.0 us an item).  Not of more than 8 queries,
+// where a second form of the tile's code costs the first its registers (37 requests of 1 to 9,001 tokens: 24.8 -> 27.0 us).
+constexpr int kFewTokens = 32;
 
-// Shared memory, two CTAs an SM.  The staged queries (8 rows a warp) and the warps' parts that are added up at an item's
+// Shared memory, two CTAs an SM.  The staged queries (16 rows at most) and the warps' parts that are added up at an item's
 // end (8 queries at a time) take turns in one region.
 struct Smem {
   static constexpr int scales = kStages * kStageBytes;  // of each stage: its keys' blocks, its values' blocks
@@ -45,7 +48,7 @@ struct Smem {
   static constexpr int lengths = misc + 128;           // the first requests' lengths
   static constexpr int bytes = lengths + 4 * kKeptLengths;
 };
-static_assert(Smem::scratch_bytes >= kConsumers * 8 * kQRowBytes, "queries are staged there too");
+static_assert(Smem::scratch_bytes >= 16 * kQRowBytes, "queries are staged there too");
 static_assert(Smem::scratch_bytes >= ((kConsumers + 1) * 32 + kDecodeJoinCounters / 2 * kDecodeJoinCtas + 2) * 4, "runs' starts too");
 static_assert(Smem::scratch % 16 == 0 && Smem::bars % 8 == 0, "alignment");
 static_assert((8 + 12 + kConsumers + 1) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
@@ -129,50 +132,81 @@ __device__ uint32_t produce(const Pages8DecodeParams& p, Cursor c, int tiles, co
   return n;
 }
 
-// Rotated, as FP16, and through shared memory into the first product's operands; `back`: what undoes each query's factor.
+// An item's query rows on their way: eight lanes a row, the CTA's consumers side by side.
+template <int NT>
+constexpr int kRowsPerLane = (8 * NT + kGroups<Kind<false>> - 1) / kGroups<Kind<false>>;
+template <int NT>
+struct MyQueries {
+  uint4 lo[kRowsPerLane<NT>], hi[kRowsPerLane<NT>];
+  LaneAngles angles;  // of up to 8 queries; those of 16 would be in the sums' way, and come as the rows are turned
+};
+
+template <int NT>
+__device__ __forceinline__ void fetch_my_queries(const Pages8DecodeParams& p, int b, int h, MyQueries<NT>& x) {
+  const int c = threadIdx.x % 8;
+  const LaneChannels at = lane_channels(p.rot, c, p.rot.table != nullptr);
+  const uint16_t* row = p.q.data + b * p.q.token_stride + (int64_t)h * p.group * p.q.head_stride;
+#pragma unroll
+  for (int i = 0; i < kRowsPerLane<NT>; ++i) {
+    const int q = threadIdx.x / 8 + i * kGroups<Kind<false>>;
+    x.lo[i] = x.hi[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (q < p.group) {
+      x.lo[i] = ldg16(row + q * p.q.head_stride + at.lo);
+      x.hi[i] = ldg16(row + q * p.q.head_stride + at.hi);
+    }
+  }
+  if (NT == 1 && at.turns) x.angles = lane_angles(p.rot, c, b);
+}
+
+// Rotated, as FP16, into shared memory, once for all consumers, and from there into the first product's operands; `back`:
+// what undoes each query's factor.
 template <bool F16, int NT>
-__device__ __forceinline__ void stage_queries(const Pages8DecodeParams& p, Queries<NT>& x, uint32_t mine, uint32_t (&qf)[NT][16],
-                                              float (&back)[NT][2]) {
+__device__ __forceinline__ void stage_queries(const Pages8DecodeParams& p, int b, MyQueries<NT>& x, uint32_t staged,
+                                              uint32_t (&qf)[NT][16], float (&back)[NT][2]) {
   const int lane = threadIdx.x % 32;
   const LaneChannels at = lane_channels(p.rot, lane % 8, p.rot.table != nullptr);
+  if (NT > 1 && at.turns) x.angles = lane_angles(p.rot, lane % 8, b);
+#pragma unroll
+  for (int i = 0; i < kRowsPerLane<NT>; ++i) {
+    const int q = threadIdx.x / 8 + i * kGroups<Kind<F16>>;
+    if (at.turns) rotate_lane<F16>(x.lo[i], x.hi[i], x.angles, p.rot.interleaved != 0);
+    const uint32_t row = staged + q * kQRowBytes;
+    if (!F16) {
+      float v[16];
+      row_values<F16>(x.lo[i], x.hi[i], nullptr, false, v);
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) top = max(top, finite_bits(v[k]));
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(kAll, top, o));
+      // 2^(14 - e) for a largest entry in [2^e, 2^(e + 1)), 2^126 at most
+      const int field = min(127 + 14 + 127 - (int)(top >> 23), kMostField);
+      const float factor = power_of_field(field);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] *= factor;
+      x.lo[i] = pack8<true>(v);
+      x.hi[i] = pack8<true>(v + 8);
+      if (q < 8 * NT && lane % 8 == 0)
+        st_shared16(row + 256, make_uint4(__float_as_uint(inverse_of_field(field)), 0u, 0u, 0u));
+    }
+    if (q < 8 * NT) {
+      st_shared16(row + at.lo * 2, x.lo[i]);
+      st_shared16(row + at.hi * 2, x.hi[i]);
+    }
+  }
+  named_barrier<kConsumers * 32>(1);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (at.turns) rotate_lane<F16>(x.lo[nt][i], x.hi[nt][i], x.angles, p.rot.interleaved != 0);
-      const uint32_t row = mine + (lane / 8 + 4 * i) * kQRowBytes;
-      if (!F16) {
-        float v[16];
-        row_values<F16>(x.lo[nt][i], x.hi[nt][i], nullptr, false, v);
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) top = max(top, finite_bits(v[k]));
-#pragma unroll
-        for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(kAll, top, o));
-        // 2^(14 - e) for a largest entry in [2^e, 2^(e + 1)), 2^126 at most
-        const int field = min(127 + 14 + 127 - (int)(top >> 23), kMostField);
-        const float factor = power_of_field(field);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] *= factor;
-        x.lo[nt][i] = pack8<true>(v);
-        x.hi[nt][i] = pack8<true>(v + 8);
-        if (lane % 8 == 0) st_shared16(row + 256, make_uint4(__float_as_uint(inverse_of_field(field)), 0u, 0u, 0u));
-      }
-      st_shared16(row + at.lo * 2, x.lo[nt][i]);
-      st_shared16(row + at.hi * 2, x.hi[nt][i]);
-    }
-    __syncwarp();
-#pragma unroll
     for (int j = 0; j < 8; ++j) {  // a product's 16 channels, four a lane
-      const uint32_t a = mine + (lane / 4) * kQRowBytes + (16 * j + 4 * (lane % 4)) * 2;
+      const uint32_t a = staged + (8 * nt + lane / 4) * kQRowBytes + (16 * j + 4 * (lane % 4)) * 2;
       asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];\n" : "=r"(qf[nt][2 * j]), "=r"(qf[nt][2 * j + 1]) : "r"(a) : "memory");
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       back[nt][j] = 1.f;
-      if (!F16) back[nt][j] = __uint_as_float(ld_shared16(mine + (2 * (lane % 4) + j) * kQRowBytes + 256).x);
+      if (!F16) back[nt][j] = __uint_as_float(ld_shared16(staged + (8 * nt + 2 * (lane % 4) + j) * kQRowBytes + 256).x);
     }
-    __syncwarp();
   }
 }
 
@@ -191,10 +225,10 @@ __device__ __forceinline__ void st_shared8(uint32_t addr, uint2 v) {
 
 // The new token of a decode step, row r of the tile: its block is brought to the scale that it needs, in the pool and over
 // what the stage holds.  Not where the request has grown past its table: its new token has no place there, and the last
-// row is a token's own.  ks, vs: the tile's scales, which may rise.
+// row is a token's own.  scales: the tile's, keys' blocks before values', which may rise.
 template <bool F16>
 __device__ __forceinline__ void place_new_token(const Pages8DecodeParams& p, const Cursor& c, uint32_t kt, uint32_t vt, int r,
-                                                float (&ks)[kTileBlocks], float (&vs)[kTileBlocks]) {
+                                                volatile float* scales) {
   if (p.lengths[c.b] != c.len) return;
   const int lane = threadIdx.x % 32, i = lane % 8;
   const bool is_v = lane / 8 == 1;
@@ -213,10 +247,7 @@ __device__ __forceinline__ void place_new_token(const Pages8DecodeParams& p, con
   for (int k = 0; k < 16; ++k) top = max(top, finite_bits(x[k]));
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(kAll, top, o));
-  float old = 0.f;
-#pragma unroll
-  for (int k = 0; k < kTileBlocks; ++k)
-    if (k == block) old = is_v ? vs[k] : ks[k];
+  const float old = scales[(is_v ? kTileBlocks : 0) + block];
   int field = needed_field(top);
   if (before > 0) field = max(field, stored_field(old));
   const float scale = power_of_field(field), inv = inverse_of_field(field);
@@ -235,9 +266,7 @@ __device__ __forceinline__ void place_new_token(const Pages8DecodeParams& p, con
 #pragma unroll
   for (int which = 0; which < 2; ++which) {  // the block's tokens so far, a lane 8 bytes
     const float from = __shfl_sync(kAll, old, 8 * which), to = __shfl_sync(kAll, scale, 8 * which);
-#pragma unroll
-    for (int k = 0; k < kTileBlocks; ++k)
-      if (k == block) (which ? vs : ks)[k] = to;
+    if (lane == 0) scales[which * kTileBlocks + block] = to;
     if (before == 0 || from == to) continue;
     uint8_t* first = (which ? p.pool.v : p.pool.k) + code_row(p.pool, max(page, 0), in_page - before, c.h);
     const uint32_t tile = which ? vt : kt;
@@ -251,15 +280,21 @@ __device__ __forceinline__ void place_new_token(const Pages8DecodeParams& p, con
   __syncwarp();
 }
 
-// What a warp keeps of its item beside its sums: the exponent field of u.
-template <bool F16, int NT>
-__device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint32_t (&qf)[NT][16], const float (&back)[NT][2],
-                                            uint32_t kt, uint32_t vt, const float (&ks)[kTileBlocks],
-                                            const float (&vs)[kTileBlocks], int seen, float c) {
+// NB blocks, of whose tokens the first `seen` belong to the request; scales: the tile's, from the first of these blocks on.
+// unit: the exponent field of u.
+template <int NB, int NT>
+__device__ __forceinline__ void attend_blocks(State<NT>& st, int& unit, const uint32_t (&qf)[NT][16], const float (&back)[NT][2],
+                                            uint32_t kt, uint32_t vt, const volatile float* scales, int seen, float c) {
   const int lane = threadIdx.x % 32;
-  float s[kTileBlocks][NT][4];
+  float ks[NB], vs[NB];
 #pragma unroll
-  for (int mt = 0; mt < kTileBlocks; ++mt) {
+  for (int i = 0; i < NB; ++i) {
+    ks[i] = scales[i];
+    vs[i] = scales[kTileBlocks + i];
+  }
+  float s[NB][NT][4];
+#pragma unroll
+  for (int mt = 0; mt < NB; ++mt) {
     float s2[NT][4];  // a chain of products for each half of the chunks
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -288,7 +323,7 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint
   // a first scale of the values, or one past the old: the sums so far count that much less
   float top_scale = vs[0];
 #pragma unroll
-  for (int mt = 1; mt < kTileBlocks; ++mt) top_scale = fmaxf(top_scale, vs[mt]);
+  for (int mt = 1; mt < NB; ++mt) top_scale = fmaxf(top_scale, vs[mt]);
   const int field = stored_field(top_scale);
   if (field > unit) {
     const float keep = unit > 0 ? power_of_field(unit) * inverse_of_field(field) : 0.f;
@@ -300,16 +335,16 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint
 #pragma unroll
         for (int i = 0; i < 4; ++i) st.o[nt][d][i] *= keep;
   }
-  float share[kTileBlocks];
+  float share[NB];
 #pragma unroll
-  for (int mt = 0; mt < kTileBlocks; ++mt) share[mt] = vs[mt] * inverse_of_field(unit);
+  for (int mt = 0; mt < NB; ++mt) share[mt] = vs[mt] * inverse_of_field(unit);
   const int g = lane / 4;
-  uint32_t pf[kTileBlocks][NT][2];
+  uint32_t pf[NB][NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    if (seen < kTile) {
+    if (seen < NB * kBlock8) {
 #pragma unroll
-      for (int mt = 0; mt < kTileBlocks; ++mt)
+      for (int mt = 0; mt < NB; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (16 * mt + g + 8 * (i / 2) >= seen) s[mt][nt][i] = -INFINITY;
@@ -319,7 +354,7 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint
     for (int j = 0; j < 2; ++j) {
       top[j] = fmaxf(s[0][nt][j], s[0][nt][2 + j]);
 #pragma unroll
-      for (int mt = 1; mt < kTileBlocks; ++mt) top[j] = fmaxf(top[j], fmaxf(s[mt][nt][j], s[mt][nt][2 + j]));
+      for (int mt = 1; mt < NB; ++mt) top[j] = fmaxf(top[j], fmaxf(s[mt][nt][j], s[mt][nt][2 + j]));
     }
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) {
@@ -343,7 +378,7 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint
       }
     }
 #pragma unroll
-    for (int mt = 0; mt < kTileBlocks; ++mt) {
+    for (int mt = 0; mt < NB; ++mt) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float m = st.m[nt][i % 2];
@@ -356,7 +391,7 @@ __device__ __forceinline__ void attend_tile(State<NT>& st, int& unit, const uint
     }
   }
 #pragma unroll
-  for (int mt = 0; mt < kTileBlocks; ++mt)
+  for (int mt = 0; mt < NB; ++mt)
 #pragma unroll
     for (int d = 0; d < 8; d += 2) {
       uint32_t r[4];
@@ -382,19 +417,20 @@ __device__ void consume(const Pages8DecodeParams& p, Cursor c, const Work& w, in
   const float cs = p.scale * kLog2e;
   float* scratch = reinterpret_cast<float*>(smem + Smem::scratch);
   const int* kept = reinterpret_cast<const int*>(smem + Smem::lengths);
-  const volatile float* scales = reinterpret_cast<const volatile float*>(smem + Smem::scales);
+  volatile float* scales = reinterpret_cast<volatile float*>(smem + Smem::scales);
   uint32_t n = 0;
   bool alive = true;  // false: a wait ran out, and the warp only keeps up with the others' barriers
   // unit of the first item's first tile
   int tile_u0 = w.u0 - w.first_unit + kItemCost;
-  Queries<NT> queries;
-  if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);
+  constexpr bool kEarly = NT == 1;  // (those of 16 queries would be in the sums' way)
+  MyQueries<NT> queries;
+  if (kEarly) fetch_my_queries<NT>(p, c.b, c.h, queries);
   while (tiles > 0) {
-    if (NT > 1) fetch_queries<NT>(p, c.b, c.h, queries);
+    if (!kEarly) fetch_my_queries<NT>(p, c.b, c.h, queries);
     const bool begins = c.t == 0, whole = begins && c.tiles <= tiles;
     uint32_t qf[NT][16];
     float back[NT][2];
-    stage_queries<F16, NT>(p, queries, base + Smem::scratch + warp * 8 * kQRowBytes, qf, back);
+    stage_queries<F16, NT>(p, c.b, queries, base + Smem::scratch, qf, back);
     State<NT> st;
     int unit = 0;
 #pragma unroll
@@ -414,20 +450,21 @@ __device__ void consume(const Pages8DecodeParams& p, Cursor c, const Work& w, in
       const int seen = c.len - c.t * kTile;
       __syncwarp();
       if (alive && seen > 0) {
-        float ks[kTileBlocks], vs[kTileBlocks];
-#pragma unroll
-        for (int i = 0; i < kTileBlocks; ++i) {
-          ks[i] = scales[s * kScaleLanes + i];
-          vs[i] = scales[s * kScaleLanes + kTileBlocks + i];
-        }
-        if (seen < kTile) {
-          // what follows the request's last token may be anything, and 0 times NaN is no 0
-          for (int i = seen * 8 + lane; i < kTile * 8; i += 32)
-            st_shared16(vt + swizzled(i / 8, i % 8), make_uint4(0u, 0u, 0u, 0u));
-        }
-        if (seen <= kTile && p.store) place_new_token<F16>(p, c, kt, vt, seen - 1, ks, vs);
+        volatile float* its = scales + s * kScaleLanes;
+        // what follows the request's last token may be anything, and 0 times NaN is no 0
+        const bool few = NT == 1 && seen <= kFewTokens;
+        const int end = few ? (seen + kBlock8 - 1) & ~(kBlock8 - 1) : kTile;
+        for (int i = seen * 8 + lane; i < end * 8; i += 32)
+          st_shared16(vt + swizzled(i / 8, i % 8), make_uint4(0u, 0u, 0u, 0u));
+        if (seen <= kTile && p.store) place_new_token<F16>(p, c, kt, vt, seen - 1, its);
         __syncwarp();
-        attend_tile<F16, NT>(st, unit, qf, back, kt, vt, ks, vs, seen, cs);
+        if (few) {
+#pragma unroll 1
+          for (int i = 0; i < end; i += kBlock8)
+            attend_blocks<1, NT>(st, unit, qf, back, kt + i * kHeadDim, vt + i * kHeadDim, its + i / kBlock8, seen - i, cs);
+        } else {
+          attend_blocks<kTileBlocks, NT>(st, unit, qf, back, kt, vt, its, seen, cs);
+        }
         if (seen <= kTile) fence_proxy_async_shared();  // TMA writes the stage again
       }
       __syncwarp();
@@ -437,7 +474,7 @@ __device__ void consume(const Pages8DecodeParams& p, Cursor c, const Work& w, in
     const Cursor done = c;
     if (tiles > 0) {  // the next item's queries come in meanwhile
       next_item<Kind<F16>>(p, kept, c);
-      if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);  // (of 16 queries they would take the sums' registers)
+      if (kEarly) fetch_my_queries<NT>(p, c.b, c.h, queries);
     }
     const float in_full = unit > 0 ? power_of_field(unit) : 0.f;
 #pragma unroll
