@@ -124,14 +124,25 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
   };
   const auto page_taken = [&](int k) { return k < freed ? given_back(freed - 1 - k) : p.free_pages[count - 1 - (k - freed)]; };
 
-  const bool fills = p.part != kPlanEnd;
-  if (fills) {
-    const int first = blockIdx.x * kThreads + tid, step = gridDim.x * kThreads;
-    for (int k = first; k < taken; k += step) {
-      const int r = find(taken_to, 0, p.batch, k);
-      p.table[(int64_t)r * p.table_stride + wish_of(p, r).have + k - taken_to[r]] = page_taken(k);
-    }
-    for (int i0 = (first / 32) * kTokensPerWarp; i0 < p.tokens; i0 += (step / 32) * kTokensPerWarp) {
+  if (p.part != kPlanEnd) {
+    // warps take kTokensPerWarp tokens each, 32 pages taken or 32 places of the list, one kind beside the other
+    const int back = refused ? 0 : max((int)left - count, 0);
+    const int token_units = (p.tokens + kTokensPerWarp - 1) / kTokensPerWarp, page_units = (taken + 31) / 32;
+    const int units = token_units + page_units + (back + 31) / 32, step = gridDim.x * (kThreads / 32);
+    for (int u = blockIdx.x * (kThreads / 32) + warp; u < units; u += step) {
+      if (u >= token_units + page_units) {
+        const int j = (u - token_units - page_units) * 32 + lane;
+        if (j < back) p.free_pages[count + j] = given_back(j);
+        continue;
+      }
+      if (u >= token_units) {
+        const int k = (u - token_units) * 32 + lane;
+        if (k >= taken) continue;
+        const int r = find(taken_to, 0, p.batch, k);
+        p.table[(int64_t)r * p.table_stride + wish_of(p, r).have + k - taken_to[r]] = page_taken(k);
+        continue;
+      }
+      const int i0 = u * kTokensPerWarp;
       // the requests of the warp's tokens
       int least = 0, requests = 1;
       if (i0 < tokens) {
@@ -164,8 +175,6 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
         if (p.positions) p.positions[i] = i < tokens ? position : 0;
       }
     }
-    if (!refused)
-      for (int j = first; j < (int)left - count; j += step) p.free_pages[count + j] = given_back(j);
     if (blockIdx.x == 0) {
       for (int r = r0; r < r1; ++r) p.begin[r] = refused ? 0 : tokens_to[r];
       if (tid == 0) p.begin[p.batch] = tokens;
