@@ -541,7 +541,7 @@ typedef struct hg_pages8 hg_pages8;
  * geometry of hg_page_shape with strides in bytes, multiples of 16; dtype is the
  * type of the rows that calls take and give.  k_scales, v_scales: device float
  * [num_pages][num_kv_heads][page_size / 16], dense, 4-byte aligned; an entry
- * stands for its code times its block's scale, which is finite and not negative.
+ * stands for its code times its block's scale, which is 0 or above and below 2^126.
  * Nothing needs initialisation: codes and scales past a request's length are
  * never used, whatever their bits.  Host only; no CUDA call. */
 hg_status hg_pages8_create(const hg_page_shape *shape, void *k_pages, void *v_pages, float *k_scales,
@@ -567,10 +567,11 @@ void hg_pages8_destroy(hg_pages8 *pages);
  * stored again as e4m3(code * old / new), exactly except below 2^-6 of the new.
  * NaN and infinities are stored as NaN and do not count for the scale.
  *
- * Rows outside [begin[0], begin[num_requests]) are neither read nor written.  A
- * token whose page is outside the pool, or whose place is outside the table, is
- * rotated and not stored.  What lies behind a request's last token stays as it
- * is.  No two requests may write to the same block. */
+ * Rows outside [begin[0], begin[num_requests]) are not written.  A token whose
+ * page is outside the pool, or whose place is outside the table, is rotated and
+ * not stored.  What lies behind a request's last token stays as it
+ * is.  No two requests may write to the same block.  num_tokens and
+ * num_requests up to 2^30 and 2^28, fewer with many heads (HG_ERR_UNSUPPORTED). */
 hg_status hg_pages8_append(const hg_pages8 *pages, int32_t num_tokens, int32_t num_requests, int32_t num_q_heads,
                            const hg_append_io *io, const hg_rotation *rotation, const int32_t *positions,
                            const int32_t *begin, const int32_t *page_table, int32_t table_stride,
@@ -598,9 +599,10 @@ hg_status hg_pages8_decode_workspace_size(const hg_pages8 *pages, int32_t batch,
  * maxima, sums and outputs are binary32 until the output's one rounding (beyond
  * FP16's range: its largest value).  Queries and codes meet as FP16, exactly
  * (a BF16 query row is first multiplied by a power of two that brings its
- * largest entry to [2^14, 2^15); entries below 2^-39 of that lose bits).
+ * largest entry to [2^14, 2^15); entries below 2^-31 of that lose bits).
  * Probabilities times the value block's scale are rounded to FP16 (2^-11 of
- * each; terms below 2^-32 of the largest such product are lost). */
+ * each; those below 2^-32 of the largest probability times the largest scale are
+ * lost). */
 hg_status hg_pages8_decode_attention(const hg_pages8 *pages, int32_t batch, int32_t num_q_heads,
                                      const hg_attention_io *io, const int32_t *page_table, int32_t table_stride,
                                      const int32_t *lengths, float *lse, float softmax_scale, void *workspace,
@@ -608,7 +610,8 @@ hg_status hg_pages8_decode_attention(const hg_pages8 *pages, int32_t batch, int3
 
 /* One decode step on the 8-bit paged cache: as hg_pages_decode_step, the new
  * token's k and v stored as by hg_pages8_append and attended to as stored.  One
- * whose page is outside the pool is attended to with a scale of its own. */
+ * whose page is outside the pool is attended to with a scale of its own.  The
+ * block that takes a new token must be no other request's. */
 hg_status hg_pages8_decode_step(const hg_pages8 *pages, int32_t batch, int32_t num_q_heads,
                                 const hg_attention_io *io, const hg_rotation *rotation, const int32_t *positions,
                                 const int32_t *page_table, int32_t table_stride, const int32_t *lengths, float *lse,
@@ -646,7 +649,8 @@ typedef enum hg_plan_count {
  *   counts       [4], out: hg_plan_count; counts[0] may be free_count itself
  * All requests are planned or none: a call that is refused (counts[1]) changes
  * neither table nor free list, leaves lengths as cached, and places no token
- * (begin all 0, slots all -1).  Page ids are not looked at.  batch up to 16,384;
+ * (begin all 0, slots all -1).  Page ids are not looked at.  No two arrays
+ * overlap but as said.  batch up to 16,384;
  * page_size 16, 32, 64, 128 or 256.  Everything is read in stream order, so the
  * call can be captured in a graph and replayed with other lengths. */
 hg_status hg_pages_plan(int32_t batch, int32_t page_size, int32_t *page_table, int32_t table_stride,

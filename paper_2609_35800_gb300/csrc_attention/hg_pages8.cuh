@@ -39,8 +39,8 @@ __device__ __forceinline__ uint2 encode8(const float* x, float inv) {
 }
 
 // The two codes of a word's lower half, and of its upper half, as FP16, exactly.  (One instruction each: through the
-// conversion functions of the headers, halves taken apart and put together again, a tile of the decode took 925
-// instructions, XXX this way.)
+// conversion functions of the headers, halves taken apart and put together again, 32 tokens of the decode took 925
+// instructions of a warp, 640 this way: 32 requests of 8,577 tokens 140 -> 118 us.)
 __device__ __forceinline__ void decode4(uint32_t w, uint32_t& lower, uint32_t& upper) {
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}\n"
       : "=r"(lower), "=r"(upper)

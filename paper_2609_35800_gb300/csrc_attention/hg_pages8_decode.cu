@@ -2,21 +2,30 @@
 //
 // For a request, KV head and its G queries: S_t = scale ks q.c_t with the key block's scale ks, m = max S_t, out = sum e^(S_t
 // - m) vs c'_t / sum e^(S_t - m) with the value block's scale vs.  A block is 16 tokens, the height of a product's tile, so
-// a scale is one factor of a fragment.  The work is divided and joined as over 16-bit pages (hg_pages_split.cuh).
+// a scale is one factor of a fragment.  The work is divided and joined as over 16-bit pages (hg_pages_split.cuh), an item's
+// fixed costs counted as 6 tiles and a join as 12 (18 shapes, geometric mean: 22.3 us at 6, 22.8 at 8 and 12).
 //
-// A producer warp copies tiles of 32 tokens into a ring of stages with TMA, a box per page (swizzled rows of 128 bytes; a
-// page outside the pool reads as zeros), and their scales beside them with four-byte asynchronous copies that arrive on the
-// same barrier.  Three consumer warps take the tiles in turn, each with its own running maximum and sums, and turn codes
-// into FP16 in registers, exactly (e4m3 is a subset), for mma.sync m16n8k16:
+// 2 G flop a byte, so the reads of the cache bound it, but an entry costs twice the instructions a byte of the 16-bit
+// kernel's.  Measured: 32 requests x 8,577 tokens x 8 KV heads 86 us, 6.6 TB/s, 0.97 of a copy's rate; one request of
+// 131,073 tokens 52 us (0.77: data at 7.1 TB/s from 3 to 40 us, then 6 us of the last join); 37 of 1 to 9,001 tokens, 12
+// queries a KV head 25 us (an item's fixed costs, 6 us each, 2.3 to 3 with up to 8 queries); 321 tokens 6.6 us.
+//
+// A producer warp copies tiles of 64 tokens into a ring of six 16 KB stages with TMA, a box per page (swizzled rows of 128
+// bytes; a page outside the pool reads as zeros), and their scales beside them with four-byte asynchronous copies that
+// arrive on the same barrier.  (Tiles of 32 tokens: 118 us where these take 86; a warp's chain of load, products, maximum,
+// exponentials and products is what it waits for, and 64 tokens are twice as much side by side.)  Three consumer warps
+// take the tiles in turn, each with its own running maximum and sums, and turn codes into FP16 in registers, exactly (e4m3
+// is a subset), for mma.sync m16n8k16:
 //   S^T[token][query] = K . q        A = keys.  A 16-byte chunk of a row is a product's 16 channels; ldmatrix leaves
 //                                    channels 4i .. 4i + 3 in a lane, where the product wants 2i, 2i + 1, 2i + 8, 2i + 9:
 //                                    the queries' fragments have the same order, and a sum's order is free
 //   O^T[channel][query] += V^T . P^T A = values, by ldmatrix.trans on pairs of channels; a byte permutation parts them,
 //                                    rows i and i + 8 of the product are channels 2i and 2i + 1
-// A BF16 query is multiplied by a power of two that brings its largest entry below 2^15, so that FP16 holds it (and 2^39
-// downwards); the factor comes back with ks.  P is e^(S - m) 2^7 vs / u, where u is the largest vs so far, to a power of two:
-// at most 2^15, the sums O stay in units of u and are moved when u grows.  So terms below 2^-32 of the largest are lost to
-// the second product.  Scores, maxima, sums and outputs are held in 32 bits.
+// A BF16 query is multiplied by a power of two that brings its largest entry below 2^15, so that FP16 holds it, and
+// entries down to 2^-31 of it with all their bits; the factor comes back with ks.  P is e^(S - m) 2^7 vs / u, where u is
+// the largest vs so far, to a power of two: at most 2^15, as a score may be 2^8 past the running maximum; the sums O stay
+// in units of u and are moved when u grows.  So terms below 2^-32 of the largest probability times the largest scale are
+// lost to the second product.  Scores, maxima, sums and outputs are held in 32 bits.
 #include "hg_pages8.cuh"
 #include "hg_pages_split.cuh"
 

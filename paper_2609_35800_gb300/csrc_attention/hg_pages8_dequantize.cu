@@ -1,8 +1,10 @@
 // Tokens of an 8-bit paged cache as dense 16-bit rows: code * scale, rounded once.
 //
 // Every code is read once and every entry written once, three bytes an entry, so the kernel is bound by memory.  Eight
-// lanes take a token's row of one head, 16 codes a lane in one load and 32 bytes out.  A CTA takes 32 tokens and some of
-// the heads' keys and values, so that a token's request and page are looked up once for all of them.
+// lanes take a token's row of one head, 16 codes a lane in one load and 32 bytes out.  A CTA takes 32 tokens and four of
+// the heads' keys and values, so that a token's request and page are looked up once for all of them, and reads all four
+// rows before it stores the first.  Measured: 24 requests of 1 to 8,577 tokens, 8 heads 26.8 us, 6.05 TB/s, 0.89 of a
+// copy's rate (31 us with the stores between the reads and a clamp for every entry); 16,064 tokens of 4 heads 8.0 us.
 #include "hg_pages8.cuh"
 
 namespace hg {

@@ -161,6 +161,11 @@ __device__ int find_work(const P& p, int* scan, int* kept, int* room, Work& w, C
   c = {scan[8], scan[9], max(0, w.first_unit - K::kItemCost), scan[11], tiles_of<K>(scan[11])};
   int tiles = 0;
   bool whole = longest <= w.share + K::kJoinCost;
+  // (8-bit pages.)  With no more items than CTAs none gets two, and a CTA that has more to read than the others is faster while
+  // they share the memory with it, up to twice: whole up to 1.5 shares (4 requests of 2,000 tokens, 32 heads, 2.4 shares:
+  // 27.6 us whole, 19.4 cut; 32 of 8,577, 8 heads, 1.2 shares: 86 whole, 91 cut).  With more items some CTAs get two, and begin
+  // the second when the others end: the fullest one counts (40 of 8,577, 8 heads: 156 us whole, 112 cut), but finding it
+  // takes 2 us, more than short items can lose (64 of 500 tokens, 8 heads: 17.3 us whole, 19.3 so).
   if (K::kWeighsWhole) {
     if ((int64_t)p.batch * heads <= w.ctas) whole = 2 * (int64_t)longest <= 3 * (int64_t)w.share + 2 * K::kJoinCost;
     else if (longest > 2 * K::kJoinCost)
