@@ -714,6 +714,8 @@ def _rotated_on(where, rotation, positions, tokens, device):
         return None, None
     if rotation.table.get_device() != device:
         _elsewhere(where, "the rotation's table", rotation.table, device)
+    if positions is None:
+        raise ValueError("%s: the rotation needs positions" % where)
     parts = rotation.positions
     if parts > 1 and positions.shape != (parts, tokens):
         _rotated_by(where, rotation, positions, tokens)

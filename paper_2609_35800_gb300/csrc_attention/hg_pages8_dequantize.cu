@@ -34,7 +34,15 @@ __global__ void __launch_bounds__(kThreads) pages8_dequantize_kernel(const __gri
   const int row0 = blockIdx.x * kTokens + threadIdx.x / 32 * 4;  // of the warp
   const int row = row0 + threadIdx.x % 32 / 8, c = threadIdx.x % 8;
   int r = request_of(p, row0);
-  while (r + 1 < p.requests && p.begin[r + 1] <= row) ++r;
+  if (r + 1 < p.requests && p.begin[r + 1] <= row) {  // a later one than the warp's first row's
+    ++r;
+    for (int n = p.requests - r; n > 1;) {
+      const int half = n / 2;
+      const bool right = p.begin[r + half] <= row;
+      r += right ? half : 0;
+      n = right ? n - half : half;
+    }
+  }
   if (row >= p.tokens || row < p.begin[0] || row >= p.begin[p.requests]) return;
   const int token = row - p.begin[r];
   const int page = page_of(p.pool, p.table + (int64_t)r * p.table_stride, p.table_stride, token);

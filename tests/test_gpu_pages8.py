@@ -369,6 +369,22 @@ def test_dequantize(dtype, heads, size, token_major, lens):
     assert torch.equal(k2[3:3 + total], k[3:3 + total]) and torch.equal(v2[3:3 + total], v[3:3 + total])
 
 
+def test_dequantize_many_requests():
+    """Most of them without a row, others with one, a few with many."""
+    g = _gen(23)
+    lens = [int(x) for x in torch.randint(0, 3, (3000,), generator=g, device="cuda").cpu()]
+    lens = [0 if i % 7 else n for i, n in enumerate(lens)]
+    lens[100], lens[2999], lens[0] = 300, 50, 0
+    tab, pages = _tables(g, lens, 16)
+    pool = _random_pool(g, pages, 2, 16)
+    total = sum(lens)
+    k, v = (torch.full((total, 2, D), NAN, dtype=BF16, device="cuda") for _ in "kv")
+    hg.hg_pages8_dequantize(pool.hg, _begins(lens), tab, k, v)
+    for i, x in enumerate((k, v)):
+        want = torch.cat([pool.rows(i, tab, b, n) for b, n in enumerate(lens) if n])
+        assert torch.equal(x, want.to(BF16))
+
+
 def test_dequantize_every_code_and_range():
     g = _gen(2)
     pool = Pool(g, 3, 1, 16, F16, fill=0)
@@ -450,7 +466,8 @@ def _random_pool(g, pages, heads, size, dtype=BF16):
 
 @pytest.mark.parametrize("batch,length,heads,group,size", [(1, 1, 4, 7, 16), (1, 70001, 2, 4, 64), (1, 20011, 1, 1, 16),
                                                           (3, 9001, 4, 7, 128), (130, 333, 2, 8, 32), (700, 40, 1, 3, 16),
-                                                          (2, 30000, 1, 16, 256), (40, 2000, 8, 8, 64)])
+                                                          (2, 30000, 1, 16, 256), (40, 2000, 8, 8, 64), (200, 9000, 2, 4, 32),
+                                                          (170, 6300, 2, 12, 64)])
 def test_decode_long_and_wide(batch, length, heads, group, size):
     g = _gen(length)
     lens = [max(1, length - 37 * b) for b in range(batch)]

@@ -289,6 +289,7 @@ def test_one_device(monkeypatch):
         pointer, positions, table = 5, 1, floats
     assert hg._rotated_on("f", Turn, ints, 3, 1) == (5, A)
     _raises(lambda: hg._rotated_on("f", Turn, ints, 3, 0), "the rotation's table is on cuda:1")
+    _raises(lambda: hg._rotated_on("f", Turn, None, 3, 1), "f: the rotation needs positions")
     monkeypatch.setattr(hg._types, "device", lambda: 0, raising=False)
     monkeypatch.setattr(hg._types, "stream", lambda device: 77 + device, raising=False)
     assert hg._stream_on("f", None, 0) == 77 and hg._stream_on("f", 5, 0) == 5
