@@ -650,8 +650,8 @@ typedef enum hg_plan_count {
  * All requests are planned or none: a call that is refused (counts[1]) changes
  * neither table nor free list, leaves lengths as cached, and places no token
  * (begin all 0, slots all -1).  Page ids are not looked at.  No two arrays
- * overlap but as said.  batch up to 16,384;
- * page_size 16, 32, 64, 128 or 256.  Everything is read in stream order, so the
+ * overlap but as said.  batch up to 16,384, batch * table_stride below 2^31,
+ * max_tokens up to 2^30; page_size 16, 32, 64, 128 or 256.  Everything is read in stream order, so the
  * call can be captured in a graph and replayed with other lengths. */
 hg_status hg_pages_plan(int32_t batch, int32_t page_size, int32_t *page_table, int32_t table_stride,
                         const int32_t *cached, const int32_t *new_tokens, int32_t *free_pages, int32_t free_capacity,

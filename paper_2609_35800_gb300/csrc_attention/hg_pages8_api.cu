@@ -227,7 +227,8 @@ hg_status hg_pages_plan(int32_t batch, int32_t page_size, int32_t* page_table, i
   if (batch > 0 && (!cached || !new_tokens || !lengths || (table_stride > 0 && !page_table))) return HG_ERR_INVALID_ARG;
   if (batch > kPlanMaxBatch || page_size < 16 || page_size > 256 || (page_size & (page_size - 1)))
     return HG_ERR_UNSUPPORTED;
-  if ((int64_t)table_stride * page_size > INT32_MAX || max_tokens > kMaxRows) return HG_ERR_UNSUPPORTED;
+  if ((int64_t)table_stride * page_size > INT32_MAX || (int64_t)batch * table_stride > INT32_MAX || max_tokens > kMaxRows)
+    return HG_ERR_UNSUPPORTED;
   for (const int32_t* x : {static_cast<const int32_t*>(page_table), cached, new_tokens, static_cast<const int32_t*>(free_pages),
                            free_count, static_cast<const int32_t*>(lengths), static_cast<const int32_t*>(begin),
                            static_cast<const int32_t*>(slots), static_cast<const int32_t*>(positions),

@@ -7,8 +7,8 @@
 // but latency.  Every CTA works out the sums for itself, in shared memory, and takes some of the tokens and pages: what it
 // reads for them no other one writes, but for lengths and counts where they are the inputs' own: then a call of up to
 // kTokensPerCta tokens is one CTA, which writes those last, and a larger one has a second launch that does it.  Measured
-// (device): 64 requests of one token, seven that end 6.0 us (7.1 with tokens, new pages and the list's places one after the
-// other); 1,000 requests, 484,000 tokens 11.4 us (one CTA 411), of which the sums take most.
+// (device): 64 requests of one token, seven that end 5.4 us (7.1 with tokens, new pages and the list's places one after the
+// other); 1,000 requests, 484,000 tokens 10.5 us (one CTA 411), of which the sums take most.
 #include "hg_attention.h"
 #include "hg_mma.cuh"
 
@@ -19,15 +19,14 @@ constexpr int kThreads = 1024;
 constexpr int kTokensPerWarp = 128, kTokensPerCta = kThreads / 32 * kTokensPerWarp;
 constexpr unsigned kAll = 0xffffffffu;
 
+// More tokens than a call may have room for, as a sum that stays there; pages stay in 32 bits, as the table's entries do.
+constexpr uint32_t kTooMany = 0x7fffffff;
 struct Sums {
-  int64_t tokens, taken, freed;
+  uint32_t tokens;
+  int taken, freed;
 };
 __device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
-  return {a.tokens + b.tokens, a.taken + b.taken, a.freed + b.freed};
-}
-
-__device__ __forceinline__ Sums operator-(const Sums& a, const Sums& b) {
-  return {a.tokens - b.tokens, a.taken - b.taken, a.freed - b.freed};
+  return {min(a.tokens + b.tokens, kTooMany), a.taken + b.taken, a.freed + b.freed};
 }
 __device__ __forceinline__ Sums from_lane(const Sums& x, int lane) {
   return {__shfl_sync(kAll, x.tokens, lane), __shfl_sync(kAll, x.taken, lane), __shfl_sync(kAll, x.freed, lane)};
@@ -48,16 +47,17 @@ struct Wish {
   bool outgrows;
 };
 __device__ __forceinline__ Wish wish_of(const PagesPlanParams& p, int r) {
-  const int mask = (1 << p.page_shift) - 1, given = p.new_tokens[r];
+  const uint32_t mask = (1u << p.page_shift) - 1;
+  const int given = p.new_tokens[r];
   Wish w;
   w.cached = max(p.cached[r], 0);
-  const int64_t after = (int64_t)w.cached + max(given, 0), want = (after + mask) >> p.page_shift;
-  w.have = (int)(((int64_t)w.cached + mask) >> p.page_shift);
   w.tokens = max(given, 0);
-  w.freed = w.taken = 0;
+  const uint32_t after = (uint32_t)w.cached + (uint32_t)w.tokens;
+  const int want = (int)(after >> p.page_shift) + ((after & mask) != 0 ? 1 : 0);
+  w.have = (w.cached >> p.page_shift) + ((w.cached & mask) != 0 ? 1 : 0);
   w.outgrows = given >= 0 && (want > p.table_stride || after > INT32_MAX);
-  if (given < 0) w.freed = min(w.have, p.table_stride);
-  else w.taken = (int)(want - w.have);
+  w.freed = given < 0 ? min(w.have, p.table_stride) : 0;
+  w.taken = given >= 0 && !w.outgrows ? want - w.have : 0;
   return w;
 }
 
@@ -75,12 +75,12 @@ __device__ __forceinline__ int find(const int* sums, int r, int n, int x) {
 __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_constant__ PagesPlanParams p) {
   extern __shared__ int sums[];
   __shared__ Sums warp_sums[kThreads / 32];
-  __shared__ int flags[2];  // some request outgrows its row; the longest length
+  __shared__ int top;  // the longest length
   grid_launch_dependents();
   grid_dependency_wait();
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   int *tokens_to = sums, *taken_to = sums + p.batch + 1, *freed_to = taken_to + p.batch + 1;
-  if (tid < 2) flags[tid] = 0;
+  if (tid == 0) top = 0;
   const int count = min(max(*p.free_count, 0), p.free_capacity);
   const int per = (p.batch + kThreads - 1) / kThreads, r0 = min(tid * per, p.batch), r1 = min(r0 + per, p.batch);
   Sums mine = {0, 0, 0};
@@ -88,36 +88,36 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
   int longest = 0, held = 0;  // after the call; before it
   for (int r = r0; r < r1; ++r) {
     const Wish w = wish_of(p, r);
-    mine = mine + Sums{w.tokens, w.taken, w.freed};
+    mine = mine + Sums{(uint32_t)w.tokens, w.taken, w.freed};
     outgrows |= w.outgrows;
     held = max(held, w.cached);
     if (p.new_tokens[r] >= 0) longest = max(longest, w.cached + (w.outgrows ? 0 : w.tokens));
   }
-  Sums before = up_to(mine, lane);
-  if (lane == 31) warp_sums[warp] = before;
+  const Sums upto = up_to(mine, lane);
+  if (lane == 31) warp_sums[warp] = upto;
+  const bool outgrown = __syncthreads_or(outgrows) != 0;
+  if (warp == 0) warp_sums[lane] = up_to(warp_sums[lane], lane);  // a lane a warp
+  Sums before = from_lane(upto, max(lane - 1, 0));
+  if (lane == 0) before = {0, 0, 0};
   __syncthreads();
-  const Sums ahead = up_to(warp_sums[lane], lane);  // (a lane a warp)
-  const Sums all = from_lane(ahead, 31), others = from_lane(ahead, max(warp - 1, 0));
-  before = before - mine;
-  if (warp > 0) before = before + others;
-  // a refused call's sums are not used: they may pass 32 bits
+  const Sums all = warp_sums[kThreads / 32 - 1];
+  if (warp > 0) before = before + warp_sums[warp - 1];
   for (int r = r0; r < r1; ++r) {
     const Wish w = wish_of(p, r);
     tokens_to[r] = (int)before.tokens;
-    taken_to[r] = (int)before.taken;
-    freed_to[r] = (int)before.freed;
-    before = before + Sums{w.tokens, w.taken, w.freed};
+    taken_to[r] = before.taken;
+    freed_to[r] = before.freed;
+    before = before + Sums{(uint32_t)w.tokens, w.taken, w.freed};
   }
-  if (outgrows) atomicOr(&flags[0], 1);
-  const int64_t left = count + all.freed - all.taken;
+  const int64_t left = (int64_t)count + all.freed - all.taken;
+  const int refused = outgrown ? -1 : all.tokens > (uint32_t)p.tokens ? -2 : left < 0 ? (int)-left
+                                                                              : left > p.free_capacity ? -3 : 0;
   __syncthreads();
-  const int refused = flags[0] ? -1 : all.tokens > p.tokens ? -2 : left < 0 ? (int)min(-left, (int64_t)INT32_MAX)
-                                                                : left > p.free_capacity ? -3 : 0;
   if (blockIdx.x == 0) {
     longest = __reduce_max_sync(kAll, refused ? held : longest);
-    if (lane == 0) atomicMax(&flags[1], longest);
+    if (lane == 0) atomicMax(&top, longest);
   }
-  const int tokens = refused ? 0 : (int)all.tokens, taken = refused ? 0 : (int)all.taken, freed = (int)all.freed;
+  const int tokens = refused ? 0 : (int)all.tokens, taken = refused ? 0 : all.taken, freed = all.freed;
   // a page of the list's end, of those given back by their number
   const auto given_back = [&](int j) {
     const int r = find(freed_to, 0, p.batch, j);
@@ -148,7 +148,9 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
       int least = 0, requests = 1;
       if (i0 < tokens) {
         least = find(tokens_to, 0, p.batch, i0);
-        requests = find(tokens_to, least, p.batch - least, min(i0 + kTokensPerWarp, tokens) - 1) - least + 1;
+        const int last = min(i0 + kTokensPerWarp, tokens) - 1;
+        while (least + requests < p.batch && tokens_to[least + requests] <= last) requests *= 2;
+        requests = min(requests, p.batch - least);
       }
       // (one step after the other for all of a lane's tokens, so that their reads are in flight together)
       constexpr int kMine = kTokensPerWarp / 32;
@@ -165,7 +167,7 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
         page[j] = 0;
         if (i >= tokens) continue;
         const int at = (cached[j] + i - tokens_to[r]) >> p.page_shift;
-        const int have = (int)(((int64_t)cached[j] + (1 << p.page_shift) - 1) >> p.page_shift);
+        const int have = (cached[j] >> p.page_shift) + ((cached[j] & ((1 << p.page_shift) - 1)) != 0 ? 1 : 0);
         page[j] = at < have ? p.table[(int64_t)r * p.table_stride + at] : page_taken(taken_to[r] + at - have);
       }
 #pragma unroll
@@ -191,7 +193,7 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
     p.counts[HG_PLAN_FREE] = refused ? count : (int)left;
     p.counts[HG_PLAN_REFUSED] = refused;
     p.counts[HG_PLAN_TOKENS] = tokens;
-    p.counts[HG_PLAN_LONGEST] = flags[1];
+    p.counts[HG_PLAN_LONGEST] = top;
   }
 }
 

@@ -171,6 +171,7 @@ def test_decode_workspace_size(lib, pages):
     (dict(batch=-1), INVALID), (dict(size=0), INVALID), (dict(stride=-1), INVALID), (dict(capacity=-1), INVALID),
     (dict(tokens=-1), INVALID), (dict(batch=16385), UNSUPPORTED), (dict(size=8), UNSUPPORTED), (dict(size=48), UNSUPPORTED),
     (dict(size=512), UNSUPPORTED), (dict(stride=1 << 27), UNSUPPORTED), (dict(tokens=(1 << 30) + 1), UNSUPPORTED),
+    (dict(batch=16384, stride=1 << 17), UNSUPPORTED),
     (dict(table=None), INVALID), (dict(cached=None), INVALID), (dict(new=None), INVALID), (dict(free=None), INVALID),
     (dict(count=None), INVALID), (dict(lengths=None), INVALID), (dict(begin=None), INVALID), (dict(slots=None), INVALID),
     (dict(counts=None), INVALID),
