@@ -7,7 +7,7 @@
 //
 // 2 G flop a byte, so the reads of the cache bound it, but an entry costs twice the instructions a byte of the 16-bit
 // kernel's.  Measured: 32 requests x 8,577 tokens x 8 KV heads 86 us, 6.6 TB/s, 0.97 of a copy's rate; one request of
-// 131,073 tokens 52 us (0.77: data at 7.1 TB/s from 3 to 40 us, then 6 us of the last join); 37 of 1 to 9,001 tokens, 12
+// 131,073 tokens 50 us (0.79: data at 7.1 TB/s from 3 to 40 us, the slowest CTA 3 us later, then the last join); 37 of 1 to 9,001 tokens, 12
 // queries a KV head 25 us (an item's fixed costs, 6 us each, 2.3 to 3 with up to 8 queries); 321 tokens 6.6 us.
 //
 // A producer warp copies tiles of 64 tokens into a ring of six 16 KB stages with TMA, a box per page (swizzled rows of 128
@@ -66,6 +66,7 @@ static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 template <bool F16>
 struct Kind {
   static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers, kItemCost = hg::kItemCost, kJoinCost = hg::kJoinCost;
+  static constexpr int kTwoLevels = 8;  // 131,073 tokens, 38 parts of 4 queries by three groups each: 50.4 us, 51.6 at 24
   static constexpr bool kWeighsWhole = true;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = 0x1p-7f;

@@ -67,6 +67,7 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
 template <bool F16>
 struct Kind {
   static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers, kItemCost = hg::kItemCost, kJoinCost = hg::kJoinCost;
+  static constexpr int kTwoLevels = 24;
   static constexpr bool kWeighsWhole = false;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = F16 ? 0x1p-7f : 1.f;

@@ -1,8 +1,9 @@
 // The paged decode kernels' division of work and what becomes of its parts: an even share of a launch's tiles for every
 // CTA whatever the requests' lengths, parts of an item joined by the last CTA to arrive, results written.  What a tile
 // holds, and how it is computed, is the kernels' own.  P: their launch parameters; K: kTile (tokens of a tile), kItemCost
-// (an item's fixed costs, in tiles), kJoinCost (a ticket and a join, in tiles), kWeighsWhole (whether the
-// fullest CTA counts, not the longest item alone), kConsumers (warps, ahead of the producer's), kF16 (the rows' type), kUnlift (1 / the factor that probabilities are lifted by), result (what an output entry becomes before it is rounded), place (a fragment's two
+// (an item's fixed costs, in tiles), kJoinCost (a ticket and a join, in tiles), kTwoLevels (parts for each of
+// the groups of threads that share a query's, from which on they are joined 16 CTAs at a time first), kWeighsWhole (whether
+// the fullest CTA counts, not the longest item alone), kConsumers (warps, ahead of the producer's), kF16 (the rows' type), kUnlift (1 / the factor that probabilities are lifted by), result (what an output entry becomes before it is rounded), place (a fragment's two
 // channels into a row of sums).
 #pragma once
 #include "hg_rows.cuh"
@@ -330,7 +331,7 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
   const int lane = threadIdx.x % 32, mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
   // up to six queries: several groups of threads share a query's parts, each takes every `subs`-th
   const int subs = max(1, kGroups<K> / p.group);
-  const bool two_levels = cta1 - cta0 >= 24 * subs;
+  const bool two_levels = cta1 - cta0 >= (subs > 1 ? K::kTwoLevels : 24) * subs;
   for (int level = two_levels ? 0 : 1; level < 2; ++level) {
     // the parts of this level: CTA `first` (level 1 of two: then the first CTA of each further 16), `stride` apart
     const int round = blockIdx.x & ~(kJoinCtas - 1);
