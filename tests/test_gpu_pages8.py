@@ -115,7 +115,8 @@ NEW = [1, 40, 30, 1, 16, 17, 0, 9, 0, 95]
 
 @TYPES
 @pytest.mark.parametrize("heads,group,size,token_major", [(4, 7, 16, False), (2, 3, 32, True), (8, 1, 256, False),
-                                                         (1, 16, 64, True), (5, 12, 128, False)])
+                                                         (1, 16, 64, True), (5, 12, 128, False), (3, 1, 32, True),
+                                                         (1, 1, 16, False)])
 def test_append(dtype, heads, group, size, token_major):
     """Without a rotation the stored values are the inputs' own: every byte and scale of the pool as defined."""
     g = _gen(heads * 10 + group)
@@ -362,6 +363,10 @@ def test_dequantize(dtype, heads, size, token_major, lens):
         want = torch.cat([pool.rows(i, tab, b, n) for b, n in enumerate(lens)])
         assert torch.equal(x[3:3 + total], want.to(dtype))
         assert bool(x[:3].isnan().all()) and bool(x[3 + total:].isnan().all())
+    # rows that are 16-byte aligned, no more
+    narrow = torch.full((total + 8, heads, D + 8), NAN, dtype=dtype, device="cuda")
+    hg.hg_pages8_dequantize(pool.hg, begin, tab, narrow[:, :, 8:], v)
+    assert torch.equal(narrow[3:3 + total, :, 8:], k[3:3 + total]) and bool(narrow[:, :, :8].isnan().all())
     # one of the two alone
     k2, v2 = torch.full_like(k, NAN), torch.full_like(v, NAN)
     hg.hg_pages8_dequantize(pool.hg, begin, tab, k2)
@@ -568,6 +573,48 @@ def test_decode_odd_places():
     assert bool((out[0] == 0).all())
     out, lse = _run_decode(pool, q, tab[:, :0], lens)
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
+@TYPES
+def test_decode_most_heads(dtype):
+    """64 KV heads of 16 queries each."""
+    g = _gen(24)
+    lens = [1, 70, 300, 1000]
+    tab, pages = _tables(g, lens, 64)
+    pool = _random_pool(g, pages, 64, 64, dtype)
+    q = _randn(g, 4, 1024, D, dtype=dtype, scale=0.2)
+    out, lse = _run_decode(pool, q, tab, lens)
+    _check_decode(q, pool, tab, lens, out, lse)
+
+
+def test_keys_and_values_in_one_tensor():
+    """Pages that lie [pages][2][heads][tokens][128], heads and tokens with room between them: append, decode, dense rows."""
+    g = _gen(25)
+    lens, heads, size = [100, 7, 65], 3, 32
+    tab, pages = _tables(g, lens, size)
+    both = torch.randint(0, 256, (pages, 2, heads + 1, size + 2, D + 16), generator=g, device="cuda", dtype=torch.uint8)
+    kept = both.clone()
+    view = both[:, :, :heads, :size, :D]
+    pool, twin = Pool(_gen(1), pages, heads, size), Pool(_gen(1), pages, heads, size)
+    pool.codes = [view[:, 0], view[:, 1]]
+    pool.hg = hg.hg_pages8_create(*pool.codes, *pool.scales, BF16)
+    k, v = (_randn(g, sum(lens), heads, D) for _ in "kv")
+    for x in (pool, twin):
+        hg.hg_pages8_append(x.hg, None, k, v, None, None, _begins(lens), tab, _ints(lens))
+    for i in range(2):
+        for b, n in enumerate(lens):
+            assert torch.equal(pool.rows(i, tab, b, n), twin.rows(i, tab, b, n))
+    q = _randn(g, 3, 2 * heads, D)
+    out, lse = _run_decode(pool, q, tab, lens)
+    want, lse2 = _run_decode(twin, q, tab, lens)
+    assert torch.equal(out, want) and torch.equal(lse, lse2)
+    rows = [torch.empty_like(k) for _ in range(4)]
+    hg.hg_pages8_dequantize(pool.hg, _begins(lens), tab, *rows[:2])
+    hg.hg_pages8_dequantize(twin.hg, _begins(lens), tab, *rows[2:])
+    assert torch.equal(rows[0], rows[2]) and torch.equal(rows[1], rows[3])
+    inside = torch.zeros_like(both, dtype=torch.bool)
+    inside[:, :, :heads, :size, :D] = True
+    assert torch.equal(both[~inside], kept[~inside])  # nothing between the rows is touched
 
 
 @pytest.mark.parametrize("scale", [0.5, 1e-3])
