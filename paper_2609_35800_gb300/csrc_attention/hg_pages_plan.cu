@@ -6,9 +6,10 @@
 // it; each token, page and place is then found by a search in its sum.  A few bytes a request and eight a token: nothing
 // but latency.  Every CTA works out the sums for itself, in shared memory, and takes some of the tokens and pages: what it
 // reads for them no other one writes, but for lengths and counts where they are the inputs' own: then a call of up to
-// kTokensPerCta tokens is one CTA, which writes those last, and a larger one has a second launch that does it.  Measured
-// (device): 64 requests of one token, seven that end 5.4 us (7.1 with tokens, new pages and the list's places one after the
-// other); 1,000 requests, 484,000 tokens 10.5 us (one CTA 411), of which the sums take most.
+// kAlone tokens is one CTA, which writes those last, and a larger one has a second launch that does it.  Measured
+// (device): 64 requests of one token, seven that end 4.2 us (7.1 with tokens, new pages and the list's places one after the
+// other); 1,000 requests, 484,000 tokens 8.2 us (one CTA 411; 64 tokens a warp 7.6 and 4.8, 128 10.5 and 5.4), most of it
+// for the sums and the searches.
 #include "hg_attention.h"
 #include "hg_mma.cuh"
 
@@ -16,7 +17,7 @@ namespace hg {
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kTokensPerWarp = 128, kTokensPerCta = kThreads / 32 * kTokensPerWarp;
+constexpr int kAlone = 4096;  // tokens that one CTA places where a second launch is the alternative
 constexpr unsigned kAll = 0xffffffffu;
 
 // More tokens than a call may have room for, as a sum that stays there; pages stay in 32 bits, as the table's entries do.
@@ -96,7 +97,10 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
   const Sums upto = up_to(mine, lane);
   if (lane == 31) warp_sums[warp] = upto;
   const bool outgrown = __syncthreads_or(outgrows) != 0;
-  if (warp == 0) warp_sums[lane] = up_to(warp_sums[lane], lane);  // a lane a warp
+  if (warp == 0) {  // a lane a warp
+    const Sums x = up_to(lane < kThreads / 32 ? warp_sums[lane] : Sums{0, 0, 0}, lane);
+    if (lane < kThreads / 32) warp_sums[lane] = x;
+  }
   Sums before = from_lane(upto, max(lane - 1, 0));
   if (lane == 0) before = {0, 0, 0};
   __syncthreads();
@@ -126,9 +130,9 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
   const auto page_taken = [&](int k) { return k < freed ? given_back(freed - 1 - k) : p.free_pages[count - 1 - (k - freed)]; };
 
   if (p.part != kPlanEnd) {
-    // warps take kTokensPerWarp tokens each, 32 pages taken or 32 places of the list, one kind beside the other
+    // a warp takes 32 tokens, pages taken or places of the list at a time, one kind beside the other
     const int back = refused ? 0 : max((int)left - count, 0);
-    const int token_units = (p.tokens + kTokensPerWarp - 1) / kTokensPerWarp, page_units = (taken + 31) / 32;
+    const int token_units = (p.tokens + 31) / 32, page_units = (taken + 31) / 32;
     const int units = token_units + page_units + (back + 31) / 32, step = gridDim.x * (kThreads / 32);
     for (int u = blockIdx.x * (kThreads / 32) + warp; u < units; u += step) {
       if (u >= token_units + page_units) {
@@ -143,39 +147,23 @@ __global__ void __launch_bounds__(kThreads) pages_plan_kernel(const __grid_const
         p.table[(int64_t)r * p.table_stride + wish_of(p, r).have + k - taken_to[r]] = page_taken(k);
         continue;
       }
-      const int i0 = u * kTokensPerWarp;
-      // the requests of the warp's tokens
-      int least = 0, requests = 1;
-      if (i0 < tokens) {
-        least = find(tokens_to, 0, p.batch, i0);
-        const int last = min(i0 + kTokensPerWarp, tokens) - 1;
+      const int i = u * 32 + lane;
+      int slot = -1, position = 0;
+      if (i < tokens) {
+        // the warp's first token's request, and how far it is to the last one's
+        const int least = find(tokens_to, 0, p.batch, u * 32), last = min(u * 32 + 31, tokens - 1);
+        int requests = 1;
         while (least + requests < p.batch && tokens_to[least + requests] <= last) requests *= 2;
-        requests = min(requests, p.batch - least);
+        const int r = find(tokens_to, least, min(requests, p.batch - least), i);
+        const int cached = max(p.cached[r], 0), mask = (1 << p.page_shift) - 1;
+        position = cached + i - tokens_to[r];
+        const int at = position >> p.page_shift, have = (cached >> p.page_shift) + ((cached & mask) != 0 ? 1 : 0);
+        const int page = at < have ? p.table[(int64_t)r * p.table_stride + at] : page_taken(taken_to[r] + at - have);
+        slot = (int)((uint32_t)page << p.page_shift) + (position & mask);
       }
-      // (one step after the other for all of a lane's tokens, so that their reads are in flight together)
-      constexpr int kMine = kTokensPerWarp / 32;
-      int request[kMine], cached[kMine], page[kMine];
-#pragma unroll
-      for (int j = 0; j < kMine; ++j) {
-        const int i = min(i0 + 32 * j + lane, tokens - 1);
-        request[j] = tokens > i0 ? find(tokens_to, least, requests, i) : 0;
-        cached[j] = tokens > i0 ? max(p.cached[request[j]], 0) : 0;
-      }
-#pragma unroll
-      for (int j = 0; j < kMine; ++j) {
-        const int i = i0 + 32 * j + lane, r = request[j];
-        page[j] = 0;
-        if (i >= tokens) continue;
-        const int at = (cached[j] + i - tokens_to[r]) >> p.page_shift;
-        const int have = (cached[j] >> p.page_shift) + ((cached[j] & ((1 << p.page_shift) - 1)) != 0 ? 1 : 0);
-        page[j] = at < have ? p.table[(int64_t)r * p.table_stride + at] : page_taken(taken_to[r] + at - have);
-      }
-#pragma unroll
-      for (int j = 0; j < kMine; ++j) {
-        const int i = i0 + 32 * j + lane, position = cached[j] + i - tokens_to[request[j]];
-        if (i >= p.tokens) continue;
-        p.slots[i] = i < tokens ? (int)((uint32_t)page[j] << p.page_shift) + (position & ((1 << p.page_shift) - 1)) : -1;
-        if (p.positions) p.positions[i] = i < tokens ? position : 0;
+      if (i < p.tokens) {
+        p.slots[i] = slot;
+        if (p.positions) p.positions[i] = position;
       }
     }
     if (blockIdx.x == 0) {
@@ -211,7 +199,7 @@ cudaError_t launch_pages_plan(const PagesPlanParams& p, cudaStream_t s) {
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
   const int smem = 3 * (p.batch + 1) * 4;
-  const int ctas = std::min((p.tokens + kTokensPerCta - 1) / kTokensPerCta, device_sms());
+  const int ctas = p.in_place && p.tokens <= kAlone ? 1 : std::min((p.tokens + kThreads - 1) / kThreads, device_sms());
   PagesPlanParams a = p;
   a.part = ctas > 1 && p.in_place ? kPlanFill : kPlanAll;
   e = launch_overlapped(pages_plan_kernel, dim3((unsigned)std::max(ctas, 1)), kThreads, smem, s, a);
