@@ -4,9 +4,10 @@
 // entries, the one of the tokens it has); code = e4m3(x / s).  A scale needs the whole block's entries before any code, so
 // a CTA takes the new tokens of one block, KV head and of the keys or the values: 16 rows, eight lanes each, 16 channels a
 // lane as hg_pages_append has them, whose largest entry passes through shared memory once.  The rows stay in registers,
-// so everything is read once and written once, and the kernel is bound by memory.  The other CTAs turn queries, two heads of a
-// token by eight lanes.  Measured: 21,400 tokens of 60 + 5 + 5 heads 144 us, 6.2 TB/s, 0.91 of a copy's rate (one head by
-// eight lanes 161 us, four 147, six 154); 1,460 tokens of 28 + 4 + 4 heads 4.8 us on the device, 16 of one token each 2.7.
+// so everything is read once and written once, and the kernel is bound by memory.  The other CTAs turn queries, two heads
+// of a token by eight lanes.  Measured: 21,400 tokens of 60 + 5 + 5 heads 142 us, 6.3 TB/s, 0.93 of a copy's rate (one
+// head by eight lanes 161 us, four 147, six 154); 1,460 tokens of 28 + 4 + 4 heads 4.8 us on the device, 16 of one token
+// each 2.7.
 //
 // Which blocks a launch touches is known on the device only.  Request r with n new tokens touches at most n / 16 + 2 of
 // them; numbered from (begin[r] - begin[0]) / 16 + 2 r on, no two requests' numbers meet, and a CTA finds its request by
