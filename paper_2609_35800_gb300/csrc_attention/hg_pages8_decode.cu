@@ -9,7 +9,7 @@
 // kernel's.  Measured: 32 requests x 8,577 tokens x 8 KV heads 86 us, 6.6 TB/s, 0.97 of a copy's rate; one request of
 // 131,073 tokens 50 us (0.79: data at 7.1 TB/s from 3 to 40 us, the slowest CTA 3 us later, then the last join); 37 of 1
 // to 9,001 tokens, 12 queries a KV head 25 us (14 tiles a CTA in five rounds of 2.2 us, start, sums and joins; an item of one
-// tile takes a CTA 6 us, 3 with up to 8 queries); 321 tokens 6.6 us.
+// tile takes a CTA 6 us, 3 with up to 8 queries); 321 tokens 6.0 us.
 //
 // A producer warp copies tiles of 64 tokens into a ring of six 16 KB stages with TMA, a box per page (swizzled rows of 128
 // bytes; a page outside the pool reads as zeros), and their scales beside them with four-byte asynchronous copies that
@@ -84,6 +84,9 @@ __device__ __forceinline__ void tma_page8(uint32_t dst, const CUtensorMap* map, 
       "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(head), "r"(page), "r"(bar)
       : "memory");
 }
+__device__ __forceinline__ void st_shared4(uint32_t addr, float x) {
+  asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(addr), "f"(x) : "memory");
+}
 // Four bytes, or zeros where `bytes` is 0.
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, int bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -138,6 +141,70 @@ __device__ uint32_t produce(const Pages8DecodeParams& p, Cursor c, int tiles, co
         cp_async4(stages + Smem::scales + (s * kScaleLanes + lane) * 4, src, there ? 4 : 0);
         cp_async_arrive(full + 8 * s);
       }
+    }
+  }
+  return n;
+}
+
+// The same for pages of 16 tokens, of which a tile is four: eight copies and as many scales' addresses are what everybody
+// waits for, so a lane keeps a page and its two scales, 32 pages of an item at a time and the next ones' numbers, and stores
+// scales from registers (32 requests x 8,577 tokens, 8 KV heads 100 -> 89 us; 321 tokens 6.6 -> 6.0).  Larger pages lose more
+// to the wait for 32 boxes' scales than they gain (pages of 64: 86 -> 89 us).
+template <class K>
+__device__ uint32_t produce_blocks(const Pages8DecodeParams& p, Cursor c, int tiles, const int* kept, uint32_t stages,
+                                   uint32_t full, uint32_t empty, volatile int* abort) {
+  constexpr uint32_t kBoxBytes = kBlock8 * kHeadDim;
+  const int lane = threadIdx.x % 32;
+  uint32_t n = 0;
+  // the pages from `first` of request `of` on, and the head whose scales are here; the 32 pages behind them
+  int of = -1, head = -1, first = 0, page = -1, next = -1;
+  float ks = 0.f, vs = 0.f;
+  for (; tiles > 0; next_item<K>(p, kept, c)) {
+    const int* ids = p.table + (int64_t)c.b * p.table_stride;
+    const int pages = (c.len + kBlock8 - 1) / kBlock8;
+    for (; c.t < c.tiles && tiles > 0; ++c.t, --tiles, ++n) {
+      const int at = c.t * kTileBlocks, valid = min(kTileBlocks, pages - at);
+      const bool fresh = of != c.b || at < first || at + kTileBlocks > first + 32;
+      if (fresh || head != c.h) {
+        if (fresh) {
+          page = of == c.b && at == first + 32 ? next : at + lane < pages ? ids[at + lane] : -1;
+          of = c.b;
+          first = at;
+          next = first + 32 + lane < pages ? ids[first + 32 + lane] : -1;
+        }
+        head = c.h;
+        const bool there = page >= 0 && page < p.pool.num_pages;
+        const int64_t place = scale_at(p.pool, there ? page : 0, 0, head);
+        ks = there ? p.pool.k_scales[place] : 0.f;
+        vs = there ? p.pool.v_scales[place] : 0.f;
+      } else if (at - first == 16 && next >= 0 && next < p.pool.num_pages) {
+        const int64_t place = scale_at(p.pool, next, 0, head);
+        prefetch_l2(p.pool.k_scales + place);
+        prefetch_l2(p.pool.v_scales + place);
+      }
+      const int s = n % kStages;
+      if (n >= kStages && !wait_warp(empty + 8 * s, (n / kStages - 1) & 1, abort, p.status)) return n;
+      int box[kTileBlocks];
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) box[i] = __shfl_sync(kAll, page, (at - first + i) & 31);
+      if (elect_one()) {
+        mbar_arrive_expect_tx(full + 8 * s, 2 * max(valid, 0) * kBoxBytes);
+#pragma unroll
+        for (int i = 0; i < kTileBlocks; ++i) {
+          if (i >= valid) break;
+          const uint32_t dst = stages + s * kStageBytes + i * kBoxBytes;
+          tma_page8(dst, &p.k_map, 0, c.h, box[i], full + 8 * s);
+          tma_page8(dst + kHalfBytes, &p.v_map, 0, c.h, box[i], full + 8 * s);
+        }
+      }
+      const int mine = lane - (at - first);
+      if (mine >= 0 && mine < kTileBlocks) {
+        const uint32_t slot = stages + Smem::scales + (s * kScaleLanes + mine) * 4;
+        st_shared4(slot, ks);
+        st_shared4(slot + 4 * kTileBlocks, vs);
+      }
+      __syncwarp();
+      if (elect_one()) mbar_arrive(full + 8 * s);
     }
   }
   return n;
@@ -505,9 +572,11 @@ __global__ void __launch_bounds__(kThreads<Kind<F16>>, 2) pages8_decode_kernel(c
   extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_u32(smem), full = base + Smem::bars, empty = full + 8 * kStages;
   volatile int* misc = reinterpret_cast<int*>(smem + Smem::misc);  // [0] abort, [1] last part, [8 ..] scan
+  const bool blocks = p.pool.page_shift == kBlock8Shift;  // pages of 16 tokens
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(full + 8 * i, 1 + kScaleLanes);
+      // the copies that are asked for, and the scales: stored (by produce_blocks), or each with a copy of its own
+      mbar_init(full + 8 * i, 1 + (blocks ? 1 : kScaleLanes));
       mbar_init(empty + 8 * i, 1);
     }
     mbar_init_fence();
@@ -529,7 +598,8 @@ __global__ void __launch_bounds__(kThreads<Kind<F16>>, 2) pages8_decode_kernel(c
   uint32_t asked = 0;
   if (threadIdx.x / 32 == kConsumers) {
     fence_proxy_async_global();  // pages written by ordinary stores of earlier launches
-    asked = produce<Kind<F16>>(p, c, tiles, kept, base, full, empty, misc);
+    asked = blocks ? produce_blocks<Kind<F16>>(p, c, tiles, kept, base, full, empty, misc)
+                   : produce<Kind<F16>>(p, c, tiles, kept, base, full, empty, misc);
   } else {
     consume<F16, NT>(p, c, w, tiles, base, smem, misc);
   }
