@@ -67,6 +67,9 @@ static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 template <bool F16>
 struct Kind {
   static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers, kItemCost = hg::kItemCost, kJoinCost = hg::kJoinCost;
+  // Two rounds of the warps: more parts cost their join more than they save (1,475 tokens, 4 KV heads 13.7 us at 1, 9.4 at 6,
+  // 10.6 at 9), with more queries three (16 requests of 4,000 tokens, 2 KV heads, 16 queries each 21.8 us at 6, 20.0 at 9).
+  static __device__ __forceinline__ int least_share(int group) { return group > 8 ? 9 : 6; }
   static constexpr int kTwoLevels = 8;  // 131,073 tokens, 38 parts of 4 queries by three groups each: 50.4 us, 51.6 at 24
   static constexpr bool kWeighsWhole = true;
   static constexpr bool kF16 = F16;

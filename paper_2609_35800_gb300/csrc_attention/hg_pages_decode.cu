@@ -67,6 +67,7 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
 template <bool F16>
 struct Kind {
   static constexpr int kTile = hg::kTile, kConsumers = hg::kConsumers, kItemCost = hg::kItemCost, kJoinCost = hg::kJoinCost;
+  static __device__ __forceinline__ int least_share(int) { return 1; }
   static constexpr int kTwoLevels = 24;
   static constexpr bool kWeighsWhole = false;
   static constexpr bool kF16 = F16;

@@ -1,11 +1,18 @@
 // The paged decode kernels' division of work and what becomes of its parts: an even share of a launch's tiles for every
 // CTA whatever the requests' lengths, parts of an item joined by the last CTA to arrive, results written.  What a tile
-// holds, and how it is computed, is the kernels' own.  P: their launch parameters; K: kTile (tokens of a tile), kItemCost
-// (an item's fixed costs, in tiles), kJoinCost (a ticket and a join, in tiles), kTwoLevels (parts for each of the groups of
-// threads that share a query's, from which on they are joined 16 CTAs at a time first), kWeighsWhole (whether the fullest
-// CTA counts, not the longest item alone), kConsumers (warps, ahead of the producer's), kF16 (the rows' type), kUnlift (1 /
-// the factor that probabilities are lifted by), result (what an output entry becomes before it is rounded), place (a
-// fragment's two channels into a row of sums).
+// holds, and how it is computed, is the kernels' own.  P: their launch parameters.  K:
+//   kTile         tokens of a tile
+//   kItemCost     an item's fixed costs, in tiles
+//   kJoinCost     a ticket and a join, in tiles
+//   least_share   units that a CTA gets where there are fewer than that for each
+//   kTwoLevels    parts for each of the groups of threads that share a query's, from which on they are joined 16 CTAs at a
+//                 time first
+//   kWeighsWhole  whether the fullest CTA counts, not the longest item alone
+//   kConsumers    warps, ahead of the producer's
+//   kF16          the rows' type
+//   kUnlift       1 / the factor that probabilities are lifted by
+//   result        what an output entry becomes before it is rounded
+//   place         a fragment's two channels into a row of sums
 #pragma once
 #include "hg_rows.cuh"
 #include "hg_wait.cuh"
@@ -138,7 +145,8 @@ __device__ int find_work(const P& p, int* scan, int* kept, int* room, Work& w, C
     longest = max(longest, scan[12 + i]);
   }
   w.total = all * heads;
-  w.ctas = min((int)gridDim.x, w.total);
+  const int least = K::least_share(p.group);
+  w.ctas = min((int)gridDim.x, (w.total + least - 1) / least);
   if ((int)blockIdx.x >= w.ctas) return 0;
   w.share = w.total / w.ctas;
   w.more = w.total - w.share * w.ctas;
