@@ -3,7 +3,7 @@
 // For a request, KV head and its G queries: S_t = scale ks q.c_t with the key block's scale ks, m = max S_t, out = sum
 // e^(S_t - m) vs c'_t / sum e^(S_t - m) with the value block's scale vs.  A block is 16 tokens, the height of a product's
 // tile, so a scale is one factor of a fragment.  The work is divided and joined as over 16-bit pages (hg_pages_split.cuh), an item's
-// fixed costs counted as 6 tiles and a join as 12 (18 shapes, geometric mean: 22.3 us at 6, 22.8 at 8 and 12).
+// fixed costs counted as 6 tiles and a join as 12 (18 shapes, geometric mean: 20.6 us; 20.7 to 20.9 with 3, 4 or 8 and 9 or 15).
 //
 // 2 G flop a byte, so the reads of the cache bound it, but an entry costs twice the instructions a byte of the 16-bit
 // kernel's.  Measured: 32 requests x 8,577 tokens x 8 KV heads 86 us, 6.6 TB/s, 0.97 of a copy's rate; one request of
