@@ -2,14 +2,15 @@
 //
 // For a request, KV head and its G queries: S_t = scale ks q.c_t with the key block's scale ks, m = max S_t, out = sum
 // e^(S_t - m) vs c'_t / sum e^(S_t - m) with the value block's scale vs.  A block is 16 tokens, the height of a product's
-// tile, so a scale is one factor of a fragment.  The work is divided and joined as over 16-bit pages (hg_pages_split.cuh), an item's
-// fixed costs counted as 6 tiles and a join as 12 (18 shapes, geometric mean: 20.6 us; 20.7 to 20.9 with 3, 4 or 8 and 9 or 15).
+// tile, so a scale is one factor of a fragment.  The work is divided and joined as over 16-bit pages (hg_pages_split.cuh),
+// an item's fixed costs counted as 6 tiles and a join as 12 (18 shapes, geometric mean: 20.6 us; 20.7 to 20.9 with 3, 4 or
+// 8, and 9 or 15).
 //
 // 2 G flop a byte, so the reads of the cache bound it, but an entry costs twice the instructions a byte of the 16-bit
 // kernel's.  Measured: 32 requests x 8,577 tokens x 8 KV heads 86 us, 6.6 TB/s, 0.97 of a copy's rate; one request of
 // 131,073 tokens 50 us (0.79: data at 7.1 TB/s from 3 to 40 us, the slowest CTA 3 us later, then the last join); 37 of 1
-// to 9,001 tokens, 12 queries a KV head 25 us (14 tiles a CTA in five rounds of 2.2 us, start, sums and joins; an item of one
-// tile takes a CTA 6 us, 3 with up to 8 queries); 321 tokens 6.0 us.
+// to 9,001 tokens, 12 queries a KV head 25 us (14 tiles a CTA in five rounds of 2.2 us, start, sums and joins; an item of
+// one tile takes a CTA 6 us, 3 with up to 8 queries); 321 tokens 6.0 us.
 //
 // A producer warp copies tiles of 64 tokens into a ring of six 16 KB stages with TMA, a box per page (swizzled rows of 128
 // bytes; a page outside the pool reads as zeros), and their scales beside them with four-byte asynchronous copies that
