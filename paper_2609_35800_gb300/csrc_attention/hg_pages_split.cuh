@@ -108,7 +108,9 @@ __device__ int fullest_of_whole(const P& p, const int* kept, int* room, const Wo
   mine = __reduce_max_sync(kAll, mine);
   if (tid % 32 == 0) atomicMax(most, mine);
   __syncthreads();
-  return *most;
+  const int units = *most;
+  __syncthreads();  // every thread has read it: the room is the kernel's again
+  return units;
 }
 
 // The CTA's work, the first tile of it and how many there are; 0: none.  Every thread adds up the units of its share of
