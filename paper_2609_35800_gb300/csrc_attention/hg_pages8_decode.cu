@@ -26,8 +26,9 @@
 // A BF16 query is multiplied by a power of two that brings its largest entry below 2^15, so that FP16 holds it, and
 // entries down to 2^-31 of it with all their bits; the factor comes back with ks.  P is e^(S - m) 2^7 vs / u, where u is
 // the largest vs so far, to a power of two: at most 2^15, as a score may be 2^8 past the running maximum; the sums O stay
-// in units of u and are moved when u grows.  So terms below 2^-32 of the largest probability times the largest scale are
-// lost to the second product.  Scores, maxima, sums and outputs are held in 32 bits.
+// in units of u, are moved when u grows, and are multiplied by u once they are divided (before, sums of values near BF16's
+// end would pass binary32's).  So terms below 2^-32 of the largest probability times the largest scale are lost to the
+// second product.  Scores, maxima, sums and outputs are held in 32 bits.
 #include "hg_pages8.cuh"
 #include "hg_pages_split.cuh"
 
@@ -75,6 +76,7 @@ struct Kind {
   static constexpr bool kWeighsWhole = true;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = 0x1p-7f;
+  static constexpr bool kUnits = true;
   static __device__ __forceinline__ float result(float x) { return in_range<F16>(x); }
   static __device__ __forceinline__ void place(float* row, int g, float first, float second) {
     *reinterpret_cast<float2*>(row + 2 * g) = make_float2(first, second);
@@ -558,15 +560,9 @@ __device__ void consume(const Pages8DecodeParams& p, Cursor c, const Work& w, in
       next_item<Kind<F16>>(p, kept, c);
       if (kEarly) fetch_my_queries<NT>(p, c.b, c.h, queries);
     }
-    const float in_full = unit > 0 ? power_of_field(unit) : 0.f;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int d = 0; d < 8; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st.o[nt][d][i] *= in_full;
     named_barrier<kConsumers * 32>(1);  // every warp has read its queries from the scratch
-    finish_item<Kind<F16>, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs);
+    finish_item<Kind<F16>, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs,
+                                     unit > 0 ? power_of_field(unit) : 0.f);
     tile_u0 += done.tiles + kItemCost;
   }
 }

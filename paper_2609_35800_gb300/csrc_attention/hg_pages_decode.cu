@@ -72,6 +72,7 @@ struct Kind {
   static constexpr bool kWeighsWhole = false;
   static constexpr bool kF16 = F16;
   static constexpr float kUnlift = F16 ? 0x1p-7f : 1.f;
+  static constexpr bool kUnits = false;
   static __device__ __forceinline__ float result(float x) { return x; }
   static __device__ __forceinline__ void place(float* row, int g, float first, float second) {
     row[g] = first;
@@ -337,7 +338,7 @@ __device__ void consume(const PagesDecodeParams& p, Cursor c, const Work& w, int
       if (NT == 1) fetch_queries<NT>(p, c.b, c.h, queries);  // (of 16 queries they would take the sums' registers)
     }
     named_barrier<kConsumers * 32>(1);  // every warp has read its queries from the scratch
-    finish_item<Kind<F16>, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs);
+    finish_item<Kind<F16>, NT>(p, st, done, whole, begins, tile_u0, w, scratch, misc, cs, 1.f);
     tile_u0 += done.tiles + kItemCost;
   }
 }

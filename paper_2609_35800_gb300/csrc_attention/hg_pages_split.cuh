@@ -11,6 +11,7 @@
 //   kConsumers    warps, ahead of the producer's
 //   kF16          the rows' type
 //   kUnlift       1 / the factor that probabilities are lifted by
+//   kUnits        whether a query's sums are in a unit of their own, a power of two
 //   result        what an output entry becomes before it is rounded
 //   place         a fragment's two channels into a row of sums
 #pragma once
@@ -23,7 +24,7 @@ namespace {
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kKeptLengths = 72;
 constexpr int kJoinCtas = kDecodeJoinCtas, kJoinCounters = kDecodeJoinCounters;
-constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l; rows 4 banks apart
+constexpr int kSumFloats = kHeadDim + 4;  // a query's sums in shared memory: 128 channels, m, l, unit; rows 4 banks apart
 
 template <class K>
 constexpr int kThreads = (K::kConsumers + 1) * 32;
@@ -271,26 +272,35 @@ __device__ __forceinline__ float* partial_of(const P& p, int cta, bool begins) {
   return p.partials + ((int64_t)cta * 2 + (begins ? 1 : 0)) * p.group * kPartialFloats;
 }
 
-// A query's sums, 16 channels of them.
+// A query's sums, 16 channels of them, in units of u (0: there are none).  The unit is applied once the sums are divided by l:
+// times the largest values of a cache they would pass binary32's end, where their average does not.
 struct Part {
-  float m = -INFINITY, l = 0.f, o[16] = {};
+  float m = -INFINITY, l = 0.f, u = 0.f, o[16] = {};
 };
+// What sums in units of u are multiplied by to be in units of `to`, not below it; powers of two, or 0.
+__device__ __forceinline__ float units_in(float u, float to) {
+  return u * __uint_as_float((uint32_t)(254 - (int)(__float_as_uint(to) >> 23)) << 23);
+}
 // Adds up N rows of sums in shared memory, `apart` floats from one to the next: one maximum, then independent terms.
-template <int N>
+template <class K, int N>
 __device__ __forceinline__ Part add_rows(const float* row, int apart, int count, int channel, float cs) {
   Part a;
   float2 ml[N];
+  float u[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     ml[i] = i < count ? *reinterpret_cast<const float2*>(row + i * apart + kHeadDim) : make_float2(-INFINITY, 0.f);
+    u[i] = K::kUnits && i < count ? row[i * apart + kHeadDim + 2] : 0.f;
     a.m = fmaxf(a.m, ml[i].x);
+    a.u = fmaxf(a.u, u[i]);
   }
   const float base = a.m == -INFINITY ? 0.f : a.m;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     if (i >= count) break;
-    const float e = exp2_approx((ml[i].x - base) * cs);
+    float e = exp2_approx((ml[i].x - base) * cs);
     a.l += ml[i].y * e;
+    if (K::kUnits) e *= units_in(u[i], a.u);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float4 x = *reinterpret_cast<const float4*>(row + i * apart + channel + 4 * k);
@@ -302,25 +312,29 @@ __device__ __forceinline__ Part add_rows(const float* row, int apart, int count,
   }
   return a;
 }
+template <class K>
 __device__ __forceinline__ void store_part(const Part& a, float* channels, float* ml, int channel) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     *reinterpret_cast<float4*>(channels + channel + 4 * i) =
         make_float4(a.o[4 * i], a.o[4 * i + 1], a.o[4 * i + 2], a.o[4 * i + 3]);
-  if (channel == 0) *reinterpret_cast<float2*>(ml) = make_float2(a.m, a.l);
+  if (channel == 0) {
+    *reinterpret_cast<float2*>(ml) = make_float2(a.m, a.l);
+    if (K::kUnits) ml[2] = a.u;
+  }
 }
 
 // out = o / l in the cache's type, and the query's log-sum-exp (o and l are lifted alike).
 template <class K, class P>
 __device__ __forceinline__ void write_query(const P& p, int b, int h, int len, int q, int channel,
                                             const Part& a) {
-  const float r = len > 0 ? 1.0f / a.l : 0.f;
+  const float r = len > 0 ? 1.0f / a.l : 0.f, u = K::kUnits ? a.u : 1.f;
   const int head = h * p.group + q;
   uint16_t* out = p.out.data + b * p.out.token_stride + head * p.out.head_stride + channel;
   uint32_t x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    x[i] = pack2<K::kF16>(K::result(a.o[2 * i] * r), K::result(a.o[2 * i + 1] * r));
+    x[i] = pack2<K::kF16>(K::result(a.o[2 * i] * r * u), K::result(a.o[2 * i + 1] * r * u));
   *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
   *reinterpret_cast<uint4*>(out + 8) = make_uint4(x[4], x[5], x[6], x[7]);
   if (p.lse && channel == 0)
@@ -374,6 +388,7 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
         const int k = k0 + lane8 * subs;
         float2 ml = make_float2(-INFINITY, 0.f);
         if (k < count) ml = __ldcg(reinterpret_cast<const float2*>(part(k) + q * kPartialFloats));
+        const float u = K::kUnits && k < count ? __ldcg(part(k) + q * kPartialFloats + 2) : 0.f;
         float e = 0.f;
 #pragma unroll
         for (int j0 = 0; j0 < 8; j0 += 4) {
@@ -391,13 +406,21 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
 #pragma unroll
             for (int i = 1; i < 8; i <<= 1) top = fmaxf(top, __shfl_xor_sync(group_mask, top, i));
             const float base = top == -INFINITY ? 0.f : top;
-            const float keep = exp2_approx((a.m - base) * cs);
+            float keep = exp2_approx((a.m - base) * cs);
             e = exp2_approx((ml.x - base) * cs);
             float l = ml.y * e;
 #pragma unroll
             for (int i = 1; i < 8; i <<= 1) l += __shfl_xor_sync(group_mask, l, i);
             a.m = top;
             a.l = a.l * keep + l;
+            if (K::kUnits) {
+              float to = fmaxf(a.u, u);
+#pragma unroll
+              for (int i = 1; i < 8; i <<= 1) to = fmaxf(to, __shfl_xor_sync(group_mask, to, i));
+              keep *= units_in(a.u, to);
+              e *= units_in(u, to);
+              a.u = to;
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) a.o[i] *= keep;
           }
@@ -417,23 +440,23 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
       }
       if (subs > 1) {  // then this is the only round
         float* row = scratch + (sub * p.group + q) * kSumFloats;
-        store_part(a, row, row + kHeadDim, channel);
+        store_part<K>(a, row, row + kHeadDim, channel);
       } else if (level == 1) {
         write_query<K>(p, b, h, len, q, channel, a);
       } else {
         float* row = part(0) + q * kPartialFloats;
-        store_part(a, row + 4, row, channel);
+        store_part<K>(a, row + 4, row, channel);
       }
     }
     if (subs > 1) {
       named_barrier<K::kConsumers * 32>(1);
       if (mine < p.group) {
-        const Part a = add_rows<kGroups<K>>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
+        const Part a = add_rows<K, kGroups<K>>(scratch + mine * kSumFloats, p.group * kSumFloats, subs, channel, cs);
         if (level == 1) {
           write_query<K>(p, b, h, len, mine, channel, a);
         } else {
           float* row = part(0) + mine * kPartialFloats;
-          store_part(a, row + 4, row, channel);
+          store_part<K>(a, row + 4, row, channel);
         }
       }
     }
@@ -442,10 +465,10 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
 }
 
 // The end of the CTA's part of an item: the warps' sums are added up, 8 queries at a time, 8 threads to a query; a whole
-// item is written, a part goes to the workspace, and the last part's CTA joins them all.
+// item is written, a part goes to the workspace, and the last part's CTA joins them all.  unit: of the warp's sums.
 template <class K, int NT, class P>
 __device__ void finish_item(const P& p, State<NT>& st, const Cursor& c, bool whole, bool begins, int tile_u0,
-                            const Work& w, float* scratch, volatile int* misc, float cs) {
+                            const Work& w, float* scratch, volatile int* misc, float cs, float unit) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, tq = lane % 4;
   const int mine = threadIdx.x / 8, channel = 16 * (threadIdx.x % 8);
 #pragma unroll
@@ -460,17 +483,20 @@ __device__ void finish_item(const P& p, State<NT>& st, const Cursor& c, bool who
       float* row = scratch + (warp * 8 + 2 * tq + j) * kSumFloats;
 #pragma unroll
       for (int d = 0; d < 8; ++d) K::place(row + 16 * d, g, st.o[nt][d][j], st.o[nt][d][2 + j]);
-      if (g == 0) *reinterpret_cast<float2*>(row + kHeadDim) = make_float2(st.m[nt][j], st.l[nt][j]);
+      if (g == 0) {
+        *reinterpret_cast<float2*>(row + kHeadDim) = make_float2(st.m[nt][j], st.l[nt][j]);
+        if (K::kUnits) row[kHeadDim + 2] = unit;
+      }
     }
     named_barrier<K::kConsumers * 32>(1);
     const int q = 8 * nt + mine;
     if (mine < 8 && q < p.group) {
-      const Part a = add_rows<K::kConsumers>(scratch + mine * kSumFloats, 8 * kSumFloats, K::kConsumers, channel, cs);
+      const Part a = add_rows<K, K::kConsumers>(scratch + mine * kSumFloats, 8 * kSumFloats, K::kConsumers, channel, cs);
       if (whole) {
         write_query<K>(p, c.b, c.h, c.len, q, channel, a);
       } else {
         float* row = partial_of(p, blockIdx.x, begins) + q * kPartialFloats;
-        store_part(a, row + 4, row, channel);
+        store_part<K>(a, row + 4, row, channel);
       }
     }
   }
