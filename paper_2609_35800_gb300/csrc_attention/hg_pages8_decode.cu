@@ -29,6 +29,8 @@
 // in units of u, are moved when u grows, and are multiplied by u once they are divided (before, sums of values near BF16's
 // end would pass binary32's).  So terms below 2^-32 of the largest probability times the largest scale are lost to the
 // second product.  Scores, maxima, sums and outputs are held in 32 bits.
+#include <cfloat>
+
 #include "hg_pages8.cuh"
 #include "hg_pages_split.cuh"
 
@@ -400,9 +402,12 @@ __device__ __forceinline__ void attend_blocks(State<NT>& st, int& unit, const ui
       }
     }
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
+      // (finite: where query and key share no channel 0 times it is 0, however large they are)
+      const float factor[2] = {fminf(ks[mt] * back[nt][0], FLT_MAX), fminf(ks[mt] * back[nt][1], FLT_MAX)};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[mt][nt][i] = (s[mt][nt][i] + s2[nt][i]) * (ks[mt] * back[nt][i % 2]);
+      for (int i = 0; i < 4; ++i) s[mt][nt][i] = (s[mt][nt][i] + s2[nt][i]) * factor[i % 2];
+    }
   }
   // a first scale of the values, or one past the old: the sums so far count that much less
   float top_scale = vs[0];

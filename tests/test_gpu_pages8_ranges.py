@@ -1,4 +1,5 @@
-"""The 8-bit paged cache at the ends of its types' ranges: values as large as BF16 holds."""
+"""The 8-bit paged cache at the ends of its types' ranges: values as large as BF16 holds, queries
+and keys whose factors are beyond binary32."""
 import pytest
 import torch
 
@@ -50,3 +51,21 @@ def test_values_that_e4m3_holds_come_back(value):
     hg.hg_pages8_decode_step(pool.hg, torch.ones_like(q), k1, torch.full_like(k1, value), None, None, tab2, _ints(lens), out, None,
                              0.0, _workspace(pool, 3, 4))
     assert torch.equal(out, torch.full_like(out, value))
+
+
+@pytest.mark.parametrize("group", [4, 12])
+@pytest.mark.parametrize("q_at,k_at", [(2.0 ** 100, 2.0 ** 60), (2.0 ** 70, 2.0 ** 90), (2.0 ** 120, 2.0 ** 119)])
+def test_decode_far_factors_of_zeros(q_at, k_at, group):
+    """Queries and keys that share no channel: every score is 0, however large both are."""
+    g = _gen(5)
+    lens = [1, 33, 500]
+    tab, pages = _tables(g, lens, 16)
+    pool = Pool(g, pages, 2, 16)
+    k, v = (_randn(g, sum(lens), 2, D) for _ in "kv")
+    k = k.clamp(-4, 4) * k_at
+    k[..., ::3] = 0.0
+    hg.hg_pages8_append(pool.hg, None, k, v, None, None, _begins(lens), tab, _ints(lens))
+    q = torch.zeros((3, 2 * group, D), dtype=BF16, device="cuda")
+    q[..., ::3] = q_at
+    out, lse = _run_decode(pool, q, tab, lens)
+    _check_decode(q, pool, tab, lens, out, lse)
