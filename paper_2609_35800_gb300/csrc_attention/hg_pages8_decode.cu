@@ -65,7 +65,7 @@ struct Smem {
 static_assert(Smem::scratch_bytes >= 16 * kQRowBytes, "queries are staged there too");
 static_assert(Smem::scratch_bytes >= ((kConsumers + 1) * 32 + kDecodeJoinCounters / 2 * kDecodeJoinCtas + 2) * 4, "runs' starts too");
 static_assert(Smem::scratch % 16 == 0 && Smem::bars % 8 == 0, "alignment");
-static_assert((8 + 12 + kConsumers + 1) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
+static_assert((8 + 16 + kConsumers + 1) * 4 <= Smem::lengths - Smem::misc, "the scan's words");
 static_assert(2 * (Smem::bytes + 1024) <= 228 * 1024, "two CTAs an SM");
 
 template <bool F16>

@@ -121,14 +121,16 @@ __device__ int find_work(const P& p, int* scan, int* kept, int* room, Work& w, C
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, heads = p.pool.heads;
   const int per = (p.batch + kThreads<K> - 1) / kThreads<K>;
   const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
-  int mine = 0, longest = 0;
+  int mine = 0, longest = 0, shortest = 0x7fffffff;
   for (int b = b0; b < b1; ++b) {
     const int len = request_length(p, b), units = tiles_of<K>(len) + K::kItemCost;
     if (b < kKeptLengths) kept[b] = len;
     mine += units;
     longest = max(longest, units);
+    shortest = min(shortest, units);
   }
   longest = __reduce_max_sync(kAll, longest);
+  if (K::kWeighsWhole) shortest = __reduce_min_sync(kAll, shortest);
   int sum = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -138,6 +140,7 @@ __device__ int find_work(const P& p, int* scan, int* kept, int* room, Work& w, C
   if (lane == 31) {
     scan[warp] = sum;
     scan[12 + warp] = longest;
+    if (K::kWeighsWhole) scan[16 + warp] = shortest;
   }
   __syncthreads();
   int before = sum - mine, all = 0;
@@ -146,6 +149,7 @@ __device__ int find_work(const P& p, int* scan, int* kept, int* room, Work& w, C
     if (i < warp) before += scan[i];
     all += scan[i];
     longest = max(longest, scan[12 + i]);
+    if (K::kWeighsWhole) shortest = min(shortest, scan[16 + i]);
   }
   w.total = all * heads;
   const int least = K::least_share(p.group);
@@ -174,16 +178,25 @@ __device__ int find_work(const P& p, int* scan, int* kept, int* room, Work& w, C
   c = {scan[8], scan[9], max(0, w.first_unit - K::kItemCost), scan[11], tiles_of<K>(scan[11])};
   int tiles = 0;
   bool whole = longest <= w.share + K::kJoinCost;
-  // (8-bit pages.)  With no more items than CTAs none gets two, and a CTA that has more to read than the others is faster while
-  // they share the memory with it, up to twice: whole up to 1.5 shares (4 requests of 2,000 tokens, 32 heads, 2.4 shares:
-  // 27.6 us whole, 19.4 cut; 32 of 8,577, 8 heads, 1.2 shares: 86 whole, 91 cut).  With more items some CTAs get two, and begin
-  // the second when the others end: the fullest one counts (40 of 8,577, 8 heads: 156 us whole, 112 cut), but finding it
-  // takes 2 us, more than short items can lose (64 of 500 tokens, 8 heads: 17.3 us whole, 19.3 so).
+  // (8-bit pages.)  With no more items than CTAs, a CTA that has more to read than the others is faster while they share the
+  // memory with it, up to twice: whole where the fullest CTA gets up to 1.5 shares (4 requests of 2,000 tokens, 32 heads, 2.4
+  // shares: 27.6 us whole, 19.4 cut; 32 of 8,577, 8 heads, 1.2 shares: 86 whole, 91 cut).  That is the longest item where no
+  // item is shorter than a run, so that none begins in another's; and the fullest CTA gets less than a share and the longest
+  // item in any case.  Otherwise, and with more items than CTAs, where some begin a second item when the others end, the
+  // fullest one is looked for (16 of 4,000 and 16 of 8,577 in turn, 8 heads: 102 us whole, 71 cut; 40 of 8,577, 8 heads: 156
+  // whole, 112 cut), which takes 2 us, more than short items can lose (64 of 500 tokens, 8 heads: 17.3 us whole, 19.3 so).
   if (K::kWeighsWhole) {
-    if ((int64_t)p.batch * heads <= w.ctas) whole = 2 * (int64_t)longest <= 3 * (int64_t)w.share + 2 * K::kJoinCost;
-    else if (longest > 2 * K::kJoinCost)
-      whole = whole && fullest_of_whole<K>(p, kept, room, w, before * heads) <= w.share + K::kJoinCost;
-    else whole = true;
+    const auto fullest = [&] { return fullest_of_whole<K>(p, kept, room, w, before * heads); };
+    if ((int64_t)p.batch * heads <= w.ctas) {
+      const int64_t most = 3 * (int64_t)w.share + 2 * K::kJoinCost;
+      whole = 2 * (int64_t)longest <= most;
+      if (whole && shortest < w.share + (w.more > 0) && 2 * ((int64_t)longest + w.share) > most)
+        whole = 2 * (int64_t)fullest() <= most;
+    } else if (longest > 2 * K::kJoinCost) {
+      whole = whole && fullest() <= w.share + K::kJoinCost;
+    } else {
+      whole = true;
+    }
   }
   if (whole) {
     // from the first item that begins at u0 or later to the last that begins before u1

@@ -59,6 +59,9 @@ int over_warp(int value, F f) {
 int __reduce_max_sync(unsigned, int value) {
   return over_warp(value, [](int a, int b) { return max(a, b); });
 }
+int __reduce_min_sync(unsigned, int value) {
+  return over_warp(value, [](int a, int b) { return min(a, b); });
+}
 void atomicMax(int* at, int value) { *at = max(*at, value); }
 constexpr int kDecodeJoinCtas = 16, kDecodeJoinCounters = 128, kHeadDim = 128;
 

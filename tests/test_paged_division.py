@@ -108,3 +108,29 @@ def test_every_tile_is_some_ctas_once(division, batch, group):
     work, _ = division.whole_launch(lengths, heads, group)
     got = [(b, h, t + i) for mine in work for b, h, t, n in mine for i in range(n)]
     assert got == [(b, h, t) for b, n in enumerate(lengths) for h in range(heads) for t in range(division.tiles(n))]
+
+
+FEW = {
+    "a third of 3 tiles": ([180 if i % 3 == 0 else 8570 for i in range(38)], 8), "the first third short": ([180] * 13 + [8570] * 25, 8),
+    "spread": ([1 + 8576 * i // 35 for i in range(36)], 8), "alike": ([8000 + 18 * i for i in range(32)], 8),
+    "two lengths": ([4000, 8577] * 16, 8), "one long": ([9001] + [3000] * 29, 8), "as many as CTAs": ([8577] * 38, 8),
+    "equal": ([8577] * 32, 8), "short": ([500, 1] * 15, 8),
+}
+
+
+@pytest.mark.parametrize("batch", list(FEW))
+def test_no_more_items_than_ctas(division, batch):
+    """Where whole items are taken, the fullest CTA has 1.5 shares and a join at most, whatever begins in its run; otherwise each
+    has its share.  (16-bit pages: whole items by the longest alone, left as it was.)"""
+    if division.tile == 32:
+        pytest.skip("another rule")
+    lengths, heads = FEW[batch]
+    assert len(lengths) * heads <= CTAS
+    work, share = division.whole_launch(lengths, heads)
+    units = [sum(n + (division.item_cost if t == 0 else 0) for _, _, t, n in mine) for mine in work]
+    whole = all(n == division.tiles(lengths[b]) for mine in work for b, _, _, n in mine)
+    # (cut: the fixed costs of an item that a run begins with may be units of the run before)
+    most = 1.5 * share + division.join_cost if whole else share + 1 + division.item_cost
+    assert max(units) <= most, "%d units, a share is %d" % (max(units), share)
+    if batch in ("equal", "as many as CTAs", "alike"):
+        assert whole  # one item a CTA
