@@ -172,26 +172,30 @@ class Paged8Runner:
         if any(x.shape[0] != total for x in (q, k, v)):
             raise ValueError("Paged8Runner: q, k and v hold %d, %d and %d rows, the prompts %d"
                              % (q.shape[0], k.shape[0], v.shape[0], total))
+        if q.shape[1:] != (self.q_heads, 128):
+            raise ValueError("Paged8Runner: q is %s, the requests have %d query heads" % (list(q.shape), self.q_heads))
         need = self._check(grown)
-        fed = torch.tensor(new, dtype=torch.int32, device=self.device)
-        lens, begin, places, counts = self._plan(fed, total)
-        q_rot = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        # everything that may fail comes before the store: a block that it stores again more coarsely stays so
+        q_rot, out = (torch.empty(q.shape, dtype=self.dtype, device=self.device) for _ in range(2))
         if k_out is None:
             k_out = torch.empty(k.shape, dtype=self.dtype, device=self.device)
         if v_out is None:
             v_out = torch.empty(v.shape, dtype=self.dtype, device=self.device)
-        hg_pages8_append(self.pages, q, k, v, self.rotation, places if positions is None else positions, begin, self.table,
-                         lens, q_rot, k_out, v_out)
         q_begin = torch.tensor([0] + new).cumsum(0).to(torch.int32)
-        if any(n and n != m for n, m in zip(new, grown)):  # tokens that are cached already: all of them from the cache
+        cached = any(n and n != m for n, m in zip(new, grown))
+        keys, values, k_begin = k_out, v_out, q_begin
+        if cached:  # tokens that are there already: all of a request's from the cache
             rows = [m if n else 0 for n, m in zip(new, grown)]
             k_begin = torch.tensor([0] + rows).cumsum(0).to(torch.int32)
+            begins = k_begin.to(self.device)
             keys, values = (torch.empty(self.kv_heads, sum(rows), 128, dtype=self.dtype, device=self.device).transpose(0, 1)
                             for _ in range(2))
-            hg_pages8_dequantize(self.pages, k_begin.to(self.device), self.table, keys, values)
-        else:
-            keys, values, k_begin = k_out, v_out, q_begin
-        out = torch.empty_like(q_rot)
+        fed = torch.tensor(new, dtype=torch.int32, device=self.device)
+        lens, begin, places, counts = self._plan(fed, total)
+        hg_pages8_append(self.pages, q, k, v, self.rotation, places if positions is None else positions, begin, self.table,
+                         lens, q_rot, k_out, v_out)
+        if cached:
+            hg_pages8_dequantize(self.pages, begins, self.table, keys, values)
         hg_prompt_attention(q_rot, keys, values, q_begin, k_begin, out, None, True, 0.0, self.prompt_ws)
         self._keep(lens, counts, grown, need)
         return out
