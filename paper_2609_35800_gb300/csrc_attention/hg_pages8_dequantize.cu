@@ -27,6 +27,15 @@ __device__ __forceinline__ int request_of(const Pages8DequantizeParams& p, int r
   return r;
 }
 
+// code * scale towards zero, its last bit set where something is left: rounding that to 16 bits rounds the product itself,
+// 28 bits of it, once (24 requests of 8,577 tokens, 8 heads: 197 us, 187 with powers of two).  What is left is found 2^24
+// higher where it could be below binary32's end.
+__device__ __forceinline__ float product_to_odd(float code, float scale) {
+  const float x = __fmul_rz(code, scale), lift = scale < 1.f ? 0x1p24f : 1.f;
+  const bool more = __fmaf_rn(code, scale * lift, -(x * lift)) != 0.f;
+  return more ? __uint_as_float(__float_as_uint(x) | 1u) : x;
+}
+
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) pages8_dequantize_kernel(const __grid_constant__ Pages8DequantizeParams p) {
   grid_launch_dependents();
@@ -71,8 +80,13 @@ __global__ void __launch_bounds__(kThreads) pages8_dequantize_kernel(const __gri
     float x[16];
     decode8(make_uint2(codes[i].x, codes[i].y), x);
     decode8(make_uint2(codes[i].z, codes[i].w), x + 8);
+    if ((__float_as_uint(scale[i]) & 0x7fffffu) == 0) {  // a power of two: exact
 #pragma unroll
-    for (int k = 0; k < 16; ++k) x[k] *= scale[i];
+      for (int k = 0; k < 16; ++k) x[k] *= scale[i];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) x[k] = product_to_odd(x[k], scale[i]);
+    }
     if (!(scale[i] * 448.f <= kMost16<F16>)) {  // the largest code would be out of the type's range
 #pragma unroll
       for (int k = 0; k < 16; ++k) x[k] = in_range<F16>(x[k]);

@@ -1,13 +1,18 @@
 """The 8-bit paged cache at the ends of its types' ranges: values as large as BF16 holds, queries
-and keys whose factors are beyond binary32."""
+and keys whose factors are beyond binary32, scales of other writers next to a 16-bit type's midpoints."""
+import math
+from fractions import Fraction
+
 import pytest
 import torch
 
 import paper_2609_35800_gb300 as hg
-from test_gpu_pages8 import BF16, D, Pool, _begins, _check_decode, _gen, _ints, _randn, _random_pool, _run_decode, _tables
-from test_gpu_pages8 import _workspace
+from pages8 import F8
+from test_gpu_pages8 import BF16, D, F16, TYPES, Pool, _begins, _check_decode, _gen, _ints, _randn, _random_pool, _run_decode
+from test_gpu_pages8 import _tables, _workspace
 
 pytestmark = pytest.mark.gpu
+MOST = {BF16: float(torch.finfo(BF16).max), F16: 65504.0}
 
 
 @pytest.mark.parametrize("group", [4, 12])
@@ -69,3 +74,50 @@ def test_decode_far_factors_of_zeros(q_at, k_at, group):
     q[..., ::3] = q_at
     out, lse = _run_decode(pool, q, tab, lens)
     _check_decode(q, pool, tab, lens, out, lse)
+
+
+def _nearest(x, dtype):
+    """x (a Fraction) rounded once to the type, ties to even, within its range."""
+    bits, least, most = (8 if dtype == BF16 else 11), (-133 if dtype == BF16 else -24), MOST[dtype]
+    if x == 0:
+        return 0.0
+    exponent = math.floor(math.log2(abs(x.numerator))) - math.floor(math.log2(x.denominator))
+    while abs(x) >= Fraction(2) ** (exponent + 1):
+        exponent += 1
+    while abs(x) < Fraction(2) ** exponent:
+        exponent -= 1
+    step = Fraction(2) ** max(exponent - bits + 1, least)
+    return max(-most, min(most, float(round(x / step) * step)))
+
+
+@TYPES
+def test_dequantize_rounds_once(dtype):
+    """Every code under scales of 24 bits that bring one of them next to a midpoint of the type: exact products, rounded once."""
+    g = _gen(9)
+    bits = 8 if dtype == BF16 else 11
+    scales = []
+    for odd in (9, 11, 13, 15):  # a code's significand in eighths
+        for j in range(6):
+            # odd * m / 2^26 next to the midpoint (2 i + 1) / 2^bits in [1, 2)
+            target = Fraction(2 * (2 ** (bits - 1) + 17 * j + 3) + 1, 2 ** bits)
+            m = round(target * 2 ** 26 / odd)
+            scales += [(m + d) * 2.0 ** -23 for d in (-1, 0, 1)]
+    scales += [0.37, 1.37, 2.0 ** -126 * 1.1, 2.0 ** -130 * 1.3, 2.0 ** -8 * 1.0625, 1000.0, 2.0 ** 126 * 0.9, 1.0, 2.0 ** -140]
+    scales += [s * 2.0 ** e for s in scales[:40] for e in (-20, -115, 90)]
+    scales = [float(torch.tensor(s, dtype=torch.float32)) for s in scales]
+    pages = len(scales)
+    pool = Pool(g, pages, 1, 16, dtype, fill=0)
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda")
+    for i in range(2):
+        pool.codes[i][:, 0, :2] = codes.view(2, D)
+        pool.scales[i].copy_(torch.tensor(scales, device="cuda").view(pages, 1, 1))
+    tab = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, pages)
+    out, v_out = (torch.empty((16 * pages, 1, D), dtype=dtype, device="cuda") for _ in "kv")
+    hg.hg_pages8_dequantize(pool.hg, _ints([0, 16 * pages]), tab, out, v_out)
+    assert torch.equal(out.view(torch.int16), v_out.view(torch.int16))
+    got = out.view(pages, 16, D)[:, :2].reshape(pages, 256).double().tolist()
+    exact = codes.cpu().view(F8).double().tolist()
+    off = [(s, c, a) for s, row in zip(scales, got) for c, a in zip(exact, row)
+           if c == c and a != _nearest(Fraction(c) * Fraction(s), dtype)]
+    assert not off, "%d off, the first: scale %r, code %r, got %r" % ((len(off),) + off[0])
+    assert bool(out.view(pages, 16, D)[:, :2].reshape(pages, 256)[:, [0x7f, 0xff]].isnan().all())
