@@ -459,6 +459,7 @@ class Pages:
         self.v_pages = v_pages
         self.shape = shape
         self.dtype = k_pages.dtype
+        self.device = max(k_pages.get_device(), 0)  # (the CPU's is -1, and refused)
 
     def __del__(self):
         if getattr(self, "handle", None) and _lib is not None:
@@ -534,143 +535,12 @@ def _rotated_by(where, rotation, positions, tokens):
     return rotation.pointer, _ints(where, "positions", positions, parts * tokens)
 
 
-def hg_pages_create(k_pages, v_pages):
-    """Descriptor of the page pool whose keys and values are these tensors, each seen as
-    [pages][kv heads][page size][128] (any strides: pages that lie [tokens][heads] are passed transposed)."""
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
-        raise ValueError("hg_pages_create: k_pages and v_pages must be [pages][heads][tokens][128] of one type")
-    if k_pages.dtype not in _types.code:
-        raise ValueError("hg_pages_create: pages must be bfloat16 or float16")
-    n, heads, size, dim = k_pages.shape
-    # the stride of an axis of length 1 is never taken: a dense one stands for it
-    strides = [tuple(s if d > 1 else dim for s, d in zip(x.stride(), x.shape)) for x in (k_pages, v_pages)]
-    if strides[0] != strides[1] or k_pages.stride(3) != 1:
-        raise ValueError("hg_pages_create: k_pages and v_pages must have the same strides and dense channels")
-    if not (k_pages.is_cuda and v_pages.is_cuda):
-        raise ValueError("hg_pages_create: k_pages and v_pages must be CUDA tensors")
-    shape = PageShape(_types.code[k_pages.dtype], n, size, heads, dim, *strides[0][:3])
-    h = ctypes.c_void_p()
-    _check(library().hg_pages_create(ctypes.byref(shape), k_pages.data_ptr(), v_pages.data_ptr(), ctypes.byref(h)),
-           "hg_pages_create")
-    return Pages(h, k_pages, v_pages, shape)
-
-
-def hg_pages_destroy(pages):
-    if pages.handle:
-        library().hg_pages_destroy(pages.handle)
-        pages.handle = None
-
-
-def hg_pages_append(pages, q, k, v, rotation, positions, slots, q_out=None, k_out=None, v_out=None, stream=None):
-    """Rotate q and k ([tokens][heads][128], any token and head strides; q None: no queries) and store k and v at
-    `slots` (int32, page * page size + place; negative: nowhere).  The rotated rows also go to q_out and, where
-    given, k_out; v to v_out."""
-    w, d = "hg_pages_append", pages.dtype
-    n, heads, hq = k.shape[0], pages.shape.num_kv_heads, 0 if q is None else q.shape[1]
-    if q is not None and q_out is None:
-        raise ValueError("hg_pages_append: q needs q_out")
-    io = _pack18(*(_rows(w, "q", q, n, hq, d) if hq else _NO_ROWS), *_rows(w, "k", k, n, heads, d),
-                     *_rows(w, "v", v, n, heads, d), *(_rows(w, "q_out", q_out, n, hq, d) if hq else _NO_ROWS),
-                     *(_NO_ROWS if k_out is None else _rows(w, "k_out", k_out, n, heads, d)),
-                     *(_NO_ROWS if v_out is None else _rows(w, "v_out", v_out, n, heads, d)))
-    rp, pp = _rotated_by(w, rotation, positions, n)
-    _check(library().hg_pages_append(pages.handle, n, hq, io, rp, pp, _ints(w, "slots", slots, n), _stream(stream)), w)
-
-
-def hg_pages_decode_workspace_size(pages, batch, num_q_heads):
-    out = ctypes.c_size_t(0)
-    _check(library().hg_pages_decode_workspace_size(pages.handle, batch, num_q_heads, ctypes.byref(out)),
-           "hg_pages_decode_workspace_size")
-    return out.value
-
-
-def _decode_table(where, page_table, lengths, batch):
-    if page_table.dim() != 2 or page_table.shape[0] < batch:
-        raise ValueError("%s: page_table must be [%d][pages]" % (where, batch))
-    per = page_table.shape[1]
-    return _ints(where, "page_table", page_table, batch * per), per, _ints(where, "lengths", lengths, batch)
-
-
 def _workspace(where, x):
     if x is None or isinstance(x, int):
         raise ValueError("%s: workspace must be a tensor" % where)
     if x.is_cuda and x.is_contiguous():
         return x.data_ptr(), x.nbytes
     _refuse(where, [(x, 0, "workspace")])
-
-
-def hg_pages_decode_attention(pages, q, page_table, lengths, out, lse, softmax_scale, workspace, stream=None):
-    """Attention of one token per request (q, out [batch][heads][128]) over the first lengths[b] tokens of its pages
-    page_table[b]; lse float32 [batch][heads] or None."""
-    w, d = "hg_pages_decode_attention", pages.dtype
-    n, hq = q.shape[0], q.shape[1]
-    io = _pack12(*_rows(w, "q", q, n, hq, d), 0, 0, 0, 0, 0, 0, *_rows(w, "out", out, n, hq, d))
-    tp, ts, lp = _decode_table(w, page_table, lengths, n)
-    _check(library().hg_pages_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse(w, lse, n, hq),
-                                               softmax_scale, *_workspace(w, workspace), _stream(stream)), w)
-
-
-def hg_pages_decode_step(pages, q, k, v, rotation, positions, page_table, lengths, out, lse, softmax_scale, workspace,
-                         stream=None):
-    """One decode step: q and the new token's k rotated, k and v stored as token lengths[b] - 1 of request b, attention
-    over its lengths[b] tokens."""
-    w, d = "hg_pages_decode_step", pages.dtype
-    n, hq, heads = q.shape[0], q.shape[1], pages.shape.num_kv_heads
-    io = _pack12(*_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, n, heads, d),
-                     *_rows(w, "v", v, n, heads, d), *_rows(w, "out", out, n, hq, d))
-    rp, pp = _rotated_by(w, rotation, positions, n)
-    tp, ts, lp = _decode_table(w, page_table, lengths, n)
-    _check(library().hg_pages_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse(w, lse, n, hq),
-                                          softmax_scale, *_workspace(w, workspace), _stream(stream)), w)
-
-
-def hg_prompt_workspace_size():
-    out = ctypes.c_size_t(0)
-    _check(library().hg_prompt_workspace_size(ctypes.byref(out)), "hg_prompt_workspace_size")
-    return out.value
-
-
-def hg_prompt_attention(q, k, v, q_begin, k_begin, out, lse, causal, softmax_scale, workspace, stream=None):
-    """Attention of packed prompts: q, out [tokens][heads][128], k, v [keys][kv heads][128] (any token and head
-    strides); prompt i has the rows q_begin[i]..q_begin[i + 1] and the keys k_begin[i]..k_begin[i + 1] (CPU int32
-    tensors [prompts + 1]); lse float32 [tokens][heads] or None."""
-    w, d = "hg_prompt_attention", q.dtype
-    code = _types.code.get(d)
-    if code is None:
-        raise ValueError("%s: q must be bfloat16 or float16" % w)
-    n, hq, _ = q.shape
-    nk, heads, _ = k.shape
-    count = q_begin.numel() - 1
-    io = _pack12(*_rows(w, "q", q, n, hq, d), *_rows(w, "k", k, nk, heads, d),
-                     *_rows(w, "v", v, nk, heads, d), *_rows(w, "out", out, n, hq, d))
-    qb, kb = _ints(w, "q_begin", q_begin, 1, False), _ints(w, "k_begin", k_begin, count + 1, False)
-    q_end, k_end = _Int.from_address(qb + 4 * count).value, _Int.from_address(kb + 4 * count).value
-    if q_end > n or k_end > nk:
-        raise ValueError("%s: the prompts end at %d and %d, q and k hold %d and %d rows" % (w, q_end, k_end, n, nk))
-    _check(library().hg_prompt_attention(code, count, hq, heads, io, qb, kb, _lse(w, lse, n, hq), 1 if causal else 0,
-                                         softmax_scale, *_workspace(w, workspace), _stream(stream)), w)
-
-
-# ---------------------------------------------------------------------------
-# Paged caches in 8 bits, page tables built on the GPU
-# ---------------------------------------------------------------------------
-
-
-class Pages8:
-    """Owning handle of an hg_pages8 descriptor (the pool's tensors stay the caller's)."""
-
-    def __init__(self, handle, k_pages, v_pages, k_scales, v_scales, shape, dtype):
-        self.handle = handle
-        self.k_pages, self.v_pages = k_pages, v_pages
-        self.k_scales, self.v_scales = k_scales, v_scales
-        self.shape = shape
-        self.dtype = dtype  # of the rows that calls take and give
-        self.device = k_pages.get_device()
-
-    def __del__(self):
-        if getattr(self, "handle", None) and _lib is not None:
-            _lib.hg_pages8_destroy(self.handle)
-            self.handle = None
 
 
 def _elsewhere(where, name, x, device):
@@ -730,6 +600,142 @@ def _stream_on(where, stream, device):
     return _types.stream(device) if stream is None else _stream(stream)
 
 
+def hg_pages_create(k_pages, v_pages):
+    """Descriptor of the page pool whose keys and values are these tensors, each seen as
+    [pages][kv heads][page size][128] (any strides: pages that lie [tokens][heads] are passed transposed)."""
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
+        raise ValueError("hg_pages_create: k_pages and v_pages must be [pages][heads][tokens][128] of one type")
+    if k_pages.dtype not in _types.code:
+        raise ValueError("hg_pages_create: pages must be bfloat16 or float16")
+    n, heads, size, dim = k_pages.shape
+    # the stride of an axis of length 1 is never taken: a dense one stands for it
+    strides = [tuple(s if d > 1 else dim for s, d in zip(x.stride(), x.shape)) for x in (k_pages, v_pages)]
+    if strides[0] != strides[1] or k_pages.stride(3) != 1:
+        raise ValueError("hg_pages_create: k_pages and v_pages must have the same strides and dense channels")
+    if not (k_pages.is_cuda and v_pages.is_cuda):
+        raise ValueError("hg_pages_create: k_pages and v_pages must be CUDA tensors")
+    if k_pages.get_device() != v_pages.get_device():
+        raise ValueError("hg_pages_create: k_pages and v_pages must be on one device")
+    shape = PageShape(_types.code[k_pages.dtype], n, size, heads, dim, *strides[0][:3])
+    h = ctypes.c_void_p()
+    _check(library().hg_pages_create(ctypes.byref(shape), k_pages.data_ptr(), v_pages.data_ptr(), ctypes.byref(h)),
+           "hg_pages_create")
+    return Pages(h, k_pages, v_pages, shape)
+
+
+def hg_pages_destroy(pages):
+    if pages.handle:
+        library().hg_pages_destroy(pages.handle)
+        pages.handle = None
+
+
+def hg_pages_append(pages, q, k, v, rotation, positions, slots, q_out=None, k_out=None, v_out=None, stream=None):
+    """Rotate q and k ([tokens][heads][128], any token and head strides; q None: no queries) and store k and v at
+    `slots` (int32, page * page size + place; negative: nowhere).  The rotated rows also go to q_out and, where
+    given, k_out; v to v_out."""
+    w, d, at = "hg_pages_append", pages.dtype, pages.device
+    n, heads, hq = k.shape[0], pages.shape.num_kv_heads, 0 if q is None else q.shape[1]
+    if q is not None and q_out is None:
+        raise ValueError("hg_pages_append: q needs q_out")
+    io = _pack18(*(_rows_on(w, "q", q, n, hq, d, at) if hq else _NO_ROWS), *_rows_on(w, "k", k, n, heads, d, at),
+                     *_rows_on(w, "v", v, n, heads, d, at), *(_rows_on(w, "q_out", q_out, n, hq, d, at) if hq else _NO_ROWS),
+                     *(_NO_ROWS if k_out is None else _rows_on(w, "k_out", k_out, n, heads, d, at)),
+                     *(_NO_ROWS if v_out is None else _rows_on(w, "v_out", v_out, n, heads, d, at)))
+    rp, pp = _rotated_on(w, rotation, positions, n, at)
+    _check(library().hg_pages_append(pages.handle, n, hq, io, rp, pp, _ints_on(w, "slots", slots, n, at),
+                                     _stream_on(w, stream, at)), w)
+
+
+def hg_pages_decode_workspace_size(pages, batch, num_q_heads):
+    out = ctypes.c_size_t(0)
+    _check(library().hg_pages_decode_workspace_size(pages.handle, batch, num_q_heads, ctypes.byref(out)),
+           "hg_pages_decode_workspace_size")
+    return out.value
+
+
+def _decode_table(where, page_table, lengths, batch, device=0):
+    if page_table.dim() != 2 or page_table.shape[0] < batch:
+        raise ValueError("%s: page_table must be [%d][pages]" % (where, batch))
+    per = page_table.shape[1]
+    return (_ints_on(where, "page_table", page_table, batch * per, device), per,
+            _ints_on(where, "lengths", lengths, batch, device))
+
+
+def hg_pages_decode_attention(pages, q, page_table, lengths, out, lse, softmax_scale, workspace, stream=None):
+    """Attention of one token per request (q, out [batch][heads][128]) over the first lengths[b] tokens of its pages
+    page_table[b]; lse float32 [batch][heads] or None."""
+    w, d, at = "hg_pages_decode_attention", pages.dtype, pages.device
+    n, hq = q.shape[0], q.shape[1]
+    io = _pack12(*_rows_on(w, "q", q, n, hq, d, at), 0, 0, 0, 0, 0, 0, *_rows_on(w, "out", out, n, hq, d, at))
+    tp, ts, lp = _decode_table(w, page_table, lengths, n, at)
+    _check(library().hg_pages_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse_on(w, lse, n, hq, at),
+                                               softmax_scale, *_workspace_on(w, workspace, at),
+                                               _stream_on(w, stream, at)), w)
+
+
+def hg_pages_decode_step(pages, q, k, v, rotation, positions, page_table, lengths, out, lse, softmax_scale, workspace,
+                         stream=None):
+    """One decode step: q and the new token's k rotated, k and v stored as token lengths[b] - 1 of request b, attention
+    over its lengths[b] tokens."""
+    w, d, at = "hg_pages_decode_step", pages.dtype, pages.device
+    n, hq, heads = q.shape[0], q.shape[1], pages.shape.num_kv_heads
+    io = _pack12(*_rows_on(w, "q", q, n, hq, d, at), *_rows_on(w, "k", k, n, heads, d, at),
+                     *_rows_on(w, "v", v, n, heads, d, at), *_rows_on(w, "out", out, n, hq, d, at))
+    rp, pp = _rotated_on(w, rotation, positions, n, at)
+    tp, ts, lp = _decode_table(w, page_table, lengths, n, at)
+    _check(library().hg_pages_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse_on(w, lse, n, hq, at),
+                                          softmax_scale, *_workspace_on(w, workspace, at), _stream_on(w, stream, at)), w)
+
+
+def hg_prompt_workspace_size():
+    out = ctypes.c_size_t(0)
+    _check(library().hg_prompt_workspace_size(ctypes.byref(out)), "hg_prompt_workspace_size")
+    return out.value
+
+
+def hg_prompt_attention(q, k, v, q_begin, k_begin, out, lse, causal, softmax_scale, workspace, stream=None):
+    """Attention of packed prompts: q, out [tokens][heads][128], k, v [keys][kv heads][128] (any token and head
+    strides); prompt i has the rows q_begin[i]..q_begin[i + 1] and the keys k_begin[i]..k_begin[i + 1] (CPU int32
+    tensors [prompts + 1]); lse float32 [tokens][heads] or None."""
+    w, d, at = "hg_prompt_attention", q.dtype, max(q.get_device(), 0)  # (the CPU's is -1, and refused)
+    code = _types.code.get(d)
+    if code is None:
+        raise ValueError("%s: q must be bfloat16 or float16" % w)
+    n, hq, _ = q.shape
+    nk, heads, _ = k.shape
+    count = q_begin.numel() - 1
+    io = _pack12(*_rows_on(w, "q", q, n, hq, d, at), *_rows_on(w, "k", k, nk, heads, d, at),
+                     *_rows_on(w, "v", v, nk, heads, d, at), *_rows_on(w, "out", out, n, hq, d, at))
+    qb, kb = _ints(w, "q_begin", q_begin, 1, False), _ints(w, "k_begin", k_begin, count + 1, False)
+    q_end, k_end = _Int.from_address(qb + 4 * count).value, _Int.from_address(kb + 4 * count).value
+    if q_end > n or k_end > nk:
+        raise ValueError("%s: the prompts end at %d and %d, q and k hold %d and %d rows" % (w, q_end, k_end, n, nk))
+    _check(library().hg_prompt_attention(code, count, hq, heads, io, qb, kb, _lse_on(w, lse, n, hq, at), 1 if causal else 0,
+                                         softmax_scale, *_workspace_on(w, workspace, at), _stream_on(w, stream, at)), w)
+
+
+# ---------------------------------------------------------------------------
+# Paged caches in 8 bits, page tables built on the GPU
+# ---------------------------------------------------------------------------
+
+
+class Pages8:
+    """Owning handle of an hg_pages8 descriptor (the pool's tensors stay the caller's)."""
+
+    def __init__(self, handle, k_pages, v_pages, k_scales, v_scales, shape, dtype):
+        self.handle = handle
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.k_scales, self.v_scales = k_scales, v_scales
+        self.shape = shape
+        self.dtype = dtype  # of the rows that calls take and give
+        self.device = k_pages.get_device()
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.hg_pages8_destroy(self.handle)
+            self.handle = None
+
+
 def hg_pages8_create(k_pages, v_pages, k_scales, v_scales, dtype=None):
     """Descriptor of the 8-bit page pool whose codes are these tensors (float8_e4m3fn, or their bytes as uint8), each
     seen as [pages][kv heads][page size][128] (any strides), and whose scales are float32 [pages][kv heads][page size /
@@ -778,14 +784,6 @@ def _requests(where, begin, page_table, device):
     return (n, _ints_on(where, "begin", begin, 1, device), _ints_on(where, "page_table", page_table, n * per, device), per)
 
 
-def _lengths_table(where, page_table, lengths, batch, device):
-    if page_table.dim() != 2 or page_table.shape[0] < batch:
-        raise ValueError("%s: page_table must be [%d][pages]" % (where, batch))
-    per = page_table.shape[1]
-    return (_ints_on(where, "page_table", page_table, batch * per, device), per,
-            _ints_on(where, "lengths", lengths, batch, device))
-
-
 def hg_pages8_append(pages, q, k, v, rotation, positions, begin, page_table, lengths, q_out=None, k_out=None, v_out=None,
                      stream=None):
     """Rotate q and k ([tokens][heads][128], any token and head strides; q None: no queries) and store k and v in 8 bits:
@@ -831,7 +829,7 @@ def hg_pages8_decode_attention(pages, q, page_table, lengths, out, lse, softmax_
     w, d, at = "hg_pages8_decode_attention", pages.dtype, pages.device
     n, hq = q.shape[0], q.shape[1]
     io = _pack12(*_rows_on(w, "q", q, n, hq, d, at), 0, 0, 0, 0, 0, 0, *_rows_on(w, "out", out, n, hq, d, at))
-    tp, ts, lp = _lengths_table(w, page_table, lengths, n, at)
+    tp, ts, lp = _decode_table(w, page_table, lengths, n, at)
     _check(library().hg_pages8_decode_attention(pages.handle, n, hq, io, tp, ts, lp, _lse_on(w, lse, n, hq, at),
                                                 softmax_scale, *_workspace_on(w, workspace, at),
                                                 _stream_on(w, stream, at)), w)
@@ -846,7 +844,7 @@ def hg_pages8_decode_step(pages, q, k, v, rotation, positions, page_table, lengt
     io = _pack12(*_rows_on(w, "q", q, n, hq, d, at), *_rows_on(w, "k", k, n, heads, d, at),
                      *_rows_on(w, "v", v, n, heads, d, at), *_rows_on(w, "out", out, n, hq, d, at))
     rp, pp = _rotated_on(w, rotation, positions, n, at)
-    tp, ts, lp = _lengths_table(w, page_table, lengths, n, at)
+    tp, ts, lp = _decode_table(w, page_table, lengths, n, at)
     _check(library().hg_pages8_decode_step(pages.handle, n, hq, io, rp, pp, tp, ts, lp, _lse_on(w, lse, n, hq, at),
                                            softmax_scale, *_workspace_on(w, workspace, at), _stream_on(w, stream, at)), w)
 
