@@ -597,12 +597,14 @@ hg_status hg_pages8_decode_workspace_size(const hg_pages8 *pages, int32_t batch,
 /* Attention of one new token per request over the 8-bit paged cache: arguments
  * and limits of hg_pages_decode_attention, keys and values code * scale.  Scores,
  * maxima, sums and outputs are binary32 until the output's one rounding (beyond
- * FP16's range: its largest value).  Queries and codes meet as FP16, exactly
+ * the type's range: its largest value).  Queries and codes meet as FP16, exactly
  * (a BF16 query row is first multiplied by a power of two that brings its
  * largest entry to [2^14, 2^15); entries below 2^-31 of that lose bits).
- * Probabilities times the value block's scale are rounded to FP16 (2^-11 of
- * each; those below 2^-32 of the largest probability times the largest scale are
- * lost). */
+ * Probabilities times the value block's scale are rounded to FP16: by 2^-11 of
+ * each, or, of those below 2^-21 of the largest probability times the largest
+ * scale so far, by up to 2^-32 of that (so those below 2^-32 of it are lost).  A
+ * score's factor, its block's scale times what undoes the query's, ends at the
+ * largest finite binary32. */
 hg_status hg_pages8_decode_attention(const hg_pages8 *pages, int32_t batch, int32_t num_q_heads,
                                      const hg_attention_io *io, const int32_t *page_table, int32_t table_stride,
                                      const int32_t *lengths, float *lse, float softmax_scale, void *workspace,

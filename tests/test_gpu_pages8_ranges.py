@@ -1,5 +1,5 @@
-"""The 8-bit paged cache at the ends of its types' ranges: values as large as BF16 holds, queries
-and keys whose factors are beyond binary32, scales of other writers next to a 16-bit type's midpoints."""
+"""The 8-bit paged cache at the ends of its types' ranges: values as large as BF16 holds, queries and keys whose factors are
+beyond binary32, blocks of great and of small values together, scales of other writers next to a 16-bit type's midpoints."""
 import math
 from fractions import Fraction
 
@@ -7,7 +7,8 @@ import pytest
 import torch
 
 import paper_2609_35800_gb300 as hg
-from pages8 import F8
+from attention16 import ROUNDOFF, attend
+from pages8 import BLOCK, F8
 from test_gpu_pages8 import BF16, D, F16, TYPES, Pool, _begins, _check_decode, _gen, _ints, _randn, _random_pool, _run_decode
 from test_gpu_pages8 import _tables, _workspace
 
@@ -74,6 +75,36 @@ def test_decode_far_factors_of_zeros(q_at, k_at, group):
     q[..., ::3] = q_at
     out, lse = _run_decode(pool, q, tab, lens)
     _check_decode(q, pool, tab, lens, out, lse)
+
+
+@TYPES
+@pytest.mark.parametrize("apart", [0, 8, 16, 20])
+def test_decode_small_values_beside_great_ones_of_small_probability(dtype, apart):
+    """Every fourth block's values are 2^apart larger, at probabilities of e^-30: the others' average is what is left.  Each
+    term of the second product, a probability times its block's scale over the largest scale, 2^7 for a token of the largest
+    score, is rounded to FP16: off by 2^-11 of it, or by 2^-25 where it is subnormal, times its code."""
+    g = _gen(40 + apart)
+    n = 2048
+    tab, pages = _tables(g, [n], 32)
+    pool = Pool(g, pages, 1, 32, dtype, fill=0)
+    q = torch.zeros((1, 6, D), dtype=dtype, device="cuda")
+    q[..., 0] = 1.0
+    pool.codes[1].copy_(torch.randint(0x28, 0x48, pool.codes[1].shape, generator=g, device="cuda", dtype=torch.uint8))  # 0.25 to 3.75
+    for s in pool.scales:
+        s.fill_(1.0)
+    great = tab[0, :n // 32:2].long()  # their first blocks
+    pool.codes[0][great, 0, :BLOCK, 0] = 0xfe  # -448
+    pool.scales[0][great, 0, 0] = 30 / 448
+    pool.scales[1][great, 0, 0] = 2.0 ** apart
+    out, lse = _run_decode(pool, q, tab, [n], scale=1.0)
+    k, v = pool.rows(0, tab, 0, n), pool.rows(1, tab, 0, n)
+    want, rlse, mean, _ = attend(q, k, v, torch.tensor([n], device="cuda"), 1.0)
+    size = torch.where(torch.arange(n, device="cuda") // BLOCK % 4 == 0, 2.0 ** apart, 1.0)
+    codes, total = (v / size[:, None, None]).sum(0)[0], n * 3 // 4
+    # (a score of 0 is exact; exponentials and sums of positive terms in binary32: 2^-19)
+    tol = ROUNDOFF[dtype] * want.abs() + 1.01 * (2.0 ** -11 + 2.0 ** -19) * mean + 2.0 ** (apart - 32) * codes / total
+    assert bool(((out.double() - want).abs() <= tol).all())
+    assert bool(((lse.double() - rlse).abs() <= 2.0 ** -18).all())
 
 
 def _nearest(x, dtype):
