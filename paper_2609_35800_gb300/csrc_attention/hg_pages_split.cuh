@@ -290,6 +290,30 @@ __device__ __forceinline__ float* partial_of(const P& p, int cta, bool begins) {
 struct Part {
   float m = -INFINITY, l = 0.f, u = 0.f, o[16] = {};
 };
+// A row's maximum, sum and unit, as they lie in a part or behind a row of sums in shared memory.
+template <class K>
+__device__ __forceinline__ float3 load_mlu(const float* at) {
+  if (K::kUnits) {
+    const float4 x = *reinterpret_cast<const float4*>(at);
+    return make_float3(x.x, x.y, x.z);
+  }
+  const float2 x = *reinterpret_cast<const float2*>(at);
+  return make_float3(x.x, x.y, 0.f);
+}
+template <class K>
+__device__ __forceinline__ float3 load_mlu_l2(const float* at) {
+  if (K::kUnits) {
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(at));
+    return make_float3(x.x, x.y, x.z);
+  }
+  const float2 x = __ldcg(reinterpret_cast<const float2*>(at));
+  return make_float3(x.x, x.y, 0.f);
+}
+template <class K>
+__device__ __forceinline__ void store_mlu(float* at, float m, float l, float u) {
+  if (K::kUnits) *reinterpret_cast<float4*>(at) = make_float4(m, l, u, 0.f);
+  else *reinterpret_cast<float2*>(at) = make_float2(m, l);
+}
 // What sums in units of u are multiplied by to be in units of `to`, not below it; powers of two, or 0.
 __device__ __forceinline__ float units_in(float u, float to) {
   return u * __uint_as_float((uint32_t)(254 - (int)(__float_as_uint(to) >> 23)) << 23);
@@ -298,22 +322,20 @@ __device__ __forceinline__ float units_in(float u, float to) {
 template <class K, int N>
 __device__ __forceinline__ Part add_rows(const float* row, int apart, int count, int channel, float cs) {
   Part a;
-  float2 ml[N];
-  float u[N];
+  float3 mlu[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    ml[i] = i < count ? *reinterpret_cast<const float2*>(row + i * apart + kHeadDim) : make_float2(-INFINITY, 0.f);
-    u[i] = K::kUnits && i < count ? row[i * apart + kHeadDim + 2] : 0.f;
-    a.m = fmaxf(a.m, ml[i].x);
-    a.u = fmaxf(a.u, u[i]);
+    mlu[i] = i < count ? load_mlu<K>(row + i * apart + kHeadDim) : make_float3(-INFINITY, 0.f, 0.f);
+    a.m = fmaxf(a.m, mlu[i].x);
+    a.u = fmaxf(a.u, mlu[i].z);
   }
   const float base = a.m == -INFINITY ? 0.f : a.m;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     if (i >= count) break;
-    float e = exp2_approx((ml[i].x - base) * cs);
-    a.l += ml[i].y * e;
-    if (K::kUnits) e *= units_in(u[i], a.u);
+    float e = exp2_approx((mlu[i].x - base) * cs);
+    a.l += mlu[i].y * e;
+    if (K::kUnits) e *= units_in(mlu[i].z, a.u);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float4 x = *reinterpret_cast<const float4*>(row + i * apart + channel + 4 * k);
@@ -331,10 +353,7 @@ __device__ __forceinline__ void store_part(const Part& a, float* channels, float
   for (int i = 0; i < 4; ++i)
     *reinterpret_cast<float4*>(channels + channel + 4 * i) =
         make_float4(a.o[4 * i], a.o[4 * i + 1], a.o[4 * i + 2], a.o[4 * i + 3]);
-  if (channel == 0) {
-    *reinterpret_cast<float2*>(ml) = make_float2(a.m, a.l);
-    if (K::kUnits) ml[2] = a.u;
-  }
+  if (channel == 0) store_mlu<K>(ml, a.m, a.l, a.u);
 }
 
 // out = o / l in the cache's type, and the query's log-sum-exp (o and l are lifted alike).
@@ -399,9 +418,8 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
       for (int k0 = subs > 1 ? sub : 0; k0 < count; k0 += 8 * subs) {
         // eight parts at a time: a lane has one's m and l, all lanes 16 channels of each, of four at once
         const int k = k0 + lane8 * subs;
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (k < count) ml = __ldcg(reinterpret_cast<const float2*>(part(k) + q * kPartialFloats));
-        const float u = K::kUnits && k < count ? __ldcg(part(k) + q * kPartialFloats + 2) : 0.f;
+        float3 mlu = make_float3(-INFINITY, 0.f, 0.f);
+        if (k < count) mlu = load_mlu_l2<K>(part(k) + q * kPartialFloats);
         float e = 0.f;
 #pragma unroll
         for (int j0 = 0; j0 < 8; j0 += 4) {
@@ -415,23 +433,23 @@ __device__ __forceinline__ void join_item(const P& p, int b, int h, int len, int
               o[j][i] = kj < count ? __ldcg(reinterpret_cast<const float4*>(row + 4 * i)) : make_float4(0.f, 0.f, 0.f, 0.f);
           }
           if (j0 == 0) {
-            float top = fmaxf(a.m, ml.x);
+            float top = fmaxf(a.m, mlu.x);
 #pragma unroll
             for (int i = 1; i < 8; i <<= 1) top = fmaxf(top, __shfl_xor_sync(group_mask, top, i));
             const float base = top == -INFINITY ? 0.f : top;
             float keep = exp2_approx((a.m - base) * cs);
-            e = exp2_approx((ml.x - base) * cs);
-            float l = ml.y * e;
+            e = exp2_approx((mlu.x - base) * cs);
+            float l = mlu.y * e;
 #pragma unroll
             for (int i = 1; i < 8; i <<= 1) l += __shfl_xor_sync(group_mask, l, i);
             a.m = top;
             a.l = a.l * keep + l;
             if (K::kUnits) {
-              float to = fmaxf(a.u, u);
+              float to = fmaxf(a.u, mlu.z);
 #pragma unroll
               for (int i = 1; i < 8; i <<= 1) to = fmaxf(to, __shfl_xor_sync(group_mask, to, i));
               keep *= units_in(a.u, to);
-              e *= units_in(u, to);
+              e *= units_in(mlu.z, to);
               a.u = to;
             }
 #pragma unroll
@@ -496,7 +514,7 @@ __device__ void finish_item(const P& p, State<NT>& st, const Cursor& c, bool who
       float* row = scratch + (warp * 8 + 2 * tq + j) * kSumFloats;
 #pragma unroll
       for (int d = 0; d < 8; ++d) K::place(row + 16 * d, g, st.o[nt][d][j], st.o[nt][d][2 + j]);
-      if (g == 0) {
+      if (g == 0) {  // (as one store of four words it spills: 16 bytes with 16 queries)
         *reinterpret_cast<float2*>(row + kHeadDim) = make_float2(st.m[nt][j], st.l[nt][j]);
         if (K::kUnits) row[kHeadDim + 2] = unit;
       }
