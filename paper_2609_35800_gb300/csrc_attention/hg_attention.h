@@ -1,5 +1,5 @@
-// Launch parameters and launchers shared by the host code and the kernels of the 16-bit caches: paged append, paged
-// decode attention and prompt attention.
+// Launch parameters and launchers shared by the host code and the kernels of the paged caches in 16 and in 8 bits (append,
+// decode attention, dense rows), page plans and prompt attention.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>

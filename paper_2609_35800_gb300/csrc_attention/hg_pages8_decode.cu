@@ -8,9 +8,9 @@
 //
 // 2 G flop a byte, so the reads of the cache bound it, but an entry costs twice the instructions a byte of the 16-bit
 // kernel's.  Measured: 32 requests x 8,577 tokens x 8 KV heads 86 us, 6.6 TB/s, 0.97 of a copy's rate; one request of
-// 131,073 tokens 50 us (0.79: data at 7.1 TB/s from 3 to 40 us, the slowest CTA 3 us later, then the last join); 37 of 1
-// to 9,001 tokens, 12 queries a KV head 25 us (14 tiles a CTA in five rounds of 2.2 us, start, sums and joins; an item of
-// one tile takes a CTA 6 us, 3 with up to 8 queries); 321 tokens 6.0 us.
+// 131,073 tokens 51 us (0.78: data at 7.1 TB/s from 3 to 40 us, the slowest CTA 3 us later, then the last join); 37 of 1
+// to 9,001 tokens, 12 queries a KV head 23 to 25 us (14 tiles a CTA in five rounds of 2.2 us, start, sums and joins; an
+// item of one tile takes a CTA 6 us, 3 with up to 8 queries); 321 tokens 6.2 us.
 //
 // A producer warp copies tiles of 64 tokens into a ring of six 16 KB stages with TMA, a box per page (swizzled rows of 128
 // bytes; a page outside the pool reads as zeros), and their scales beside them with four-byte asynchronous copies that
@@ -27,8 +27,8 @@
 // entries down to 2^-31 of it with all their bits; the factor comes back with ks.  P is e^(S - m) 2^7 vs / u, where u is
 // the largest vs so far, to a power of two: at most 2^15, as a score may be 2^8 past the running maximum; the sums O stay
 // in units of u, are moved when u grows, and are multiplied by u once they are divided (before, sums of values near BF16's
-// end would pass binary32's).  So terms below 2^-32 of the largest probability times the largest scale are lost to the
-// second product.  Scores, maxima, sums and outputs are held in 32 bits.
+// end would pass binary32's).  Below 2^-21 of the largest probability times the largest scale so far terms lose
+// bits, and below 2^-32 of it they are lost to the second product.  Scores, maxima, sums and outputs are held in 32 bits.
 #include <cfloat>
 
 #include "hg_pages8.cuh"
